@@ -413,6 +413,186 @@ mma_status_t mma_kv_fetch_noalloc(const mma_kv_layout_t* layout, const void* hos
  * (Section 3.3 ordering requirement). */
 mma_status_t mma_digest_u32(const void* dev_ptr, uint64_t bytes, uint64_t* dev_out, void* stream);
 
+/* ------------------------------------------------- operators on the paged cache */
+
+/* What a decode step does with the paged KV cache that the calls above move: new
+ * tokens written into it (append), attention over it (attention), a verified draft
+ * moved together (commit), and the entries that little attention went to dropped
+ * before the rest is offloaded (evict). All four work on the GPU layer tensors of
+ * mma_kv_layout_t, in each of its block layouts, and are ordered on `stream` like a
+ * kernel launch: they allocate nothing, wait for nothing and may be captured.
+ *
+ * `layout` is the one of the transfers; of it num_layers (commit only),
+ * block_tokens, kv_heads, head_dim, elem_bytes, gpu_num_blocks and gpu_layout are
+ * used. head_dim * elem_bytes has to be a multiple of 16, head_dim a multiple of 8
+ * and at most 256, layer tensors 16-byte aligned, in every layout.
+ * `cache_type` is what the cache holds: MMA_TYPE_BF16, MMA_TYPE_F16 (elem_bytes 2) or
+ * MMA_TYPE_F8 (elem_bytes 1: 4 exponent and 3 mantissa bits, largest value 448).
+ * 8-bit entries are stored divided by a scale per KV head (k_scale, v_scale: device
+ * arrays of kv_heads floats; NULL: 1) and read times it. `type` (bf16 or f16) is what
+ * queries, new keys and values and outputs are in; a 16-bit cache is of the same type.
+ *
+ * Tables, lengths and every index array are device memory, read when the kernels
+ * run. What they hold is not checked by the call; the kernels keep to the tensors
+ * whatever they find: a block table entry outside [0, gpu_num_blocks) is a block that
+ * is not there (nothing is written to it, its entries are as if masked), negative
+ * lengths are 0, and token ranges are cut to num_tokens. */
+#define MMA_TYPE_BF16 0u
+#define MMA_TYPE_F16 1u
+#define MMA_TYPE_F8 2u
+
+/* The sequences of a call. Entry j of sequence s lies in block
+ * block_table[s * table_stride + j / block_tokens], at token j % block_tokens. The
+ * call's tokens of sequence s are rows q_start[s] .. q_start[s + 1] - 1 of its token
+ * tensors (NULL: max_tokens rows each), and token i of them is entry lens[s] + i. */
+typedef struct mma_kv_seqs {
+  const int32_t* block_table;
+  const int32_t* lens;      /* entries that a sequence has before this call's tokens */
+  const int32_t* q_start;   /* num_seqs + 1 of them, ascending, or NULL */
+  uint32_t num_seqs;
+  uint32_t table_stride;    /* blocks in a row of block_table */
+  uint32_t max_tokens;      /* no sequence has more tokens in the call (further ones are left out) */
+  uint32_t max_len;         /* no sequence has more entries, the call's tokens included (further ones
+                               are left out); at most table_stride * block_tokens */
+} mma_kv_seqs_t;
+
+/* Rows [token][head][head_dim] of `type`: strides in elements, the last axis contiguous,
+ * any alignment of an element. Tokens of no sequence are left alone. */
+typedef struct mma_rows {
+  void* data;
+  uint64_t token_stride;
+  uint64_t head_stride;
+} mma_rows_t;
+
+/* Positions: how the frequencies of a rotary embedding of rot_dim values are scaled for
+ * contexts longer than those of the training (kind), from f_i = base^(-2 i / rot_dim).
+ *   NONE    f_i
+ *   LINEAR  f_i / factor
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) for base: the lowest frequency is
+ *           divided by factor, the highest kept
+ *   RAMP    f_i / factor for pairs that turn less than `low` times over original_len,
+ *           f_i for those that turn more than `high` times, and between them a linear
+ *           blend by index (YaRN, arXiv 2309.00071); cos and sin times
+ *           0.1 ln(factor) + 1
+ *   BANDS   the same ends, blended linearly in the number of turns, cos and sin as they are */
+#define MMA_ROPE_NONE 0u
+#define MMA_ROPE_LINEAR 1u
+#define MMA_ROPE_BASE 2u
+#define MMA_ROPE_RAMP 3u
+#define MMA_ROPE_BANDS 4u
+typedef struct mma_rope {
+  uint32_t rot_dim;      /* even */
+  uint32_t kind;
+  double base;
+  double factor;         /* >= 1 */
+  double original_len;   /* RAMP, BANDS */
+  double low, high;      /* RAMP, BANDS: 0 < low < high */
+} mma_rope_t;
+
+/* Host only: the table that mma_kv_append reads, out[rows][rot_dim]: of position p the
+ * rot_dim / 2 cosines, then the sines, computed in 64 bits. `out` is host memory;
+ * copied to the GPU once, it serves a model's every call. */
+mma_status_t mma_rope_table(const mma_rope_t* rope, uint64_t rows, float* out);
+
+typedef struct mma_kv_append {
+  mma_rows_t q, k, v;       /* inputs: q_heads, kv_heads, kv_heads heads */
+  mma_rows_t q_out;         /* may be q itself, with its strides */
+  const int32_t* positions; /* [num_tokens]: row of `rope`; below 0: the first, past the end: the last */
+  const float* rope;        /* [rope_rows][rot_dim], 16-byte aligned (mma_rope_table); NULL: no rotation */
+  const void* q_weight;     /* [head_dim] of `type`; NULL: queries are not normalised */
+  const void* k_weight;
+  const float* k_scale;
+  const float* v_scale;
+  uint32_t num_tokens;
+  uint32_t q_heads;         /* a multiple of kv_heads */
+  uint32_t type, cache_type;
+  uint32_t rot_dim;         /* the first rot_dim of head_dim values rotate; even */
+  uint32_t rope_rows;
+  uint32_t interleaved;     /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1) */
+  float eps;
+} mma_kv_append_t;
+
+/* Of every token: q and k of each head times 1 / sqrt(mean of squares + eps) and the
+ * weight, then each pair (a, b) turned to (a cos - b sin, b cos + a sin); q to q_out,
+ * k and v to their entry of the cache. One rounding, at the store. 8-bit entries past
+ * 448 are stored as 448 of their sign, NaN as NaN. */
+mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
+                           const mma_kv_append_t* args, void* stream);
+
+typedef struct mma_kv_attention {
+  mma_rows_t q, out;        /* q_heads heads; `out` may be q itself, with its strides */
+  const uint64_t* tree;     /* [num_tokens][tree_words]: bit d of a token's row: it sees token d of its
+                               sequence's tokens in this call; NULL: token i sees 0 .. i */
+  float* lse;               /* [num_tokens][q_heads] or NULL */
+  const float* scores_in;   /* [num_seqs][kv_heads][scores_stride] or NULL (0) */
+  float* scores_out;        /* the same shape; may be scores_in; NULL: no scores */
+  const float* k_scale;
+  const float* v_scale;
+  void* workspace;          /* mma_kv_attention_workspace bytes of device memory, 256-byte aligned, the
+                               call's own until `stream` has passed it */
+  uint64_t workspace_bytes;
+  uint32_t num_tokens;
+  uint32_t q_heads;         /* a multiple of kv_heads: head a reads KV head a / (q_heads / kv_heads) */
+  uint32_t type, cache_type;
+  uint32_t tree_words;
+  uint32_t scores_stride;   /* at least max_len */
+  float scale;              /* of the products, e.g. 1 / sqrt(head_dim) */
+  float decay;              /* of scores_in */
+} mma_kv_attention_t;
+
+/* Of every token and head: p = softmax over the entries it sees of scale * q . K, and
+ * out = sum of p V; lse = log of the sum of exp. It sees its sequence's lens[s] entries
+ * and of the call's own tokens (which mma_kv_append has written) those that `tree` says.
+ * A row that sees nothing is 0 with lse -infinity. What lies in entries that a row does
+ * not see, infinities and NaN among it, does not reach the row.
+ * scores_out[s][h][j] = decay * scores_in[s][h][j], for j < lens[s], plus the p of entry
+ * j summed over the call's tokens and the heads of KV head h; for the entries that the
+ * sequence has, the call's tokens included, and unwritten past them. */
+mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
+                              const mma_kv_attention_t* args, void* stream);
+
+/* Host only: the workspace of that call. Of args num_tokens, q_heads, type, cache_type, and of
+ * its pointers only scores_out (NULL or not) matter. */
+mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs,
+                                        const mma_kv_attention_t* args, uint64_t* bytes);
+
+typedef struct mma_kv_commit {
+  const int32_t* accepted;  /* [num_seqs][accepted_stride]: drafted tokens, ascending */
+  const int32_t* counts;    /* [num_seqs]: how many of a row */
+  int32_t* lens_out;        /* [num_seqs] or NULL: lens + counts; not seqs->lens */
+  float* const* scores;     /* host array of num_layers device pointers, each to
+                               [num_seqs][kv_heads][scores_stride], or NULL */
+  uint32_t accepted_stride;
+  uint32_t scores_stride;   /* at least max_len */
+} mma_kv_commit_t;
+
+/* Entry lens[s] + accepted[s][i] moves to lens[s] + i, in place, for i < counts[s]: K and V
+ * of every layer, and its scores. A list ends where an index is negative, not above the
+ * one before, or not below the sequence's tokens in the call, and counts past
+ * accepted_stride end there; lens_out counts what was moved. gpu_layers: num_layers device pointers, copied before return. */
+mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_seqs_t* seqs,
+                           const mma_kv_commit_t* args, void* stream);
+
+typedef struct mma_kv_evict {
+  const int32_t* dst_table; /* [num_seqs][dst_stride]: blocks that no sequence of the call holds */
+  const float* scores;      /* [num_seqs][kv_heads][scores_stride] */
+  int32_t* entries;         /* [num_seqs][kv_heads][keep]: the entries kept, ascending, -1 behind them */
+  float* scores_out;        /* [num_seqs][kv_heads][keep] or NULL: their scores, 0 behind them */
+  int32_t* lens_out;        /* [num_seqs] or NULL; not seqs->lens */
+  uint32_t dst_stride;      /* at least keep / block_tokens, rounded up */
+  uint32_t scores_stride;   /* at least max_len */
+  uint32_t keep;            /* at least sinks + recent, and 1 */
+  uint32_t sinks, recent;   /* the first and the last entries, kept whatever their scores */
+} mma_kv_evict_t;
+
+/* Of each sequence (lens entries; q_start and max_tokens are not used) and KV head, keep
+ * min(keep, lens) entries: the first `sinks`, the last `recent`, and of the others those
+ * with the highest scores, ties to the lower entry, a NaN below every number. Kept ones
+ * keep their order and become entries 0, 1, ... of the blocks in dst_table; each KV head
+ * has its own. */
+mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
+                          const mma_kv_evict_t* args, void* stream);
+
 /* ------------------------------------------------------------------- status */
 
 /* Counters since mma_init or mma_reset_stats. They cover every transfer retired so far;

@@ -51,6 +51,15 @@ MMA_COPY_IN_FLIGHT = 2
 MMA_TASK_CU_ONLY = 1
 MMA_TASK_SDMA_ONLY = 2
 
+MMA_TYPE_BF16 = 0
+MMA_TYPE_F16 = 1
+MMA_TYPE_F8 = 2
+MMA_ROPE_NONE = 0
+MMA_ROPE_LINEAR = 1
+MMA_ROPE_BASE = 2
+MMA_ROPE_RAMP = 3
+MMA_ROPE_BANDS = 4
+
 STATUS = {
     0: "MMA_OK", -1: "MMA_ERR_NOT_INITIALIZED", -2: "MMA_ERR_INVALID_ARG", -3: "MMA_ERR_NOT_PINNED",
     -4: "MMA_ERR_HIP", -5: "MMA_ERR_HSA", -6: "MMA_ERR_TRANSFER_FAILED", -7: "MMA_ERR_ALREADY_INITIALIZED",
@@ -130,6 +139,52 @@ class mma_plan_entry_t(ctypes.Structure):
                 ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
+class mma_kv_seqs_t(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("q_start", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_uint32), ("table_stride", ctypes.c_uint32),
+                ("max_tokens", ctypes.c_uint32), ("max_len", ctypes.c_uint32)]
+
+
+class mma_rows_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_uint64), ("head_stride", ctypes.c_uint64)]
+
+
+class mma_rope_t(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_uint32), ("kind", ctypes.c_uint32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
+
+
+class mma_kv_append_t(ctypes.Structure):
+    _fields_ = [("q", mma_rows_t), ("k", mma_rows_t), ("v", mma_rows_t), ("q_out", mma_rows_t),
+                ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("num_tokens", ctypes.c_uint32), ("q_heads", ctypes.c_uint32), ("type", ctypes.c_uint32),
+                ("cache_type", ctypes.c_uint32), ("rot_dim", ctypes.c_uint32), ("rope_rows", ctypes.c_uint32),
+                ("interleaved", ctypes.c_uint32), ("eps", ctypes.c_float)]
+
+
+class mma_kv_attention_t(ctypes.Structure):
+    _fields_ = [("q", mma_rows_t), ("out", mma_rows_t), ("tree", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("scores_in", ctypes.c_void_p), ("scores_out", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+                ("num_tokens", ctypes.c_uint32), ("q_heads", ctypes.c_uint32), ("type", ctypes.c_uint32),
+                ("cache_type", ctypes.c_uint32), ("tree_words", ctypes.c_uint32), ("scores_stride", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("decay", ctypes.c_float)]
+
+
+class mma_kv_commit_t(ctypes.Structure):
+    _fields_ = [("accepted", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("lens_out", ctypes.c_void_p),
+                ("scores", ctypes.c_void_p), ("accepted_stride", ctypes.c_uint32), ("scores_stride", ctypes.c_uint32)]
+
+
+class mma_kv_evict_t(ctypes.Structure):
+    _fields_ = [("dst_table", ctypes.c_void_p), ("scores", ctypes.c_void_p), ("entries", ctypes.c_void_p),
+                ("scores_out", ctypes.c_void_p), ("lens_out", ctypes.c_void_p), ("dst_stride", ctypes.c_uint32),
+                ("scores_stride", ctypes.c_uint32), ("keep", ctypes.c_uint32), ("sinks", ctypes.c_uint32),
+                ("recent", ctypes.c_uint32)]
+
+
 _P = ctypes.c_void_p
 _U64 = ctypes.c_uint64
 _I32 = ctypes.c_int32
@@ -155,6 +210,17 @@ _SIGNATURES = {
     "mma_kv_offload": ([ctypes.POINTER(mma_kv_layout_t), _P, _P, _P, _P, _U64, _P], _S),
     "mma_kv_fetch_noalloc": ([ctypes.POINTER(mma_kv_layout_t), _P, _P, _P, _P, _U64, _P], _S),
     "mma_digest_u32": ([_P, _U64, _P, _P], _S),
+    "mma_rope_table": ([ctypes.POINTER(mma_rope_t), _U64, _P], _S),
+    "mma_kv_append": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
+                       ctypes.POINTER(mma_kv_append_t), _P], _S),
+    "mma_kv_attention": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
+                          ctypes.POINTER(mma_kv_attention_t), _P], _S),
+    "mma_kv_attention_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(mma_kv_seqs_t),
+                                    ctypes.POINTER(mma_kv_attention_t), ctypes.POINTER(_U64)], _S),
+    "mma_kv_commit": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
+                       ctypes.POINTER(mma_kv_commit_t), _P], _S),
+    "mma_kv_evict": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
+                      ctypes.POINTER(mma_kv_evict_t), _P], _S),
     "mma_get_stats": ([ctypes.POINTER(mma_stats_t)], _S),
     "mma_reset_stats": ([], _S),
     "mma_status_str": ([_S], ctypes.c_char_p),
@@ -371,6 +437,206 @@ def mma_kv_offload(layout: mma_kv_layout_t, host_pool, gpu_layers, gpu_blocks, h
 
 def mma_digest_u32(dev_ptr, nbytes: int, dev_out, stream=None) -> None:
     _check(lib.mma_digest_u32(_ptr(dev_ptr), nbytes, _ptr(dev_out), _stream(stream)), "mma_digest_u32")
+
+
+# ------------------------------------------------------------------ operators on the paged cache
+_TYPES = {torch.bfloat16: MMA_TYPE_BF16, torch.float16: MMA_TYPE_F16}
+
+
+def _want(name: str, t: torch.Tensor, dtype, shape=None) -> int:
+    """Address of a contiguous GPU tensor of the given type and, where given, shape."""
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name}: a contiguous {dtype} GPU tensor{'' if shape is None else f' of shape {shape}'} is "
+                         f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _maybe(name: str, t: Optional[torch.Tensor], dtype, shape=None) -> int:
+    return 0 if t is None else _want(name, t, dtype, shape)
+
+
+def _rows(name: str, t: torch.Tensor, dtype, tokens: int, dim: int) -> Tuple[int, int, int]:
+    """(address, token stride, head stride) of [tokens][heads][dim] rows."""
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{name}: [{tokens}][heads][{dim}] of {dtype} on the GPU is wanted, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    token, head, last = t.stride()
+    if last != 1 and dim > 1:
+        raise ValueError(f"{name}: the values of a head have to be contiguous, strides {t.stride()}")
+    return t.data_ptr(), token, head
+
+
+def _types(q: torch.Tensor, layout: mma_kv_layout_t) -> Tuple[int, int]:
+    kind = _TYPES.get(q.dtype)
+    if kind is None:
+        raise ValueError(f"queries of {q.dtype}: bfloat16 or float16 is wanted")
+    return kind, MMA_TYPE_F8 if layout.elem_bytes == 1 else kind
+
+
+def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
+    """A new tensor whose memory is `stream`'s (a torch stream, a handle, or None for the current one)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class KVSeqs:
+    """The sequences of a call (``mma_kv_seqs_t``) and the tensors that it points to. Built once per step, or
+    kept while its tensors' addresses and the two bounds stay: what the tensors hold may change between calls."""
+
+    def __init__(self, block_table: torch.Tensor, lens: torch.Tensor, q_start: Optional[torch.Tensor] = None, *,
+                 max_tokens: int, max_len: int):
+        if block_table.dim() != 2:
+            raise ValueError("block_table: [sequences][blocks] is wanted")
+        n, width = block_table.shape
+        self.tensors = block_table, lens, q_start
+        self.num_seqs, self.max_tokens, self.max_len = n, max_tokens, max_len
+        self.device = block_table.device
+        self.c = mma_kv_seqs_t(_want("block_table", block_table, torch.int32), _want("lens", lens, torch.int32, (n,)),
+                               _maybe("q_start", q_start, torch.int32, (n + 1,)), n, width, max_tokens, max_len)
+
+
+def kv_seqs(block_table, lens, q_start=None, *, max_tokens: int = 1, max_len: int) -> KVSeqs:
+    return KVSeqs(block_table, lens, q_start, max_tokens=max_tokens, max_len=max_len)
+
+
+def mma_rope_table(rows: int, rot_dim: int, base: float = 10000.0, kind: int = MMA_ROPE_NONE, factor: float = 1.0,
+                   original_len: float = 0.0, low: float = 1.0, high: float = 32.0) -> np.ndarray:
+    """float32 [rows][rot_dim]: cosines, then sines, of each position (host memory)."""
+    out = np.empty((rows, rot_dim), np.float32)
+    r = mma_rope_t(rot_dim, kind, base, factor, original_len, low, high)
+    _check(lib.mma_rope_table(ctypes.byref(r), rows, out.ctypes.data), "mma_rope_table")
+    return out
+
+
+def mma_kv_append(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                  positions: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None, *,
+                  q_out: Optional[torch.Tensor] = None, interleaved: bool = False,
+                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """Normalise and rotate q and k, write k and v into `layer`; returns the queries (q_out, or a new tensor)."""
+    kind, cache = _types(q, layout)
+    n, heads, dim, dt = q.shape[0], layout.kv_heads, layout.head_dim, q.dtype
+    if q_out is None:
+        q_out = _empty_on(stream, q.shape, dt, q.device)
+    if k.shape[1] != heads or v.shape[1] != heads or q_out.shape[1] != q.shape[1]:
+        raise ValueError(f"k, v: {heads} heads are wanted, and of q_out as many as of q")
+    if rope is not None and (rope.dim() != 2 or positions is None):
+        raise ValueError("rope: [positions][rot_dim] is wanted, and positions with it")
+    a = mma_kv_append_t(
+        _rows("q", q, dt, n, dim), _rows("k", k, dt, n, dim), _rows("v", v, dt, n, dim),
+        _rows("q_out", q_out, dt, n, dim), _maybe("positions", positions, torch.int32, (n,)),
+        _maybe("rope", rope, torch.float32), _maybe("q_weight", q_weight, dt, (dim,)),
+        _maybe("k_weight", k_weight, dt, (dim,)), _maybe("k_scale", k_scale, torch.float32, (heads,)),
+        _maybe("v_scale", v_scale, torch.float32, (heads,)), n, q.shape[1], kind, cache,
+        0 if rope is None else rope.shape[1], 0 if rope is None else rope.shape[0], interleaved, eps)
+    _check(lib.mma_kv_append(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_append")
+    return q_out
+
+
+def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tensor, *,
+                     out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                     tree: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                     scores_in: Optional[torch.Tensor] = None, scores_out: Optional[torch.Tensor] = None,
+                     decay: float = 1.0, k_scale: Optional[torch.Tensor] = None,
+                     v_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Attention of the call's tokens over their sequences' entries; returns `out` (or a new tensor). `tree`: int64
+    [tokens][words] bits. `scale`: 1 / sqrt(head_dim) unless given. `workspace`: a uint8 tensor of
+    kv_attention_workspace() bytes or more; a new one of the stream's unless given."""
+    kind, cache = _types(q, layout)
+    n, heads, dim, dt = q.shape[0], layout.kv_heads, layout.head_dim, q.dtype
+    if out is None:
+        out = _empty_on(stream, q.shape, dt, q.device)
+    if out.shape[1] != q.shape[1]:
+        raise ValueError("out: as many heads as q has are wanted")
+    if tree is not None and (tree.dim() != 2 or tree.shape[0] != n):
+        raise ValueError(f"tree: [{n}][words] is wanted, got {tuple(tree.shape)}")
+    width = 0
+    if scores_out is not None:
+        if scores_out.dim() != 3 or tuple(scores_out.shape[:2]) != (seqs.num_seqs, heads):
+            raise ValueError(f"scores_out: [{seqs.num_seqs}][{heads}][entries] is wanted, got {tuple(scores_out.shape)}")
+        width = scores_out.shape[2]
+    elif scores_in is not None:
+        raise ValueError("scores_in without scores_out")
+    a = mma_kv_attention_t(
+        _rows("q", q, dt, n, dim), _rows("out", out, dt, n, dim), _maybe("tree", tree, torch.int64),
+        _maybe("lse", lse, torch.float32, (n, q.shape[1])),
+        _maybe("scores_in", scores_in, torch.float32, None if scores_out is None else tuple(scores_out.shape)),
+        _maybe("scores_out", scores_out, torch.float32), _maybe("k_scale", k_scale, torch.float32, (heads,)),
+        _maybe("v_scale", v_scale, torch.float32, (heads,)), 0, 0, n, q.shape[1], kind, cache,
+        0 if tree is None else tree.shape[1], width, dim ** -0.5 if scale is None else scale, decay)
+    if workspace is None:
+        need = _U64()
+        _check(lib.mma_kv_attention_workspace(layout, seqs.c, a, need), "mma_kv_attention_workspace")
+        if need.value:
+            workspace = _empty_on(stream, (need.value,), torch.uint8, q.device)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _want("workspace", workspace, torch.uint8), workspace.numel()
+    _check(lib.mma_kv_attention(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_attention")
+    return out
+
+
+def kv_attention_workspace(layout: mma_kv_layout_t, seqs: KVSeqs, num_tokens: int, q_heads: int, dtype: torch.dtype,
+                           scores: bool = False) -> int:
+    """Bytes of workspace of an attention call of these sizes."""
+    kind = _TYPES[dtype]
+    a = mma_kv_attention_t(num_tokens=num_tokens, q_heads=q_heads, type=kind, scores_out=1 if scores else None,
+                           cache_type=MMA_TYPE_F8 if layout.elem_bytes == 1 else kind)
+    need = _U64()
+    _check(lib.mma_kv_attention_workspace(layout, seqs.c, a, need), "mma_kv_attention_workspace")
+    return need.value
+
+
+def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch.Tensor, counts: torch.Tensor, *,
+                  scores=None, scores_stride: Optional[int] = None, stream=None) -> torch.Tensor:
+    """Move the accepted drafted entries together in every layer (in place); returns the new lengths. `layers`,
+    `scores`: tensors, or a layer_table (then scores_stride is needed)."""
+    n = seqs.num_seqs
+    if accepted.dim() != 2 or accepted.shape[0] != n:
+        raise ValueError(f"accepted: [{n}][drafted tokens] is wanted, got {tuple(accepted.shape)}")
+    if scores is not None and not isinstance(scores, ctypes.Array):
+        shape = tuple(scores[0].shape)
+        if len(shape) != 3 or shape[:2] != (n, layout.kv_heads):
+            raise ValueError(f"scores: [{n}][{layout.kv_heads}][entries] is wanted, got {shape}")
+        for t in scores:
+            _want("scores", t, torch.float32, shape)
+        scores_stride = shape[2]
+    lt = layer_table(layers)  # locals, so that the arrays outlive the call
+    st = None if scores is None else layer_table(scores)
+    if len(lt) < layout.num_layers or (st is not None and (len(st) < layout.num_layers or scores_stride is None)):
+        raise ValueError(f"{layout.num_layers} layers are wanted, and as many scores with their stride")
+    lens = _empty_on(stream, (n,), torch.int32, seqs.device)
+    a = mma_kv_commit_t(_want("accepted", accepted, torch.int32), _want("counts", counts, torch.int32, (n,)),
+                        lens.data_ptr(), 0 if st is None else ctypes.addressof(st), accepted.shape[1],
+                        scores_stride or 0)
+    _check(lib.mma_kv_commit(layout, lt, seqs.c, a, _stream(stream)), "mma_kv_commit")
+    return lens
+
+
+def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.Tensor, scores: torch.Tensor, keep: int,
+                 *, sinks: int = 0, recent: int = 0, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Keep the `keep` entries of each sequence and KV head that attention went to, moved into the blocks of
+    dst_table; returns (entries kept, their scores, new lengths)."""
+    n, heads = seqs.num_seqs, layout.kv_heads
+    if dst_table.dim() != 2 or dst_table.shape[0] != n:
+        raise ValueError(f"dst_table: [{n}][blocks] is wanted, got {tuple(dst_table.shape)}")
+    if scores.dim() != 3 or tuple(scores.shape[:2]) != (n, heads):
+        raise ValueError(f"scores: [{n}][{heads}][entries] is wanted, got {tuple(scores.shape)}")
+    if keep < 1:
+        raise ValueError("keep: at least 1")
+    entries = _empty_on(stream, (n, heads, keep), torch.int32, seqs.device)
+    kept = _empty_on(stream, (n, heads, keep), torch.float32, seqs.device)
+    lens = _empty_on(stream, (n,), torch.int32, seqs.device)
+    a = mma_kv_evict_t(_want("dst_table", dst_table, torch.int32), _want("scores", scores, torch.float32),
+                       entries.data_ptr(), kept.data_ptr(), lens.data_ptr(), dst_table.shape[1], scores.shape[2], keep,
+                       sinks, recent)
+    _check(lib.mma_kv_evict(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_evict")
+    return entries, kept, lens
 
 
 # ------------------------------------------------------------------ status

@@ -30,6 +30,9 @@ SOURCES = {
     "mma_kernels.hip": DEVICE,
     "mma_runtime.cpp": ["-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{os.path.join(ROCM, 'include')}"],
     "mma_plan.cpp": ["-x", "c++"],
+    "mma_ops.cpp": ["-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{os.path.join(ROCM, 'include')}"],
+    "mma_attention.hip": DEVICE,
+    "mma_kv_ops.hip": DEVICE,
 }
 
 

@@ -15,6 +15,7 @@
 
 #include "mma_engine.h"
 #include "mma_noalloc.h"
+#include "mma_ops.h"
 
 namespace mma {
 
@@ -528,6 +529,15 @@ mma_status_t boundary_error(const char* api) noexcept {
 }
 
 }  // namespace
+
+// ------------------------------------------------------------ for the operators (mma_ops.h)
+mma_status_t ops_ready(int* device) {
+  if (mma_status_t s = check_ready()) return s;
+  *device = g_rt->dev;
+  return MMA_OK;
+}
+mma_status_t ops_device_range(const void* p, uint64_t bytes) { return device_range(p, bytes); }
+mma_status_t ops_boundary_error(const char* func) { return boundary_error(func); }
 }  // namespace mma
 
 using namespace mma;

@@ -1,0 +1,627 @@
+"""The operators on the paged KV cache against the 64-bit reference (oracle.kv_ops).
+
+Tolerances, from the types and the arithmetic before any run:
+  - a value rounded once to a type with b mantissa bits is within 2^-(b+1) of itself (relative), and within
+    half its smallest step where it is subnormal;
+  - sums in 32 bits: a logit is a sum of head_dim exact products, whose error stays below
+    head_dim * 2^-24 of the sum of their magnitudes (B); p carries twice that (its own logit and the row's sum), plus
+    the exponential's and the sum's own few 2^-23;
+  - attention rounds p to 16 bits for the product with V: 2^-(b+1) of sum p |V| at most.
+Bytes that are moved, entries that are kept and everything that no operator writes are compared exactly.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_ops as ok
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2512_16056_amd as mma  # noqa: E402
+from gpu_helpers import log, session  # noqa: E402
+
+LAYOUTS = {"piece": mma.MMA_KV_LAYOUT_PIECE, "hnd": mma.MMA_KV_LAYOUT_HND, "xpacked": mma.MMA_KV_LAYOUT_XPACKED}
+BF16, F16, F8 = torch.bfloat16, torch.float16, ok.F8
+BITS = {BF16: 7, F16: 10, F8: 3}
+STEP = {BF16: 2.0 ** -133, F16: 2.0 ** -24, F8: 2.0 ** -9}
+EPS = 2.0 ** -23
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    with session():
+        yield
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def normal(g, *shape, std=1.0):
+    return torch.randn(shape, generator=g) * std
+
+
+def to_cache(x, dtype):
+    """Elements as the flat cache holds them: 8-bit ones as uint8."""
+    return x.clamp(-448, 448).to(F8).view(torch.uint8) if dtype is F8 else x.to(dtype)
+
+
+class Case:
+    """A cache layer with random contents, tables in random block order, and the sequences of a call."""
+
+    def __init__(self, layout, cache, lens, counts, dim=128, heads=2, group=4, tokens=16, dtype=BF16, seed=0, layers=1,
+                 room=0, q_start=True):
+        self.g = gen(seed)
+        self.dtype, self.group, self.counts, self.lens, self.layers = dtype, group, counts, lens, layers
+        need = [max(1, -(-(n + t + room) // tokens)) for n, t in zip(lens, counts)]
+        blocks = sum(need) + 3
+        self.c = ok.Cache(layout, cache, blocks, tokens, heads, dim)
+        order = torch.randperm(blocks, generator=self.g).int()
+        self.table = torch.full((len(lens), max(need)), -1, dtype=torch.int32)
+        at = 0
+        for s, n in enumerate(need):
+            self.table[s, :n] = order[at: at + n]
+            at += n
+        self.spare = order[at:]
+        self.flat = to_cache(normal(self.g, layers * 2 * blocks * self.c.piece), cache).view(layers, -1)
+        self.q_start = torch.tensor([0] + list(np.cumsum(counts)), dtype=torch.int32) if q_start else None
+        self.total = sum(counts)
+        self.max_tokens = max(counts + [1])
+        self.max_len = max([n + t for n, t in zip(lens, counts)] + [1])
+        self.heads_q = heads * group
+        self.k_scale = self.v_scale = None
+        if cache is F8:
+            self.k_scale = torch.rand(heads, generator=self.g) + 0.5
+            self.v_scale = torch.rand(heads, generator=self.g) + 0.5
+
+    def layout(self):
+        return mma.kv_layout(self.layers, self.c.tokens, self.c.heads, self.c.dim, self.c.elem, self.c.blocks, 1,
+                             LAYOUTS[self.c.layout])
+
+    def seqs(self, **kw):
+        kw = {"max_tokens": self.max_tokens, "max_len": self.max_len, **kw}
+        return mma.kv_seqs(self.table.cuda(), torch.tensor(self.lens, dtype=torch.int32).cuda(),
+                           None if self.q_start is None else self.q_start.cuda(), **kw)
+
+    def spans(self, **kw):
+        kw = {"num_tokens": self.total, "max_tokens": self.max_tokens, "max_len": self.max_len, **kw}
+        return ok.spans(self.c, self.table, self.lens, self.q_start, **kw)
+
+    def scales(self):
+        return {"k_scale": None if self.k_scale is None else self.k_scale.cuda(),
+                "v_scale": None if self.v_scale is None else self.v_scale.cuda()}
+
+
+def same_bits(a, b):
+    a, b = (x.contiguous().view(torch.uint8) for x in (a, b))
+    return torch.equal(a, b)
+
+
+def rounded_close(got, want, dtype, slack):
+    """|got - want| within one rounding of `dtype` and `slack` (absolute, of the arithmetic before it)."""
+    got, want = got.double(), want.double()
+    if dtype is F8:
+        want = want.clamp(-448, 448)
+    tol = want.abs() * 2.0 ** -(BITS[dtype] + 1) * (1 + 2.0 ** -6) + STEP[dtype] / 2 + slack
+    worst = ((got - want).abs() / tol).max().item() if got.numel() else 0.0
+    assert worst <= 1, f"{worst:.3g} of the tolerance"
+
+
+# ------------------------------------------------------------------ append
+def check_append(c, rot, interleaved, norm, q_view=None, positions=None, in_place=False):
+    n, D = c.total, c.c.dim
+    q = normal(c.g, n, c.heads_q, D, std=1.5).to(c.dtype)
+    k = normal(c.g, n, c.c.heads, D, std=1.5).to(c.dtype)
+    v = normal(c.g, n, c.c.heads, D, std=1.5).to(c.dtype)
+    qw, kw = ((1 + normal(c.g, D, std=0.2)).to(c.dtype) for _ in range(2)) if norm else (None, None)
+    table = torch.from_numpy(mma.mma_rope_table(c.max_len + 1, rot, 10000.0)) if rot else None
+    if positions is None:
+        positions = torch.tensor([m + i for m, t in zip(c.lens, c.counts) for i in range(t)], dtype=torch.int32)
+    wq, wk, wv = ok.append(q, k, v, positions, table, interleaved, qw, kw, 1e-6)
+    dev = [x if x is None else x.cuda() for x in (q, k, v, positions, table, qw, kw)]
+    if q_view is not None:
+        dev[:3] = [q_view(x) for x in dev[:3]]
+    layer = c.flat[0].cuda()
+    out = mma.mma_kv_append(c.layout(), layer, c.seqs(), *dev[:3], dev[3] if rot else None, dev[4],
+                            q_out=dev[0] if in_place else None, interleaved=interleaved, q_weight=dev[5], k_weight=dev[6],
+                            **c.scales())
+    torch.cuda.synchronize()
+    # norm: a sum of D squares, a root, a division and two products; rotation: two products and a sum
+    slack = lambda x: (D + 16) * EPS * x.abs().amax(-1, keepdim=True)  # noqa: E731
+    rounded_close(out.cpu(), wq, c.dtype, slack(wq))
+    got, rest = layer.cpu(), c.flat[0].clone()
+    for s, (a, t, m, total) in enumerate(c.spans()):
+        for i in range(total - m):
+            at = c.c.entry(c.table[s], m + i)
+            if at is None:
+                continue
+            for h in range(c.c.heads):
+                for which, want, scale in ((0, wk[a + i, h], c.k_scale), (1, wv[a + i, h], c.v_scale)):
+                    want = want / float(scale[h]) if scale is not None else want
+                    index = c.c.index(which, *at, h)
+                    rounded_close(c.c.values(got, index), want, c.c.dtype, slack(want))
+                    rest[index] = got[index]
+    assert same_bits(got, rest), "something else in the cache changed"
+    return out
+
+
+APPEND = [
+    # layout, cache, dim, rot, interleaved, norm, tokens, heads, group
+    ("piece", BF16, 128, 128, False, True, 16, 2, 4),
+    ("hnd", F16, 128, 128, False, False, 16, 2, 4),
+    ("xpacked", F8, 128, 32, True, True, 16, 2, 4),
+    ("xpacked", BF16, 64, 64, True, True, 8, 3, 1),
+    ("piece", F8, 80, 24, False, True, 5, 1, 7),
+    ("hnd", BF16, 96, 50, False, False, 1, 2, 3),
+    ("xpacked", F16, 256, 250, False, True, 32, 1, 2),
+    ("piece", BF16, 8, 2, True, True, 3, 5, 1),
+    ("hnd", F8, 256, 0, False, False, 24, 1, 1),
+    ("piece", F16, 72, 10, False, True, 7, 2, 2),
+]
+
+
+@pytest.mark.parametrize("layout,cache,dim,rot,interleaved,norm,tokens,heads,group", APPEND)
+def test_append(layout, cache, dim, rot, interleaved, norm, tokens, heads, group):
+    log(f"append {layout} {cache} dim {dim} rot {rot}")
+    dtype = F16 if cache is F16 else BF16
+    check_append(Case(layout, cache, [0, 37, 5, 64], [1, 9, 0, 23], dim, heads, group, tokens, dtype), rot, interleaved, norm)
+
+
+def test_append_single_token_and_many_sequences():
+    check_append(Case("piece", BF16, [999], [1]), 128, False, True)
+    n = 70  # more sequences than a wave has lanes
+    check_append(Case("hnd", BF16, [i % 11 for i in range(n)], [i % 3 for i in range(n)], dim=64, heads=1, group=1), 64, False, True)
+
+
+def test_append_strides_alignment_and_in_place():
+    def odd(x):  # rows that start at any 2 bytes, heads outermost
+        n, h, d = x.shape
+        buf = torch.zeros(h, n, d + 3, dtype=x.dtype, device="cuda")
+        view = buf[:, :, 1: 1 + d].permute(1, 0, 2)
+        view.copy_(x)
+        return view
+    check_append(Case("piece", BF16, [3, 20], [7, 4], dim=72, tokens=8), 36, False, True, q_view=odd)
+    c = Case("hnd", F16, [3, 20], [7, 4], dtype=F16)
+    check_append(c, 128, True, True, in_place=True)
+
+
+def test_append_positions_out_of_range_and_missing_blocks():
+    c = Case("xpacked", BF16, [3, 20], [7, 14])
+    c.table[1, 1] = -1          # entries 16 .. 31 of sequence 1
+    c.table[0, 0] = c.c.blocks  # and all of sequence 0's have no block
+    pos = torch.randint(-5, 60, (c.total,), generator=c.g).int()
+    check_append(c, 128, False, True, positions=pos)
+
+
+def test_append_without_q_start_and_zero_norm():
+    c = Case("piece", BF16, [5, 0, 17], [2, 2, 2], q_start=False)
+    check_append(c, 64, False, True)
+    # a row of zeros is zero after the norm, not NaN
+    c = Case("piece", BF16, [5], [1])
+    q = torch.zeros(1, 8, 128, dtype=BF16, device="cuda")
+    w = torch.ones(128, dtype=BF16, device="cuda")
+    out = mma.mma_kv_append(c.layout(), c.flat[0].cuda(), c.seqs(), q, q[:, :2], q[:, :2], q_weight=w, k_weight=w)
+    assert torch.equal(out, torch.zeros_like(out))
+
+
+def test_append_f8_saturates_and_keeps_nan():
+    c = Case("hnd", F8, [0], [1])
+    c.k_scale = c.v_scale = torch.full((2,), 0.5)
+    x = torch.zeros(1, 2, 128, dtype=BF16)
+    x[0, 0, :4] = torch.tensor([1e6, -1e6, math.inf, math.nan])
+    layer = c.flat[0].cuda()
+    mma.mma_kv_append(c.layout(), layer, c.seqs(), torch.zeros(1, 8, 128, dtype=BF16, device="cuda"), x.cuda(), x.cuda(), **c.scales())
+    for which in (0, 1):
+        got = c.c.values(layer.cpu(), c.c.index(which, int(c.table[0, 0]), 0, 0))[:4]
+        assert got[:3].tolist() == [448, -448, 448] and math.isnan(got[3])
+
+
+# ------------------------------------------------------------------ attention
+def tree_bits(counts, g, width=None, empty=False):
+    words = width or max(1, (max(counts) + 63) // 64)
+    rows = []
+    for t in counts:
+        bits = []
+        for i in range(t):
+            up = bits[int(torch.randint(max(0, i - 6), i, (1,), generator=g))] if i else 0
+            bits.append(up | 1 << i)
+        if empty and t:
+            bits[0] = 0
+        rows += [[(b >> 64 * w) & (2 ** 64 - 1) for w in range(words)] for b in bits]
+    return torch.from_numpy(np.array(rows, dtype=np.uint64).reshape(-1, words).view(np.int64))
+
+
+def check_attention(c, tree=None, scores=False, q=None, q_view=None, in_place=False, std=2.0, stream=None, scale=None,
+                    seqs=None, spans=None):
+    D = c.c.dim
+    if q is None:
+        q = normal(c.g, c.total, c.heads_q, D, std=std).to(c.dtype)
+    scale = D ** -0.5 if scale is None else scale
+    span = spans or c.spans()
+    s_in = torch.rand(len(c.lens), c.c.heads, c.max_len + 5, generator=c.g) if scores else None
+    want = ok.attention(c.c, c.flat[0], c.table, span, q, c.group, scale, tree, c.k_scale, c.v_scale, s_in, 0.5)
+    dev = q.cuda() if q_view is None else q_view(q.cuda())
+    lse = torch.full((c.total, c.heads_q), 7.0, device="cuda")
+    more = {}
+    if scores:
+        s_out = torch.full_like(s_in, -3.0).cuda()
+        more = {"scores_in": s_in.cuda(), "scores_out": s_out, "decay": 0.5}
+    layer = c.flat[0].cuda()
+    out = mma.mma_kv_attention(c.layout(), layer, seqs or c.seqs(), dev, out=dev if in_place else None, scale=scale,
+                               tree=None if tree is None else tree.cuda(), lse=lse, **c.scales(), **more)
+    torch.cuda.synchronize()
+    assert same_bits(layer.cpu(), c.flat[0])
+    covered = torch.zeros(c.total, dtype=torch.bool)
+    for a, t, _, _ in span:
+        covered[a: a + t] = True
+    out, lse = out.cpu()[covered].double(), lse.cpu()[covered].double()
+    w = {x: want[x][covered] for x in ("out", "lse", "mag", "big")}
+    finite = torch.isfinite(w["out"]) & torch.isfinite(w["mag"])
+    assert torch.equal(torch.isnan(w["out"]), torch.isnan(out))
+    assert torch.equal(w["out"][~finite & ~torch.isnan(out)], out[~finite & ~torch.isnan(out)])
+    u = 2.0 ** -(BITS[c.dtype] + 1)
+    p_err = (2 * D * EPS * w["big"] + 64 * EPS)[..., None]
+    tol = u * w["out"].abs() * (1 + 2 * u) + (u + p_err) * w["mag"] * (1 + 2 * u) + STEP[c.dtype]
+    worst = ((out - w["out"]).abs() / tol)[finite].max().item() if finite.any() else 0.0
+    assert worst <= 1, f"out: {worst:.3g} of the tolerance"
+    empty = w["lse"] == -math.inf
+    assert torch.equal(lse == -math.inf, empty) and not out[empty].any()
+    ok_lse = ~empty & torch.isfinite(w["lse"])
+    err = (lse - w["lse"]).abs() / (2 * D * EPS * w["big"] + 64 * EPS * (1 + w["lse"].abs()))
+    assert not ok_lse.any() or err[ok_lse].max().item() <= 1
+    if scores:
+        got = more["scores_out"].cpu().double()
+        written = torch.zeros(got.shape, dtype=torch.bool)
+        for s, (_, _, _, m) in enumerate(span):
+            written[s, :, :m] = True
+        assert (got[~written] == -3).all(), "scores past the entries changed"
+        exact = torch.zeros_like(got)
+        exact[:, :, : want["scores"].shape[2]] = want["scores"]
+        rel = 2 * D * EPS * want["big"].max() + 64 * EPS
+        err = ((got - exact).abs() / (rel * (1 + exact.abs())))[written]
+        assert not err.numel() or err.max().item() <= 1, f"scores: {err.max().item():.3g} of the tolerance"
+    return out
+
+
+ATTENTION = [
+    # layout, cache, dim, tokens, heads, group, lens, counts
+    ("piece", BF16, 128, 16, 2, 4, [101], [1]),
+    ("hnd", F16, 128, 16, 2, 4, [0, 1, 31, 32, 33, 700], [1, 1, 1, 1, 1, 1]),
+    ("xpacked", F8, 128, 16, 2, 4, [63, 0, 250], [24, 3, 70]),
+    ("xpacked", BF16, 64, 8, 1, 8, [5, 129], [2, 33]),
+    ("piece", F8, 80, 24, 1, 7, [77, 20], [9, 1]),
+    ("hnd", BF16, 96, 1, 2, 1, [40, 3], [5, 2]),
+    ("xpacked", F16, 256, 32, 1, 2, [300, 17], [3, 40]),
+    ("piece", F16, 256, 7, 1, 3, [90], [20]),
+    ("piece", BF16, 8, 3, 3, 2, [50, 0], [4, 1]),
+    ("hnd", F8, 64, 16, 2, 16, [500], [5]),
+    ("xpacked", F8, 256, 16, 1, 1, [70], [66]),
+    ("hnd", BF16, 72, 24, 1, 5, [200, 64, 65], [1, 13, 0]),
+]
+
+
+@pytest.mark.parametrize("kind", ["chain", "tree", "scores"])
+@pytest.mark.parametrize("layout,cache,dim,tokens,heads,group,lens,counts", ATTENTION)
+def test_attention(layout, cache, dim, tokens, heads, group, lens, counts, kind):
+    log(f"attention {kind} {layout} {cache} dim {dim} {lens} {counts}")
+    c = Case(layout, cache, lens, counts, dim, heads, group, tokens, F16 if cache is F16 else BF16)
+    check_attention(c, tree_bits(counts, c.g) if kind != "chain" else None, kind == "scores")
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_attention_over_many_splits(layout):
+    """Contexts long enough to be split and joined, next to short and empty ones."""
+    c = Case(layout, BF16, [3000, 10, 0, 1025], [2, 1, 1, 3], heads=1, group=2, dim=64)
+    check_attention(c, None, True)
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_attention_rows_that_see_nothing(layout):
+    """No context and a tree row without bits: zeros, lse -infinity, and no part in the scores."""
+    c = Case(layout, BF16, [0, 0, 40], [3, 1, 2], heads=1, group=4)
+    check_attention(c, tree_bits(c.counts, c.g, empty=True), True)
+
+
+@pytest.mark.parametrize("cache", [BF16, F16, F8])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_attention_infinities_where_nobody_looks(layout, cache):
+    """Stale blocks, entries past the end and drafted tokens that a row does not see hold NaN and infinities."""
+    c = Case(layout, cache, [21, 40], [9, 5], heads=1, group=4, room=30, dtype=F16 if cache is F16 else BF16)
+    bad = [math.nan] if cache is F8 else [math.nan, math.inf, -math.inf]
+    vals = to_cache(torch.tensor(bad * 400)[:400], cache)
+    if cache is F8:
+        vals = torch.full((400,), 0x7F, dtype=torch.uint8)
+    flat = c.flat[0]
+    for s, (_, t, n, m) in enumerate(c.spans()):
+        for j in range(m, c.table.shape[1] * c.c.tokens):
+            at = c.c.entry(c.table[s], j)
+            for which in (0, 1):
+                if at is not None:
+                    flat[c.c.index(which, *at, 0)] = vals[: c.c.dim]
+    for b in c.spare.tolist():
+        for tok in range(c.c.tokens):
+            flat[c.c.index(0, b, tok, 0)] = flat[c.c.index(1, b, tok, 0)] = vals[: c.c.dim]
+    tree = tree_bits(c.counts, c.g)
+    out = check_attention(c, tree, True)
+    assert torch.isfinite(out).all()
+    # drafted token 2 of sequence 0: seen by itself and its children alone
+    at = c.c.entry(c.table[0], 21 + 2)
+    for which in (0, 1):
+        flat[c.c.index(which, *at, 0)] = vals[: c.c.dim]
+    tree[:9, 0] &= ~(1 << 2)
+    out = check_attention(c, tree, False)
+    assert torch.isfinite(out).all()
+    keep = flat[c.c.index(0, *at, 0)].clone()
+    flat[c.c.index(0, *at, 0)] = to_cache(torch.ones(c.c.dim), cache)
+    tree[4, 0] |= 1 << 2  # row 4 sees an infinite V: infinite or NaN itself, the others are not
+    out = check_attention(c, tree, False)
+    assert not torch.isfinite(out[4]).all() and torch.isfinite(out[:4]).all() and torch.isfinite(out[5:]).all()
+    flat[c.c.index(0, *at, 0)] = keep
+
+
+def test_attention_missing_blocks():
+    for layout in LAYOUTS:
+        c = Case(layout, BF16, [70, 33], [5, 2], heads=1)
+        c.table[0, 1] = -1
+        c.table[0, 4] = c.c.blocks + 7
+        c.table[1, :] = -1  # nothing there at all
+        check_attention(c, tree_bits(c.counts, c.g), True)
+
+
+def test_attention_large_and_equal_logits():
+    c = Case("hnd", BF16, [300], [4], heads=1)
+    check_attention(c, std=60.0)
+    c = Case("hnd", BF16, [300], [4], heads=1)
+    check_attention(c, q=torch.zeros(4, 4, 128, dtype=BF16), scores=True)  # all weights equal
+    c = Case("hnd", F16, [300], [4], heads=1, dtype=F16)
+    check_attention(c, scale=-0.3)
+
+
+def test_attention_strides_alignment_and_in_place():
+    def odd(x):
+        n, h, d = x.shape
+        buf = torch.zeros(h, n, d + 3, dtype=x.dtype, device="cuda")
+        view = buf[:, :, 1: 1 + d].permute(1, 0, 2)
+        view.copy_(x)
+        return view
+    for in_place in (False, True):
+        c = Case("piece", BF16, [30, 100], [7, 40], dim=72, tokens=8)
+        check_attention(c, tree_bits(c.counts, c.g), q_view=odd, in_place=in_place)
+        c = Case("hnd", BF16, [30, 2000], [7, 3], heads=1)
+        check_attention(c, in_place=in_place)
+
+
+def test_attention_bounds_of_the_call():
+    """Lengths, starts and bounds that do not fit: what is past them is left out, and nothing else is touched."""
+    c = Case("piece", BF16, [-5, 40, 1000], [3, 4, 2], heads=1)
+    c.lens[2] = 20
+    c = Case("piece", BF16, [0, 40, 20], [3, 4, 2], heads=1)
+    c.lens[0] = -5
+    check_attention(c)
+    c = Case("piece", BF16, [10, 40, 20], [3, 4, 2], heads=1)
+    c.q_start = torch.tensor([2, 5, 4, 9999], dtype=torch.int32)
+    check_attention(c)
+    c = Case("piece", BF16, [10, 40, 20], [3, 4, 2], heads=1)
+    c.max_tokens, c.max_len = 2, 30
+    check_attention(c)
+    c = Case("piece", BF16, [10, 40, 20], [3, 3, 3], heads=1, q_start=False)
+    check_attention(c, scores=True)
+
+
+def test_attention_trees_wider_than_a_word_and_short_ones():
+    c = Case("hnd", BF16, [100, 3], [130, 70], heads=1, group=2, dim=64)
+    check_attention(c, tree_bits(c.counts, c.g), True)
+    c = Case("hnd", BF16, [100, 3], [130, 70], heads=1, group=2, dim=64)
+    check_attention(c, tree_bits(c.counts, c.g)[:, :1].contiguous())  # drafted tokens past the words are not seen
+
+
+def test_attention_on_another_stream_and_captured():
+    c = Case("hnd", BF16, [3000, 70], [2, 3], heads=2)
+    q = normal(c.g, c.total, c.heads_q, 128).to(BF16).cuda()
+    layer, seqs, lay = c.flat[0].cuda(), c.seqs(), c.layout()
+    want = mma.mma_kv_attention(lay, layer, seqs, q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = mma.mma_kv_attention(lay, layer, seqs, q, stream=side)
+    side.synchronize()
+    assert same_bits(got, want)
+    out = torch.empty_like(q)
+    ws = torch.empty(mma.kv_attention_workspace(lay, seqs, q.shape[0], q.shape[1], q.dtype), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mma.mma_kv_attention(lay, layer, seqs, q, out=out, workspace=ws)
+    for _ in range(3):
+        out.zero_()
+        ws.random_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same_bits(out, want)
+
+
+# ------------------------------------------------------------------ commit
+@pytest.mark.parametrize("layout,cache,dim,tokens", [("piece", BF16, 128, 16), ("hnd", F8, 80, 5), ("xpacked", F16, 64, 8),
+                                                     ("xpacked", F8, 128, 16), ("piece", F8, 16, 1)])
+def test_commit(layout, cache, dim, tokens):
+    log(f"commit {layout} {cache}")
+    c = Case(layout, cache, [7, 0, 30, 12, 3], [12, 9, 20, 6, 8], dim, 2, 2, tokens, layers=3)
+    acc = torch.full((5, 10), -1, dtype=torch.int32)
+    lists = [[0, 2, 3, 7, 8, 9, 11], [0, 1, 2], [], [1, 3, 3, 4], [0, 5, 99, 6]]  # the last two stop short
+    for s, a in enumerate(lists):
+        acc[s, : len(a)] = torch.tensor(a, dtype=torch.int32)
+    counts = torch.tensor([7, 3, -2, 4, 4], dtype=torch.int32)
+    moves, lens = ok.commit_moves(acc, counts, c.spans())
+    assert [len(m) for m in moves] == [7, 3, 0, 2, 2]
+    layers = [x.clone().cuda() for x in c.flat]
+    scores = [torch.rand(5, 2, c.max_len + 3, generator=c.g) for _ in layers]
+    dev = [x.cuda() for x in scores]
+    new = mma.mma_kv_commit(c.layout(), layers, c.seqs(), acc.cuda(), counts.cuda(), scores=dev)
+    assert new.tolist() == lens
+    for l in range(3):
+        want, sc = c.flat[l], scores[l].clone()
+        for s in range(5):
+            want = ok.move_entries(c.c, want, c.table[s], c.table[s], moves[s])
+            for a, b in moves[s]:
+                sc[s, :, b] = sc[s, :, a]
+        assert same_bits(layers[l].cpu(), want) and torch.equal(dev[l].cpu(), sc)
+    again = [x.clone().cuda() for x in c.flat]
+    mma.mma_kv_commit(c.layout(), again, c.seqs(), acc.cuda(), counts.cuda())
+    assert all(same_bits(a, b) for a, b in zip(again, layers))
+
+
+def test_commit_more_layers_than_a_launch_and_missing_blocks():
+    c = Case("hnd", BF16, [7, 20], [12, 9], 16, 1, 1, 4, layers=200)
+    c.table[0, 3] = -1
+    acc = torch.tensor([[1, 4, 6, 11], [0, 3, 5, 8]], dtype=torch.int32)
+    counts = torch.tensor([4, 9], dtype=torch.int32)  # the second is cut to the width
+    moves, lens = ok.commit_moves(acc, counts, c.spans())
+    layers = [x.clone().cuda() for x in c.flat]
+    assert mma.mma_kv_commit(c.layout(), layers, c.seqs(), acc.cuda(), counts.cuda()).tolist() == lens == [11, 24]
+    for l in (0, 1, 191, 192, 199):
+        want = c.flat[l]
+        for s in range(2):
+            want = ok.move_entries(c.c, want, c.table[s], c.table[s], moves[s])
+        assert same_bits(layers[l].cpu(), want), l
+
+
+# ------------------------------------------------------------------ evict
+def check_evict(c, keep, sinks, recent, scores):
+    S, H = len(c.lens), c.c.heads
+    width = -(-keep // c.c.tokens)
+    free = [b for b in range(c.c.blocks) if b not in set(c.table.flatten().tolist())]
+    dst = torch.full((S, width), -1, dtype=torch.int32)
+    for s, n in enumerate(c.lens):
+        for b in range(-(-min(max(n, 0), keep) // c.c.tokens)):
+            dst[s, b] = free.pop()
+    layer = c.flat[0].cuda()
+    got, kept, lens = mma.mma_kv_evict(c.layout(), layer, c.seqs(), dst.cuda(), scores.cuda(), keep, sinks=sinks, recent=recent)
+    torch.cuda.synchronize()
+    want, out = c.flat[0], torch.full((S, H, keep), -1, dtype=torch.int32)
+    ws = torch.zeros(S, H, keep)
+    for s, n in enumerate(c.lens):
+        n = min(max(n, 0), c.max_len)
+        for h in range(H):
+            stay = ok.evict_select(scores[s, h], n, keep, sinks, recent)
+            out[s, h, : len(stay)] = torch.tensor(stay, dtype=torch.int32)
+            ws[s, h, : len(stay)] = scores[s, h, stay]
+            want = ok.move_entries(c.c, want, c.table[s], dst[s], [(j, i) for i, j in enumerate(stay)], [h])
+    assert lens.tolist() == [min(max(n, 0), keep, c.max_len) for n in c.lens]
+    assert torch.equal(got.cpu(), out)
+    assert same_bits(kept.cpu(), ws)
+    assert same_bits(layer.cpu(), want)
+
+
+def evict_case(layout, cache, lens, keep, dim=64, heads=2, tokens=16, seed=0):
+    c = Case(layout, cache, lens, [0] * len(lens), dim, heads, 1, tokens, seed=seed)
+    extra = sum(-(-min(max(n, 0), keep) // tokens) for n in lens)  # blocks for what stays
+    c.c = ok.Cache(layout, cache, c.c.blocks + extra, tokens, heads, dim)
+    c.flat = to_cache(normal(c.g, 2 * c.c.blocks * c.c.piece), cache).view(1, -1)
+    c.max_len = max(lens + [1])
+    return c
+
+
+@pytest.mark.parametrize("layout,cache,tokens", [("piece", BF16, 16), ("hnd", F8, 5), ("xpacked", F16, 8), ("xpacked", F8, 16)])
+@pytest.mark.parametrize("keep,sinks,recent", [(40, 4, 10), (33, 0, 0), (20, 4, 16), (1, 0, 1), (1, 0, 0)])
+def test_evict(layout, cache, tokens, keep, sinks, recent):
+    log(f"evict {layout} {cache} keep {keep}")
+    c = evict_case(layout, cache, [100, 0, 1, keep, keep + 1, 77], keep, tokens=tokens)
+    check_evict(c, keep, sinks, recent, torch.rand(6, 2, c.max_len + 3, generator=c.g))
+
+
+@pytest.mark.parametrize("n,keep", [(5000, 1200), (1025, 1024), (3000, 1)])
+def test_evict_long(n, keep):
+    c = evict_case("hnd", F8, [n, n // 2 + 1], keep, dim=16, heads=2)
+    check_evict(c, keep, 0, min(3, keep), torch.exp(3 * normal(c.g, 2, 2, n)))
+
+
+def test_evict_ties_and_special_scores():
+    """Equal scores go to the lower entry, zeros of both signs are equal, NaN is below -infinity."""
+    c = evict_case("piece", BF16, [300, 200], 90)
+    s = torch.randint(0, 4, (2, 2, 300), generator=c.g).float()
+    s[0, 1] = 0
+    s[1, 0, ::3] = -0.0
+    s[1, 1] = torch.tensor([math.nan, -math.inf, math.inf, -1.0, 1e-42, -0.0, 0.0, 3e38]).repeat(38)[:300]
+    check_evict(c, 90, 2, 5, s)
+    c = evict_case("piece", BF16, [300, 200], 90)
+    check_evict(c, 90, 0, 0, -torch.exp(normal(c.g, 2, 2, 300)))
+
+
+def test_evict_missing_blocks():
+    c = evict_case("piece", BF16, [100], 40)
+    c.table[0, 2] = -1
+    check_evict(c, 40, 4, 4, torch.rand(1, 2, 100, generator=c.g))
+
+
+# ------------------------------------------------------------------ refusals
+def refused(call, name="MMA_ERR_INVALID_ARG"):
+    with pytest.raises(mma.MMAError) as e:
+        call()
+    assert e.value.name == name, e.value
+
+
+def test_refusals():
+    c = Case("piece", BF16, [40], [3], heads=2)
+    lay, seqs, layer = c.layout(), c.seqs(), c.flat[0].cuda()
+    q = torch.zeros(3, 8, 128, dtype=BF16, device="cuda")
+    k = q[:, :2]
+    att = lambda lay=lay, layer=layer, seqs=seqs, q=q, **kw: mma.mma_kv_attention(lay, layer, seqs, q, **kw)  # noqa: E731
+    app = lambda lay=lay, layer=layer, seqs=seqs, q=q, k=k, **kw: mma.mma_kv_append(lay, layer, seqs, q, k, k, **kw)  # noqa: E731
+
+    def other(**kw):
+        f = dict(num_layers=1, block_tokens=16, kv_heads=2, head_dim=128, elem_bytes=2, gpu_num_blocks=c.c.blocks,
+                 host_num_slots=1, gpu_layout=0)
+        f.update(kw)
+        return mma.kv_layout(*f.values())
+    for bad in (dict(gpu_layout=3), dict(block_tokens=0), dict(elem_bytes=4), dict(gpu_num_blocks=c.c.blocks + 1000),
+                dict(gpu_layout=1, block_tokens=4)):
+        refused(lambda: att(other(**bad)))
+    wide = torch.zeros(3, 8, 264, dtype=BF16, device="cuda")
+    refused(lambda: att(other(head_dim=264), q=wide))
+    refused(lambda: att(other(head_dim=12), q=wide[:, :, :12]))
+    refused(lambda: att(other(kv_heads=3, gpu_num_blocks=1)))      # 8 query heads over 3
+    refused(lambda: att(layer=layer.data_ptr() + 2))               # 16-byte alignment
+    refused(lambda: att(layer=torch.zeros(64)))                    # host memory
+    refused(lambda: att(layer=0))
+    refused(lambda: att(seqs=c.seqs(max_len=0)))
+    refused(lambda: att(seqs=c.seqs(max_len=c.table.shape[1] * 16 + 1)))
+    refused(lambda: att(scores_out=torch.zeros(1, 2, c.max_len - 1, device="cuda")))
+    refused(lambda: att(out=torch.zeros(1, 8, 128, dtype=BF16, device="cuda").expand(3, 8, 128)))  # rows overlap
+    refused(lambda: app(q_out=torch.zeros(3, 1, 128, dtype=BF16, device="cuda").expand(3, 8, 128)))
+    pos = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for rot in (7, 130):
+        refused(lambda: app(positions=pos, rope=torch.zeros(64, rot, device="cuda")))
+    refused(lambda: app(q_weight=torch.ones(128, dtype=BF16, device="cuda"), eps=-1.0))
+    long = Case("piece", BF16, [4000], [3], heads=2)
+    refused(lambda: mma.mma_kv_attention(long.layout(), long.flat[0].cuda(), long.seqs(), q,
+                                         workspace=torch.empty(256, dtype=torch.uint8, device="cuda")), "MMA_ERR_BUFFER_TOO_SMALL")
+    dst = torch.zeros(1, 2, dtype=torch.int32, device="cuda")
+    sc = torch.zeros(1, 2, 64, device="cuda")
+    ev = lambda keep, dst=dst, sc=sc, **kw: mma.mma_kv_evict(lay, layer, seqs, dst, sc, keep, **kw)  # noqa: E731
+    refused(lambda: ev(33))                       # two blocks hold 32
+    refused(lambda: ev(20, sinks=10, recent=11))
+    refused(lambda: ev(20, sc=torch.zeros(1, 2, 42, device="cuda")))
+    acc = torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+    refused(lambda: mma.mma_kv_commit(lay, [0], seqs, acc, acc[:, 0].contiguous()))
+    refused(lambda: mma.mma_kv_commit(lay, [layer], seqs, acc, acc[0, :1], scores=[torch.zeros(1, 2, 20, device="cuda")]))
+    a = mma.mma_kv_commit_t(acc.data_ptr(), acc.data_ptr(), seqs.tensors[1].data_ptr(), 0, 4, 0)
+    assert mma.lib.mma_kv_commit(lay, mma.layer_table([layer]), seqs.c, a, 0) == mma.MMA_ERR_INVALID_ARG
+    for call in (lambda: att(q=q.float()), lambda: att(q=q[:, :, :64]), lambda: app(k=q[:, :3]),
+                 lambda: att(tree=torch.zeros(2, 1, dtype=torch.int64, device="cuda")), lambda: att(q=q.cpu()),
+                 lambda: att(lse=torch.zeros(3, 7, device="cuda")), lambda: app(rope=torch.zeros(4, 8, device="cuda")),
+                 lambda: att(scores_in=sc), lambda: ev(0)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_nothing_to_do():
+    c = Case("piece", BF16, [40], [0], heads=2)
+    q = torch.zeros(0, 8, 128, dtype=BF16, device="cuda")
+    layer = c.flat[0].cuda()
+    assert mma.mma_kv_attention(c.layout(), layer, c.seqs(), q).shape == (0, 8, 128)
+    assert mma.mma_kv_append(c.layout(), layer, c.seqs(), q, q[:, :2], q[:, :2]).shape == (0, 8, 128)
+    assert same_bits(layer.cpu(), c.flat[0])
