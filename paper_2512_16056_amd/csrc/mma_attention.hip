@@ -14,11 +14,15 @@
 // a row are a lane's own but for two exchanges between its 4 lanes, and a lane's 8 keys lie
 // in one block (if blocks hold a multiple of 8). The same holds for the head's values in
 // Q K^T, which is what lets 8-bit keys be read 16 bytes at a time.
-// V^T comes as 8 keys' rows of the lane's head values, turned in registers (v_perm), or
-// from the x-packed layout, where 8 tokens of a value are contiguous, as it stands.
+//
+// Two kernels share that arithmetic. attention_stream_kernel, for up to 32 rows, reads keys
+// and values from memory straight into the registers of the instructions; its waves split the
+// entries. attention_rows_kernel, for more rows, brings tiles to LDS once for the
+// workgroup's 128 rows; its waves split the rows.
 #include "mma_ops.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mma {
 namespace {
@@ -79,21 +83,6 @@ __device__ __forceinline__ float to_float(uint32_t bits16) {
 
 __device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, kOpsWave); }
 
-// Shape of a kernel: head padded to DP values; CE values of an entry's V in one lane, over
-// 16 lanes and NP panels; KS instructions of 32 values for a tile of keys.
-template <bool F8, int DP, bool VX>
-struct Shape {
-  static constexpr int E = F8 ? 1 : 2;
-  static constexpr int KS = DP / 32;
-  static constexpr int CE = DP == 64 ? 4 : 8;
-  static constexpr int NP = DP / (16 * CE);
-  static constexpr int NC = NP * CE;  // instructions of 16 head values
-  // Head value of V^T row r (0..15) of instruction c.
-  static __device__ __forceinline__ uint32_t value_at(int c, uint32_t r) {
-    return VX ? c * 16 + r : (c / CE) * 16 * CE + r * CE + c % CE;
-  }
-};
-
 // 8 consecutive values of one row from global memory, elements at any alignment if not wide.
 __device__ __forceinline__ u32x4 load_row8(const uint8_t* p, bool wide) {
   if (wide) return *reinterpret_cast<const u32x4*>(p);
@@ -105,187 +94,20 @@ __device__ __forceinline__ u32x4 load_row8(const uint8_t* p, bool wide) {
 }
 
 // Q of 16 rows as the second operand of K Q^T. The head values of instruction s of lane
-// group g start at 32 s + 8 g, or for 8-bit keys at 64 (s / 2) + 16 g + 8 (s % 2).
-template <bool F8, int KS>
+// group g start at 32 s + 8 g, or where 8-bit keys are in registers at 64 (s / 2) + 16 g + 8 (s % 2).
+template <bool PAIRED, int KS>
 __device__ __forceinline__ void load_q(const AttnArgs& a, uint32_t head, uint32_t token, bool live, uint32_t g, u32x4* q) {
   const uint8_t* p = a.q.data + 2 * (token * a.q.token + head * a.q.head);
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    const uint32_t d = F8 ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8;
+    const uint32_t d = PAIRED ? (s / 2) * 64 + g * 16 + (s % 2) * 8 : s * 32 + g * 8;
     q[s] = live && d < a.c.dim ? load_row8(p + 2 * d, a.wide_q) : u32x4{0, 0, 0, 0};
   }
 }
 
-// Blocks of the 8 keys key .. key + 7 (a lane's own): one if blocks hold a multiple of 8.
-struct Keys {
-  int32_t block[8];
-  uint32_t token[8];
-  uint32_t ok;  // bit j: key + j is below `end` and its block is there
-};
-
-// A tile of keys as the first operand: halves t, instruction s. Raw bytes for 8-bit keys:
-// 16 of them serve instructions 2 s and 2 s + 1.
-template <bool F8, int KS>
-struct KeyTile {
-  static constexpr int N = F8 ? KS / 2 : KS;
-  u32x4 w[2][N];
-  template <class T>
-  __device__ __forceinline__ u32x4 operand(int t, int s) const {
-    if constexpr (!F8) {
-      return w[t][s];
-    } else {
-      const uint32_t x = w[t][s / 2][(s % 2) * 2], y = w[t][s / 2][(s % 2) * 2 + 1];
-      return u32x4{Type<T>::from_f8(x, false), Type<T>::from_f8(x, true), Type<T>::from_f8(y, false),
-                   Type<T>::from_f8(y, true)};
-    }
-  }
-};
-
-// Address of a key's first byte, with its block clamped into the cache.
-__device__ __forceinline__ const uint8_t* key_at(const CacheArgs& c, const int32_t* row, uint32_t key, uint32_t head) {
-  uint32_t token;
-  const int32_t id = block_at(c, row, key, &token);
-  return c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * c.block_bytes + head * c.k_head + token * c.k_token;
-}
-
-// Keys base .. base + 31 of one head; `last` is the last entry that may be looked up.
-template <bool F8, int KS>
-__device__ __forceinline__ void load_keys(const CacheArgs& c, const int32_t* row, uint32_t base, uint32_t last, uint32_t head,
-                                          uint32_t g, uint32_t m, KeyTile<F8, KS>& k) {
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    uint32_t key = base + (m / 4) * 8 + t * 4 + m % 4;
-    if (key > last) key = last;
-    const uint8_t* p = key_at(c, row, key, head);
-#pragma unroll
-    for (int s = 0; s < KeyTile<F8, KS>::N; ++s) {
-      const uint32_t chunk = s * 4 + g;  // of 16 bytes
-      k.w[t][s] = chunk * (F8 ? 16 : 8) < c.dim ? *reinterpret_cast<const u32x4*>(p + static_cast<uint64_t>(chunk) * c.k_chunk)
-                                                : u32x4{0, 0, 0, 0};
-    }
-  }
-}
-
-// V^T of a tile: operand c has head value value_at(c, m) of keys base + 8 g .. + 7.
-template <class T, bool F8, int DP, bool VX>
-struct ValueTile {
-  typedef Shape<F8, DP, VX> S;
-  u32x4 op[S::NC];
-
-  __device__ __forceinline__ void load(const CacheArgs& c, const int32_t* row, uint32_t base, uint32_t last, uint32_t head,
-                                       uint32_t g, uint32_t m) {
-    const uint8_t* at[8];
-    const uint32_t first = base + g * 8;
-    const bool one = c.tokens % 8 == 0;
-    if constexpr (VX) {
-      uint32_t token;
-      const int32_t id = block_at(c, row, first > last ? last - last % 8 : first, &token);
-      const uint8_t* p = c.v + static_cast<uint64_t>(id < 0 ? 0 : id) * c.block_bytes + head * c.v_head + token * c.v_token;
-#pragma unroll
-      for (int n = 0; n < S::NC; ++n) {
-        const uint32_t d = S::value_at(n, m);
-        const uint8_t* q = p + static_cast<uint64_t>(d) * c.v_chunk;
-        if constexpr (F8) {
-          const u32x2 w = d < c.dim ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
-          op[n] = u32x4{Type<T>::from_f8(w[0], false), Type<T>::from_f8(w[0], true), Type<T>::from_f8(w[1], false),
-                        Type<T>::from_f8(w[1], true)};
-        } else {
-          op[n] = d < c.dim ? *reinterpret_cast<const u32x4*>(q) : u32x4{0, 0, 0, 0};
-        }
-      }
-    } else {
-      if (one) {
-        uint32_t token;
-        const int32_t id = block_at(c, row, first > last ? last : first, &token);
-        const uint32_t stay = first > last ? 0 : 1;  // past the end: the last entry, eight times
-        const uint8_t* p = c.v + static_cast<uint64_t>(id < 0 ? 0 : id) * c.block_bytes + head * c.v_head;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) at[j] = p + static_cast<uint64_t>(token + j * stay) * c.v_token;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t token;
-          const int32_t id = block_at(c, row, first + j > last ? last : first + j, &token);
-          at[j] = c.v + static_cast<uint64_t>(id < 0 ? 0 : id) * c.block_bytes + head * c.v_head +
-                  static_cast<uint64_t>(token) * c.v_token;
-        }
-      }
-      constexpr int W = S::CE / 2;  // dwords of 16-bit values in a lane's part of a panel
-#pragma unroll
-      for (int n = 0; n < S::NP; ++n) {
-        const uint32_t d = n * 16 * S::CE + m * S::CE;
-        const bool live = d < c.dim;
-        uint32_t w[8][W];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint8_t* q = at[j] + d * S::E;  // a row is contiguous
-          if constexpr (F8) {
-            uint32_t b[W / 2];
-            if constexpr (W == 4) {
-              const u32x2 x = live ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
-              b[0] = x[0];
-              b[1] = x[1];
-            } else {
-              b[0] = live ? *reinterpret_cast<const uint32_t*>(q) : 0;
-            }
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[j][i] = Type<T>::from_f8(b[i / 2], i % 2);
-          } else if constexpr (W == 4) {
-            const u32x4 x = live ? *reinterpret_cast<const u32x4*>(q) : u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < W; ++i) w[j][i] = x[i];
-          } else {
-            const u32x2 x = live ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
-            w[j][0] = x[0];
-            w[j][1] = x[1];
-          }
-        }
-        // 8 keys x CE values: value e of keys 2 i and 2 i + 1 side by side
-#pragma unroll
-        for (int e = 0; e < S::CE; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            op[n * S::CE + e][i] =
-                __builtin_amdgcn_perm(w[2 * i + 1][e / 2], w[2 * i][e / 2], e % 2 ? 0x07060302u : 0x05040100u);
-      }
-    }
-  }
-
-  // Keys whose bit in `ok` is clear count as 0.
-  __device__ __forceinline__ void keep(uint32_t ok) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t mask = (ok >> (2 * i) & 1 ? 0xffffu : 0u) | (ok >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
-#pragma unroll
-      for (int n = 0; n < S::NC; ++n) op[n][i] &= mask;
-    }
-  }
-  // Bits of the keys with an infinity or NaN among the lane's values, which become 0.
-  __device__ __forceinline__ uint32_t drop_nonfinite() {
-    uint32_t bad = 0;
-#pragma unroll
-    for (int n = 0; n < S::NC; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t w = op[n][i], lo = w & 0xffffu, hi = w >> 16, x = Type<T>::kExponent;
-        const bool l = (lo & x) == x, h = (hi & x) == x;
-        bad |= (l ? 1u : 0u) << (2 * i) | (h ? 1u : 0u) << (2 * i + 1);
-        op[n][i] = (l ? 0 : lo) | (h ? 0 : hi << 16);
-      }
-    return bad;
-  }
-};
-
-// The value at head value d of one entry, as a float.
-template <class T, bool F8, bool VX>
-__device__ __forceinline__ float value_of(const CacheArgs& c, const int32_t* row, uint32_t key, uint32_t head, uint32_t d) {
-  uint32_t token;
-  const int32_t id = block_at(c, row, key, &token);
-  if (id < 0 || d >= c.dim) return 0;
-  const uint8_t* p = c.v + static_cast<uint64_t>(id) * c.block_bytes + head * c.v_head + static_cast<uint64_t>(token) * c.v_token +
-                     (VX ? static_cast<uint64_t>(d) * c.v_chunk : static_cast<uint64_t>(d) * (F8 ? 1 : 2));
-  if constexpr (F8) return to_float<T>(Type<T>::from_f8(*p, false));
-  return to_float<T>(*reinterpret_cast<const uint16_t*>(p));
+template <class T>
+__device__ __forceinline__ u32x4 widen(uint32_t x, uint32_t y) {  // 8 values of 8 bits to 16 bits
+  return u32x4{Type<T>::from_f8(x, false), Type<T>::from_f8(x, true), Type<T>::from_f8(y, false), Type<T>::from_f8(y, true)};
 }
 
 // Bit j: entry first + j, below `end`, has a block.
@@ -303,30 +125,214 @@ __device__ __forceinline__ uint32_t keys_there(const CacheArgs& c, const int32_t
 
 // Bit j: token `token` of a sequence (row `first` + token of the call) sees entry key + j.
 __device__ __forceinline__ uint32_t keys_seen(const AttnArgs& a, const SeqSpan& sp, uint32_t token, uint32_t key) {
-  uint32_t seen = 0;
-#pragma unroll
-  for (uint32_t j = 0; j < 8; ++j) {
-    bool see = key + j < sp.before;
-    if (!see) {
-      const uint32_t d = key + j - sp.before;
-      if (!a.tree)
-        see = d <= token;
-      else if (d / 64 < a.tree_words)
-        see = a.tree[static_cast<uint64_t>(sp.first + token) * a.tree_words + d / 64] >> (d % 64) & 1;
-    }
-    seen |= (see ? 1u : 0u) << j;
+  const int32_t d = static_cast<int32_t>(key) - static_cast<int32_t>(sp.before);  // the first key's token, below 0 for the context
+  if (d <= -8) return 0xff;
+  if (!a.tree) {
+    const int32_t n = static_cast<int32_t>(token) + 1 - d;  // keys up to its own
+    return n >= 8 ? 0xffu : n <= 0 ? 0u : (1u << n) - 1;
   }
-  return seen;
+  const uint64_t* bits = a.tree + static_cast<uint64_t>(sp.first + token) * a.tree_words;
+  const uint32_t from = d < 0 ? 0 : d, word = from / 64, shift = from % 64;
+  uint64_t w = word < a.tree_words ? bits[word] >> shift : 0;
+  if (shift > 56 && word + 1 < a.tree_words) w |= bits[word + 1] << (64 - shift);
+  return d < 0 ? ((static_cast<uint32_t>(w) << -d) | ((1u << -d) - 1)) & 0xff : static_cast<uint32_t>(w) & 0xff;
 }
 
-// ---------------------------------------------------------------- the main kernel
+// 16-bit halves of an operand whose keys' bits are set; the others 0.
+__device__ __forceinline__ u32x4 only_keys(u32x4 w, uint32_t keys) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] &= (keys >> (2 * i) & 1 ? 0xffffu : 0u) | (keys >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+  return w;
+}
+// Bits of the keys whose value is infinite or NaN.
+template <class T>
+__device__ __forceinline__ uint32_t nonfinite_keys(u32x4 w) {
+  uint32_t bad = 0;
+  constexpr uint32_t x = Type<T>::kExponent;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= ((w[i] & x) == x ? 1u : 0u) << (2 * i) | ((w[i] >> 16 & x) == x ? 1u : 0u) << (2 * i + 1);
+  return bad;
+}
+
+// O^T += V^T P^T over 32 keys: operand c of V^T from op(c).
+template <class T, int R, int NC, class Op>
+__device__ __forceinline__ void add_values(Op op, const u32x4 (&p)[R], f32x4 (&o)[R][NC]) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const u32x4 v = op(c);
+#pragma unroll
+    for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[r], o[r][c]);
+  }
+}
+
+// The same where not every row sees every key: keys outside `ok` (stale ones in registers) count
+// as 0, and an infinite or NaN value of a key reaches the rows that see the key, no others,
+// though a product with a probability of 0 would bring NaN to all. Such keys are left out of the
+// joint product and added one by one to the rows that see them.
+template <class T, int R, int NC, class Op>
+__device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[R], const uint32_t (&seen)[R], uint32_t ok,
+                                                  uint32_t g, uint32_t m, f32x4 (&o)[R][NC]) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    u32x4 v = only_keys(op(c), ok);
+    const uint32_t n = nonfinite_keys<T>(v);
+    bad |= n;
+    v = only_keys(v, ~n);
+#pragma unroll
+    for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[r], o[r][c]);
+  }
+  if (!__any(bad)) return;
+  for (uint32_t j = 0; j < kTile; ++j) {
+    if (!__any(g == j / 8 && (bad >> (j % 8) & 1))) continue;
+    const uint32_t mine = g == j / 8 ? 1u << (j % 8) : 0u;
+    uint32_t sees[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) sees[r] = __shfl(seen[r], (j / 8) * 16 + m, kOpsWave) >> (j % 8) & 1;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      u32x4 v = only_keys(op(c), mine & ok);
+      v = only_keys(v, nonfinite_keys<T>(v));
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const f32x4 d = Type<T>::mfma(v, only_keys(p[r], mine), f32x4{0, 0, 0, 0});
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[r][c][i] = sees[r] ? o[r][c][i] + d[i] : o[r][c][i];
+      }
+    }
+  }
+}
+
+// What a row's result goes to: the output and lse, or with several splits this split's part of them.
+template <class T, int DP, int NC, class At>
+__device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uint32_t qh, uint32_t split, uint32_t g, float top,
+                                          float sum, float v_scale, const f32x4 (&o)[NC], At value_at) {
+  const uint64_t unit = static_cast<uint64_t>(token) * a.q_heads + qh;
+  if (a.part_ml && !g) {
+    float* ml = a.part_ml + 2 * (unit * a.splits + split);
+    ml[0] = top;
+    ml[1] = sum;
+  }
+  if (a.splits > 1) {
+    float* to = a.part + (unit * a.splits + split) * DP;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[value_at(c, g * 4 + i)] = o[c][i] * v_scale;
+    return;
+  }
+  const float by = sum == 0 ? 0.0f : v_scale / sum;
+  T* to = reinterpret_cast<T*>(a.out.data) + token * a.out.token + qh * a.out.head;
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t d = value_at(c, g * 4 + i);
+      if (d < a.c.dim) to[d] = static_cast<T>(o[c][i] * by);
+    }
+  if (!g) {
+    const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    if (a.lse) a.lse[unit] = l2 * kLn2;
+    if (a.lse2) a.lse2[unit] = l2;
+  }
+}
+
+// ---------------------------------------------------------------- few rows
 // A workgroup has R tiles of rows of one sequence and KV head and one split of its
 // entries; its 4 waves take the split's tiles in turn, each with its own running maximum
 // and sum, and are joined in LDS at the end. Nothing is shared before that: a tile's
-// bytes go from memory to the registers that the matrix instructions read.
+// bytes go from memory to the registers that the matrix instructions read. V^T comes as 8
+// keys' rows of the lane's head values, turned in registers (v_perm), or from the x-packed
+// layout, where 8 tokens of a value are contiguous, as it stands. Blocks hold a multiple of 8
+// tokens here: a lane's keys of a tile and its values' keys are in one block each, whose
+// table entries are read two tiles ahead, keys one tile ahead, values in the tile.
+template <bool F8, int DP, bool VX>
+struct Stream {
+  static constexpr int KS = DP / 32;                  // instructions of 32 head values
+  static constexpr int NK = F8 ? KS / 2 : KS;         // 16-byte chunks of a key in one lane
+  static constexpr int CE = DP == 64 ? 4 : 8;         // values of an entry's V in one lane and panel
+  static constexpr int NP = DP / (16 * CE);           // panels
+  static constexpr int NC = DP / 16;                  // instructions of 16 head values
+  static constexpr int VW = VX ? (F8 ? 2 : 4) : CE / (F8 ? 4 : 2);  // dwords of a load of V
+  static constexpr int NV = VX ? NC : NP * 8;                       // loads of V
+  // Head value of V^T row r (0..15) of instruction c.
+  static __device__ __forceinline__ uint32_t value_at(int c, uint32_t r) {
+    return VX ? c * 16 + r : (c / CE) * 16 * CE + r * CE + c % CE;
+  }
+
+  u32x4 k[2][NK];
+  uint32_t v[NV][VW];
+
+  __device__ __forceinline__ void load_keys(const CacheArgs& c, int32_t id, uint32_t key, uint32_t head, uint32_t g) {
+    const uint32_t token = key - block_of(c, key) * c.tokens;  // of the first half's key
+    const uint8_t* p = c.k + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.k_head +
+                       static_cast<uint64_t>(token) * c.k_token + static_cast<uint64_t>(g) * c.k_chunk;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const bool live = (s * 4 + g) * (F8 ? 16 : 8) < c.dim;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        k[t][s] = live ? *reinterpret_cast<const u32x4*>(p + static_cast<uint64_t>(s * 4) * c.k_chunk + t * 4 * static_cast<uint64_t>(c.k_token))
+                       : u32x4{0, 0, 0, 0};
+    }
+  }
+  template <class T>
+  __device__ __forceinline__ u32x4 key(int t, int s) const {
+    if constexpr (!F8) return k[t][s];
+    else return widen<T>(k[t][s / 2][s % 2 * 2], k[t][s / 2][s % 2 * 2 + 1]);
+  }
+
+  __device__ __forceinline__ void load_values(const CacheArgs& c, int32_t id, uint32_t first, uint32_t head, uint32_t m) {
+    const uint32_t token = first - block_of(c, first) * c.tokens;
+    const uint8_t* p = c.v + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.v_head +
+                       static_cast<uint64_t>(token) * c.v_token;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const uint32_t d = VX ? n * 16 + m : n / 8 * 16 * CE + m * CE;
+      const uint8_t* q = VX ? p + static_cast<uint64_t>(d) * c.v_chunk
+                            : p + static_cast<uint64_t>(n % 8) * c.v_token + d * (F8 ? 1 : 2);
+      const bool live = d < c.dim;
+      if constexpr (VW == 4) {
+        const u32x4 x = live ? *reinterpret_cast<const u32x4*>(q) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[n][i] = x[i];
+      } else if constexpr (VW == 2) {
+        const u32x2 x = live ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
+        v[n][0] = x[0];
+        v[n][1] = x[1];
+      } else {
+        v[n][0] = live ? *reinterpret_cast<const uint32_t*>(q) : 0;
+      }
+    }
+  }
+  // Operand c of V^T: value value_at(c, m) of the lane's 8 keys.
+  template <class T>
+  __device__ __forceinline__ u32x4 value(int c) const {
+    if constexpr (VX) {
+      if constexpr (F8) return widen<T>(v[c][0], v[c][1]);
+      else return u32x4{v[c][0], v[c][1], v[c][2], v[c][3]};
+    } else {
+      const int n = c / CE * 8, e = c % CE;
+      const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;  // value e of keys 2 i and 2 i + 1 side by side
+      u32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (F8)
+          r[i] = __builtin_amdgcn_perm(Type<T>::from_f8(v[n + 2 * i + 1][e / 4], e % 4 / 2),
+                                       Type<T>::from_f8(v[n + 2 * i][e / 4], e % 4 / 2), sel);
+        else
+          r[i] = __builtin_amdgcn_perm(v[n + 2 * i + 1][e / 2], v[n + 2 * i][e / 2], sel);
+      }
+      return r;
+    }
+  }
+};
+
 template <class T, bool F8, int DP, bool VX, int R>
-__global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
-  typedef Shape<F8, DP, VX> S;
+__global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
+  typedef Stream<F8, DP, VX> S;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t split = blockIdx.x % a.splits, group = blockIdx.x / a.splits;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
@@ -364,46 +370,71 @@ __global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
     for (int c = 0; c < S::NC; ++c) o[r][c] = f32x4{0, 0, 0, 0};
   }
 
+  // Keys of the first half: 8 (m / 4) + m % 4; a block's id of the lane's keys and of its values' keys,
+  // 0 where there is none (then the tile is masked). Past the end: the last entry's.
+  const uint32_t step = 4 * kTile;
   uint32_t base = begin + wave * kTile;
-  KeyTile<F8, S::KS> k;
-  if (base < end) load_keys<F8, S::KS>(a.c, table, base, end - 1, head, g, m, k);
-  for (; base < end; base += 4 * kTile) {
-    ValueTile<T, F8, DP, VX> v;
-    v.load(a.c, table, base, end - 1, head, g, m);
-    f32x4 s[R][2];
+  // All 8 keys of a group at once: the group's first key decides, and past the end it is the last key's group.
+  const auto clamp = [&](uint32_t first) { return first < end ? first : (end - 1) & ~7u; };
+  const auto id_of = [&](uint32_t first) { return table[block_of(a.c, clamp(first))]; };
+  const auto there = [&](int32_t id) { return static_cast<uint32_t>(id) < a.c.num_blocks; };
+  S s;
+  int32_t kid = 0, vid = 0;  // of this tile (values) and the next (keys)
+  if (base < end) {
+    kid = id_of(base + (m / 4) * 8);
+    vid = id_of(base + g * 8);
+    s.load_keys(a.c, there(kid) ? kid : 0, clamp(base + (m / 4) * 8) + m % 4, head, g);
+  }
+  int32_t next_kid = base + step < end ? id_of(base + step + (m / 4) * 8) : 0;
+  float* logits[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    logits[r] = a.logits && live[r] ? a.logits + ((static_cast<uint64_t>(seq) * a.c.heads + head) * a.logit_rows + row0 + r * 16 + m) * a.logit_stride + g * 8
+                                    : nullptr;
+  const auto tile = [&](auto masked, bool have) {
+    constexpr bool kMasked = decltype(masked)::value;
+    s.load_values(a.c, have ? vid : 0, clamp(base + g * 8), head, m);
+    f32x4 x[R][2];
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) s[r][t] = f32x4{0, 0, 0, 0};
+      for (int t = 0; t < 2; ++t) x[r][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < S::KS; ++i)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const u32x4 x = k.template operand<T>(t, i);
+        const u32x4 k = s.template key<T>(t, i);
 #pragma unroll
-        for (int r = 0; r < R; ++r) s[r][t] = Type<T>::mfma(x, q[r][i], s[r][t]);
+        for (int r = 0; r < R; ++r) x[r][t] = Type<T>::mfma(k, q[r][i], x[r][t]);
       }
-    if (base + 4 * kTile < end) load_keys<F8, S::KS>(a.c, table, base + 4 * kTile, end - 1, head, g, m, k);
-
-    const uint32_t ok = keys_there(a.c, table, base + g * 8, end);
-    const bool inner = base + kTile <= sp.before;  // every row sees every entry
-    const bool plain = __all(ok == 0xff) && inner;
+    if (base + step < end) {
+      s.load_keys(a.c, there(next_kid) ? next_kid : 0, clamp(base + step + (m / 4) * 8) + m % 4, head, g);
+      vid = id_of(base + step + g * 8);
+      if (base + 2 * step < end) next_kid = id_of(base + 2 * step + (m / 4) * 8);
+    }
+    uint32_t okay = 0xff, seen[R];
+    if constexpr (kMasked) {
+      const uint32_t first = base + g * 8;
+      okay = !have || first >= end ? 0 : end - first >= 8 ? 0xffu : (1u << (end - first)) - 1;
+    }
     u32x4 p[R];
-    uint32_t seen[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float x[8];
+      float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = s[r][j / 4][j % 4] * to_log2;
-      seen[r] = 0xff;
-      if (!plain) {
-        seen[r] = inner ? ok : ok & keys_seen(a, sp, token[r], base + g * 8);
+      for (int j = 0; j < 8; ++j) y[j] = x[r][j / 4][j % 4] * to_log2;
+      if constexpr (kMasked) {
+        seen[r] = okay & keys_seen(a, sp, token[r], base + g * 8);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = seen[r] >> j & 1 ? x[j] : -INFINITY;
+        for (int j = 0; j < 8; ++j) y[j] = seen[r] >> j & 1 ? y[j] : -INFINITY;
+      }
+      if (logits[r]) {  // kept for the entries' weights
+        *reinterpret_cast<f32x4*>(logits[r] + base) = f32x4{y[0], y[1], y[2], y[3]};
+        *reinterpret_cast<f32x4*>(logits[r] + base + 4) = f32x4{y[4], y[5], y[6], y[7]};
       }
       float mx = top[r];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, x[j]);
+      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, y[j]);
       mx = fmaxf(mx, across(mx, 16));
       mx = fmaxf(mx, across(mx, 32));
       const float fade = __builtin_amdgcn_exp2f(top[r] - mx);
@@ -411,47 +442,34 @@ __global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
       float add = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        x[j] = __builtin_amdgcn_exp2f(x[j] - mx);
-        add += x[j];
+        y[j] = __builtin_amdgcn_exp2f(y[j] - mx);
+        add += y[j];
       }
       sum[r] = sum[r] * fade + add;  // this lane's keys; its 4 lanes are joined at the end
       // The probabilities are rounded to the type's 16 bits for the product with V, as the
       // output is: an error of the same size as the output's own. Their sum is not rounded.
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[r][i] = Type<T>::pack(x[2 * i], x[2 * i + 1]);
+      for (int i = 0; i < 4; ++i) p[r][i] = Type<T>::pack(y[2 * i], y[2 * i + 1]);
 #pragma unroll
       for (int c = 0; c < S::NC; ++c) o[r][c] *= fade;
     }
-    uint32_t bad = 0;
-    if (!plain) {
-      v.keep(ok);
-      if (!inner) bad = v.drop_nonfinite();
-    }
-#pragma unroll
-    for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-      for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v.op[c], p[r], o[r][c]);
-    if (!plain && !inner && __any(bad)) {
-      // A drafted token's V is infinite or NaN: it reaches the rows that see it, no others.
-      for (uint32_t j = 0; j < kTile; ++j) {
-        if (!__any(bad >> (j % 8) & 1 && g == j / 8)) continue;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const uint32_t from = (j / 8) * 16 + m;
-          const uint32_t sees = __shfl(seen[r], from, kOpsWave) >> (j % 8) & 1;
-          const uint32_t pw = j % 8 < 2 ? p[r][0] : j % 8 < 4 ? p[r][1] : j % 8 < 6 ? p[r][2] : p[r][3];
-          const uint32_t pj = __shfl(pw, from, kOpsWave) >> (j % 2 * 16) & 0xffff;
-          if (!sees || !live[r]) continue;
-#pragma unroll
-          for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x = value_of<T, F8, VX>(a.c, table, base + j, head, S::value_at(c, g * 4 + i));
-              if (!__builtin_isfinite(x)) o[r][c][i] += to_float<T>(pj) * x;
-            }
-        }
-      }
-    }
+    const auto op = [&](int c) { return s.template value<T>(c); };
+    if constexpr (kMasked)
+      add_values_masked<T>(op, p, seen, okay, g, m, o);
+    else
+      add_values<T>(op, p, o);
+    base += step;
+  };
+  // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not there), masked ones.
+  const uint32_t whole = end < sp.before ? end : sp.before;
+  bool have = there(vid);
+  while (base + kTile <= whole && __all(have)) {
+    tile(std::false_type(), true);
+    have = there(vid);
+  }
+  while (base < end) {
+    tile(std::true_type(), have);
+    have = there(vid);
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -463,9 +481,9 @@ __global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
   constexpr int NO = R * S::NC * 4;
   __shared__ float part[2][NO + 2 * R][kOpsWave];
 #pragma unroll
-  for (uint32_t step = 2; step >= 1; step /= 2) {
-    if (wave >= step && wave < 2 * step) {
-      float(*to)[kOpsWave] = part[wave - step];
+  for (uint32_t half = 2; half >= 1; half /= 2) {
+    if (wave >= half && wave < 2 * half) {
+      float(*to)[kOpsWave] = part[wave - half];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         to[NO + 2 * r][lane] = top[r];
@@ -477,108 +495,497 @@ __global__ __launch_bounds__(256) void attention_kernel(AttnArgs a) {
       }
     }
     __syncthreads();
-    if (wave < step) {
+    if (wave < half) {
       const float(*from)[kOpsWave] = part[wave];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float t = from[NO + 2 * r][lane], u = from[NO + 2 * r + 1][lane];
         const float mx = fmaxf(top[r], t);
-        const float x = __builtin_amdgcn_exp2f(top[r] - mx), y = __builtin_amdgcn_exp2f(t - mx);
+        const float f = __builtin_amdgcn_exp2f(top[r] - mx), h = __builtin_amdgcn_exp2f(t - mx);
         top[r] = mx;
-        sum[r] = sum[r] * x + u * y;
+        sum[r] = sum[r] * f + u * h;
 #pragma unroll
         for (int c = 0; c < S::NC; ++c)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[r][c][i] = o[r][c][i] * x + from[(r * S::NC + c) * 4 + i][lane] * y;
+          for (int i = 0; i < 4; ++i) o[r][c][i] = o[r][c][i] * f + from[(r * S::NC + c) * 4 + i][lane] * h;
       }
     }
     __syncthreads();
   }
   if (wave) return;
-
   const float v_scale = a.v_scale ? a.v_scale[head] : 1.0f;
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    if (!live[r]) continue;
-    const uint32_t row = row0 + r * 16 + m, qh = head * a.group + row % a.group;
-    const uint64_t unit = static_cast<uint64_t>(sp.first + token[r]) * a.q_heads + qh;
-    if (a.splits > 1) {
-      float* to = a.part + (unit * a.splits + split) * DP;
+  for (int r = 0; r < R; ++r)
+    if (live[r])
+      store_row<T, DP>(a, sp.first + token[r], head * a.group + (row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r],
+                       S::value_at);
+}
+
+// ---------------------------------------------------------------- many rows
+// A workgroup has 64 RW rows of one sequence and KV head and one split of its entries; each
+// of its 4 waves has RW tiles of 16 rows and goes through all tiles of KT entries, which
+// the workgroup brings to LDS, two buffers in turn, one barrier a tile.
+//
+// 16-bit caches go from memory to LDS without registers (a lane's 16 bytes land at 16 times
+// its index, so the order within the tile is made by which chunk a lane asks for); 8-bit ones
+// pass through registers, where they are widened once for all waves. Rows of an entry lie
+// DP values apart with their 16-byte chunks exchanged by the entry's number in the tile (bits
+// 0, 1, 3, 4: what tells the 16 lanes of a read apart), so that neither the 16-byte reads of K
+// nor the transposing 8-byte reads of V (ds_read_b64_tr_b16: of 4 entries' 16 values each lane of
+// 16 gets one value of the 4) meet in a bank. x-packed values are V^T already.
+//
+// The maximum that probabilities are taken from follows the row's own only where it would
+// be passed by more than 2^8: the factor is 1 otherwise and nothing is scaled.
+template <bool F8, int DP, bool VX>
+struct Tiles {
+  static constexpr int KT = DP == 256 ? 32 : 64;  // entries of a tile
+  static constexpr int SUB = KT / 32;
+  static constexpr int KS = DP / 32;
+  static constexpr int NC = DP / 16;
+  static constexpr int C = DP / 8;                // 16-byte chunks of an entry
+  static constexpr int VC = KT / 8;               // x-packed: 16-byte chunks of a value
+  static constexpr uint32_t kBytes = KT * DP * 2; // of K or V of a tile
+  static constexpr int N = KT * C / 256;          // chunks of a thread (16-bit)
+  static constexpr int N8 = (KT * C / 2 + 255) / 256;  // 16-byte loads of a thread (8-bit)
+  static constexpr int NL = F8 ? N8 : N;
+
+  static __device__ __forceinline__ uint32_t swizzle(uint32_t entry) {
+    const uint32_t f = (entry & 3) | (entry >> 3 & 3) << 2;
+    return C == 8 ? f >> 1 : f;
+  }
+  static __device__ __forceinline__ uint32_t at(uint32_t entry, uint32_t chunk) {
+    return (entry * C + (chunk ^ swizzle(entry))) * 16;
+  }
+  static __device__ __forceinline__ uint32_t at_x(uint32_t d, uint32_t chunk) {  // V^T: chunk of 8 entries of value d
+    return (d * VC + (chunk ^ (VC == 8 ? d >> 1 & 7 : d >> 2 & 3))) * 16;
+  }
+};
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(1))) const uint8_t global_u8;
+
+__device__ __forceinline__ u32x2 read_turned(const uint8_t* p) {  // 16 lanes: 4 rows of 16 values, a column to each
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
+}
+
+template <class T, bool F8, int DP, bool VX, int RW>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(AttnArgs a, uint32_t row_groups, uint32_t units) {
+  typedef Tiles<F8, DP, VX> S;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][S::kBytes];  // [buffer][K, V]
+  __shared__ uint32_t absent[2];  // number of the last tile in the buffer that had entries without a block
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kOpsWave), lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
+  // Workgroups go to the 8 XCDs in turn. Those with the same keys (row groups of a split) are
+  // neighbours here, and an XCD gets a run of neighbours, so that they share its L2.
+  uint32_t u = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+  if (u >= units) return;
+  const uint32_t group = row_groups - 1 - u % row_groups;  // the last rows first: without a tree they see most
+  u /= row_groups;
+  const uint32_t split = u % a.splits;
+  u /= a.splits;
+  const uint32_t head = u % a.c.heads, seq = u / a.c.heads;
+  const SeqSpan sp = span_of(a.s, seq);
+  const uint32_t rows = sp.count * a.group;
+  const uint32_t row0 = group * 64 * RW;
+  if (row0 >= rows) return;
+  const uint32_t begin = split * a.split_len;
+  if (begin >= sp.total && split) return;
+  const auto last_token = [&](uint32_t first, uint32_t n) { return (first + n < rows ? first + n - 1 : rows - 1) / a.group; };
+  uint32_t end = begin + a.split_len < sp.total ? begin + a.split_len : sp.total;
+  if (!a.tree && end > sp.before + last_token(row0, 64 * RW) + 1) end = sp.before + last_token(row0, 64 * RW) + 1;
+  const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
+
+  float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
+  // A negative factor goes into Q, so that the largest product is the largest logit; 0 to a number that keeps -infinity.
+  const uint32_t flip = to_log2 < 0 ? 0x80008000u : 0u;
+  to_log2 = fmaxf(fabsf(to_log2), 1e-30f);
+  u32x4 q[RW][S::KS];
+  uint32_t token[RW];
+  bool live[RW];
+  const uint32_t my_row0 = row0 + wave * RW * 16;
 #pragma unroll
-      for (int c = 0; c < S::NC; ++c)
+  for (int r = 0; r < RW; ++r) {
+    const uint32_t row = my_row0 + r * 16 + m;
+    live[r] = row < rows;
+    token[r] = live[r] ? row / a.group : 0;
+    load_q<false, S::KS>(a, head * a.group + (live[r] ? row % a.group : 0), sp.first + token[r], live[r], g, q[r]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[S::value_at(c, g * 4 + i)] = o[r][c][i] * v_scale;
-      if (!g) {
-        float* ml = a.part_ml + 2 * (unit * a.splits + split);
-        ml[0] = top[r];
-        ml[1] = sum[r];
+    for (int i = 0; i < S::KS; ++i) q[r][i] ^= flip;
+  }
+  // Entries that this wave's rows may see.
+  const bool work = my_row0 < rows;
+  const uint32_t my_end = !work ? 0 : a.tree ? end : sp.before + last_token(my_row0, RW * 16) + 1;
+
+  f32x4 o[RW][S::NC];
+  float top[RW], sum[RW];
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    top[r] = kLowest;
+    sum[r] = 0;
+#pragma unroll
+    for (int c = 0; c < S::NC; ++c) o[r][c] = f32x4{0, 0, 0, 0};
+  }
+
+  // Chunks past head_dim are never written: K's count as 0.
+  if (a.c.dim < DP)
+    for (uint32_t i = threadIdx.x; i < 4 * S::kBytes / 16; i += 256) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
+  if (threadIdx.x < 2) absent[threadIdx.x] = 0;
+  __syncthreads();
+
+  // This thread's part of a tile. 16 bits: chunk i of K (and V) is slot 256 i + thread of the tile.
+  const auto k_entry = [&](int i) { return F8 ? (i * 256 + threadIdx.x) / (S::C / 2) : (i * 256 + threadIdx.x) / S::C; };
+  const auto x_entry = [&](int i) -> uint32_t {  // x-packed values: the first of the chunk's entries
+    const uint32_t slot = i * 256 + threadIdx.x;
+    if (F8) return slot % (S::VC / 2) * 16;
+    const uint32_t d = slot / S::VC;
+    return ((slot % S::VC) ^ (S::VC == 8 ? d >> 1 & 7 : d >> 2 & 3)) * 8;
+  };
+  int32_t id[S::NL], vid[VX ? S::NL : 1];  // blocks of the part of the tile after the next
+  const auto look_up = [&](uint32_t base) {
+#pragma unroll
+    for (int i = 0; i < S::NL; ++i) {
+      const uint32_t e = base + k_entry(i);
+      id[i] = table[block_of(a.c, e < end ? e : end - 1)];
+      if constexpr (VX) {
+        const uint32_t f = base + x_entry(i);
+        vid[i] = table[block_of(a.c, f < end ? f : end - 1)];
       }
-      continue;
     }
-    const float by = sum[r] == 0 ? 0.0f : v_scale / sum[r];
-    T* to = reinterpret_cast<T*>(a.out.data) + (sp.first + token[r]) * a.out.token + qh * a.out.head;
+  };
+  u32x4 held_k[F8 ? S::NL : 1], held_v[F8 ? S::NL : 1];
+  const auto in_tile = [&](int i) { return !F8 || (i * 256 + threadIdx.x) * 2 < static_cast<uint32_t>(S::KT * S::C); };
+  // Start bringing the tile at `base` (number n) to buffer b.
+  const auto fetch = [&](uint32_t base, uint32_t n, int b) {
+    bool missing = false;
 #pragma unroll
-    for (int c = 0; c < S::NC; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t d = S::value_at(c, g * 4 + i);
-        if (d < a.c.dim) to[d] = static_cast<T>(o[r][c][i] * by);
+    for (int i = 0; i < S::NL; ++i) {
+      const uint32_t slot = i * 256 + threadIdx.x;
+      const bool mine = in_tile(i);
+      {
+        const uint32_t e = base + k_entry(i), bl = block_of(a.c, e < end ? e : end - 1), t = e - bl * a.c.tokens;
+        const bool has = static_cast<uint32_t>(id[i]) < a.c.num_blocks, ok = e < end && has;
+        missing |= mine && !has;
+        const uint64_t block = ok ? static_cast<uint64_t>(static_cast<uint32_t>(id[i])) * a.c.block_bytes : 0;
+        const uint8_t* kp = a.c.k + block + head * a.c.k_head + static_cast<uint64_t>(t) * a.c.k_token;
+        const uint8_t* vp = a.c.v + block + head * a.c.v_head + static_cast<uint64_t>(t) * a.c.v_token;
+        if constexpr (F8) {
+          const uint32_t chunk = slot % (S::C / 2);
+          const bool in = ok && mine && chunk * 16 < a.c.dim;
+          held_k[i] = in ? *reinterpret_cast<const u32x4*>(kp + static_cast<uint64_t>(chunk) * a.c.k_chunk) : u32x4{0, 0, 0, 0};
+          if constexpr (!VX) held_v[i] = in ? *reinterpret_cast<const u32x4*>(vp + chunk * 16) : u32x4{0, 0, 0, 0};
+        } else {
+          const uint32_t chunk = (slot % S::C) ^ S::swizzle(k_entry(i));
+          if (chunk * 8 < a.c.dim) {
+            if (ok) {
+              __builtin_amdgcn_global_load_lds((global_u8*)(kp + static_cast<uint64_t>(chunk) * a.c.k_chunk),
+                                               (lds_u8*)(lds[b][0] + (i * 256 + wave * 64) * 16), 16, 0, 0);
+              if constexpr (!VX)
+                __builtin_amdgcn_global_load_lds((global_u8*)(vp + chunk * 16), (lds_u8*)(lds[b][1] + (i * 256 + wave * 64) * 16), 16, 0, 0);
+            } else {
+              *reinterpret_cast<u32x4*>(lds[b][0] + slot * 16) = u32x4{0, 0, 0, 0};
+              if constexpr (!VX) *reinterpret_cast<u32x4*>(lds[b][1] + slot * 16) = u32x4{0, 0, 0, 0};
+            }
+          }
+        }
       }
-    if (!g) {
-      const float l2 = sum[r] == 0 ? -INFINITY : top[r] + __builtin_amdgcn_logf(sum[r]);
-      if (a.lse) a.lse[unit] = l2 * kLn2;
-      if (a.scores_out) a.part_ml[unit] = l2;
+      if constexpr (VX) {
+        const uint32_t per = F8 ? 16 : 8, d = F8 ? slot / (S::VC / 2) : slot / S::VC;
+        const uint32_t e = base + x_entry(i), bl = block_of(a.c, e < end ? e : end - 1), t = e - bl * a.c.tokens;
+        const bool has = static_cast<uint32_t>(vid[i]) < a.c.num_blocks, in = e < end && has && mine && d < a.c.dim;
+        const uint32_t left = in ? end - e : 0;  // of the chunk's entries, those before the end
+        const uint8_t* vp = a.c.v + (in ? static_cast<uint64_t>(static_cast<uint32_t>(vid[i])) * a.c.block_bytes : 0) + head * a.c.v_head +
+                            static_cast<uint64_t>(in ? d : 0) * a.c.v_chunk + static_cast<uint64_t>(in ? t : 0) * a.c.v_token;
+        if constexpr (F8) {
+          held_v[i] = in ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
+          if (left < per) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+              held_v[i][j] &= left >= 4 * j + 4 ? ~0u : left <= 4 * j ? 0u : (1u << (left - 4 * j) * 8) - 1;
+          }
+        } else if (left >= per) {
+          __builtin_amdgcn_global_load_lds((global_u8*)vp, (lds_u8*)(lds[b][1] + (i * 256 + wave * 64) * 16), 16, 0, 0);
+        } else {
+          const u32x4 w = in ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4*>(lds[b][1] + slot * 16) = only_keys(w, (1u << left) - 1);
+        }
+      }
     }
+    if (__any(missing) && lane == 0) absent[b] = n;
+  };
+  // 8 bits: widen what fetch() holds into buffer b.
+  const auto widen_to = [&](int b) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int i = 0; i < S::NL; ++i) {
+        if (!in_tile(i)) continue;
+        const uint32_t slot = i * 256 + threadIdx.x, e = k_entry(i), chunk = slot % (S::C / 2) * 2;
+        const u32x4 x = held_k[i], y = held_v[i];
+        *reinterpret_cast<u32x4*>(lds[b][0] + S::at(e, chunk)) = widen<T>(x[0], x[1]);
+        *reinterpret_cast<u32x4*>(lds[b][0] + S::at(e, chunk + 1)) = widen<T>(x[2], x[3]);
+        if constexpr (VX) {
+          const uint32_t d = slot / (S::VC / 2), c = x_entry(i) / 8;
+          *reinterpret_cast<u32x4*>(lds[b][1] + S::at_x(d, c)) = widen<T>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(lds[b][1] + S::at_x(d, c + 1)) = widen<T>(y[2], y[3]);
+        } else {
+          *reinterpret_cast<u32x4*>(lds[b][1] + S::at(e, chunk)) = widen<T>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(lds[b][1] + S::at(e, chunk + 1)) = widen<T>(y[2], y[3]);
+        }
+      }
+    }
+  };
+
+  // Where this lane reads: instruction s of K is at k_at ^ 64 s, halves 4 entries apart; of V
+  // instruction c at v_at ^ 32 c (16 values are 2 chunks), halves 4 entries apart too.
+  const uint32_t k_at = S::at((m / 4) * 8 + m % 4, g);
+  const uint32_t v_at = VX ? 0 : S::at(g * 8 + m / 4, m >> 1 & 1) + (m & 1) * 8;
+
+  uint32_t number = 1;
+  int b = 0;
+  if (begin < end) {
+    look_up(begin);
+    fetch(begin, number, 0);
+    widen_to(0);
+    if (begin + S::KT < end) look_up(begin + S::KT);
+  }
+  uint32_t base = begin;
+  const auto arrive = [&]() {  // the tile at `base` is in buffer b, and the next one is on its way
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the tile is in LDS
+    __syncthreads();                                  // and everyone's, and the other buffer is no longer read
+    if (base + S::KT < end) {
+      fetch(base + S::KT, number + 1, b ^ 1);
+      if (base + 2 * S::KT < end) look_up(base + 2 * S::KT);
+    }
+  };
+  const auto leave = [&]() {
+    if (base + S::KT < end) widen_to(b ^ 1);
+    base += S::KT;
+    ++number;
+    b ^= 1;
+  };
+  const auto tile = [&](auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;
+    const uint8_t* const kl = lds[b][0];
+    const uint8_t* const vl = lds[b][1];
+    f32x4 x[RW][S::SUB][2];
+#pragma unroll
+    for (int r = 0; r < RW; ++r)
+#pragma unroll
+      for (int j = 0; j < S::SUB; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) x[r][j][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < S::KS; ++i)
+#pragma unroll
+      for (int j = 0; j < S::SUB; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 k = *reinterpret_cast<const u32x4*>(kl + (k_at ^ (i * 64)) + (j * 32 + t * 4) * S::C * 16);
+#pragma unroll
+          for (int r = 0; r < RW; ++r) x[r][j][t] = Type<T>::mfma(k, q[r][i], x[r][j][t]);
+        }
+    uint32_t seen[S::SUB][RW];
+    if constexpr (kMasked) {
+#pragma unroll
+      for (int j = 0; j < S::SUB; ++j) {
+        const uint32_t okay = keys_there(a.c, table, base + j * 32 + g * 8, end);
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+          seen[j][r] = okay & keys_seen(a, sp, token[r], base + j * 32 + g * 8);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[r][j][i / 4][i % 4] = seen[j][r] >> i & 1 ? x[r][j][i / 4][i % 4] : -INFINITY;
+        }
+      }
+    }
+    float mx[RW];
+    bool rise = false;
+#pragma unroll
+    for (int r = 0; r < RW; ++r) {
+      float y = x[r][0][0][0];
+#pragma unroll
+      for (int j = 0; j < S::SUB; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y = fmaxf(y, x[r][j][i / 4][i % 4]);
+      y = fmaxf(y, across(y, 16));
+      y = fmaxf(y, across(y, 32));
+      mx[r] = y * to_log2;
+      rise |= mx[r] > top[r] + 8.0f;
+    }
+    if (__any(rise)) {
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        const float y = fmaxf(top[r], mx[r]);
+        const float fade = __builtin_amdgcn_exp2f(top[r] - y);
+        top[r] = y;
+        sum[r] *= fade;
+#pragma unroll
+        for (int c = 0; c < S::NC; ++c) o[r][c] *= fade;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < S::SUB; ++j) {
+      u32x4 p[RW];
+#pragma unroll
+      for (int r = 0; r < RW; ++r) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[i] = __builtin_amdgcn_exp2f(fmaf(x[r][j][i / 4][i % 4], to_log2, -top[r]));
+          sum[r] += y[i];
+        }
+        // Rounded to 16 bits for the product with V (an error of the size of the output's own rounding), not in the sum.
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[r][i] = Type<T>::pack(y[2 * i], y[2 * i + 1]);
+      }
+      const auto op = [&](int c) {
+        if constexpr (VX) {
+          return *reinterpret_cast<const u32x4*>(vl + S::at_x(c * 16 + m, j * 4 + g));
+        } else {
+          const uint8_t* at = vl + (v_at ^ (c * 32)) + j * 32 * S::C * 16;
+          const u32x2 lo = read_turned(at), hi = read_turned(at + 4 * S::C * 16);
+          return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        }
+      };
+      if constexpr (kMasked)
+        add_values_masked<T>(op, p, seen[j], 0xff, g, m, o);  // entries that are not there are 0 in LDS
+      else
+        add_values<T>(op, p, o);
+    }
+  };
+  // Tiles that every row sees whole; from the first other one on, masked ones where a wave has any to mask.
+  const uint32_t whole = end < sp.before ? end : sp.before;
+  bool done = false;
+  while (base + S::KT <= whole) {
+    arrive();
+    if (absent[b] == number) {
+      done = true;
+      break;
+    }
+    if (work) tile(std::false_type());
+    leave();
+  }
+  while (base < end) {
+    if (!done) arrive();
+    done = false;
+    if (base < my_end) tile(std::true_type());
+    leave();
+  }
+  const float v_scale = a.v_scale ? a.v_scale[head] : 1.0f;
+#pragma unroll
+  for (int r = 0; r < RW; ++r) {
+    sum[r] += across(sum[r], 16);
+    sum[r] += across(sum[r], 32);
+    if (live[r])
+      store_row<T, DP>(a, sp.first + token[r], head * a.group + (my_row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r],
+                       [](int c, uint32_t i) { return c * 16 + i; });
   }
 }
 
 // ---------------------------------------------------------------- joining the splits
-// Splits of one row: out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i. A wave has one row.
-template <class T, int DP>
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnArgs a) {
+// Splits that a sequence with `total` entries has.
+__device__ __forceinline__ uint32_t splits_of(const AttnArgs& a, uint32_t total) {
+  const uint32_t n = (total + a.split_len - 1) / a.split_len;
+  return n ? n : 1;
+}
+
+// Maximum and sum of a row over its n splits, by a whole wave.
+__device__ __forceinline__ void join_ml(const float* ml, uint32_t n, float* top, float* sum) {
   const uint32_t lane = threadIdx.x % kOpsWave;
-  const uint32_t row = blockIdx.x * 4 + threadIdx.x / kOpsWave, head = blockIdx.y, seq = blockIdx.z;
-  const SeqSpan sp = span_of(a.s, seq);
-  if (row >= sp.count * a.group) return;
+  float t = kLowest, s = 0;
+  for (uint32_t i = lane; i < n; i += kOpsWave) {
+    const float y = fmaxf(t, ml[2 * i]);
+    s = s * __builtin_amdgcn_exp2f(t - y) + ml[2 * i + 1] * __builtin_amdgcn_exp2f(ml[2 * i] - y);
+    t = y;
+  }
+#pragma unroll
+  for (int x = 1; x < kOpsWave; x *= 2) {
+    const float u = across(t, x), v = across(s, x), y = fmaxf(t, u);
+    s = s * __builtin_amdgcn_exp2f(t - y) + v * __builtin_amdgcn_exp2f(u - y);
+    t = y;
+  }
+  *top = t;
+  *sum = s;
+}
+
+// A row: out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i over its splits. A workgroup has one
+// row; DP / 4 lanes read a split, and 1024 / DP splits are read at once.
+template <class T, int DP>
+__device__ __forceinline__ void join_row(const AttnArgs& a, const SeqSpan& sp, uint32_t row, uint32_t head, f32x4* lds) {
+  constexpr uint32_t L = DP / 4, W = 256 / L;
   const uint32_t token = sp.first + row / a.group, qh = head * a.group + row % a.group;
   const uint64_t unit = static_cast<uint64_t>(token) * a.q_heads + qh;
-  uint32_t n = (sp.total + a.split_len - 1) / a.split_len;
-  if (!n) n = 1;
+  const uint32_t n = splits_of(a, sp.total), l = threadIdx.x % L, w = threadIdx.x / L;
   const float* ml = a.part_ml + 2 * unit * a.splits;
-  float top = kLowest;
-  for (uint32_t i = lane; i < n; i += kOpsWave) top = fmaxf(top, ml[2 * i]);
-#pragma unroll
-  for (int x = 1; x < kOpsWave; x *= 2) top = fmaxf(top, across(top, x));
-  float sum = 0;
-  constexpr int V = DP / kOpsWave;
-  float o[V] = {};
-  const float* part = a.part + unit * a.splits * DP + lane * V;
-  for (uint32_t i = 0; i < n; ++i) {
-    const float w = __builtin_amdgcn_exp2f(ml[2 * i] - top);
-    sum += w * ml[2 * i + 1];
-#pragma unroll
-    for (int j = 0; j < V; ++j) o[j] += w * part[static_cast<uint64_t>(i) * DP + j];
+  float top, sum;
+  join_ml(ml, n, &top, &sum);
+  if (threadIdx.x == 0) {
+    const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    if (a.lse) a.lse[unit] = l2 * kLn2;
+    if (a.lse2) a.lse2[unit] = l2;
   }
+  const f32x4* part = reinterpret_cast<const f32x4*>(a.part + unit * a.splits * DP) + l;
+  f32x4 o = {0, 0, 0, 0};
+#pragma unroll 4
+  for (uint32_t i = w; i < n; i += W) o += part[static_cast<uint64_t>(i) * L] * __builtin_amdgcn_exp2f(ml[2 * i] - top);
+  lds[threadIdx.x] = o;
+  __syncthreads();
+  if (w) return;
+  for (uint32_t i = 1; i < W; ++i) o += lds[i * L + l];
   const float by = sum == 0 ? 0.0f : 1.0f / sum;
   T* to = reinterpret_cast<T*>(a.out.data) + token * a.out.token + qh * a.out.head;
 #pragma unroll
-  for (int j = 0; j < V; ++j)
-    if (lane * V + j < a.c.dim) to[lane * V + j] = static_cast<T>(o[j] * by);
-  if (!lane) {
-    const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-    if (a.lse) a.lse[unit] = l2 * kLn2;
-    if (a.scores_out) a.part_ml[static_cast<uint64_t>(a.s.num_tokens) * a.q_heads * a.splits * 2 + unit] = l2;
-  }
+  for (int j = 0; j < 4; ++j)
+    if (l * 4 + j < a.c.dim) to[l * 4 + j] = static_cast<T>(o[j] * by);
 }
 
-// ---------------------------------------------------------------- weights of the entries
-// scores_out = decay scores_in + sum over the rows of p: with every row's sum known, Q K^T
-// once more, this time rows down and keys across, so that a lane adds up its key's rows.
-// A wave has 32 keys and goes through the rows; each score has one writer, so that the
-// result does not depend on the order of waves.
+constexpr uint32_t kWeigh = 1024;  // entries of a workgroup that adds up kept logits
+
+// Rows of the call first (`joins` of them), then, where logits were kept, the weights of the entries:
+// scores_out = decay scores_in + sum over the rows of 2^(logit - lse).
+template <class T, int DP>
+__global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint32_t joins) {
+  __shared__ f32x4 lds[256];
+  const uint32_t head = blockIdx.y, seq = blockIdx.z;
+  const SeqSpan sp = span_of(a.s, seq);
+  const uint32_t rows = sp.count * a.group;
+  if (blockIdx.x < joins) {
+    if (blockIdx.x < rows) join_row<T, DP>(a, sp, blockIdx.x, head, lds);
+    return;
+  }
+  const uint32_t first = (blockIdx.x - joins) * kWeigh;
+  if (first >= sp.total) return;
+  float* l2 = reinterpret_cast<float*>(lds);  // of the rows: at most 16
+  const uint32_t n = splits_of(a, sp.total);
+  for (uint32_t r = threadIdx.x / kOpsWave; r < rows; r += 4) {
+    const uint64_t unit = static_cast<uint64_t>(sp.first + r / a.group) * a.q_heads + head * a.group + r % a.group;
+    float top, sum;
+    join_ml(a.part_ml + 2 * unit * a.splits, n, &top, &sum);
+    if (threadIdx.x % kOpsWave == 0) l2[r] = sum == 0 ? INFINITY : top + __builtin_amdgcn_logf(sum);
+  }
+  __syncthreads();
+  const uint32_t key = first + threadIdx.x * 4;
+  if (key >= sp.total) return;
+  const uint64_t pair = static_cast<uint64_t>(seq) * a.c.heads + head;
+  const float* x = a.logits + pair * a.logit_rows * a.logit_stride + key;
+  f32x4 w = {0, 0, 0, 0};
+  for (uint32_t r = 0; r < rows; ++r) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(x + static_cast<uint64_t>(r) * a.logit_stride);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] += __builtin_amdgcn_exp2f(y[j] - l2[r]);
+  }
+  const uint64_t at = pair * a.scores_stride + key;
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j)
+    if (key + j < sp.total) a.scores_out[at + j] = (a.scores_in && key + j < sp.before ? a.decay * a.scores_in[at + j] : 0.0f) + w[j];
+}
+
+// ---------------------------------------------------------------- weights of the entries, many rows
+// With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
+// lane adds up its key's rows. A wave has 32 keys and goes through the rows; each score has one
+// writer, so that the result does not depend on the order of waves.
 template <class T, bool F8, int DP>
-__global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a, const float* lse2) {
-  constexpr int KS = DP / 32;
+__global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
+  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
@@ -586,19 +993,25 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a, const
   if (base >= sp.total) return;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
   const uint32_t rows = sp.count * a.group;
-  KeyTile<F8, KS> k;
-  load_keys<F8, KS>(a.c, table, base, sp.total - 1, head, g, m, k);
-  const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
-  const bool inner = base + kTile <= sp.before;
+  u32x4 k[2][NK];
   uint32_t key[2];
   bool there[2];
   float sum[2] = {0, 0};
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     uint32_t in_block;
-    key[t] = base + (m / 4) * 8 + t * 4 + m % 4;
-    there[t] = key[t] < sp.total && block_at(a.c, table, key[t], &in_block) >= 0;
+    key[t] = base + t * 16 + m;
+    const int32_t id = block_at(a.c, table, key[t] < sp.total ? key[t] : sp.total - 1, &in_block);
+    there[t] = key[t] < sp.total && id >= 0;
+    const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + static_cast<uint64_t>(in_block) * a.c.k_token;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const uint32_t chunk = s * 4 + g;
+      k[t][s] = chunk * (F8 ? 16 : 8) < a.c.dim ? *reinterpret_cast<const u32x4*>(p + static_cast<uint64_t>(chunk) * a.c.k_chunk) : u32x4{0, 0, 0, 0};
+    }
   }
+  const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
+  const bool inner = base + kTile <= sp.before;
   for (uint32_t row0 = 0; row0 < rows; row0 += 16) {
     if (!a.tree && !inner && sp.before + (row0 + 15 < rows ? row0 + 15 : rows - 1) / a.group < base) continue;
     u32x4 q[KS];
@@ -611,15 +1024,19 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a, const
     for (int i = 0; i < 4; ++i) {
       const uint32_t x = row0 + g * 4 + i;
       token[i] = x / a.group;
-      l2[i] = x < rows ? lse2[static_cast<uint64_t>(sp.first + token[i]) * a.q_heads + head * a.group + x % a.group]
-                       : INFINITY;
+      l2[i] = x < rows ? a.lse2[static_cast<uint64_t>(sp.first + token[i]) * a.q_heads + head * a.group + x % a.group] : INFINITY;
       if (l2[i] == -INFINITY) l2[i] = INFINITY;  // a row that sees nothing
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       f32x4 s = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < KS; ++i) s = Type<T>::mfma(q[i], k.template operand<T>(t, i), s);
+      for (int i = 0; i < KS; ++i) {
+        u32x4 w;
+        if constexpr (F8) w = widen<T>(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1]);
+        else w = k[t][i];
+        s = Type<T>::mfma(q[i], w, s);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         bool see = there[t] && row0 + g * 4 + i < rows;
@@ -647,21 +1064,31 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a, const
 
 template <class T, bool F8, int DP, bool VX>
 hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.splits * p.row_groups, a.c.heads, a.s.num_seqs);
-  if (p.tiles_per_wg == 1)
-    attention_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a);
-  else
-    attention_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a);
+  if (p.stream) {
+    const dim3 grid(p.splits * p.row_groups, a.c.heads, a.s.num_seqs);
+    if (p.tiles_per_wave == 1) {
+      attention_stream_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a);
+    } else {
+      if constexpr (DP < 256) attention_stream_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a);
+    }
+  } else {
+    const uint32_t units = p.splits * p.row_groups * a.c.heads * a.s.num_seqs, grid = (units + 7) / 8 * 8;
+    if (p.tiles_per_wave == 1)
+      attention_rows_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a, p.row_groups, units);
+    else
+      attention_rows_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a, p.row_groups, units);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.splits > 1) {
-    attention_join_kernel<T, DP><<<dim3((p.rows + 3) / 4, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
+  const uint32_t joins = p.splits > 1 ? p.rows : 0;
+  const uint32_t weighs = a.logits ? (a.s.max_len + kWeigh - 1) / kWeigh : 0;
+  if (joins + weighs) {
+    attention_finish_kernel<T, DP><<<dim3(joins + weighs, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a, joins);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.scores_out) {
-    const float* lse2 = a.part_ml + (p.splits > 1 ? static_cast<uint64_t>(a.s.num_tokens) * a.q_heads * p.splits * 2 : 0);
+  if (a.lse2) {
     attention_scores_kernel<T, F8, DP>
-        <<<dim3((a.s.max_len + 4 * kTile - 1) / (4 * kTile), a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a, lse2);
+        <<<dim3((a.s.max_len + 4 * kTile - 1) / (4 * kTile), a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
     e = hipGetLastError();
   }
   return e;

@@ -205,18 +205,23 @@ mma_status_t launched(hipError_t e, const char* what) {
 
 uint32_t up(uint64_t n, uint32_t to) { return static_cast<uint32_t>((n + to - 1) / to); }
 
+uint64_t up_to(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
+
 // How an attention call is cut. Rows of one sequence and KV head (a token and a head of
 // the group each) go in tiles of 16; the entries go in splits, joined afterwards, where
 // sequences, heads and rows alone are too few workgroups for 256 CUs.
-AttnPlan attention_plan(const CacheArgs& c, const mma_kv_seqs_t& q, const mma_kv_attention_t& a) {
+AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& q, const mma_kv_attention_t& a) {
   AttnPlan p{};
   const uint32_t group = a.q_heads / c.heads;
   const uint64_t tokens = std::min(q.max_tokens, a.num_tokens);
-  p.rows = static_cast<uint32_t>(std::min<uint64_t>(tokens * group, INT32_MAX));
+  p.rows = static_cast<uint32_t>(tokens * group);
   p.dim_pad = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-  p.row_tiles = up(p.rows, 16);
-  p.tiles_per_wg = p.row_tiles > 1 ? 2 : 1;
-  p.row_groups = up(p.row_tiles, p.tiles_per_wg);
+  // Up to two tiles of rows have their keys in registers (one with heads above 128: the second would
+  // not fit them), if a lane's 8 keys share a block.
+  p.stream = p.rows <= (p.dim_pad == 256 ? 16u : 32u) && c.tokens % 8 == 0;
+  const uint32_t per_tile = p.stream ? 16 : 64;
+  p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
+  p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
   const uint64_t want = 1024, least = 256;  // workgroups in all, entries of a split
   uint64_t splits = wgs >= want ? 1 : (want + wgs - 1) / std::max<uint64_t>(wgs, 1);
@@ -224,9 +229,18 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_seqs_t& q, const mma_kv
   p.split_len = up(up(q.max_len, static_cast<uint32_t>(splits)), 128) * 128;
   p.splits = up(q.max_len, p.split_len);
   const uint64_t units = static_cast<uint64_t>(a.num_tokens) * a.q_heads;
-  if (p.splits > 1) p.part_bytes = units * p.splits * p.dim_pad * 4;
-  p.ml_bytes = (p.splits > 1 ? units * p.splits * 8 : 0) + (a.scores_out ? units * 4 : 0);
-  p.bytes = p.part_bytes + p.ml_bytes;
+  if (p.splits > 1) p.part_bytes = up_to(units * p.splits * p.dim_pad * 4, 256);
+  if (a.scores_out) {
+    // Keeping a row's logit writes and reads 8 bytes an entry; doing its products again reads the entry's key.
+    p.logits = p.stream && p.tiles_per_wave == 1 && 8ull * p.rows <= c.dim * elem / 2;
+    p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
+    if (p.logits)
+      p.logit_bytes = up_to(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows * p.logit_stride * 4, 256);
+    else
+      p.lse_bytes = up_to(units * 4, 256);
+  }
+  if (p.splits > 1 || p.logits) p.ml_bytes = up_to(units * p.splits * 8, 256);
+  p.bytes = p.part_bytes + p.ml_bytes + p.lse_bytes + p.logit_bytes;
   return p;
 }
 
@@ -349,7 +363,7 @@ mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma
   if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
   Call call;
   if (mma_status_t s = check_attention_sizes(layout, seqs, a, &call)) return s;
-  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, *seqs, *a).bytes : 0;
+  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, layout->elem_bytes, *seqs, *a).bytes : 0;
   return MMA_OK;
 } catch (...) {
   return ops_boundary_error("mma_kv_attention_workspace");
@@ -380,7 +394,10 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   if ((s = array("scores_out", a->scores_out, score_bytes, 4, true))) return s;
   if ((s = array("k_scale", a->k_scale, 4ull * H, 4, true))) return s;
   if ((s = array("v_scale", a->v_scale, 4ull * H, 4, true))) return s;
-  const AttnPlan p = attention_plan(call.c, *seqs, *a);
+  const AttnPlan p = attention_plan(call.c, layout->elem_bytes, *seqs, *a);
+  if (static_cast<uint64_t>(p.row_groups) * p.splits * H * seqs->num_seqs >= 1ull << 24)
+    return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
+                seqs->num_seqs, seqs->max_tokens, H);
   if (p.bytes) {
     if (a->workspace_bytes < p.bytes)
       return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
@@ -395,15 +412,24 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.scores_out = a->scores_out;
   k.k_scale = a->cache_type == MMA_TYPE_F8 ? a->k_scale : nullptr;
   k.v_scale = a->cache_type == MMA_TYPE_F8 ? a->v_scale : nullptr;
-  k.part = static_cast<float*>(a->workspace);
-  k.part_ml = k.part + p.part_bytes / 4;
+  char* ws = static_cast<char*>(a->workspace);
+  const auto take = [&](uint64_t bytes) {
+    float* at = bytes ? reinterpret_cast<float*>(ws) : nullptr;
+    ws += bytes;
+    return at;
+  };
+  k.part = take(p.part_bytes);
+  k.part_ml = take(p.ml_bytes);
+  k.lse2 = take(p.lse_bytes);
+  k.logits = take(p.logit_bytes);
+  k.logit_rows = p.rows;
+  k.logit_stride = p.logit_stride;
   k.q_heads = a->q_heads;
   k.group = a->q_heads / H;
   k.tree_words = a->tree_words;
   k.scores_stride = a->scores_stride;
   k.splits = p.splits;
   k.split_len = p.split_len;
-  k.row_tiles = p.row_tiles;
   k.wide_q = rows_wide(k.q);
   k.wide_out = rows_wide(k.out);
   k.scale = a->scale;

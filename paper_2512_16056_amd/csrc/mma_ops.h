@@ -68,11 +68,13 @@ struct AttnArgs {
   float* scores_out;
   const float* k_scale;
   const float* v_scale;
-  float* part;      // partial sums [unit][DP], in units of one row of one split
-  float* part_ml;   // their maxima and sums
+  float* part;      // of each row and split: the sum of p V
+  float* part_ml;   // and the maximum (in powers of 2) and sum of p; NULL where neither is read
+  float* lse2;      // of each row, base 2: for the scores kernel, else NULL
+  float* logits;    // [sequence][KV head][logit_rows][logit_stride], base 2, or NULL
+  uint32_t logit_rows, logit_stride;
   uint32_t q_heads, group, tree_words, scores_stride;
   uint32_t splits, split_len;  // entries of a split: a multiple of the tile
-  uint32_t row_tiles;          // of 16 rows, of one sequence and KV head
   uint32_t wide_q, wide_out;   // rows start at 16 bytes
   float scale, decay;
 };
@@ -108,13 +110,15 @@ struct OpsKind {
 
 // Split of an attention call (mma_ops.cpp: attention_plan).
 struct AttnPlan {
-  uint32_t rows;       // most rows (token, head of a group) of one sequence and KV head
-  uint32_t row_tiles;  // of 16
-  uint32_t tiles_per_wg;
-  uint32_t row_groups;
+  bool stream;              // attention_stream_kernel, else attention_rows_kernel
+  uint32_t rows;            // most rows (token, head of a group) of one sequence and KV head
+  uint32_t tiles_per_wave;  // of 16 rows
+  uint32_t row_groups;      // workgroups that the rows take
   uint32_t splits, split_len;
   uint32_t dim_pad;
-  uint64_t part_bytes, ml_bytes, bytes;
+  bool logits;              // scores from logits that the main kernel keeps
+  uint32_t logit_stride;
+  uint64_t part_bytes, ml_bytes, lse_bytes, logit_bytes, bytes;
 };
 
 hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stream);
