@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Iterable, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -442,35 +443,54 @@ def mma_digest_u32(dev_ptr, nbytes: int, dev_out, stream=None) -> None:
 # ------------------------------------------------------------------ operators on the paged cache
 _TYPES = {torch.bfloat16: MMA_TYPE_BF16, torch.float16: MMA_TYPE_F16}
 
+# A decode step makes these calls for every layer, so their set-up counts: the argument structs are packed
+# in one go (0.7 us; filling a ctypes structure takes 3 us) and handed over by address. That pointers are
+# device memory of the right size is the library's check.
+_APPEND_T = struct.Struct("@12Q6Q7If")
+_ATTENTION_T = struct.Struct("@6Q8Q6I2f")
+_WORKSPACE_T = struct.Struct("@2Q")
+_WORKSPACE_AT = mma_kv_attention_t.workspace.offset
+_COMMIT_T = struct.Struct("@4Q2I")
+_EVICT_T = struct.Struct("@5Q5I4x")
+assert (_APPEND_T.size, _ATTENTION_T.size, _COMMIT_T.size, _EVICT_T.size) == tuple(
+    ctypes.sizeof(x) for x in (mma_kv_append_t, mma_kv_attention_t, mma_kv_commit_t, mma_kv_evict_t))
+
+
+def _packed_call(name):
+    f = lib[name]
+    f.argtypes, f.restype = [_P] * 5, _S
+    return f
+
+
+_append, _attention, _commit, _evict = (_packed_call("mma_kv_" + x) for x in ("append", "attention", "commit", "evict"))
+_workspace = lib["mma_kv_attention_workspace"]
+_workspace.argtypes, _workspace.restype = [_P] * 4, _S
+
 
 def _want(name: str, t: torch.Tensor, dtype, shape=None) -> int:
-    """Address of a contiguous GPU tensor of the given type and, where given, shape."""
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    """Address of a contiguous tensor of the given type and, where given, shape."""
+    if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: a contiguous {dtype} GPU tensor{'' if shape is None else f' of shape {shape}'} is "
                          f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
     return t.data_ptr()
 
 
-def _maybe(name: str, t: Optional[torch.Tensor], dtype, shape=None) -> int:
-    return 0 if t is None else _want(name, t, dtype, shape)
-
-
-def _rows(name: str, t: torch.Tensor, dtype, tokens: int, dim: int) -> Tuple[int, int, int]:
+def _rows(name: str, t: torch.Tensor, dtype, shape) -> Tuple[int, int, int]:
     """(address, token stride, head stride) of [tokens][heads][dim] rows."""
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError(f"{name}: [{tokens}][heads][{dim}] of {dtype} on the GPU is wanted, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on the GPU is wanted, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
     token, head, last = t.stride()
-    if last != 1 and dim > 1:
+    if last != 1 and shape[2] > 1:
         raise ValueError(f"{name}: the values of a head have to be contiguous, strides {t.stride()}")
     return t.data_ptr(), token, head
 
 
-def _types(q: torch.Tensor, layout: mma_kv_layout_t) -> Tuple[int, int]:
+def _kind(q: torch.Tensor, layout: mma_kv_layout_t) -> int:
     kind = _TYPES.get(q.dtype)
-    if kind is None:
-        raise ValueError(f"queries of {q.dtype}: bfloat16 or float16 is wanted")
-    return kind, MMA_TYPE_F8 if layout.elem_bytes == 1 else kind
+    if kind is None or q.dim() != 3 or q.shape[2] != layout.head_dim:
+        raise ValueError(f"q: [tokens][heads][{layout.head_dim}] of bfloat16 or float16 is wanted, got {q.dtype} {tuple(q.shape)}")
+    return kind
 
 
 def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
@@ -496,7 +516,9 @@ class KVSeqs:
         self.num_seqs, self.max_tokens, self.max_len = n, max_tokens, max_len
         self.device = block_table.device
         self.c = mma_kv_seqs_t(_want("block_table", block_table, torch.int32), _want("lens", lens, torch.int32, (n,)),
-                               _maybe("q_start", q_start, torch.int32, (n + 1,)), n, width, max_tokens, max_len)
+                               0 if q_start is None else _want("q_start", q_start, torch.int32, (n + 1,)), n, width,
+                               max_tokens, max_len)
+        self.address = ctypes.addressof(self.c)
 
 
 def kv_seqs(block_table, lens, q_start=None, *, max_tokens: int = 1, max_len: int) -> KVSeqs:
@@ -519,22 +541,33 @@ def mma_kv_append(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tensor,
                   k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
     """Normalise and rotate q and k, write k and v into `layer`; returns the queries (q_out, or a new tensor)."""
-    kind, cache = _types(q, layout)
-    n, heads, dim, dt = q.shape[0], layout.kv_heads, layout.head_dim, q.dtype
+    kind, dt = _kind(q, layout), q.dtype
+    shape = q.shape
+    n, q_heads, dim = shape
+    heads = layout.kv_heads
     if q_out is None:
-        q_out = _empty_on(stream, q.shape, dt, q.device)
-    if k.shape[1] != heads or v.shape[1] != heads or q_out.shape[1] != q.shape[1]:
-        raise ValueError(f"k, v: {heads} heads are wanted, and of q_out as many as of q")
-    if rope is not None and (rope.dim() != 2 or positions is None):
-        raise ValueError("rope: [positions][rot_dim] is wanted, and positions with it")
-    a = mma_kv_append_t(
-        _rows("q", q, dt, n, dim), _rows("k", k, dt, n, dim), _rows("v", v, dt, n, dim),
-        _rows("q_out", q_out, dt, n, dim), _maybe("positions", positions, torch.int32, (n,)),
-        _maybe("rope", rope, torch.float32), _maybe("q_weight", q_weight, dt, (dim,)),
-        _maybe("k_weight", k_weight, dt, (dim,)), _maybe("k_scale", k_scale, torch.float32, (heads,)),
-        _maybe("v_scale", v_scale, torch.float32, (heads,)), n, q.shape[1], kind, cache,
-        0 if rope is None else rope.shape[1], 0 if rope is None else rope.shape[0], interleaved, eps)
-    _check(lib.mma_kv_append(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_append")
+        q_out = _empty_on(stream, shape, dt, q.device)
+    kv_shape = (n, heads, dim)
+    pos = table = qw = kw = ks = vs = rot = rows = 0
+    if rope is not None:
+        if rope.dim() != 2 or positions is None:
+            raise ValueError("rope: [positions][rot_dim] is wanted, and positions with it")
+        rows, rot = rope.shape
+        pos, table = _want("positions", positions, torch.int32, (n,)), _want("rope", rope, torch.float32)
+    if q_weight is not None:
+        qw = _want("q_weight", q_weight, dt, (dim,))
+    if k_weight is not None:
+        kw = _want("k_weight", k_weight, dt, (dim,))
+    if k_scale is not None:
+        ks = _want("k_scale", k_scale, torch.float32, (heads,))
+    if v_scale is not None:
+        vs = _want("v_scale", v_scale, torch.float32, (heads,))
+    a = _APPEND_T.pack(*_rows("q", q, dt, shape), *_rows("k", k, dt, kv_shape), *_rows("v", v, dt, kv_shape),
+                       *_rows("q_out", q_out, dt, shape), pos, table, qw, kw, ks, vs, n, q_heads, kind,
+                       MMA_TYPE_F8 if layout.elem_bytes == 1 else kind, rot, rows, 1 if interleaved else 0, eps)
+    st = _append(ctypes.byref(layout), _ptr(layer), seqs.address, a, _stream(stream))
+    if st:
+        _check(st, "mma_kv_append")
     return q_out
 
 
@@ -548,36 +581,48 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
     """Attention of the call's tokens over their sequences' entries; returns `out` (or a new tensor). `tree`: int64
     [tokens][words] bits. `scale`: 1 / sqrt(head_dim) unless given. `workspace`: a uint8 tensor of
     kv_attention_workspace() bytes or more; a new one of the stream's unless given."""
-    kind, cache = _types(q, layout)
-    n, heads, dim, dt = q.shape[0], layout.kv_heads, layout.head_dim, q.dtype
+    kind, dt = _kind(q, layout), q.dtype
+    shape = q.shape
+    n, q_heads, dim = shape
+    heads = layout.kv_heads
     if out is None:
-        out = _empty_on(stream, q.shape, dt, q.device)
-    if out.shape[1] != q.shape[1]:
-        raise ValueError("out: as many heads as q has are wanted")
-    if tree is not None and (tree.dim() != 2 or tree.shape[0] != n):
-        raise ValueError(f"tree: [{n}][words] is wanted, got {tuple(tree.shape)}")
-    width = 0
+        out = _empty_on(stream, shape, dt, q.device)
+    bits = l = s_in = s_out = ks = vs = words = width = 0
+    if tree is not None:
+        if tree.dim() != 2 or tree.shape[0] != n:
+            raise ValueError(f"tree: [{n}][words] is wanted, got {tuple(tree.shape)}")
+        bits, words = _want("tree", tree, torch.int64), tree.shape[1]
+    if lse is not None:
+        l = _want("lse", lse, torch.float32, (n, q_heads))
     if scores_out is not None:
-        if scores_out.dim() != 3 or tuple(scores_out.shape[:2]) != (seqs.num_seqs, heads):
+        if scores_out.dim() != 3 or scores_out.shape[:2] != (seqs.num_seqs, heads):
             raise ValueError(f"scores_out: [{seqs.num_seqs}][{heads}][entries] is wanted, got {tuple(scores_out.shape)}")
-        width = scores_out.shape[2]
+        s_out, width = _want("scores_out", scores_out, torch.float32), scores_out.shape[2]
+        if scores_in is not None:
+            s_in = _want("scores_in", scores_in, torch.float32, scores_out.shape)
     elif scores_in is not None:
         raise ValueError("scores_in without scores_out")
-    a = mma_kv_attention_t(
-        _rows("q", q, dt, n, dim), _rows("out", out, dt, n, dim), _maybe("tree", tree, torch.int64),
-        _maybe("lse", lse, torch.float32, (n, q.shape[1])),
-        _maybe("scores_in", scores_in, torch.float32, None if scores_out is None else tuple(scores_out.shape)),
-        _maybe("scores_out", scores_out, torch.float32), _maybe("k_scale", k_scale, torch.float32, (heads,)),
-        _maybe("v_scale", v_scale, torch.float32, (heads,)), 0, 0, n, q.shape[1], kind, cache,
-        0 if tree is None else tree.shape[1], width, dim ** -0.5 if scale is None else scale, decay)
+    if k_scale is not None:
+        ks = _want("k_scale", k_scale, torch.float32, (heads,))
+    if v_scale is not None:
+        vs = _want("v_scale", v_scale, torch.float32, (heads,))
+    a = _ATTENTION_T.pack(*_rows("q", q, dt, shape), *_rows("out", out, dt, shape), bits, l, s_in, s_out, ks, vs, 0, 0, n,
+                          q_heads, kind, MMA_TYPE_F8 if layout.elem_bytes == 1 else kind, words, width,
+                          dim ** -0.5 if scale is None else scale, decay)
+    lay = ctypes.byref(layout)
     if workspace is None:
         need = _U64()
-        _check(lib.mma_kv_attention_workspace(layout, seqs.c, a, need), "mma_kv_attention_workspace")
+        st = _workspace(lay, seqs.address, a, ctypes.byref(need))
+        if st:
+            _check(st, "mma_kv_attention_workspace")
         if need.value:
             workspace = _empty_on(stream, (need.value,), torch.uint8, q.device)
     if workspace is not None:
-        a.workspace, a.workspace_bytes = _want("workspace", workspace, torch.uint8), workspace.numel()
-    _check(lib.mma_kv_attention(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_attention")
+        a = (a[:_WORKSPACE_AT] + _WORKSPACE_T.pack(_want("workspace", workspace, torch.uint8), workspace.numel()) +
+             a[_WORKSPACE_AT + 16:])
+    st = _attention(lay, _ptr(layer), seqs.address, a, _stream(stream))
+    if st:
+        _check(st, "mma_kv_attention")
     return out
 
 
@@ -596,7 +641,7 @@ def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch
                   scores=None, scores_stride: Optional[int] = None, stream=None) -> torch.Tensor:
     """Move the accepted drafted entries together in every layer (in place); returns the new lengths. `layers`,
     `scores`: tensors, or a layer_table (then scores_stride is needed)."""
-    n = seqs.num_seqs
+    n, num_layers = seqs.num_seqs, layout.num_layers
     if accepted.dim() != 2 or accepted.shape[0] != n:
         raise ValueError(f"accepted: [{n}][drafted tokens] is wanted, got {tuple(accepted.shape)}")
     if scores is not None and not isinstance(scores, ctypes.Array):
@@ -608,13 +653,14 @@ def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch
         scores_stride = shape[2]
     lt = layer_table(layers)  # locals, so that the arrays outlive the call
     st = None if scores is None else layer_table(scores)
-    if len(lt) < layout.num_layers or (st is not None and (len(st) < layout.num_layers or scores_stride is None)):
-        raise ValueError(f"{layout.num_layers} layers are wanted, and as many scores with their stride")
+    if len(lt) < num_layers or (st is not None and (len(st) < num_layers or scores_stride is None)):
+        raise ValueError(f"{num_layers} layers are wanted, and as many scores with their stride")
     lens = _empty_on(stream, (n,), torch.int32, seqs.device)
-    a = mma_kv_commit_t(_want("accepted", accepted, torch.int32), _want("counts", counts, torch.int32, (n,)),
-                        lens.data_ptr(), 0 if st is None else ctypes.addressof(st), accepted.shape[1],
-                        scores_stride or 0)
-    _check(lib.mma_kv_commit(layout, lt, seqs.c, a, _stream(stream)), "mma_kv_commit")
+    a = _COMMIT_T.pack(_want("accepted", accepted, torch.int32), _want("counts", counts, torch.int32, (n,)),
+                       lens.data_ptr(), 0 if st is None else ctypes.addressof(st), accepted.shape[1], scores_stride or 0)
+    rc = _commit(ctypes.byref(layout), lt, seqs.address, a, _stream(stream))
+    if rc:
+        _check(rc, "mma_kv_commit")
     return lens
 
 
@@ -625,17 +671,18 @@ def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.
     n, heads = seqs.num_seqs, layout.kv_heads
     if dst_table.dim() != 2 or dst_table.shape[0] != n:
         raise ValueError(f"dst_table: [{n}][blocks] is wanted, got {tuple(dst_table.shape)}")
-    if scores.dim() != 3 or tuple(scores.shape[:2]) != (n, heads):
+    if scores.dim() != 3 or scores.shape[:2] != (n, heads):
         raise ValueError(f"scores: [{n}][{heads}][entries] is wanted, got {tuple(scores.shape)}")
     if keep < 1:
         raise ValueError("keep: at least 1")
     entries = _empty_on(stream, (n, heads, keep), torch.int32, seqs.device)
     kept = _empty_on(stream, (n, heads, keep), torch.float32, seqs.device)
     lens = _empty_on(stream, (n,), torch.int32, seqs.device)
-    a = mma_kv_evict_t(_want("dst_table", dst_table, torch.int32), _want("scores", scores, torch.float32),
-                       entries.data_ptr(), kept.data_ptr(), lens.data_ptr(), dst_table.shape[1], scores.shape[2], keep,
-                       sinks, recent)
-    _check(lib.mma_kv_evict(layout, _ptr(layer), seqs.c, a, _stream(stream)), "mma_kv_evict")
+    a = _EVICT_T.pack(_want("dst_table", dst_table, torch.int32), _want("scores", scores, torch.float32), entries.data_ptr(),
+                      kept.data_ptr(), lens.data_ptr(), dst_table.shape[1], scores.shape[2], keep, sinks, recent)
+    rc = _evict(ctypes.byref(layout), _ptr(layer), seqs.address, a, _stream(stream))
+    if rc:
+        _check(rc, "mma_kv_evict")
     return entries, kept, lens
 
 

@@ -17,8 +17,17 @@ constexpr uint32_t kMaxDim = 256;
 constexpr uint32_t kMaxGrid = 65535;  // sequences and heads are grid axes
 constexpr uint64_t kMaxRows = 1ull << 26;  // tokens x heads: a launch has below 2^32 threads
 
+// An allocation found by a check of this call. Allocations live as long as the call that is handed
+// pointers into them, so what lies inside one already found needs no question to the runtime (0.07 us
+// each; a commit of 32 layers and their scores would ask 64 times).
+struct Known {
+  uint64_t base = 0, size = 0;
+};
+
 struct Call {
   int device = 0;
+  Known known[4];
+  uint32_t next = 0;
   CacheArgs c{};
   SeqArgs s{};
   uint64_t piece = 0, layer_bytes = 0;
@@ -47,19 +56,31 @@ uint64_t extent(uint64_t n, uint64_t m, uint64_t bytes) {
   return r;
 }
 
+mma_status_t device_range(Call* call, const void* p, uint64_t bytes) {
+  const uint64_t at = reinterpret_cast<uint64_t>(p);
+  for (const Known& k : call->known)
+    if (at >= k.base && bytes <= k.size && at - k.base <= k.size - bytes) return MMA_OK;
+  Known& k = call->known[call->next++ % 4];
+  k = Known{};
+  Known got;
+  if (mma_status_t s = ops_device_range(p, bytes, &got.base, &got.size)) return s;
+  k = got;
+  return MMA_OK;
+}
+
 // A device array of the call; NULL only where it may be absent.
-mma_status_t array(const char* what, const void* p, uint64_t bytes, uintptr_t align, bool optional = false) {
+mma_status_t array(Call* call, const char* what, const void* p, uint64_t bytes, uintptr_t align, bool optional = false) {
   if (!p) {
     if (optional) return MMA_OK;
     return fail(MMA_ERR_INVALID_ARG, "%s is NULL", what);
   }
   if (!aligned(p, align)) return fail(MMA_ERR_INVALID_ARG, "%s has to be %u-byte aligned", what, static_cast<unsigned>(align));
   if (bytes == UINT64_MAX) return fail(MMA_ERR_INVALID_ARG, "%s: its size is beyond 64 bits", what);
-  return bytes ? ops_device_range(p, bytes) : MMA_OK;
+  return bytes ? device_range(call, p, bytes) : MMA_OK;
 }
 
 // Token rows [tokens][heads][dim] of 2-byte values.
-mma_status_t rows(const char* what, const mma_rows_t& r, uint32_t tokens, uint32_t heads, uint32_t dim, bool written,
+mma_status_t rows(Call* call, const char* what, const mma_rows_t& r, uint32_t tokens, uint32_t heads, uint32_t dim, bool written,
                   RowArgs* out) {
   uint64_t a, b, n;
   if (__builtin_mul_overflow(static_cast<uint64_t>(tokens - 1), r.token_stride, &a) ||
@@ -71,7 +92,7 @@ mma_status_t rows(const char* what, const mma_rows_t& r, uint32_t tokens, uint32
     const bool by_head = (tokens == 1 || r.token_stride >= dim) && (heads == 1 || r.head_stride >= a + dim);
     if (!by_token && !by_head) return fail(MMA_ERR_INVALID_ARG, "%s: its rows overlap", what);
   }
-  if (mma_status_t s = array(what, r.data, 2 * n, 2)) return s;
+  if (mma_status_t s = array(call, what, r.data, 2 * n, 2)) return s;
   out->data = static_cast<uint8_t*>(r.data);
   out->token = r.token_stride;
   out->head = r.head_stride;
@@ -153,7 +174,7 @@ mma_status_t check_layout(const mma_kv_layout_t* lay, Call* call) {
 }
 
 mma_status_t check_layer(const void* layer, Call* call) {
-  if (mma_status_t s = array("the layer tensor", layer, call->layer_bytes, 16)) return s;
+  if (mma_status_t s = array(call, "the layer tensor", layer, call->layer_bytes, 16)) return s;
   call->c.k = static_cast<uint8_t*>(const_cast<void*>(layer));
   call->c.v = call->c.k + call->piece * call->c.num_blocks;
   return MMA_OK;
@@ -172,9 +193,9 @@ mma_status_t check_seqs_sizes(const mma_kv_seqs_t* q, uint32_t block_tokens) {
 mma_status_t check_seqs(const mma_kv_seqs_t* q, uint32_t block_tokens, uint32_t num_tokens, Call* call) {
   mma_status_t s;
   if ((s = check_seqs_sizes(q, block_tokens))) return s;
-  if ((s = array("block_table", q->block_table, extent(q->num_seqs, q->table_stride, 4), 4))) return s;
-  if ((s = array("lens", q->lens, 4ull * q->num_seqs, 4))) return s;
-  if ((s = array("q_start", q->q_start, 4ull * q->num_seqs + 4, 4, true))) return s;
+  if ((s = array(call, "block_table", q->block_table, extent(q->num_seqs, q->table_stride, 4), 4))) return s;
+  if ((s = array(call, "lens", q->lens, 4ull * q->num_seqs, 4))) return s;
+  if ((s = array(call, "q_start", q->q_start, 4ull * q->num_seqs + 4, 4, true))) return s;
   SeqArgs& a = call->s;
   a.table = q->block_table;
   a.lens = q->lens;
@@ -325,18 +346,18 @@ mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma
   if ((s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
   AppendArgs k{};
-  if ((s = rows("q", a->q, n, a->q_heads, D, false, &k.q))) return s;
-  if ((s = rows("k", a->k, n, H, D, false, &k.k))) return s;
-  if ((s = rows("v", a->v, n, H, D, false, &k.v))) return s;
-  if ((s = rows("q_out", a->q_out, n, a->q_heads, D, true, &k.out))) return s;
+  if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
+  if ((s = rows(&call, "k", a->k, n, H, D, false, &k.k))) return s;
+  if ((s = rows(&call, "v", a->v, n, H, D, false, &k.v))) return s;
+  if ((s = rows(&call, "q_out", a->q_out, n, a->q_heads, D, true, &k.out))) return s;
   if (a->rope) {
-    if ((s = array("rope", a->rope, extent(a->rope_rows, a->rot_dim, 4), 16))) return s;
-    if ((s = array("positions", a->positions, 4ull * n, 4))) return s;
+    if ((s = array(&call, "rope", a->rope, extent(a->rope_rows, a->rot_dim, 4), 16))) return s;
+    if ((s = array(&call, "positions", a->positions, 4ull * n, 4))) return s;
   }
-  if ((s = array("q_weight", a->q_weight, 2ull * D, 2, true))) return s;
-  if ((s = array("k_weight", a->k_weight, 2ull * D, 2, true))) return s;
-  if ((s = array("k_scale", a->k_scale, 4ull * H, 4, true))) return s;
-  if ((s = array("v_scale", a->v_scale, 4ull * H, 4, true))) return s;
+  if ((s = array(&call, "q_weight", a->q_weight, 2ull * D, 2, true))) return s;
+  if ((s = array(&call, "k_weight", a->k_weight, 2ull * D, 2, true))) return s;
+  if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
+  if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
   k.c = call.c;
   k.s = call.s;
   k.positions = a->positions;
@@ -385,15 +406,15 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   if ((s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
   AttnArgs k{};
-  if ((s = rows("q", a->q, n, a->q_heads, D, false, &k.q))) return s;
-  if ((s = rows("out", a->out, n, a->q_heads, D, true, &k.out))) return s;
-  if ((s = array("tree", a->tree, extent(n, a->tree_words, 8), 8, true))) return s;
-  if ((s = array("lse", a->lse, extent(n, a->q_heads, 4), 4, true))) return s;
+  if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
+  if ((s = rows(&call, "out", a->out, n, a->q_heads, D, true, &k.out))) return s;
+  if ((s = array(&call, "tree", a->tree, extent(n, a->tree_words, 8), 8, true))) return s;
+  if ((s = array(&call, "lse", a->lse, extent(n, a->q_heads, 4), 4, true))) return s;
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
-  if ((s = array("scores_in", a->scores_in, score_bytes, 4, true))) return s;
-  if ((s = array("scores_out", a->scores_out, score_bytes, 4, true))) return s;
-  if ((s = array("k_scale", a->k_scale, 4ull * H, 4, true))) return s;
-  if ((s = array("v_scale", a->v_scale, 4ull * H, 4, true))) return s;
+  if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
+  if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
+  if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
   const AttnPlan p = attention_plan(call.c, layout->elem_bytes, *seqs, *a);
   if (static_cast<uint64_t>(p.row_groups) * p.splits * H * seqs->num_seqs >= 1ull << 24)
     return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
@@ -402,7 +423,7 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
     if (a->workspace_bytes < p.bytes)
       return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
                   static_cast<unsigned long long>(a->workspace_bytes), static_cast<unsigned long long>(p.bytes));
-    if ((s = array("workspace", a->workspace, p.bytes, 256))) return s;
+    if ((s = array(&call, "workspace", a->workspace, p.bytes, 256))) return s;
   }
   k.c = call.c;
   k.s = call.s;
@@ -454,13 +475,13 @@ mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layer
   if (!seqs->num_seqs || !a->accepted_stride) return MMA_OK;
   Device dev(call.device);
   if ((s = check_seqs(seqs, layout->block_tokens, INT32_MAX, &call))) return s;
-  if ((s = array("accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4), 4))) return s;
-  if ((s = array("counts", a->counts, 4ull * seqs->num_seqs, 4))) return s;
-  if ((s = array("lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
+  if ((s = array(&call, "accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4), 4))) return s;
+  if ((s = array(&call, "counts", a->counts, 4ull * seqs->num_seqs, 4))) return s;
+  if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads, a->scores_stride, 4);
   for (uint32_t l = 0; l < layout->num_layers; ++l) {
-    if ((s = array("a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
-    if (a->scores && (s = array("a layer's scores", a->scores[l], score_bytes, 4))) return s;
+    if ((s = array(&call, "a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
+    if (a->scores && (s = array(&call, "a layer's scores", a->scores[l], score_bytes, 4))) return s;
   }
   static thread_local CommitArgs k;
   k.c = call.c;
@@ -506,11 +527,11 @@ mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_
   if ((s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, 0, &call))) return s;
   const uint64_t heads = static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads;
-  if ((s = array("dst_table", a->dst_table, extent(seqs->num_seqs, a->dst_stride, 4), 4))) return s;
-  if ((s = array("scores", a->scores, extent(heads, a->scores_stride, 4), 4))) return s;
-  if ((s = array("entries", a->entries, extent(heads, a->keep, 4), 4))) return s;
-  if ((s = array("scores_out", a->scores_out, extent(heads, a->keep, 4), 4, true))) return s;
-  if ((s = array("lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
+  if ((s = array(&call, "dst_table", a->dst_table, extent(seqs->num_seqs, a->dst_stride, 4), 4))) return s;
+  if ((s = array(&call, "scores", a->scores, extent(heads, a->scores_stride, 4), 4))) return s;
+  if ((s = array(&call, "entries", a->entries, extent(heads, a->keep, 4), 4))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, extent(heads, a->keep, 4), 4, true))) return s;
+  if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
   EvictArgs k{};
   k.c = call.c;
   k.s = call.s;

@@ -12,7 +12,9 @@ namespace mma {
 
 // ------------------------------------------------------------ of the runtime
 mma_status_t ops_ready(int* device);  // after mma_init, no sticky failure
-mma_status_t ops_device_range(const void* p, uint64_t bytes);
+// Checks that [p, p + bytes) lies in one allocation of the device; *base and *size get that allocation (or the
+// range itself), so that a caller need not ask again for what it knows to be inside.
+mma_status_t ops_device_range(const void* p, uint64_t bytes, uint64_t* base, uint64_t* size);
 mma_status_t ops_boundary_error(const char* func);  // in a catch (...) block
 
 // ------------------------------------------------------------ kernel arguments

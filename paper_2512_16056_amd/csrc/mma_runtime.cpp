@@ -341,10 +341,13 @@ mma_status_t host_range(const void* p, uint64_t bytes, uint64_t* dev_addr, bool*
   return MMA_OK;
 }
 
-mma_status_t device_range(const void* p, uint64_t bytes) {
+mma_status_t device_range(const void* p, uint64_t bytes, RangeCache::Entry* known = nullptr) {
   const uint64_t id = buffer_id(p);
   RangeCache::Entry e;
-  if (id && g_ranges.find(id, false, reinterpret_cast<uint64_t>(p), bytes, &e)) return MMA_OK;
+  if (id && g_ranges.find(id, false, reinterpret_cast<uint64_t>(p), bytes, &e)) {
+    if (known) *known = e;
+    return MMA_OK;
+  }
   hipPointerAttribute_t a{};
   if (hipPointerGetAttributes(&a, p) != hipSuccess || a.type != hipMemoryTypeDevice) {
     (void)hipGetLastError();
@@ -536,7 +539,15 @@ mma_status_t ops_ready(int* device) {
   *device = g_rt->dev;
   return MMA_OK;
 }
-mma_status_t ops_device_range(const void* p, uint64_t bytes) { return device_range(p, bytes); }
+mma_status_t ops_device_range(const void* p, uint64_t bytes, uint64_t* base, uint64_t* size) {
+  RangeCache::Entry e;
+  e.base = reinterpret_cast<uint64_t>(p);
+  e.size = bytes;
+  const mma_status_t s = device_range(p, bytes, &e);
+  *base = e.base;
+  *size = e.size;
+  return s;
+}
 mma_status_t ops_boundary_error(const char* func) { return boundary_error(func); }
 }  // namespace mma
 
