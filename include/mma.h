@@ -457,7 +457,7 @@ typedef struct mma_kv_seqs {
 } mma_kv_seqs_t;
 
 /* Rows [token][head][head_dim] of `type`: strides in elements, the last axis contiguous,
- * any alignment of an element. Tokens of no sequence are left alone. */
+ * any alignment of an element. */
 typedef struct mma_rows {
   void* data;
   uint64_t token_stride;
@@ -514,7 +514,7 @@ typedef struct mma_kv_append {
 
 /* Of every token: q and k of each head times 1 / sqrt(mean of squares + eps) and the
  * weight, then each pair (a, b) turned to (a cos - b sin, b cos + a sin); q to q_out,
- * k and v to their entry of the cache. One rounding, at the store. 8-bit entries past
+ * k and v to their entry of the cache (those of a token of no sequence nowhere). One rounding, at the store. 8-bit entries past
  * 448 are stored as 448 of their sign, NaN as NaN. */
 mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
                            const mma_kv_append_t* args, void* stream);
@@ -541,7 +541,7 @@ typedef struct mma_kv_attention {
 } mma_kv_attention_t;
 
 /* Of every token and head: p = softmax over the entries it sees of scale * q . K, and
- * out = sum of p V; lse = log of the sum of exp. It sees its sequence's lens[s] entries
+ * out = sum of p V; lse = log of the sum of exp (rows of no sequence are left alone). It sees its sequence's lens[s] entries
  * and of the call's own tokens (which mma_kv_append has written) those that `tree` says.
  * A row that sees nothing is 0 with lse -infinity. What lies in entries that a row does
  * not see, infinities and NaN among it, does not reach the row.

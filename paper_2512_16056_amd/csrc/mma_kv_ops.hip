@@ -4,6 +4,7 @@
 #include "mma_ops.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mma {
 namespace {
@@ -96,184 +97,325 @@ __device__ __forceinline__ uint32_t seq_of(const SeqArgs& s, uint32_t token) {
   return n ? n - 1 : 0;
 }
 
-// L lanes have a row of a token: L * 8 >= head_dim values. Rows of a token are its query
-// heads, then its keys, then its values.
+constexpr uint32_t kRun = 16;  // tokens whose x-packed values a workgroup turns
+
+// Where a token's entry lies: its block, or -1, and its place in it.
+__device__ __forceinline__ int32_t entry_of(const AppendArgs& a, uint32_t seq, uint32_t token, uint32_t* at) {
+  *at = 0;
+  if (seq >= a.s.num_seqs) return -1;
+  const SeqSpan sp = span_of(a.s, seq);
+  const uint32_t i = token - sp.first, entry = sp.before + i;
+  if (token < sp.first || i >= sp.count || entry >= sp.total) return -1;
+  return block_at(a.c, a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride, entry, at);
+}
+
+// x-packed values of kRun tokens and one head: through LDS, so that the tokens of a block, which lie side by
+// side for each value, are written by one workgroup, in one store where the run fills an aligned part of it.
+template <class T, bool F8>
+__device__ __forceinline__ void append_turned(const AppendArgs& a, uint32_t first, uint32_t head, uint16_t* tile, int32_t* ids,
+                                              uint32_t* ats) {
+  const uint32_t n = a.s.num_tokens - first < kRun ? a.s.num_tokens - first : kRun, D = a.c.dim;
+  const uint32_t wave = threadIdx.x / kOpsWave;
+  constexpr uint32_t S = kRun + 2;  // of a value's row in LDS: an odd number of dwords
+  for (uint32_t t = wave; t < n; t += 4) {  // seq_of is a whole wave's
+    const uint32_t seq = seq_of(a.s, first + t);
+    if (threadIdx.x % kOpsWave == 0) {
+      uint32_t at;
+      ids[t] = entry_of(a, seq, first + t, &at);
+      ats[t] = at;
+    }
+  }
+  const float scale = a.v_scale ? a.v_scale[head] : 1.0f;
+  for (uint32_t u = threadIdx.x; u < n * (D / 8); u += 256) {
+    const uint32_t t = u / (D / 8), d0 = u % (D / 8) * 8;
+    const u32x4 w = load8(a.v.data + 2 * ((first + t) * a.v.token + head * a.v.head + d0), a.wide);
+    if constexpr (F8) {
+      float x[8];
+      unpack8<T>(w, x);
+      const u32x2 y = to_f8(x, scale);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tile[(d0 + j) * S + t] = y[j / 4] >> (j % 4 * 8) & 0xff;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tile[(d0 + j) * S + t] = static_cast<uint16_t>(w[j / 2] >> (j % 2 * 16));
+    }
+  }
+  __syncthreads();
+  bool whole = n == kRun && ids[0] >= 0 && ats[0] % kRun == 0;  // blocks hold a multiple of 8 (16 of 8 bits)
+  for (uint32_t t = 1; t < n; ++t) whole = whole && ids[t] == ids[0] && ats[t] == ats[0] + t;
+  for (uint32_t d = threadIdx.x; d < D; d += 256) {
+    const uint16_t* row = tile + d * S;
+    uint8_t* const base = a.c.v + head * a.c.v_head + static_cast<uint64_t>(d) * a.c.v_chunk;
+    if (whole) {
+      uint8_t* to = base + static_cast<uint64_t>(ids[0]) * a.c.block_bytes + static_cast<uint64_t>(ats[0]) * a.c.v_token;
+      u32x4 w[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (F8) {
+          if (i < 4) w[0][i] = row[4 * i] | row[4 * i + 1] << 8 | row[4 * i + 2] << 16 | static_cast<uint32_t>(row[4 * i + 3]) << 24;
+        } else {
+          w[i / 4][i % 4] = row[2 * i] | static_cast<uint32_t>(row[2 * i + 1]) << 16;
+        }
+      }
+      *reinterpret_cast<u32x4*>(to) = w[0];
+      if constexpr (!F8) *reinterpret_cast<u32x4*>(to + 16) = w[1];
+    } else {
+      for (uint32_t t = 0; t < n; ++t) {
+        if (ids[t] < 0) continue;
+        uint8_t* to = base + static_cast<uint64_t>(ids[t]) * a.c.block_bytes + static_cast<uint64_t>(ats[t]) * a.c.v_token;
+        if constexpr (F8)
+          *to = static_cast<uint8_t>(row[t]);
+        else
+          *reinterpret_cast<uint16_t*>(to) = row[t];
+      }
+    }
+  }
+}
+
+// L lanes have a row of a token: L * 8 >= head_dim values. Rows of a token are its query heads,
+// then its keys, then (but for x-packed values) its values; a workgroup takes `parts`-th parts of
+// them. Where there are many tokens it takes all: what the rows share (position, place in the
+// cache, cosines and sines) is then read once. Workgroups past those turn x-packed values.
 template <class T, bool F8, bool VX, int L>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t parts) {
   constexpr uint32_t kRows = 256 / L;
-  __shared__ float turn[kRows][L * 8 + 1];
+  constexpr uint32_t kTurn = kRows * (L * 8 + 1) * 4, kTile = VX ? L * 8 * (kRun + 2) * 2 : 0;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kTurn > kTile ? kTurn : kTile];
+  const uint32_t row_blocks = a.s.num_tokens * parts;
+  if constexpr (VX) {
+    __shared__ int32_t ids[kRun];
+    __shared__ uint32_t ats[kRun];
+    if (blockIdx.x >= row_blocks) {
+      const uint32_t u = blockIdx.x - row_blocks;
+      append_turned<T, F8>(a, u / a.c.heads * kRun, u % a.c.heads, reinterpret_cast<uint16_t*>(lds), ids, ats);
+      return;
+    }
+  }
+  float(*turn)[L * 8 + 1] = reinterpret_cast<float(*)[L * 8 + 1]>(lds);
   const uint32_t lane = threadIdx.x % L, slot = threadIdx.x / L;
-  const uint32_t token = blockIdx.x;
-  const uint32_t row = blockIdx.y * kRows + slot, heads = a.c.heads;
-  const uint32_t d0 = lane * 8, D = a.c.dim, R = a.rot_dim;
+  const uint32_t token = blockIdx.x / parts, part = blockIdx.x % parts;
+  const uint32_t heads = a.c.heads, rows = a.q_heads + (VX ? 1 : 2) * heads;
+  const uint32_t d0 = lane * 8, D = a.c.dim, R = a.rot_dim, half = R / 2;
+  // Pairs a multiple of 8 apart: a lane's 8 partners are another lane's 8 values, its cosines 32 bytes in a row.
+  const bool paired = !a.interleaved && half % 8 == 0;
   const uint32_t seq = seq_of(a.s, token);  // by all lanes of a wave
-  const bool in = row < a.q_heads + 2 * heads;
-  const uint32_t kind = row < a.q_heads ? 0 : row < a.q_heads + heads ? 1 : 2;
-  const uint32_t head = kind == 0 ? row : kind == 1 ? row - a.q_heads : row - a.q_heads - heads;
-  const bool on = in && d0 < D;
-  float x[8] = {};
-  if (on) {
-    const RowArgs& src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-    unpack8<T>(load8(src.data + 2 * (token * src.token + head * src.head + d0), a.wide), x);
-  }
-  const void* weight = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
-  float sq = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) sq += x[i] * x[i];
-#pragma unroll
-  for (int i = 1; i < L; i *= 2) sq += __shfl_xor(sq, i, kOpsWave);
-  if (weight && on) {
-    const float by = 1.0f / sqrtf(sq / D + a.eps);
-    float w[8];
-    unpack8<T>(load8(static_cast<const uint8_t*>(weight) + 2 * d0, a.wide), w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * by * w[i];
-  }
+  float cs[8], sn[8];
   if (R) {
     int32_t p = a.positions[token];
     p = p < 0 ? 0 : p >= static_cast<int64_t>(a.rope_rows) ? static_cast<int32_t>(a.rope_rows - 1) : p;
-    const float* cs = a.rope + static_cast<uint64_t>(p) * R;
-    const uint32_t half = R / 2;
-    if (a.interleaved) {
-      if (on && kind < 2) {
+    const float* t = a.rope + static_cast<uint64_t>(p) * R;
+    if (d0 < R) {
+      if (paired) {
+        const uint32_t j = d0 < half ? d0 : d0 - half;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t d = d0 + 2 * i;
-          if (d < R) {
-            const float c = cs[d / 2], s = cs[half + d / 2], u = x[2 * i], v = x[2 * i + 1];
-            x[2 * i] = u * c - v * s;
-            x[2 * i + 1] = v * c + u * s;
+        for (int i = 0; i < 8; i += 4) {
+          const f32x4 c = *reinterpret_cast<const f32x4*>(t + j + i), s = *reinterpret_cast<const f32x4*>(t + half + j + i);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            cs[i + k] = c[k];
+            sn[i + k] = s[k];
           }
         }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) turn[slot][i * L + lane] = x[i];
-      __syncthreads();
-      if (on && kind < 2) {
+      } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const uint32_t d = d0 + i;
-          if (d < R) {
-            const bool low = d < half;
-            const uint32_t j = low ? d : d - half, o = low ? d + half : j;
-            const float c = cs[j], s = cs[half + j], v = turn[slot][o % 8 * L + o / 8];
-            x[i] = low ? x[i] * c - v * s : x[i] * c + v * s;
-          }
+          const uint32_t d = d0 + i < R ? d0 + i : R - 1, j = a.interleaved ? d / 2 : d < half ? d : d - half;
+          cs[i] = t[j];
+          sn[i] = t[half + j];
         }
       }
     }
   }
-  if (!on) return;
-  const u32x4 w = {pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])};
-  if (kind == 0) {
-    store8(a.out.data + 2 * (token * a.out.token + head * a.out.head + d0), w, a.wide);
-    return;
-  }
-  if (seq >= a.s.num_seqs) return;
-  const SeqSpan sp = span_of(a.s, seq);
-  const uint32_t i = token - sp.first, entry = sp.before + i;
-  if (token < sp.first || i >= sp.count || entry >= sp.total) return;
-  uint32_t at;
-  const int32_t id = block_at(a.c, a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride, entry, &at);
-  if (id < 0) return;
-  const uint64_t block = static_cast<uint64_t>(id) * a.c.block_bytes;
-  if (kind == 2 && VX) {
-    uint8_t* to = a.c.v + block + head * a.c.v_head + static_cast<uint64_t>(at) * a.c.v_token;
-    if constexpr (F8) {
-      const u32x2 b = to_f8(x, a.v_scale ? a.v_scale[head] : 1.0f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) to[static_cast<uint64_t>(d0 + j) * a.c.v_chunk] = static_cast<uint8_t>(b[j / 4] >> (j % 4 * 8));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint16_t*>(to + static_cast<uint64_t>(d0 + j) * a.c.v_chunk) = static_cast<uint16_t>(w[j / 2] >> (j % 2 * 16));
+  int32_t id = -1;
+  uint32_t at = 0;
+  if (part * kRows + 255 / L >= a.q_heads || parts == 1) id = entry_of(a, seq, token, &at);
+  const uint64_t block = static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes;
+  for (uint32_t row0 = part * kRows; row0 < rows; row0 += parts * kRows) {
+    const uint32_t row = row0 + slot;
+    const uint32_t kind = row < a.q_heads ? 0 : row < a.q_heads + heads ? 1 : 2;
+    const uint32_t head = kind == 0 ? row : kind == 1 ? row - a.q_heads : row - a.q_heads - heads;
+    const bool on = row < rows && d0 < D;
+    float x[8] = {};
+    if (on) {
+      const RowArgs& src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+      unpack8<T>(load8(src.data + 2 * (token * src.token + head * src.head + d0), a.wide), x);
     }
-    return;
-  }
-  uint8_t* to = kind == 1 ? a.c.k + block + head * a.c.k_head + static_cast<uint64_t>(at) * a.c.k_token
-                          : a.c.v + block + head * a.c.v_head + static_cast<uint64_t>(at) * a.c.v_token;
-  const uint64_t chunk = kind == 1 ? a.c.k_chunk : a.c.v_chunk;
-  if constexpr (F8) {
-    const float* scale = kind == 1 ? a.k_scale : a.v_scale;
-    *reinterpret_cast<u32x2*>(to + d0 / 16 * chunk + d0 % 16) = to_f8(x, scale ? scale[head] : 1.0f);
-  } else {
-    *reinterpret_cast<u32x4*>(to + d0 / 8 * chunk) = w;
+    const void* weight = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
+    if (a.q_weight || a.k_weight) {
+      float sq = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sq += x[i] * x[i];
+#pragma unroll
+      for (int i = 1; i < L; i *= 2) sq += __shfl_xor(sq, i, kOpsWave);
+      if (weight && on) {
+        const float by = 1.0f / sqrtf(sq / D + a.eps);
+        float w[8];
+        unpack8<T>(load8(static_cast<const uint8_t*>(weight) + 2 * d0, a.wide), w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * by * w[i];
+      }
+    }
+    if (R && row0 < a.q_heads + heads) {
+      const bool turns = on && kind < 2 && d0 < R, low = d0 < half;
+      if (a.interleaved) {
+        if (turns) {
+#pragma unroll
+          for (int i = 0; i < 8; i += 2)
+            if (d0 + i < R) {
+              const float u = x[i], v = x[i + 1];
+              x[i] = u * cs[i] - v * sn[i];
+              x[i + 1] = v * cs[i] + u * sn[i];
+            }
+        }
+      } else if (paired) {
+        const uint32_t other = threadIdx.x % kOpsWave / L * L + (low ? lane + half / 8 : lane - half / 8) % L;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = __shfl(x[i], other, kOpsWave);
+          if (turns) x[i] = low ? x[i] * cs[i] - v * sn[i] : x[i] * cs[i] + v * sn[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) turn[slot][i * L + lane] = x[i];
+        __syncthreads();
+        if (turns) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t d = d0 + i;
+            if (d < R) {
+              const uint32_t o = d < half ? d + half : d - half;
+              const float v = turn[slot][o % 8 * L + o / 8];
+              x[i] = d < half ? x[i] * cs[i] - v * sn[i] : x[i] * cs[i] + v * sn[i];
+            }
+          }
+        }
+        __syncthreads();
+      }
+    }
+    if (!on) continue;
+    const u32x4 w = {pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7])};
+    if (kind == 0) {
+      store8(a.out.data + 2 * (token * a.out.token + head * a.out.head + d0), w, a.wide);
+      continue;
+    }
+    if (id < 0) continue;
+    uint8_t* to = kind == 1 ? a.c.k + block + head * a.c.k_head + static_cast<uint64_t>(at) * a.c.k_token
+                            : a.c.v + block + head * a.c.v_head + static_cast<uint64_t>(at) * a.c.v_token;
+    const uint64_t chunk = kind == 1 ? a.c.k_chunk : a.c.v_chunk;
+    if constexpr (F8) {
+      const float* scale = kind == 1 ? a.k_scale : a.v_scale;
+      *reinterpret_cast<u32x2*>(to + d0 / 16 * chunk + d0 % 16) = to_f8(x, scale ? scale[head] : 1.0f);
+    } else {
+      *reinterpret_cast<u32x4*>(to + d0 / 8 * chunk) = w;
+    }
   }
 }
 
 // ---------------------------------------------------------------- commit
 // A thread has one 16-byte chunk (or x-packed value) of a head and takes the accepted
 // entries in order: with ascending indices entry i's place is never the source of a later
-// one, so that nothing but a thread's own order matters and no barrier is needed.
-constexpr uint32_t kAhead = 4;  // entries loaded before the first of them is stored
+// one, so that nothing but a thread's own order matters. What bounds it is the chain of
+// loads from a sequence's length over the list and the block table to the entries, so one
+// wave walks it once, for all threads, and a thread has 8 entries in flight.
+constexpr uint32_t kAhead = 8;    // entries loaded before the first of them is stored
+constexpr uint32_t kMoves = 64;   // entries listed at a time, one per lane of the first wave
 
-// How many of a row's accepted tokens are moved: up to the first that is out of order or range.
-__device__ __forceinline__ uint32_t accepted_count(const CommitArgs& a, uint32_t seq, uint32_t tokens, uint32_t* first_bad) {
-  const int32_t* acc = a.accepted + static_cast<uint64_t>(seq) * a.accepted_stride;
-  const int32_t c = a.counts[seq];
-  const uint32_t n = c < 0 ? 0 : static_cast<uint32_t>(c) > a.accepted_stride ? a.accepted_stride : static_cast<uint32_t>(c);
-  if (threadIdx.x == 0) *first_bad = n;
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x)
-    if (acc[i] < 0 || static_cast<uint32_t>(acc[i]) >= tokens || (i && acc[i] <= acc[i - 1])) atomicMin(first_bad, i);
-  __syncthreads();
-  return *first_bad;
-}
+struct Moves {
+  int32_t src[kMoves], dst[kMoves];      // blocks; dst is -1 where nothing moves
+  uint32_t src_at[kMoves], dst_at[kMoves];
+  int32_t token[kMoves];
+  int32_t before;  // entries of the sequence
+  int32_t count;  // of this time
+  bool last;
+};
 
 template <class U>
-__device__ __forceinline__ void move_entries(const CommitArgs& a, const int32_t* table, const int32_t* acc, uint32_t n,
-                                             uint32_t before, uint8_t* base, uint32_t token_stride) {
-  for (uint32_t i0 = 0; i0 < n; i0 += kAhead) {
+__device__ __forceinline__ void move_entries(const Moves& l, uint64_t block_bytes, uint8_t* base, uint32_t token_stride) {
+  for (int32_t i0 = 0; i0 < l.count; i0 += kAhead) {
     U x[kAhead];
-    uint8_t* to[kAhead];
+    uint64_t to[kAhead];
+    bool on[kAhead];
 #pragma unroll
     for (uint32_t j = 0; j < kAhead; ++j) {
-      to[j] = nullptr;
-      const uint32_t i = i0 + j;
-      if (i >= n || acc[i] == static_cast<int32_t>(i)) continue;
-      uint32_t st, dt;
-      const int32_t sb = block_at(a.c, table, before + acc[i], &st), db = block_at(a.c, table, before + i, &dt);
-      if (sb < 0 || db < 0) continue;
-      x[j] = *reinterpret_cast<const U*>(base + static_cast<uint64_t>(sb) * a.c.block_bytes + static_cast<uint64_t>(st) * token_stride);
-      to[j] = base + static_cast<uint64_t>(db) * a.c.block_bytes + static_cast<uint64_t>(dt) * token_stride;
+      const uint32_t i = i0 + j < kMoves ? i0 + j : kMoves - 1;
+      on[j] = static_cast<int32_t>(i0 + j) < l.count && l.dst[i] >= 0;
+      if (!on[j]) continue;
+      to[j] = static_cast<uint64_t>(l.dst[i]) * block_bytes + static_cast<uint64_t>(l.dst_at[i]) * token_stride;
+      x[j] = *reinterpret_cast<const U*>(base + static_cast<uint64_t>(l.src[i]) * block_bytes + static_cast<uint64_t>(l.src_at[i]) * token_stride);
     }
 #pragma unroll
     for (uint32_t j = 0; j < kAhead; ++j)
-      if (to[j]) *reinterpret_cast<U*>(to[j]) = x[j];
+      if (on[j]) *reinterpret_cast<U*>(base + to[j]) = x[j];
   }
 }
 
 template <bool F8, bool VX>
 __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a) {
   constexpr uint32_t E = F8 ? 1 : 2;
-  __shared__ uint32_t first_bad;
-  const uint32_t layer = blockIdx.x, seq = blockIdx.y;
-  const SeqSpan sp = span_of(a.s, seq);
-  const uint32_t n = accepted_count(a, seq, sp.total - sp.before, &first_bad);
-  if (layer == 0 && threadIdx.x == 0 && a.lens_out) a.lens_out[seq] = static_cast<int32_t>(sp.before + n);
+  __shared__ Moves list;
+  const uint32_t layer = blockIdx.y, seq = blockIdx.z, lane = threadIdx.x % kOpsWave;
   const int32_t* acc = a.accepted + static_cast<uint64_t>(seq) * a.accepted_stride;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
   const uint32_t chunks = a.c.dim * E / 16, vs = VX ? a.c.dim : chunks, per = chunks + vs;
   uint8_t* const base = reinterpret_cast<uint8_t*>(a.layer[layer]);
-  for (uint32_t u = threadIdx.x; u < a.c.heads * per; u += blockDim.x) {
-    const uint32_t head = u / per, i = u % per;
-    if (i < chunks) {
-      move_entries<u32x4>(a, table, acc, n, sp.before, base + head * a.c.k_head + static_cast<uint64_t>(i) * a.c.k_chunk, a.c.k_token);
-    } else {
-      uint8_t* v = base + a.v_offset + head * a.c.v_head + static_cast<uint64_t>(i - chunks) * a.c.v_chunk;
-      if constexpr (!VX)
-        move_entries<u32x4>(a, table, acc, n, sp.before, v, a.c.v_token);
-      else if constexpr (F8)
-        move_entries<uint8_t>(a, table, acc, n, sp.before, v, a.c.v_token);
-      else
-        move_entries<uint16_t>(a, table, acc, n, sp.before, v, a.c.v_token);
+  const uint32_t u = blockIdx.x * 256 + threadIdx.x, head = u / per, i = u % per;
+  float* const scores = reinterpret_cast<float*>(a.scores[layer]);
+  for (uint32_t first = 0;; first += kMoves) {
+    if (threadIdx.x < kOpsWave) {
+      const uint32_t at = first + lane;
+      const int32_t j = at < a.accepted_stride ? acc[at] : -1, before = at && at < a.accepted_stride ? acc[at - 1] : -1;
+      const int32_t c = a.counts[seq];
+      const SeqSpan sp = span_of(a.s, seq);
+      const uint32_t n = c < 0 ? 0 : static_cast<uint32_t>(c) > a.accepted_stride ? a.accepted_stride : static_cast<uint32_t>(c);
+      const bool good = at < n && j >= 0 && static_cast<uint32_t>(j) < sp.total - sp.before && j > before;
+      const uint64_t bad = ~__ballot(good);
+      const uint32_t count = bad ? __builtin_ctzll(bad) : kOpsWave;
+      if (lane < count) {
+        uint32_t st, dt;
+        const int32_t sb = block_at(a.c, table, sp.before + j, &st), db = block_at(a.c, table, sp.before + at, &dt);
+        list.src[lane] = sb;
+        list.src_at[lane] = st;
+        list.dst[lane] = static_cast<uint32_t>(j) == at || sb < 0 ? -1 : db;
+        list.dst_at[lane] = dt;
+        list.token[lane] = j;
+      }
+      if (!lane) {
+        list.before = static_cast<int32_t>(sp.before);
+        list.count = count;
+        list.last = bad != 0;
+        if (a.lens_out && bad && !layer && !blockIdx.x) a.lens_out[seq] = static_cast<int32_t>(sp.before + first + count);
+      }
     }
-  }
-  if (!a.scores[layer]) return;
-  for (uint32_t head = threadIdx.x; head < a.c.heads; head += blockDim.x) {
-    float* w = reinterpret_cast<float*>(a.scores[layer]) + (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + sp.before;
-    for (uint32_t i = 0; i < n; ++i) w[i] = w[acc[i]];
+    __syncthreads();
+    if (head < a.c.heads) {
+      if (i < chunks) {
+        move_entries<u32x4>(list, a.c.block_bytes, base + head * a.c.k_head + static_cast<uint64_t>(i) * a.c.k_chunk, a.c.k_token);
+      } else {
+        uint8_t* v = base + a.v_offset + head * a.c.v_head + static_cast<uint64_t>(i - chunks) * a.c.v_chunk;
+        if constexpr (!VX)
+          move_entries<u32x4>(list, a.c.block_bytes, v, a.c.v_token);
+        else if constexpr (F8)
+          move_entries<uint8_t>(list, a.c.block_bytes, v, a.c.v_token);
+        else
+          move_entries<uint16_t>(list, a.c.block_bytes, v, a.c.v_token);
+      }
+    }
+    if (scores) {  // a wave has a head's, 4 heads on their way at once
+      const uint32_t step = gridDim.x * 4;
+      for (uint32_t h0 = blockIdx.x * 4 + threadIdx.x / kOpsWave; h0 < a.c.heads; h0 += 4 * step) {
+        float* w = scores + (static_cast<uint64_t>(seq) * a.c.heads + h0) * a.scores_stride + list.before;
+        float x[4];
+        const bool on = static_cast<int32_t>(lane) < list.count;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+          if (on && h0 + k * step < a.c.heads) x[k] = w[static_cast<uint64_t>(k) * step * a.scores_stride + list.token[lane]];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+          if (on && h0 + k * step < a.c.heads) w[static_cast<uint64_t>(k) * step * a.scores_stride + first + lane] = x[k];
+      }
+    }
+    if (list.last) return;
+    __syncthreads();
   }
 }
 
@@ -287,9 +429,11 @@ __device__ __forceinline__ uint32_t order_of(float f) {
 }
 
 constexpr uint32_t kSelect = 1024;  // threads of a selection
+constexpr uint32_t kWaves = kSelect / kOpsWave;
+constexpr uint32_t kCopies = 32;    // of the counters: a lane of each half wave has its own bank
 
-// Sum over the workgroup of values below this thread's, and of all (LDS: one word per wave and one more).
-__device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* lds, uint32_t* total) {
+// Sum over the workgroup of values of threads below this one (LDS: a word per wave).
+__device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* lds) {
   const uint32_t lane = threadIdx.x % kOpsWave, wave = threadIdx.x / kOpsWave;
   uint32_t x = v;
 #pragma unroll
@@ -300,23 +444,25 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* lds, ui
   __syncthreads();
   if (lane == kOpsWave - 1) lds[wave] = x;
   __syncthreads();
-  uint32_t before = 0, all = 0;
-  for (uint32_t w = 0; w < kSelect / kOpsWave; ++w) {
-    const uint32_t n = lds[w];
-    if (w < wave) before += n;
-    all += n;
-  }
-  *total = all;
+  uint32_t before = 0;
+#pragma unroll
+  for (uint32_t w = 0; w < kWaves; ++w) before += w < wave ? lds[w] : 0;
   return before + x - v;
 }
 
-// Which entries of one sequence and KV head stay: the number of scores wanted among those
-// that compete gives a threshold, found 8 bits at a time from the top by counting (four
-// passes over the scores), then one pass in order writes the entries above it and, of those
-// equal to it, the first ones still wanted.
+// Which entries of one sequence and KV head stay: the number wanted among the scores that
+// compete gives a threshold, found 8 bits at a time from the top by counting, then the
+// entries above it and, of those equal to it, the first ones still wanted are written in order.
+// A thread has every 1024th score, N of them at a time in registers: up to 1024 N are read
+// once; longer rows are read in each of the (up to six) passes. Counters are kept 32 times
+// over, side by side: scores that share their high bits, as most do, would otherwise queue at one.
+// Ranks come from ballots: what a wave keeps of its k-th scores is a number for each (k, wave), in
+// the order of the entries, summed up by one scan.
+template <uint32_t N>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t bins[256], scan[kSelect / kOpsWave + 1], found[2];
-  const uint32_t head = blockIdx.x, seq = blockIdx.y;
+  __shared__ uint32_t bins[256 * kCopies];
+  __shared__ uint32_t scan[kWaves], found[3], counts[N * kWaves];
+  const uint32_t head = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x % kOpsWave, wave = threadIdx.x / kOpsWave;
   const int32_t len = a.s.lens[seq];
   uint32_t n = len < 0 ? 0 : static_cast<uint32_t>(len);
   if (n > a.s.max_len) n = a.s.max_len;
@@ -338,106 +484,226 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     return;
   }
   const uint32_t lo = a.sinks, hi = n - a.recent;  // those that compete
-  uint32_t want = a.keep - a.sinks - a.recent;
-  uint32_t prefix = 0, equal = 0;  // the threshold's bits so far; how many of those equal to it stay
+  const uint32_t segments = (n + N * kSelect - 1) / (N * kSelect);
+  uint32_t order[N];  // of the thread's scores
+  const auto load = [&](uint32_t seg) {
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
+      order[k] = order_of(i < n ? w[i] : 0.0f);
+    }
+  };
+  const auto step = []() { if constexpr (N > 16) __builtin_amdgcn_sched_barrier(0); };  // keeps one score's ballot in registers, not all
+  load(0);
+  uint32_t want = a.keep - a.sinks - a.recent, prefix = 0;
+  bool ties = false;  // more entries equal the threshold than are wanted
   if (want) {
     for (int shift = 24; shift >= 0; shift -= 8) {
-      for (uint32_t i = threadIdx.x; i < 256; i += kSelect) bins[i] = 0;
+      for (uint32_t i = threadIdx.x; i < 256 * kCopies; i += kSelect) bins[i] = 0;
       __syncthreads();
-      for (uint32_t i = lo + threadIdx.x; i < hi; i += kSelect) {
-        const uint32_t u = order_of(w[i]);
-        if (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&bins[u >> shift & 255], 1u);
+      for (uint32_t seg = 0; seg < segments; ++seg) {
+        if (segments > 1) load(seg);
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k) {
+          const uint32_t i = (seg * N + k) * kSelect + threadIdx.x, u = order[k];
+          if (i >= lo && i < hi && (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8)))
+            atomicAdd(&bins[(u >> shift & 255) * kCopies + lane % kCopies], 1u);
+        }
       }
       __syncthreads();
-      if (threadIdx.x == 0) {
-        uint32_t left = want, b = 255;
-        while (b && bins[b] < left) left -= bins[b--];
-        found[0] = b;
-        found[1] = left;
+      // 4 threads a bin, 8 copies each; then the first wave finds the bin, 4 bins a lane from the top.
+      uint32_t sum = 0;
+#pragma unroll
+      for (uint32_t c = 0; c < kCopies / 4; ++c) sum += bins[threadIdx.x / 4 * kCopies + (threadIdx.x % 4) * (kCopies / 4) + (c + threadIdx.x) % (kCopies / 4)];
+      sum += __shfl_xor(sum, 1, kOpsWave);
+      sum += __shfl_xor(sum, 2, kOpsWave);
+      __syncthreads();
+      if (threadIdx.x % 4 == 0) bins[threadIdx.x / 4] = sum;
+      __syncthreads();
+      if (wave == 0) {
+        uint32_t b[4], all = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) all += b[i] = bins[255 - (lane * 4 + i)];
+        uint32_t above = all;
+#pragma unroll
+        for (int i = 1; i < kOpsWave; i *= 2) {
+          const uint32_t y = __shfl_up(above, i, kOpsWave);
+          if (lane >= static_cast<uint32_t>(i)) above += y;
+        }
+        above -= all;  // in the lanes before: in higher bins
+        if (above < want && above + all >= want) {  // one lane
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            if (above < want && above + b[i] >= want) {
+              found[0] = 255 - (lane * 4 + i);
+              found[1] = want - above;
+              found[2] = b[i];
+            }
+            above += b[i];
+          }
+        }
       }
       __syncthreads();
       prefix |= found[0] << shift;
       want = found[1];
+      ties = found[2] > want;
       __syncthreads();
     }
-    equal = want;
   }
-  const bool none = a.keep == a.sinks + a.recent;
+  const bool some = a.keep > a.sinks + a.recent;
   uint32_t base = 0, equals = 0;
-  for (uint32_t i0 = 0; i0 < n; i0 += kSelect) {
-    const uint32_t i = i0 + threadIdx.x;
-    const bool live = i < n, fixed = live && (i < lo || i >= hi);
-    const float f = live ? w[i] : 0;
-    const uint32_t u = order_of(f);
-    const bool competes = live && !fixed && !none;
-    uint32_t total;
-    const bool eq = competes && u == prefix;
-    const uint32_t eq_before = equals + exclusive_scan(eq, scan, &total);
-    equals += total;
-    const bool stay = fixed || (competes && u > prefix) || (eq && eq_before < equal);
-    const uint32_t at = base + exclusive_scan(stay, scan, &total);
-    base += total;
-    if (stay && at < a.keep) {
-      out[at] = static_cast<int32_t>(i);
-      if (ws) ws[at] = f;
+  for (uint32_t seg = 0; seg < segments; ++seg) {
+    if (segments > 1) load(seg);
+    const auto competes = [&](uint32_t i) { return some && i >= lo && i < hi; };
+    // Ranks among the equal ones, where not all of them stay.
+    if (ties) {
+#pragma unroll
+      for (uint32_t k = 0; k < N; ++k) {
+        const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
+        const uint64_t m = __ballot(competes(i) && order[k] == prefix);
+        if (!lane) counts[k * kWaves + wave] = __popcll(m);
+        step();
+      }
+      __syncthreads();
+      for (uint32_t i0 = 0; i0 < N * kWaves; i0 += kSelect) {
+        const uint32_t i = i0 + threadIdx.x, c = i < N * kWaves ? counts[i] : 0, at = equals + exclusive_scan(c, scan);
+        if (i < N * kWaves) counts[i] = at;
+        if (threadIdx.x == kSelect - 1) found[0] = at + c;
+        __syncthreads();
+        equals = found[0];
+      }
     }
+    const auto stays = [&](uint32_t k, uint32_t eq_before) {
+      const uint32_t i = (seg * N + k) * kSelect + threadIdx.x, u = order[k];
+      const bool eq = competes(i) && u == prefix;
+      bool s = i < n && (i < lo || i >= hi || (competes(i) && u > prefix));
+      if (!ties) return s || eq;
+      const uint64_t m = __ballot(eq);
+      return s || (eq && eq_before + __popcll(m & ((1ull << lane) - 1)) < want);
+    };
+    uint64_t kept_bits = 0;  // bit k: this thread's k-th score stays
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      if (stays(k, ties ? counts[k * kWaves + wave] : 0)) kept_bits |= 1ull << k;
+      step();
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint64_t m = __ballot(kept_bits >> k & 1);
+      if (!lane) counts[k * kWaves + wave] = __popcll(m);
+      step();
+    }
+    __syncthreads();
+    for (uint32_t i0 = 0; i0 < N * kWaves; i0 += kSelect) {
+      const uint32_t i = i0 + threadIdx.x, c = i < N * kWaves ? counts[i] : 0, at = base + exclusive_scan(c, scan);
+      if (i < N * kWaves) counts[i] = at;
+      if (threadIdx.x == kSelect - 1) found[1] = at + c;
+      __syncthreads();
+      base = found[1];
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) {
+      const uint64_t m = __ballot(kept_bits >> k & 1);
+      const uint32_t at = counts[k * kWaves + wave] + __popcll(m & ((1ull << lane) - 1));
+      if ((kept_bits >> k & 1) && at < a.keep) {
+        const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
+        out[at] = static_cast<int32_t>(i);
+        if (ws) ws[at] = w[i];
+      }
+      step();
+    }
+    __syncthreads();
   }
 }
 
-// The kept entries to their new blocks: 8 of one head per row of threads.
+// The kept entries to their new blocks: kMoved of one head in a workgroup. Where they come from and go to is looked up
+// once for all their chunks, and a thread has 4 chunks in flight.
+constexpr uint32_t kMoved = 64;
+
 template <bool F8, bool VX>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
   constexpr uint32_t E = F8 ? 1 : 2;
-  const uint32_t head = blockIdx.y, seq = blockIdx.z, first = blockIdx.x * 32;
+  __shared__ uint64_t from[kMoved], to[kMoved];  // of the blocks
+  __shared__ uint32_t from_at[kMoved], to_at[kMoved];
+  const uint32_t head = blockIdx.y, seq = blockIdx.z, first = blockIdx.x * kMoved;
   const int32_t len = a.s.lens[seq];
   uint32_t n = len < 0 ? 0 : static_cast<uint32_t>(len);
   if (n > a.s.max_len) n = a.s.max_len;
   const uint32_t kept = n < a.keep ? n : a.keep;
   if (first >= kept) return;
-  const uint32_t count = kept - first < 32 ? kept - first : 32;
-  const int32_t* from = a.entries + (static_cast<uint64_t>(seq) * a.c.heads + head) * a.keep + first;
-  const int32_t* src = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
-  const int32_t* dst = a.dst_table + static_cast<uint64_t>(seq) * a.dst_stride;
-  const uint32_t chunks = a.c.dim * E / 16, per = VX ? chunks : 2 * chunks;
-  for (uint32_t u = threadIdx.x; u < count * per; u += blockDim.x) {
-    const uint32_t e = u / per, i = u % per;
+  const uint32_t count = kept - first < kMoved ? kept - first : kMoved;
+  constexpr uint64_t kNone = ~0ull;
+  if (threadIdx.x < count) {
+    const uint32_t e = first + threadIdx.x;
     uint32_t st, dt;
-    const int32_t sb = block_at(a.c, src, static_cast<uint32_t>(from[e]), &st), db = block_at(a.c, dst, first + e, &dt);
-    if (sb < 0 || db < 0) continue;
-    const bool key = i < chunks;
-    uint8_t* base = key ? a.c.k + head * a.c.k_head + static_cast<uint64_t>(i) * a.c.k_chunk
-                        : a.c.v + head * a.c.v_head + static_cast<uint64_t>(i - chunks) * a.c.v_chunk;
-    const uint64_t ts = key ? a.c.k_token : a.c.v_token;
-    *reinterpret_cast<u32x4*>(base + static_cast<uint64_t>(db) * a.c.block_bytes + dt * ts) =
-        *reinterpret_cast<const u32x4*>(base + static_cast<uint64_t>(sb) * a.c.block_bytes + st * ts);
+    const int32_t db = block_at(a.c, a.dst_table + static_cast<uint64_t>(seq) * a.dst_stride, e, &dt);
+    const uint32_t src = static_cast<uint32_t>(a.entries[(static_cast<uint64_t>(seq) * a.c.heads + head) * a.keep + e]);
+    const int32_t sb = block_at(a.c, a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride, src, &st);
+    from[threadIdx.x] = static_cast<uint64_t>(sb < 0 ? 0 : sb) * a.c.block_bytes;
+    from_at[threadIdx.x] = st;
+    to[threadIdx.x] = sb < 0 || db < 0 ? kNone : static_cast<uint64_t>(db) * a.c.block_bytes;
+    to_at[threadIdx.x] = dt;
+  }
+  __syncthreads();
+  const uint32_t chunks = a.c.dim * E / 16, per = VX ? chunks : 2 * chunks, total = count * per;
+  constexpr uint32_t kU = 4;
+  for (uint32_t u0 = threadIdx.x; u0 < total; u0 += 256 * kU) {
+    u32x4 x[kU];
+    uint8_t* p[kU];
+#pragma unroll
+    for (uint32_t j = 0; j < kU; ++j) {
+      const uint32_t u = u0 + j * 256, e = u / per, i = u % per;
+      p[j] = nullptr;
+      if (u >= total || to[e] == kNone) continue;
+      const bool key = i < chunks;
+      uint8_t* base = key ? a.c.k + head * a.c.k_head + static_cast<uint64_t>(i) * a.c.k_chunk
+                          : a.c.v + head * a.c.v_head + static_cast<uint64_t>(i - chunks) * a.c.v_chunk;
+      const uint64_t ts = key ? a.c.k_token : a.c.v_token;
+      x[j] = *reinterpret_cast<const u32x4*>(base + from[e] + from_at[e] * ts);
+      p[j] = base + to[e] + to_at[e] * ts;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kU; ++j)
+      if (p[j]) *reinterpret_cast<u32x4*>(p[j]) = x[j];
   }
   if constexpr (VX) {
-    for (uint32_t u = threadIdx.x; u < count * a.c.dim; u += blockDim.x) {
-      const uint32_t d = u / count, e = u % count;
-      uint32_t st, dt;
-      const int32_t sb = block_at(a.c, src, static_cast<uint32_t>(from[e]), &st), db = block_at(a.c, dst, first + e, &dt);
-      if (sb < 0 || db < 0) continue;
-      uint8_t* base = a.c.v + head * a.c.v_head + static_cast<uint64_t>(d) * a.c.v_chunk;
-      const uint8_t* s = base + static_cast<uint64_t>(sb) * a.c.block_bytes + st * E;
-      uint8_t* t = base + static_cast<uint64_t>(db) * a.c.block_bytes + dt * E;
-      if constexpr (F8)
-        *t = *s;
-      else
-        *reinterpret_cast<uint16_t*>(t) = *reinterpret_cast<const uint16_t*>(s);
+    // A value of consecutive entries lies side by side where they go: consecutive threads write it.
+    typedef typename std::conditional<F8, uint8_t, uint16_t>::type U;
+    const uint32_t values = count * a.c.dim;
+    for (uint32_t u0 = threadIdx.x; u0 < values; u0 += 256 * kU) {
+      U x[kU];
+      uint8_t* p[kU];
+#pragma unroll
+      for (uint32_t j = 0; j < kU; ++j) {
+        const uint32_t u = u0 + j * 256, d = u / count, e = u % count;
+        p[j] = nullptr;
+        if (u >= values || to[e] == kNone) continue;
+        uint8_t* base = a.c.v + head * a.c.v_head + static_cast<uint64_t>(d) * a.c.v_chunk;
+        x[j] = *reinterpret_cast<const U*>(base + from[e] + from_at[e] * E);
+        p[j] = base + to[e] + to_at[e] * E;
+      }
+#pragma unroll
+      for (uint32_t j = 0; j < kU; ++j)
+        if (p[j]) *reinterpret_cast<U*>(p[j]) = x[j];
     }
   }
 }
 
 template <class T, bool F8, bool VX>
 hipError_t append_of(const AppendArgs& a, hipStream_t stream) {
-  const uint32_t lanes = a.c.dim <= 64 ? 8 : a.c.dim <= 128 ? 16 : 32, rows = 256 / lanes;
-  const dim3 grid(a.s.num_tokens, (a.q_heads + 2 * a.c.heads + rows - 1) / rows);
+  const uint32_t lanes = a.c.dim <= 64 ? 8 : a.c.dim <= 128 ? 16 : 32, per = 256 / lanes, n = a.s.num_tokens;
+  const uint32_t all = (a.q_heads + (VX ? 1 : 2) * a.c.heads + per - 1) / per;
+  // One workgroup for a token's rows where tokens alone fill the GPU, else one for each part of them.
+  const uint32_t parts = n >= 1024 ? 1 : all;
+  const uint32_t grid = n * parts + (VX ? (n + kRun - 1) / kRun * a.c.heads : 0);
   if (lanes == 8)
-    append_kernel<T, F8, VX, 8><<<grid, 256, 0, stream>>>(a);
+    append_kernel<T, F8, VX, 8><<<grid, 256, 0, stream>>>(a, parts);
   else if (lanes == 16)
-    append_kernel<T, F8, VX, 16><<<grid, 256, 0, stream>>>(a);
+    append_kernel<T, F8, VX, 16><<<grid, 256, 0, stream>>>(a, parts);
   else
-    append_kernel<T, F8, VX, 32><<<grid, 256, 0, stream>>>(a);
+    append_kernel<T, F8, VX, 32><<<grid, 256, 0, stream>>>(a, parts);
   return hipGetLastError();
 }
 
@@ -456,7 +722,8 @@ hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stre
 
 hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stream) {
   const bool f8 = k.cache_type == MMA_TYPE_F8, vx = k.layout == MMA_KV_LAYOUT_XPACKED;
-  const dim3 grid(a.layers, a.s.num_seqs);
+  const uint32_t chunks = a.c.dim * (f8 ? 1 : 2) / 16, units = a.c.heads * (chunks + (vx ? a.c.dim : chunks));
+  const dim3 grid((units + 255) / 256, a.layers, a.s.num_seqs);
   if (f8 && vx)
     commit_kernel<true, true><<<grid, 256, 0, stream>>>(a);
   else if (f8)
@@ -470,11 +737,17 @@ hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stre
 
 hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream) {
   const bool f8 = k.cache_type == MMA_TYPE_F8, vx = k.layout == MMA_KV_LAYOUT_XPACKED;
-  evict_select_kernel<<<dim3(a.c.heads, a.s.num_seqs), kSelect, 0, stream>>>(a);
+  const dim3 pairs(a.c.heads, a.s.num_seqs);
+  if (a.s.max_len <= 4 * kSelect)
+    evict_select_kernel<4><<<pairs, kSelect, 0, stream>>>(a);
+  else if (a.s.max_len <= 16 * kSelect)
+    evict_select_kernel<16><<<pairs, kSelect, 0, stream>>>(a);
+  else
+    evict_select_kernel<64><<<pairs, kSelect, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint32_t most = std::min(a.keep, a.s.max_len);
-  const dim3 grid((most + 31) / 32, a.c.heads, a.s.num_seqs);
+  const dim3 grid((most + kMoved - 1) / kMoved, a.c.heads, a.s.num_seqs);
   if (f8 && vx)
     evict_move_kernel<true, true><<<grid, 256, 0, stream>>>(a);
   else if (f8)

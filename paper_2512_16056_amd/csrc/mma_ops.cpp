@@ -244,7 +244,7 @@ AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& 
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
-  const uint64_t want = 1024, least = 256;  // workgroups in all, entries of a split
+  const uint64_t want = p.stream ? 1024 : 512, least = 256;  // workgroups in all, entries of a split
   uint64_t splits = wgs >= want ? 1 : (want + wgs - 1) / std::max<uint64_t>(wgs, 1);
   splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, up(q.max_len, least)));
   p.split_len = up(up(q.max_len, static_cast<uint32_t>(splits)), 128) * 128;
