@@ -579,6 +579,8 @@ typedef struct mma_kv_evict {
   int32_t* entries;         /* [num_seqs][kv_heads][keep]: the entries kept, ascending, -1 behind them */
   float* scores_out;        /* [num_seqs][kv_heads][keep] or NULL: their scores, 0 behind them */
   int32_t* lens_out;        /* [num_seqs] or NULL; not seqs->lens */
+  void* workspace;          /* mma_kv_evict_workspace bytes of device memory, 8-byte aligned, as for attention */
+  uint64_t workspace_bytes;
   uint32_t dst_stride;      /* at least keep / block_tokens, rounded up */
   uint32_t scores_stride;   /* at least max_len */
   uint32_t keep;            /* at least sinks + recent, and 1 */
@@ -592,6 +594,10 @@ typedef struct mma_kv_evict {
  * has its own. */
 mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
                           const mma_kv_evict_t* args, void* stream);
+
+/* Host only: the workspace of that call: 8 bytes and 8 for every 1024 of max_len, for each
+ * sequence and KV head. */
+mma_status_t mma_kv_evict_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, uint64_t* bytes);
 
 /* ------------------------------------------------------------------- status */
 

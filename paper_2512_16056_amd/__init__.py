@@ -181,7 +181,8 @@ class mma_kv_commit_t(ctypes.Structure):
 
 class mma_kv_evict_t(ctypes.Structure):
     _fields_ = [("dst_table", ctypes.c_void_p), ("scores", ctypes.c_void_p), ("entries", ctypes.c_void_p),
-                ("scores_out", ctypes.c_void_p), ("lens_out", ctypes.c_void_p), ("dst_stride", ctypes.c_uint32),
+                ("scores_out", ctypes.c_void_p), ("lens_out", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_uint64), ("dst_stride", ctypes.c_uint32),
                 ("scores_stride", ctypes.c_uint32), ("keep", ctypes.c_uint32), ("sinks", ctypes.c_uint32),
                 ("recent", ctypes.c_uint32)]
 
@@ -222,6 +223,7 @@ _SIGNATURES = {
                        ctypes.POINTER(mma_kv_commit_t), _P], _S),
     "mma_kv_evict": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
                       ctypes.POINTER(mma_kv_evict_t), _P], _S),
+    "mma_kv_evict_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(mma_kv_seqs_t), ctypes.POINTER(_U64)], _S),
     "mma_get_stats": ([ctypes.POINTER(mma_stats_t)], _S),
     "mma_reset_stats": ([], _S),
     "mma_status_str": ([_S], ctypes.c_char_p),
@@ -451,7 +453,7 @@ _ATTENTION_T = struct.Struct("@6Q8Q6I2f")
 _WORKSPACE_T = struct.Struct("@2Q")
 _WORKSPACE_AT = mma_kv_attention_t.workspace.offset
 _COMMIT_T = struct.Struct("@4Q2I")
-_EVICT_T = struct.Struct("@5Q5I4x")
+_EVICT_T = struct.Struct("@7Q5I4x")
 assert (_APPEND_T.size, _ATTENTION_T.size, _COMMIT_T.size, _EVICT_T.size) == tuple(
     ctypes.sizeof(x) for x in (mma_kv_append_t, mma_kv_attention_t, mma_kv_commit_t, mma_kv_evict_t))
 
@@ -664,10 +666,18 @@ def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch
     return lens
 
 
+def kv_evict_workspace(layout: mma_kv_layout_t, seqs: KVSeqs) -> int:
+    """Bytes of workspace of an eviction call."""
+    need = _U64()
+    _check(lib.mma_kv_evict_workspace(layout, seqs.c, need), "mma_kv_evict_workspace")
+    return need.value
+
+
 def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.Tensor, scores: torch.Tensor, keep: int,
-                 *, sinks: int = 0, recent: int = 0, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+                 *, sinks: int = 0, recent: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Keep the `keep` entries of each sequence and KV head that attention went to, moved into the blocks of
-    dst_table; returns (entries kept, their scores, new lengths)."""
+    dst_table; returns (entries kept, their scores, new lengths). `workspace`: a uint8 tensor of kv_evict_workspace()
+    bytes or more; a new one of the stream's unless given."""
     n, heads = seqs.num_seqs, layout.kv_heads
     if dst_table.dim() != 2 or dst_table.shape[0] != n:
         raise ValueError(f"dst_table: [{n}][blocks] is wanted, got {tuple(dst_table.shape)}")
@@ -678,8 +688,12 @@ def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.
     entries = _empty_on(stream, (n, heads, keep), torch.int32, seqs.device)
     kept = _empty_on(stream, (n, heads, keep), torch.float32, seqs.device)
     lens = _empty_on(stream, (n,), torch.int32, seqs.device)
+    if workspace is None:
+        workspace = _empty_on(stream, (kv_evict_workspace(layout, seqs),), torch.uint8, seqs.device)
+    else:
+        _want("workspace", workspace, torch.uint8)
     a = _EVICT_T.pack(_want("dst_table", dst_table, torch.int32), _want("scores", scores, torch.float32), entries.data_ptr(),
-                      kept.data_ptr(), lens.data_ptr(), dst_table.shape[1], scores.shape[2], keep, sinks, recent)
+                      kept.data_ptr(), lens.data_ptr(), workspace.data_ptr(), workspace.numel(), dst_table.shape[1], scores.shape[2], keep, sinks, recent)
     rc = _evict(ctypes.byref(layout), _ptr(layer), seqs.address, a, _stream(stream))
     if rc:
         _check(rc, "mma_kv_evict")

@@ -420,17 +420,42 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a) {
 }
 
 // ---------------------------------------------------------------- evict
-// Order of scores as unsigned numbers: NaN lowest, the two zeros equal.
+// Order of scores as unsigned numbers: NaN below all, the two zeros equal. 0 and kFixed are no score's.
+constexpr uint32_t kFixed = 0xffffffffu;
 __device__ __forceinline__ uint32_t order_of(float f) {
   uint32_t u = __builtin_bit_cast(uint32_t, f);
-  if (f != f) return 0;
+  if (f != f) return 1;
   if (u == 0x80000000u) u = 0;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
 constexpr uint32_t kSelect = 1024;  // threads of a selection
 constexpr uint32_t kWaves = kSelect / kOpsWave;
-constexpr uint32_t kCopies = 32;    // of the counters: a lane of each half wave has its own bank
+constexpr uint32_t kDigit = 11;     // bits of the threshold found at a time: 11, 11, 10
+constexpr uint32_t kBins = 1u << kDigit;
+constexpr uint32_t kCopies = 8;     // of the counters, for neighbouring lanes
+constexpr uint32_t kCopyBins = kBins + 8;  // a counter's copies lie in different banks
+constexpr uint32_t kListed = 16;    // longer rows (in 1024 entries) have their kept entries listed by a launch of its own
+
+// The first and last entries have the highest order there is, places past the end the lowest: with more
+// entries than are kept neither needs a condition of its own.
+__device__ __forceinline__ uint32_t order_at(const EvictArgs& a, const float* w, uint32_t i, uint32_t n) {
+  if (i >= n) return 0;
+  return i < a.sinks || i >= n - a.recent ? kFixed : order_of(w[i]);
+}
+
+__device__ __forceinline__ uint32_t entries_of(const EvictArgs& a, uint32_t seq) {
+  const int32_t len = a.s.lens[seq];
+  const uint32_t n = len < 0 ? 0 : static_cast<uint32_t>(len);
+  return n > a.s.max_len ? a.s.max_len : n;
+}
+
+// What the selection of a row (sequence and KV head) tells the workgroups that list its entries, in the
+// workspace: { threshold, how many of those equal to it stay }, then for each 1024 entries { how many
+// before them are above the threshold, how many equal to it }.
+__device__ __forceinline__ uint32_t* selected(const EvictArgs& a, uint64_t row) {
+  return a.chosen + row * 2 * (1 + (a.s.max_len + kSelect - 1) / kSelect);
+}
 
 // Sum over the workgroup of values of threads below this one (LDS: a word per wave).
 __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* lds) {
@@ -450,22 +475,20 @@ __device__ __forceinline__ uint32_t exclusive_scan(uint32_t v, uint32_t* lds) {
   return before + x - v;
 }
 
-// Which entries of one sequence and KV head stay: the number wanted among the scores that
-// compete gives a threshold, found 8 bits at a time from the top by counting, then the
-// entries above it and, of those equal to it, the first ones still wanted are written in order.
-// A thread has every 1024th score, N of them at a time in registers: up to 1024 N are read
-// once; longer rows are read in each of the (up to six) passes. Counters are kept 32 times
-// over, side by side: scores that share their high bits, as most do, would otherwise queue at one.
-// Ranks come from ballots: what a wave keeps of its k-th scores is a number for each (k, wave), in
-// the order of the entries, summed up by one scan.
+// Which entries of one row stay. First the threshold, the order of the last that stays, found 11 bits at
+// a time from the top by counting; where all entries that share the bits found so far stay, the rest need not
+// be known. A thread has every 1024th score, N of them at a time in registers: up to 1024 N are read
+// once; longer rows are read in each pass. Then counts of those above the threshold and equal to it, from ballots: a
+// wave's k-th scores are 64 entries in a row, so (k, wave) is their order. Rows of up to 16 x 1024 are
+// listed here; of longer ones, whose 64 scores a thread would go over some more times, the counts go to
+// the workgroups of evict_list_kernel.
+// What bounds it is one CU's arithmetic: about 10 instructions a score and pass.
 template <uint32_t N>
 __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t bins[256 * kCopies];
+  __shared__ __attribute__((aligned(8))) uint32_t bins[kCopyBins * kCopies];
   __shared__ uint32_t scan[kWaves], found[3], counts[N * kWaves];
   const uint32_t head = blockIdx.x, seq = blockIdx.y, lane = threadIdx.x % kOpsWave, wave = threadIdx.x / kOpsWave;
-  const int32_t len = a.s.lens[seq];
-  uint32_t n = len < 0 ? 0 : static_cast<uint32_t>(len);
-  if (n > a.s.max_len) n = a.s.max_len;
+  const uint32_t n = entries_of(a, seq);
   const uint64_t row = static_cast<uint64_t>(seq) * a.c.heads + head;
   const float* w = a.scores + row * a.scores_stride;
   int32_t* out = a.entries + row * a.keep;
@@ -476,150 +499,184 @@ __global__ __launch_bounds__(kSelect) void evict_select_kernel(EvictArgs a) {
     out[i] = -1;
     if (ws) ws[i] = 0;
   }
-  if (n <= a.keep) {
+  if (n <= a.keep) {  // all stay
     for (uint32_t i = threadIdx.x; i < n; i += kSelect) {
       out[i] = static_cast<int32_t>(i);
       if (ws) ws[i] = w[i];
     }
     return;
   }
-  const uint32_t lo = a.sinks, hi = n - a.recent;  // those that compete
   const uint32_t segments = (n + N * kSelect - 1) / (N * kSelect);
-  uint32_t order[N];  // of the thread's scores
+  uint32_t order[N];
   const auto load = [&](uint32_t seg) {
+    const uint32_t first = seg * N * kSelect + threadIdx.x;
+    // Of this thread's: those below `some` exist, those from `lo` below `hi` compete.
+    const auto below = [&](uint32_t i) -> uint32_t { return i <= first ? 0 : (i - first + kSelect - 1) / kSelect; };
+    const uint32_t some = below(n), lo = below(a.sinks), hi = below(n - a.recent);
 #pragma unroll
-    for (uint32_t k = 0; k < N; ++k) {
-      const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
-      order[k] = order_of(i < n ? w[i] : 0.0f);
-    }
+    for (uint32_t k = 0; k < N; ++k) order[k] = k < some ? __builtin_bit_cast(uint32_t, w[first + k * kSelect]) : 0;
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k)
+      order[k] = k >= some ? 0 : k < lo || k >= hi ? kFixed : order_of(__builtin_bit_cast(float, order[k]));
   };
-  const auto step = []() { if constexpr (N > 16) __builtin_amdgcn_sched_barrier(0); };  // keeps one score's ballot in registers, not all
   load(0);
-  uint32_t want = a.keep - a.sinks - a.recent, prefix = 0;
-  bool ties = false;  // more entries equal the threshold than are wanted
-  if (want) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (uint32_t i = threadIdx.x; i < 256 * kCopies; i += kSelect) bins[i] = 0;
-      __syncthreads();
-      for (uint32_t seg = 0; seg < segments; ++seg) {
-        if (segments > 1) load(seg);
+  uint32_t want = a.keep, prefix = 0;
+  bool ties = true;  // more entries equal the threshold than are wanted
+  for (int top = 32; top > 0 && ties; top -= kDigit) {
+    const uint32_t shift = top > static_cast<int>(kDigit) ? top - kDigit : 0, digit = (1u << (top - shift)) - 1;
 #pragma unroll
-        for (uint32_t k = 0; k < N; ++k) {
-          const uint32_t i = (seg * N + k) * kSelect + threadIdx.x, u = order[k];
-          if (i >= lo && i < hi && (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8)))
-            atomicAdd(&bins[(u >> shift & 255) * kCopies + lane % kCopies], 1u);
-        }
-      }
-      __syncthreads();
-      // 4 threads a bin, 8 copies each; then the first wave finds the bin, 4 bins a lane from the top.
-      uint32_t sum = 0;
+    for (uint32_t i = 0; i < kCopies; ++i) *reinterpret_cast<u32x2*>(&bins[i * kCopyBins + threadIdx.x * 2]) = u32x2{0, 0};
+    __syncthreads();
+    for (uint32_t seg = 0; seg < segments; ++seg) {
+      if (segments > 1) load(seg);
+      const uint32_t mask = top == 32 ? 0 : ~0u << top;
 #pragma unroll
-      for (uint32_t c = 0; c < kCopies / 4; ++c) sum += bins[threadIdx.x / 4 * kCopies + (threadIdx.x % 4) * (kCopies / 4) + (c + threadIdx.x) % (kCopies / 4)];
-      sum += __shfl_xor(sum, 1, kOpsWave);
-      sum += __shfl_xor(sum, 2, kOpsWave);
-      __syncthreads();
-      if (threadIdx.x % 4 == 0) bins[threadIdx.x / 4] = sum;
-      __syncthreads();
-      if (wave == 0) {
-        uint32_t b[4], all = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) all += b[i] = bins[255 - (lane * 4 + i)];
-        uint32_t above = all;
-#pragma unroll
-        for (int i = 1; i < kOpsWave; i *= 2) {
-          const uint32_t y = __shfl_up(above, i, kOpsWave);
-          if (lane >= static_cast<uint32_t>(i)) above += y;
-        }
-        above -= all;  // in the lanes before: in higher bins
-        if (above < want && above + all >= want) {  // one lane
-#pragma unroll
-          for (uint32_t i = 0; i < 4; ++i) {
-            if (above < want && above + b[i] >= want) {
-              found[0] = 255 - (lane * 4 + i);
-              found[1] = want - above;
-              found[2] = b[i];
-            }
-            above += b[i];
-          }
-        }
-      }
-      __syncthreads();
-      prefix |= found[0] << shift;
-      want = found[1];
-      ties = found[2] > want;
-      __syncthreads();
+      for (uint32_t k = 0; k < N; ++k)
+        if (((order[k] ^ prefix) & mask) == 0) atomicAdd(&bins[lane % kCopies * kCopyBins + (order[k] >> shift & digit)], 1u);
     }
+    __syncthreads();
+    // A thread has two bins, counted from the top; the one where the sum passes what is wanted is found by a scan.
+    uint32_t b[2] = {0, 0};
+#pragma unroll
+    for (uint32_t c = 0; c < kCopies; ++c) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(&bins[c * kCopyBins + kBins - 2 - threadIdx.x * 2]);
+      b[0] += x[1];
+      b[1] += x[0];
+    }
+    uint32_t above = exclusive_scan(b[0] + b[1], scan);
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+      if (above < want && above + b[i] >= want) {  // one thread
+        found[0] = kBins - 1 - (threadIdx.x * 2 + i);
+        found[1] = want - above;
+        found[2] = b[i];
+      }
+      above += b[i];
+    }
+    __syncthreads();
+    prefix |= found[0] << shift;
+    want = found[1];
+    ties = found[2] != want;  // else all of the bin stay: those at its lowest order and above
+    __syncthreads();
   }
-  const bool some = a.keep > a.sinks + a.recent;
-  uint32_t base = 0, equals = 0;
-  for (uint32_t seg = 0; seg < segments; ++seg) {
-    if (segments > 1) load(seg);
-    const auto competes = [&](uint32_t i) { return some && i >= lo && i < hi; };
-    // Ranks among the equal ones, where not all of them stay.
-    if (ties) {
+  if (!ties) want = ~0u;
+  const auto step = []() { if constexpr (N > kListed) __builtin_amdgcn_sched_barrier(0); };  // keeps one ballot in registers, not all
+
+  if constexpr (N > kListed) {
+    uint32_t* to = selected(a, row);
+    if (!threadIdx.x) {
+      to[0] = prefix;
+      to[1] = want;
+    }
+    uint32_t above = 0, equal = 0;
+    for (uint32_t seg = 0; seg < segments; ++seg) {
+      if (segments > 1) load(seg);
 #pragma unroll
       for (uint32_t k = 0; k < N; ++k) {
-        const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
-        const uint64_t m = __ballot(competes(i) && order[k] == prefix);
-        if (!lane) counts[k * kWaves + wave] = __popcll(m);
+        const uint32_t c = __popcll(__ballot(order[k] > prefix)) << 16 | __popcll(__ballot(order[k] == prefix));
+        if (!lane) counts[k * kWaves + wave] = c;
         step();
       }
       __syncthreads();
-      for (uint32_t i0 = 0; i0 < N * kWaves; i0 += kSelect) {
-        const uint32_t i = i0 + threadIdx.x, c = i < N * kWaves ? counts[i] : 0, at = equals + exclusive_scan(c, scan);
-        if (i < N * kWaves) counts[i] = at;
-        if (threadIdx.x == kSelect - 1) found[0] = at + c;
-        __syncthreads();
-        equals = found[0];
+      if (wave == 0) {
+        uint32_t c = 0;  // at most 1024 in each half
+        if (lane < N)
+#pragma unroll
+          for (uint32_t i = 0; i < kWaves; ++i) c += counts[lane * kWaves + i];
+        uint32_t hi = c >> 16, lo = c & 0xffff;
+        const uint32_t my_hi = hi, my_lo = lo;
+#pragma unroll
+        for (uint32_t i = 1; i < N; i *= 2) {
+          const uint32_t x = __shfl_up(hi, i, kOpsWave), y = __shfl_up(lo, i, kOpsWave);
+          if (lane >= i) {
+            hi += x;
+            lo += y;
+          }
+        }
+        const uint32_t chunk = seg * N + lane;
+        if (lane < N && chunk * kSelect < n) {
+          to[2 + 2 * chunk] = above + hi - my_hi;
+          to[3 + 2 * chunk] = equal + lo - my_lo;
+        }
+        above += __builtin_amdgcn_readlane(hi, N - 1);
+        equal += __builtin_amdgcn_readlane(lo, N - 1);
       }
-    }
-    const auto stays = [&](uint32_t k, uint32_t eq_before) {
-      const uint32_t i = (seg * N + k) * kSelect + threadIdx.x, u = order[k];
-      const bool eq = competes(i) && u == prefix;
-      bool s = i < n && (i < lo || i >= hi || (competes(i) && u > prefix));
-      if (!ties) return s || eq;
-      const uint64_t m = __ballot(eq);
-      return s || (eq && eq_before + __popcll(m & ((1ull << lane) - 1)) < want);
-    };
-    uint64_t kept_bits = 0;  // bit k: this thread's k-th score stays
-#pragma unroll
-    for (uint32_t k = 0; k < N; ++k) {
-      if (stays(k, ties ? counts[k * kWaves + wave] : 0)) kept_bits |= 1ull << k;
-      step();
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t k = 0; k < N; ++k) {
-      const uint64_t m = __ballot(kept_bits >> k & 1);
-      if (!lane) counts[k * kWaves + wave] = __popcll(m);
-      step();
-    }
-    __syncthreads();
-    for (uint32_t i0 = 0; i0 < N * kWaves; i0 += kSelect) {
-      const uint32_t i = i0 + threadIdx.x, c = i < N * kWaves ? counts[i] : 0, at = base + exclusive_scan(c, scan);
-      if (i < N * kWaves) counts[i] = at;
-      if (threadIdx.x == kSelect - 1) found[1] = at + c;
       __syncthreads();
-      base = found[1];
     }
+    return;
+  }
+
+  // One segment. Both counts of a place in one word: at most 1024 N = 16384 of each.
+  const auto sum_up = [&]() {
     __syncthreads();
+    const uint32_t c = threadIdx.x < N * kWaves ? counts[threadIdx.x] : 0, at = exclusive_scan(c, scan);
+    if (threadIdx.x < N * kWaves) counts[threadIdx.x] = at;
+    __syncthreads();
+  };
 #pragma unroll
-    for (uint32_t k = 0; k < N; ++k) {
-      const uint64_t m = __ballot(kept_bits >> k & 1);
-      const uint32_t at = counts[k * kWaves + wave] + __popcll(m & ((1ull << lane) - 1));
-      if ((kept_bits >> k & 1) && at < a.keep) {
-        const uint32_t i = (seg * N + k) * kSelect + threadIdx.x;
-        out[at] = static_cast<int32_t>(i);
-        if (ws) ws[at] = w[i];
-      }
-      step();
+  for (uint32_t k = 0; k < N; ++k) {
+    const uint32_t c = __popcll(__ballot(order[k] > prefix)) << 16 | __popcll(__ballot(order[k] == prefix));
+    if (!lane) counts[k * kWaves + wave] = c;
+  }
+  sum_up();
+  const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+  for (uint32_t k = 0; k < N; ++k) {
+    const uint32_t before = counts[k * kWaves + wave];
+    const uint64_t gts = __ballot(order[k] > prefix), eqs = __ballot(order[k] == prefix);
+    const uint32_t eq = (before & 0xffff) + __popcll(eqs & lower), at = (before >> 16) + __popcll(gts & lower) + (eq < want ? eq : want);
+    if ((order[k] > prefix || (order[k] == prefix && eq < want)) && at < a.keep) {
+      out[at] = static_cast<int32_t>(k * kSelect + threadIdx.x);
+      if (ws) ws[at] = w[k * kSelect + threadIdx.x];
     }
-    __syncthreads();
+  }
+}
+
+// Of 1024 entries of a long row, those that stay, to their place in the list.
+__global__ __launch_bounds__(256) void evict_list_kernel(EvictArgs a) {
+  constexpr uint32_t kMine = kSelect / 256;
+  __shared__ uint32_t counts[kWaves];
+  const uint32_t head = blockIdx.y, seq = blockIdx.z, first = blockIdx.x * kSelect, lane = threadIdx.x % kOpsWave, wave = threadIdx.x / kOpsWave;
+  const uint32_t n = entries_of(a, seq);
+  if (first >= n || n <= a.keep) return;
+  const uint64_t row = static_cast<uint64_t>(seq) * a.c.heads + head;
+  const float* w = a.scores + row * a.scores_stride;
+  const uint32_t* chosen = selected(a, row);
+  const uint32_t threshold = chosen[0], want = chosen[1], above = chosen[2 + 2 * blockIdx.x], equal = chosen[3 + 2 * blockIdx.x];
+  uint32_t order[kMine];
+  float f[kMine];
+  uint64_t gts[kMine], eqs[kMine];
+#pragma unroll
+  for (uint32_t k = 0; k < kMine; ++k) {  // a wave has 256 entries in a row
+    const uint32_t i = first + (wave * kMine + k) * kOpsWave + lane;
+    f[k] = i < n ? w[i] : 0.0f;
+    order[k] = order_at(a, w, i, n);
+  }
+#pragma unroll
+  for (uint32_t k = 0; k < kMine; ++k) {
+    gts[k] = __ballot(order[k] > threshold);
+    eqs[k] = __ballot(order[k] == threshold);
+    if (!lane) counts[wave * kMine + k] = __popcll(gts[k]) << 16 | __popcll(eqs[k]);
+  }
+  __syncthreads();
+  uint32_t before = 0;
+#pragma unroll
+  for (uint32_t p = 0; p < kWaves; ++p) before += p < wave * kMine ? counts[p] : 0;
+  const uint64_t lower = (1ull << lane) - 1;
+#pragma unroll
+  for (uint32_t k = 0; k < kMine; ++k) {
+    const uint32_t eq = equal + (before & 0xffff) + __popcll(eqs[k] & lower);
+    const uint32_t at = above + (before >> 16) + __popcll(gts[k] & lower) + (eq < want ? eq : want);
+    if ((order[k] > threshold || (order[k] == threshold && eq < want)) && at < a.keep) {
+      a.entries[row * a.keep + at] = static_cast<int32_t>(first + (wave * kMine + k) * kOpsWave + lane);
+      if (a.scores_out) a.scores_out[row * a.keep + at] = f[k];
+    }
+    before += __popcll(gts[k]) << 16 | __popcll(eqs[k]);
   }
 }
 
 // The kept entries to their new blocks: kMoved of one head in a workgroup. Where they come from and go to is looked up
-// once for all their chunks, and a thread has 4 chunks in flight.
+// once for all their chunks, and a thread has 4 chunks in flight. Reads and writes at the rate of a copy.
 constexpr uint32_t kMoved = 64;
 
 template <bool F8, bool VX>
@@ -628,10 +685,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a) {
   __shared__ uint64_t from[kMoved], to[kMoved];  // of the blocks
   __shared__ uint32_t from_at[kMoved], to_at[kMoved];
   const uint32_t head = blockIdx.y, seq = blockIdx.z, first = blockIdx.x * kMoved;
-  const int32_t len = a.s.lens[seq];
-  uint32_t n = len < 0 ? 0 : static_cast<uint32_t>(len);
-  if (n > a.s.max_len) n = a.s.max_len;
-  const uint32_t kept = n < a.keep ? n : a.keep;
+  const uint32_t n = entries_of(a, seq), kept = n < a.keep ? n : a.keep;
   if (first >= kept) return;
   const uint32_t count = kept - first < kMoved ? kept - first : kMoved;
   constexpr uint64_t kNone = ~0ull;
@@ -738,16 +792,20 @@ hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stre
 hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream) {
   const bool f8 = k.cache_type == MMA_TYPE_F8, vx = k.layout == MMA_KV_LAYOUT_XPACKED;
   const dim3 pairs(a.c.heads, a.s.num_seqs);
-  if (a.s.max_len <= 4 * kSelect)
-    evict_select_kernel<4><<<pairs, kSelect, 0, stream>>>(a);
-  else if (a.s.max_len <= 16 * kSelect)
-    evict_select_kernel<16><<<pairs, kSelect, 0, stream>>>(a);
+  const bool listed = a.s.max_len <= kListed * kSelect;
+  if (a.s.max_len <= 8 * kSelect)
+    evict_select_kernel<8><<<pairs, kSelect, 0, stream>>>(a);
+  else if (listed)
+    evict_select_kernel<kListed><<<pairs, kSelect, 0, stream>>>(a);
   else
     evict_select_kernel<64><<<pairs, kSelect, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const uint32_t most = std::min(a.keep, a.s.max_len);
-  const dim3 grid((most + kMoved - 1) / kMoved, a.c.heads, a.s.num_seqs);
+  if (!listed) {
+    evict_list_kernel<<<dim3((a.s.max_len + kSelect - 1) / kSelect, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const dim3 grid((std::min(a.keep, a.s.max_len) + kMoved - 1) / kMoved, a.c.heads, a.s.num_seqs);
   if (f8 && vx)
     evict_move_kernel<true, true><<<grid, 256, 0, stream>>>(a);
   else if (f8)

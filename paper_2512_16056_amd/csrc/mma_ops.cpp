@@ -265,6 +265,10 @@ AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& 
   return p;
 }
 
+uint64_t evict_workspace(const mma_kv_seqs_t* q, uint32_t kv_heads) {
+  return static_cast<uint64_t>(q->num_seqs) * kv_heads * 8 * (1 + up(q->max_len, 1024));
+}
+
 // What the split goes by, checked where no pointer is needed.
 mma_status_t check_attention_sizes(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, const mma_kv_attention_t* a,
                                    Call* call) {
@@ -506,6 +510,18 @@ mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layer
   return ops_boundary_error("mma_kv_commit");
 }
 
+mma_status_t mma_kv_evict_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, uint64_t* bytes) try {
+  if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  Call call;
+  mma_status_t s;
+  if ((s = check_layout(layout, &call))) return s;
+  if ((s = check_seqs_sizes(seqs, layout->block_tokens))) return s;
+  *bytes = evict_workspace(seqs, layout->kv_heads);
+  return MMA_OK;
+} catch (...) {
+  return ops_boundary_error("mma_kv_evict_workspace");
+}
+
 mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
                           const mma_kv_evict_t* a, void* stream) try {
   mma_status_t s;
@@ -532,7 +548,13 @@ mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_
   if ((s = array(&call, "entries", a->entries, extent(heads, a->keep, 4), 4))) return s;
   if ((s = array(&call, "scores_out", a->scores_out, extent(heads, a->keep, 4), 4, true))) return s;
   if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
+  const uint64_t need = evict_workspace(seqs, layout->kv_heads);
+  if (a->workspace_bytes < need)
+    return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
+                static_cast<unsigned long long>(a->workspace_bytes), static_cast<unsigned long long>(need));
+  if ((s = array(&call, "workspace", a->workspace, need, 8))) return s;
   EvictArgs k{};
+  k.chosen = static_cast<uint32_t*>(a->workspace);
   k.c = call.c;
   k.s = call.s;
   k.dst_table = a->dst_table;

@@ -102,6 +102,7 @@ struct EvictArgs {
   int32_t* entries;
   float* scores_out;
   int32_t* lens_out;
+  uint32_t* chosen;  // workspace: 2 (1 + max_len / 1024, rounded up) words a row
   uint32_t dst_stride, scores_stride, keep, sinks, recent;
 };
 
