@@ -11,8 +11,8 @@ library has not been built this import fails loudly -- there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
-import struct
 from typing import Iterable, List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -445,54 +445,12 @@ def mma_digest_u32(dev_ptr, nbytes: int, dev_out, stream=None) -> None:
 # ------------------------------------------------------------------ operators on the paged cache
 _TYPES = {torch.bfloat16: MMA_TYPE_BF16, torch.float16: MMA_TYPE_F16}
 
-# A decode step makes these calls for every layer, so their set-up counts: the argument structs are packed
-# in one go (0.7 us; filling a ctypes structure takes 3 us) and handed over by address. That pointers are
-# device memory of the right size is the library's check.
-_APPEND_T = struct.Struct("@12Q6Q7If")
-_ATTENTION_T = struct.Struct("@6Q8Q6I2f")
-_WORKSPACE_T = struct.Struct("@2Q")
-_WORKSPACE_AT = mma_kv_attention_t.workspace.offset
-_COMMIT_T = struct.Struct("@4Q2I")
-_EVICT_T = struct.Struct("@7Q5I4x")
-assert (_APPEND_T.size, _ATTENTION_T.size, _COMMIT_T.size, _EVICT_T.size) == tuple(
-    ctypes.sizeof(x) for x in (mma_kv_append_t, mma_kv_attention_t, mma_kv_commit_t, mma_kv_evict_t))
-
-
-def _packed_call(name):
-    f = lib[name]
-    f.argtypes, f.restype = [_P] * 5, _S
-    return f
-
-
-_append, _attention, _commit, _evict = (_packed_call("mma_kv_" + x) for x in ("append", "attention", "commit", "evict"))
-_workspace = lib["mma_kv_attention_workspace"]
-_workspace.argtypes, _workspace.restype = [_P] * 4, _S
-
-
 def _want(name: str, t: torch.Tensor, dtype, shape=None) -> int:
     """Address of a contiguous tensor of the given type and, where given, shape."""
     if t.dtype is not dtype or not t.is_contiguous() or not t.is_cuda or (shape is not None and t.shape != shape):
         raise ValueError(f"{name}: a contiguous {dtype} GPU tensor{'' if shape is None else f' of shape {shape}'} is "
                          f"wanted, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
     return t.data_ptr()
-
-
-def _rows(name: str, t: torch.Tensor, dtype, shape) -> Tuple[int, int, int]:
-    """(address, token stride, head stride) of [tokens][heads][dim] rows."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} on the GPU is wanted, got {t.dtype} {tuple(t.shape)} "
-                         f"on {t.device}")
-    token, head, last = t.stride()
-    if last != 1 and shape[2] > 1:
-        raise ValueError(f"{name}: the values of a head have to be contiguous, strides {t.stride()}")
-    return t.data_ptr(), token, head
-
-
-def _kind(q: torch.Tensor, layout: mma_kv_layout_t) -> int:
-    kind = _TYPES.get(q.dtype)
-    if kind is None or q.dim() != 3 or q.shape[2] != layout.head_dim:
-        raise ValueError(f"q: [tokens][heads][{layout.head_dim}] of bfloat16 or float16 is wanted, got {q.dtype} {tuple(q.shape)}")
-    return kind
 
 
 def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
@@ -543,34 +501,10 @@ def mma_kv_append(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tensor,
                   k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
                   stream=None) -> torch.Tensor:
     """Normalise and rotate q and k, write k and v into `layer`; returns the queries (q_out, or a new tensor)."""
-    kind, dt = _kind(q, layout), q.dtype
-    shape = q.shape
-    n, q_heads, dim = shape
-    heads = layout.kv_heads
-    if q_out is None:
-        q_out = _empty_on(stream, shape, dt, q.device)
-    kv_shape = (n, heads, dim)
-    pos = table = qw = kw = ks = vs = rot = rows = 0
-    if rope is not None:
-        if rope.dim() != 2 or positions is None:
-            raise ValueError("rope: [positions][rot_dim] is wanted, and positions with it")
-        rows, rot = rope.shape
-        pos, table = _want("positions", positions, torch.int32, (n,)), _want("rope", rope, torch.float32)
-    if q_weight is not None:
-        qw = _want("q_weight", q_weight, dt, (dim,))
-    if k_weight is not None:
-        kw = _want("k_weight", k_weight, dt, (dim,))
-    if k_scale is not None:
-        ks = _want("k_scale", k_scale, torch.float32, (heads,))
-    if v_scale is not None:
-        vs = _want("v_scale", v_scale, torch.float32, (heads,))
-    a = _APPEND_T.pack(*_rows("q", q, dt, shape), *_rows("k", k, dt, kv_shape), *_rows("v", v, dt, kv_shape),
-                       *_rows("q_out", q_out, dt, shape), pos, table, qw, kw, ks, vs, n, q_heads, kind,
-                       MMA_TYPE_F8 if layout.elem_bytes == 1 else kind, rot, rows, 1 if interleaved else 0, eps)
-    st = _append(ctypes.byref(layout), _ptr(layer), seqs.address, a, _stream(stream))
-    if st:
-        _check(st, "mma_kv_append")
-    return q_out
+    if stream is not None and q_out is None:
+        q_out = _empty_on(stream, q.shape, q.dtype, q.device)
+    return _kv_ops.append(layout, layer, seqs.address, q, k, v, positions, rope, q_out, interleaved, q_weight, k_weight,
+                          eps, k_scale, v_scale, _stream(stream))
 
 
 def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tensor, *,
@@ -583,55 +517,22 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
     """Attention of the call's tokens over their sequences' entries; returns `out` (or a new tensor). `tree`: int64
     [tokens][words] bits. `scale`: 1 / sqrt(head_dim) unless given. `workspace`: a uint8 tensor of
     kv_attention_workspace() bytes or more; a new one of the stream's unless given."""
-    kind, dt = _kind(q, layout), q.dtype
-    shape = q.shape
-    n, q_heads, dim = shape
-    heads = layout.kv_heads
-    if out is None:
-        out = _empty_on(stream, shape, dt, q.device)
-    bits = l = s_in = s_out = ks = vs = words = width = 0
-    if tree is not None:
-        if tree.dim() != 2 or tree.shape[0] != n:
-            raise ValueError(f"tree: [{n}][words] is wanted, got {tuple(tree.shape)}")
-        bits, words = _want("tree", tree, torch.int64), tree.shape[1]
-    if lse is not None:
-        l = _want("lse", lse, torch.float32, (n, q_heads))
-    if scores_out is not None:
-        if scores_out.dim() != 3 or scores_out.shape[:2] != (seqs.num_seqs, heads):
-            raise ValueError(f"scores_out: [{seqs.num_seqs}][{heads}][entries] is wanted, got {tuple(scores_out.shape)}")
-        s_out, width = _want("scores_out", scores_out, torch.float32), scores_out.shape[2]
-        if scores_in is not None:
-            s_in = _want("scores_in", scores_in, torch.float32, scores_out.shape)
-    elif scores_in is not None:
-        raise ValueError("scores_in without scores_out")
-    if k_scale is not None:
-        ks = _want("k_scale", k_scale, torch.float32, (heads,))
-    if v_scale is not None:
-        vs = _want("v_scale", v_scale, torch.float32, (heads,))
-    a = _ATTENTION_T.pack(*_rows("q", q, dt, shape), *_rows("out", out, dt, shape), bits, l, s_in, s_out, ks, vs, 0, 0, n,
-                          q_heads, kind, MMA_TYPE_F8 if layout.elem_bytes == 1 else kind, words, width,
-                          dim ** -0.5 if scale is None else scale, decay)
-    lay = ctypes.byref(layout)
-    if workspace is None:
-        need = _U64()
-        st = _workspace(lay, seqs.address, a, ctypes.byref(need))
-        if st:
-            _check(st, "mma_kv_attention_workspace")
-        if need.value:
-            workspace = _empty_on(stream, (need.value,), torch.uint8, q.device)
-    if workspace is not None:
-        a = (a[:_WORKSPACE_AT] + _WORKSPACE_T.pack(_want("workspace", workspace, torch.uint8), workspace.numel()) +
-             a[_WORKSPACE_AT + 16:])
-    st = _attention(lay, _ptr(layer), seqs.address, a, _stream(stream))
-    if st:
-        _check(st, "mma_kv_attention")
-    return out
+    if stream is not None:
+        if out is None:
+            out = _empty_on(stream, q.shape, q.dtype, q.device)
+        if workspace is None:
+            need = kv_attention_workspace(layout, seqs, q.shape[0], q.shape[1], q.dtype, scores_out is not None)
+            workspace = _empty_on(stream, (need,), torch.uint8, q.device)
+    return _kv_ops.attention(layout, layer, seqs.address, q, out, scale, tree, lse, scores_in, scores_out, decay, k_scale,
+                             v_scale, workspace, _stream(stream))
 
 
 def kv_attention_workspace(layout: mma_kv_layout_t, seqs: KVSeqs, num_tokens: int, q_heads: int, dtype: torch.dtype,
                            scores: bool = False) -> int:
     """Bytes of workspace of an attention call of these sizes."""
-    kind = _TYPES[dtype]
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise ValueError(f"queries of {dtype}: bfloat16 or float16 is wanted")
     a = mma_kv_attention_t(num_tokens=num_tokens, q_heads=q_heads, type=kind, scores_out=1 if scores else None,
                            cache_type=MMA_TYPE_F8 if layout.elem_bytes == 1 else kind)
     need = _U64()
@@ -643,27 +544,20 @@ def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch
                   scores=None, scores_stride: Optional[int] = None, stream=None) -> torch.Tensor:
     """Move the accepted drafted entries together in every layer (in place); returns the new lengths. `layers`,
     `scores`: tensors, or a layer_table (then scores_stride is needed)."""
-    n, num_layers = seqs.num_seqs, layout.num_layers
-    if accepted.dim() != 2 or accepted.shape[0] != n:
-        raise ValueError(f"accepted: [{n}][drafted tokens] is wanted, got {tuple(accepted.shape)}")
     if scores is not None and not isinstance(scores, ctypes.Array):
         shape = tuple(scores[0].shape)
-        if len(shape) != 3 or shape[:2] != (n, layout.kv_heads):
-            raise ValueError(f"scores: [{n}][{layout.kv_heads}][entries] is wanted, got {shape}")
+        if len(shape) != 3 or shape[:2] != (seqs.num_seqs, layout.kv_heads):
+            raise ValueError(f"scores: [{seqs.num_seqs}][{layout.kv_heads}][entries] is wanted, got {shape}")
         for t in scores:
             _want("scores", t, torch.float32, shape)
         scores_stride = shape[2]
-    lt = layer_table(layers)  # locals, so that the arrays outlive the call
-    st = None if scores is None else layer_table(scores)
-    if len(lt) < num_layers or (st is not None and (len(st) < num_layers or scores_stride is None)):
-        raise ValueError(f"{num_layers} layers are wanted, and as many scores with their stride")
-    lens = _empty_on(stream, (n,), torch.int32, seqs.device)
-    a = _COMMIT_T.pack(_want("accepted", accepted, torch.int32), _want("counts", counts, torch.int32, (n,)),
-                       lens.data_ptr(), 0 if st is None else ctypes.addressof(st), accepted.shape[1], scores_stride or 0)
-    rc = _commit(ctypes.byref(layout), lt, seqs.address, a, _stream(stream))
-    if rc:
-        _check(rc, "mma_kv_commit")
-    return lens
+    if scores is not None:
+        scores = layer_table(scores)
+        if scores_stride is None:
+            raise ValueError("a table of scores needs scores_stride")
+    lens = None if stream is None else _empty_on(stream, (seqs.num_seqs,), torch.int32, seqs.device)
+    return _kv_ops.commit(layout, layer_table(layers), seqs.address, accepted, counts, scores, scores_stride, lens,
+                          _stream(stream))
 
 
 def kv_evict_workspace(layout: mma_kv_layout_t, seqs: KVSeqs) -> int:
@@ -674,30 +568,36 @@ def kv_evict_workspace(layout: mma_kv_layout_t, seqs: KVSeqs) -> int:
 
 
 def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.Tensor, scores: torch.Tensor, keep: int,
-                 *, sinks: int = 0, recent: int = 0, workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+                 *, sinks: int = 0, recent: int = 0, workspace: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Keep the `keep` entries of each sequence and KV head that attention went to, moved into the blocks of
     dst_table; returns (entries kept, their scores, new lengths). `workspace`: a uint8 tensor of kv_evict_workspace()
     bytes or more; a new one of the stream's unless given."""
-    n, heads = seqs.num_seqs, layout.kv_heads
-    if dst_table.dim() != 2 or dst_table.shape[0] != n:
-        raise ValueError(f"dst_table: [{n}][blocks] is wanted, got {tuple(dst_table.shape)}")
-    if scores.dim() != 3 or scores.shape[:2] != (n, heads):
-        raise ValueError(f"scores: [{n}][{heads}][entries] is wanted, got {tuple(scores.shape)}")
-    if keep < 1:
-        raise ValueError("keep: at least 1")
-    entries = _empty_on(stream, (n, heads, keep), torch.int32, seqs.device)
-    kept = _empty_on(stream, (n, heads, keep), torch.float32, seqs.device)
-    lens = _empty_on(stream, (n,), torch.int32, seqs.device)
-    if workspace is None:
-        workspace = _empty_on(stream, (kv_evict_workspace(layout, seqs),), torch.uint8, seqs.device)
-    else:
-        _want("workspace", workspace, torch.uint8)
-    a = _EVICT_T.pack(_want("dst_table", dst_table, torch.int32), _want("scores", scores, torch.float32), entries.data_ptr(),
-                      kept.data_ptr(), lens.data_ptr(), workspace.data_ptr(), workspace.numel(), dst_table.shape[1], scores.shape[2], keep, sinks, recent)
-    rc = _evict(ctypes.byref(layout), _ptr(layer), seqs.address, a, _stream(stream))
-    if rc:
-        _check(rc, "mma_kv_evict")
-    return entries, kept, lens
+    entries = kept = lens = None
+    if stream is not None:
+        shape = (seqs.num_seqs, layout.kv_heads, keep)
+        entries, kept = (_empty_on(stream, shape, t, seqs.device) for t in (torch.int32, torch.float32))
+        lens = _empty_on(stream, shape[:1], torch.int32, seqs.device)
+        if workspace is None:
+            workspace = _empty_on(stream, (kv_evict_workspace(layout, seqs),), torch.uint8, seqs.device)
+    return _kv_ops.evict(layout, layer, seqs.address, dst_table, scores, keep, sinks, recent, entries, kept, lens,
+                         workspace, _stream(stream))
+
+
+def _load_kv_ops():
+    """The operators' binding, a compiled module next to libmma.so, given the library's entry points."""
+    path = os.path.join(_HERE, "_kv_ops.so")
+    if not os.path.exists(path):
+        raise ImportError(f"{path} is missing: build it with `python paper_2512_16056_amd/build.py`")
+    spec = importlib.util.spec_from_file_location("_kv_ops", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    names = ("append", "attention", "attention_workspace", "commit", "evict", "evict_workspace")
+    m.attach(*(ctypes.cast(getattr(lib, "mma_kv_" + x), _P).value for x in names), _check, _ptr)
+    return m
+
+
+_kv_ops = _load_kv_ops()
 
 
 # ------------------------------------------------------------------ status

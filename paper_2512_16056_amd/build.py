@@ -16,6 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build", "obj")
 LIB = os.path.join(HERE, "libmma.so")
 NATIVE_LIB = os.path.join(HERE, "libmma_native.so")  # hipMemcpyAsync comparators for the benchmark
+KV_OPS_LIB = os.path.join(HERE, "_kv_ops.so")  # Python binding of the operators on the paged cache
 INTERPOSE_LIB = os.path.join(HERE, "libmma_interpose.so")  # LD_PRELOAD: hipMemcpy* -> libmma
 NATIVE_BATCH = os.path.join(HERE, "native_batch")  # hipMemcpyBatchAsync comparator (its own process)
 CXX = os.environ.get("CXX", "g++")
@@ -43,6 +44,22 @@ def _run(cmd):
     return r
 
 
+def _build_kv_ops() -> None:
+    """The compiled binding: host C++ against torch's headers; libmma.so's entry points are given to it when it is loaded."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = KV_OPS_LIB + ".tmp"
+    _run([CXX, "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          *(f"-isystem{p}" for p in cpp_extension.include_paths()), f"-isystem{os.path.join(ROCM, 'include')}",
+          f"-isystem{sysconfig.get_paths()['include']}", os.path.join(CSRC, "mma_python.cpp"), "-o", tmp, f"-L{lib}",
+          "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, KV_OPS_LIB)
+
+
 def build(verbose: bool = False) -> str:
     """Compile every source and link libmma.so; returns the library path."""
     os.makedirs(OBJ, exist_ok=True)
@@ -51,10 +68,12 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(OBJ, src + ".o")
         cmd = [HIPCC, *extra, *COMMON, "-c", os.path.join(CSRC, src), "-o", obj]
         jobs.append((cmd, obj))
-    with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
+    with ThreadPoolExecutor(max_workers=len(jobs) + 1) as ex:
+        kv_ops = ex.submit(_build_kv_ops)
         for r in ex.map(lambda j: _run(j[0]), jobs):
             if verbose and (r.stdout or r.stderr):
                 print(r.stdout, r.stderr, file=sys.stderr)
+        kv_ops.result()
     tmp = LIB + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *[o for _, o in jobs], "-o", tmp,
           f"-L{os.path.join(ROCM, 'lib')}", "-lhsa-runtime64", "-lpthread"])
