@@ -83,6 +83,16 @@ __device__ __forceinline__ float to_float(uint32_t bits16) {
 
 __device__ __forceinline__ float across(float v, int mask) { return __shfl_xor(v, mask, kOpsWave); }
 
+// Maximum and sum over the 4 lanes that have a row's keys (16 and 32 apart), by exchanging rows of lanes between two
+// registers instead of through LDS.
+__device__ __forceinline__ float max_of_row(float v) {
+  uint32_t x = __builtin_bit_cast(uint32_t, v);
+  auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, static_cast<uint32_t>(a[0])), __builtin_bit_cast(float, static_cast<uint32_t>(a[1]))));
+  a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return fmaxf(__builtin_bit_cast(float, static_cast<uint32_t>(a[0])), __builtin_bit_cast(float, static_cast<uint32_t>(a[1])));
+}
+
 // 8 consecutive values of one row from global memory, elements at any alignment if not wide.
 __device__ __forceinline__ u32x4 load_row8(const uint8_t* p, bool wide) {
   if (wide) return *reinterpret_cast<const u32x4*>(p);
@@ -205,6 +215,11 @@ __device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[R], co
   }
 }
 
+// lse2 of a token's query head: rows of a KV head side by side.
+__device__ __forceinline__ uint64_t lse2_at(const AttnArgs& a, uint32_t token, uint32_t qh) {
+  return (static_cast<uint64_t>(qh / a.group) * a.s.num_tokens + token) * a.group + qh % a.group;
+}
+
 // What a row's result goes to: the output and lse, or with several splits this split's part of them.
 template <class T, int DP, int NC, class At>
 __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uint32_t qh, uint32_t split, uint32_t g, float top,
@@ -235,7 +250,7 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uin
   if (!g) {
     const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
     if (a.lse) a.lse[unit] = l2 * kLn2;
-    if (a.lse2) a.lse2[unit] = l2;
+    if (a.lse2) a.lse2[lse2_at(a, token, qh)] = l2;
   }
 }
 
@@ -265,18 +280,23 @@ struct Stream {
   u32x4 k[2][NK];
   uint32_t v[NV][VW];
 
+  // Loads have no conditions: lanes past head_dim read the row's start instead; their keys are then cleared, their
+  // values come to nothing but outputs that are not stored.
   __device__ __forceinline__ void load_keys(const CacheArgs& c, int32_t id, uint32_t key, uint32_t head, uint32_t g) {
     const uint32_t token = key - block_of(c, key) * c.tokens;  // of the first half's key
-    const uint8_t* p = c.k + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.k_head +
-                       static_cast<uint64_t>(token) * c.k_token + static_cast<uint64_t>(g) * c.k_chunk;
+    const uint8_t* p = c.k + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.k_head + token * c.k_token;
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
-      const bool live = (s * 4 + g) * (F8 ? 16 : 8) < c.dim;
+      const uint32_t chunk = s * 4 + g, at = chunk * (F8 ? 16 : 8) < c.dim ? chunk * c.k_chunk : 0;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-        k[t][s] = live ? *reinterpret_cast<const u32x4*>(p + static_cast<uint64_t>(s * 4) * c.k_chunk + t * 4 * static_cast<uint64_t>(c.k_token))
-                       : u32x4{0, 0, 0, 0};
+      for (int t = 0; t < 2; ++t) k[t][s] = *reinterpret_cast<const u32x4*>(p + at + t * 4 * c.k_token);
     }
+  }
+  __device__ __forceinline__ void clear_keys(const CacheArgs& c, uint32_t g) {
+    if (c.dim == DP) return;
+#pragma unroll
+    for (int s = 0; s < NK; ++s)
+      if ((s * 4 + g) * (F8 ? 16 : 8) >= c.dim) k[0][s] = k[1][s] = u32x4{0, 0, 0, 0};
   }
   template <class T>
   __device__ __forceinline__ u32x4 key(int t, int s) const {
@@ -286,24 +306,22 @@ struct Stream {
 
   __device__ __forceinline__ void load_values(const CacheArgs& c, int32_t id, uint32_t first, uint32_t head, uint32_t m) {
     const uint32_t token = first - block_of(c, first) * c.tokens;
-    const uint8_t* p = c.v + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.v_head +
-                       static_cast<uint64_t>(token) * c.v_token;
+    const uint8_t* p = c.v + static_cast<uint64_t>(static_cast<uint32_t>(id)) * c.block_bytes + head * c.v_head + token * c.v_token;
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      const uint32_t d = VX ? n * 16 + m : n / 8 * 16 * CE + m * CE;
-      const uint8_t* q = VX ? p + static_cast<uint64_t>(d) * c.v_chunk
-                            : p + static_cast<uint64_t>(n % 8) * c.v_token + d * (F8 ? 1 : 2);
-      const bool live = d < c.dim;
+      uint32_t d = VX ? n * 16 + m : n / 8 * 16 * CE + m * CE;
+      d = d < c.dim ? d : 0;
+      const uint8_t* q = VX ? p + d * c.v_chunk : p + (n % 8) * c.v_token + d * (F8 ? 1 : 2);
       if constexpr (VW == 4) {
-        const u32x4 x = live ? *reinterpret_cast<const u32x4*>(q) : u32x4{0, 0, 0, 0};
+        const u32x4 x = *reinterpret_cast<const u32x4*>(q);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[n][i] = x[i];
       } else if constexpr (VW == 2) {
-        const u32x2 x = live ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
+        const u32x2 x = *reinterpret_cast<const u32x2*>(q);
         v[n][0] = x[0];
         v[n][1] = x[1];
       } else {
-        v[n][0] = live ? *reinterpret_cast<const uint32_t*>(q) : 0;
+        v[n][0] = *reinterpret_cast<const uint32_t*>(q);
       }
     }
   }
@@ -331,15 +349,18 @@ struct Stream {
 };
 
 template <class T, bool F8, int DP, bool VX, int R>
-__global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kernel(AttnArgs a) {
   typedef Stream<F8, DP, VX> S;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
-  const uint32_t split = blockIdx.x % a.splits, group = blockIdx.x / a.splits;
-  const uint32_t head = blockIdx.y, seq = blockIdx.z;
+  // Workgroups go to the 8 XCDs in turn: heads and sequences first, so that each XCD has early and late splits alike
+  // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 141 us instead of 120
+  // for 32 sequences of up to 8k).
+  const uint32_t pairs = a.c.heads * a.s.num_seqs, pair = blockIdx.x % pairs, split = blockIdx.x / pairs;
+  const uint32_t head = pair % a.c.heads, seq = pair / a.c.heads;
   const SeqSpan sp = span_of(a.s, seq);
   const uint32_t rows = sp.count * a.group;
-  const uint32_t row0 = group * R * 16;
-  if (row0 >= rows) return;
+  constexpr uint32_t row0 = 0;
+  if (!rows) return;
   const uint32_t begin = split * a.split_len;
   if (begin >= sp.total && split) return;  // the first split also writes the rows that have no entries
   // Without a tree no row of the workgroup sees entries past its last token's.
@@ -394,6 +415,7 @@ __global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
   const auto tile = [&](auto masked, bool have) {
     constexpr bool kMasked = decltype(masked)::value;
     s.load_values(a.c, have ? vid : 0, clamp(base + g * 8), head, m);
+    s.clear_keys(a.c, g);
     f32x4 x[R][2];
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -435,8 +457,7 @@ __global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
       float mx = top[r];
 #pragma unroll
       for (int j = 0; j < 8; ++j) mx = fmaxf(mx, y[j]);
-      mx = fmaxf(mx, across(mx, 16));
-      mx = fmaxf(mx, across(mx, 32));
+      mx = max_of_row(mx);
       const float fade = __builtin_amdgcn_exp2f(top[r] - mx);
       top[r] = mx;
       float add = 0;
@@ -461,7 +482,8 @@ __global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
     base += step;
   };
   // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not there), masked ones.
-  const uint32_t whole = end < sp.before ? end : sp.before;
+  uint32_t whole = a.tree ? sp.before : sp.before + row0 / a.group + 1;
+  if (whole > end) whole = end;
   bool have = there(vid);
   while (base + kTile <= whole && __all(have)) {
     tile(std::false_type(), true);
@@ -538,7 +560,8 @@ __global__ __launch_bounds__(256) void attention_stream_kernel(AttnArgs a) {
 // be passed by more than 2^8: the factor is 1 otherwise and nothing is scaled.
 template <bool F8, int DP, bool VX>
 struct Tiles {
-  static constexpr int KT = DP == 256 ? 32 : 64;  // entries of a tile
+  static constexpr int KT = DP == 256 || (F8 && DP == 128) ? 32 : 64;  // entries of a tile
+  static constexpr int AHEAD = F8 ? 2 : 1;        // tiles on their way while one is worked on
   static constexpr int SUB = KT / 32;
   static constexpr int KS = DP / 32;
   static constexpr int NC = DP / 16;
@@ -546,8 +569,7 @@ struct Tiles {
   static constexpr int VC = KT / 8;               // x-packed: 16-byte chunks of a value
   static constexpr uint32_t kBytes = KT * DP * 2; // of K or V of a tile
   static constexpr int N = KT * C / 256;          // chunks of a thread (16-bit)
-  static constexpr int N8 = (KT * C / 2 + 255) / 256;  // 16-byte loads of a thread (8-bit)
-  static constexpr int NL = F8 ? N8 : N;
+  static constexpr int NL = F8 ? N / 2 : N;        // 16-byte loads of a thread
 
   static __device__ __forceinline__ uint32_t swizzle(uint32_t entry) {
     const uint32_t f = (entry & 3) | (entry >> 3 & 3) << 2;
@@ -571,19 +593,34 @@ __device__ __forceinline__ u32x2 read_turned(const uint8_t* p) {  // 16 lanes: 4
 }
 
 template <class T, bool F8, int DP, bool VX, int RW>
-__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(AttnArgs a, uint32_t row_groups, uint32_t units) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(AttnArgs a, uint32_t row_groups, uint32_t cells) {
   typedef Tiles<F8, DP, VX> S;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][2][S::kBytes];  // [buffer][K, V]
-  __shared__ uint32_t absent[2];  // number of the last tile in the buffer that had entries without a block
+  // Two buffers, each of its own so that the compiler can tell reads of one from loads on their way to the other and
+  // does not wait for those: code that knows its buffer takes it as a constant B.
+  __shared__ __attribute__((aligned(1024))) uint8_t k0[S::kBytes], v0[S::kBytes], k1[S::kBytes], v1[S::kBytes];
+  const auto k_of = [&](auto b) -> uint8_t* {
+    if constexpr (std::is_same<decltype(b), int>::value) return b ? k1 : k0;
+    else if constexpr (decltype(b)::value) return k1;
+    else return k0;
+  };
+  const auto v_of = [&](auto b) -> uint8_t* {
+    if constexpr (std::is_same<decltype(b), int>::value) return b ? v1 : v0;
+    else if constexpr (decltype(b)::value) return v1;
+    else return v0;
+  };
+  const auto other = [](auto b) {
+    if constexpr (std::is_same<decltype(b), int>::value) return b ^ 1;
+    else return std::bool_constant<!decltype(b)::value>();
+  };
+  __shared__ uint64_t rows_at[4][S::KT], groups_at[4][VX ? S::VC : 1];  // of every four tiles, addresses of their entries, 0 where there is none
+  __shared__ uint32_t absent[4];  // number of the last tile of every four that had entries without a block
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kOpsWave), lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
-  // Workgroups go to the 8 XCDs in turn. Those with the same keys (row groups of a split) are
-  // neighbours here, and an XCD gets a run of neighbours, so that they share its L2.
-  uint32_t u = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-  if (u >= units) return;
-  const uint32_t group = row_groups - 1 - u % row_groups;  // the last rows first: without a tree they see most
-  u /= row_groups;
-  const uint32_t split = u % a.splits;
-  u /= a.splits;
+  // Workgroups go to the 8 XCDs in turn. Row groups with the same keys follow each other on one XCD, so that they
+  // share its L2; what they belong to (heads and sequences first, then splits) goes round the XCDs.
+  const uint32_t slot = blockIdx.x / 8, cell = slot / row_groups * 8 + blockIdx.x % 8;
+  if (cell >= cells) return;
+  const uint32_t group = row_groups - 1 - slot % row_groups;  // the last rows first: without a tree they see most
+  const uint32_t pairs = a.c.heads * a.s.num_seqs, split = cell / pairs, u = cell % pairs;
   const uint32_t head = u % a.c.heads, seq = u / a.c.heads;
   const SeqSpan sp = span_of(a.s, seq);
   const uint32_t rows = sp.count * a.group;
@@ -629,107 +666,122 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
 
   // Chunks past head_dim are never written: K's count as 0.
   if (a.c.dim < DP)
-    for (uint32_t i = threadIdx.x; i < 4 * S::kBytes / 16; i += 256) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
-  if (threadIdx.x < 2) absent[threadIdx.x] = 0;
+    for (uint32_t i = threadIdx.x; i < S::kBytes / 16; i += 256) {
+      reinterpret_cast<u32x4*>(k0)[i] = u32x4{0, 0, 0, 0};
+      reinterpret_cast<u32x4*>(k1)[i] = u32x4{0, 0, 0, 0};
+    }
+  if (threadIdx.x < 4) absent[threadIdx.x] = 0;
   __syncthreads();
 
-  // This thread's part of a tile. 16 bits: chunk i of K (and V) is slot 256 i + thread of the tile.
-  const auto k_entry = [&](int i) { return F8 ? (i * 256 + threadIdx.x) / (S::C / 2) : (i * 256 + threadIdx.x) / S::C; };
-  const auto x_entry = [&](int i) -> uint32_t {  // x-packed values: the first of the chunk's entries
-    const uint32_t slot = i * 256 + threadIdx.x;
-    if (F8) return slot % (S::VC / 2) * 16;
-    const uint32_t d = slot / S::VC;
-    return ((slot % S::VC) ^ (S::VC == 8 ? d >> 1 & 7 : d >> 2 & 3)) * 8;
-  };
-  int32_t id[S::NL], vid[VX ? S::NL : 1];  // blocks of the part of the tile after the next
+  // Where a tile's entries (and, x-packed, the 8 or 16 entries of a chunk of values) lie, found once for all threads that
+  // bring parts of them: a thread an entry, its address a tile before it is used, its block a tile before that.
+  constexpr uint32_t kPer = F8 ? 16 : 8, kGroups = VX ? S::KT / kPer : 0;
+  const bool finds = threadIdx.x < S::KT, finds_x = VX && threadIdx.x >= S::KT && threadIdx.x < S::KT + kGroups;
+  const uint32_t found = finds ? threadIdx.x : (threadIdx.x - S::KT) * kPer;  // the entry of the tile
+  int32_t id = 0;
   const auto look_up = [&](uint32_t base) {
-#pragma unroll
-    for (int i = 0; i < S::NL; ++i) {
-      const uint32_t e = base + k_entry(i);
-      id[i] = table[block_of(a.c, e < end ? e : end - 1)];
-      if constexpr (VX) {
-        const uint32_t f = base + x_entry(i);
-        vid[i] = table[block_of(a.c, f < end ? f : end - 1)];
-      }
+    const uint32_t e = base + found;
+    if (finds || finds_x) id = table[block_of(a.c, e < end ? e : end - 1)];
+  };
+  const auto publish = [&](uint32_t base, uint32_t n) {
+    if (!finds && !finds_x) return;
+    const uint32_t e = base + found;
+    const bool has = static_cast<uint32_t>(id) < a.c.num_blocks;
+    uint64_t p = 0;
+    if (e < end && has) {
+      const uint32_t t = e - block_of(a.c, e) * a.c.tokens;
+      p = static_cast<uint64_t>(static_cast<uint32_t>(id)) * a.c.block_bytes;
+      if (finds)
+        p += reinterpret_cast<uint64_t>(a.c.k) + head * a.c.k_head + static_cast<uint64_t>(t) * a.c.k_token;
+      else
+        p += reinterpret_cast<uint64_t>(a.c.v) + head * a.c.v_head + static_cast<uint64_t>(t) * a.c.v_token;
+    }
+    if (finds) {
+      rows_at[n % 4][threadIdx.x] = p;
+      if (e < end && !has) absent[n % 4] = n;
+    } else {
+      groups_at[n % 4][threadIdx.x - S::KT] = p;
     }
   };
-  u32x4 held_k[F8 ? S::NL : 1], held_v[F8 ? S::NL : 1];
-  const auto in_tile = [&](int i) { return !F8 || (i * 256 + threadIdx.x) * 2 < static_cast<uint32_t>(S::KT * S::C); };
-  // Start bringing the tile at `base` (number n) to buffer b.
-  const auto fetch = [&](uint32_t base, uint32_t n, int b) {
-    bool missing = false;
+
+  // This thread's part of a tile: chunk i of K (and V) is slot 256 i + thread; 16 bits: of the tile in LDS, 8 bits: of the
+  // tile in memory.
+  constexpr uint32_t kRowChunks = F8 ? S::C / 2 : S::C, kXChunks = F8 ? S::VC / 2 : S::VC;
+  const auto k_entry = [&](int i) { return (i * 256 + threadIdx.x) / kRowChunks; };
+  const auto k_chunk = [&](int i) { return F8 ? threadIdx.x % kRowChunks : (threadIdx.x % kRowChunks) ^ S::swizzle(k_entry(i)); };
+  const auto x_value = [&](int i) { return (i * 256 + threadIdx.x) / kXChunks; };
+  const auto x_chunk = [&](int i) -> uint32_t {
+    const uint32_t d = x_value(i), c = threadIdx.x % kXChunks;
+    return F8 ? c : c ^ (S::VC == 8 ? d >> 1 & 7 : d >> 2 & 3);
+  };
+  const uint64_t v_from_k = a.c.v - a.c.k;
+  u32x4 held_k[2][F8 ? S::NL : 1], held_v[2][F8 ? S::NL : 1];
+  // Start bringing tile n, at `base`, to buffer b (8 bits: to the registers that go there).
+  const auto fetch = [&](uint32_t base, uint32_t n, auto b) {
+    uint8_t* const kl = k_of(b);
+    uint8_t* const vl = v_of(b);
+    const bool tail = base + S::KT > end;
 #pragma unroll
     for (int i = 0; i < S::NL; ++i) {
-      const uint32_t slot = i * 256 + threadIdx.x;
-      const bool mine = in_tile(i);
-      {
-        const uint32_t e = base + k_entry(i), bl = block_of(a.c, e < end ? e : end - 1), t = e - bl * a.c.tokens;
-        const bool has = static_cast<uint32_t>(id[i]) < a.c.num_blocks, ok = e < end && has;
-        missing |= mine && !has;
-        const uint64_t block = ok ? static_cast<uint64_t>(static_cast<uint32_t>(id[i])) * a.c.block_bytes : 0;
-        const uint8_t* kp = a.c.k + block + head * a.c.k_head + static_cast<uint64_t>(t) * a.c.k_token;
-        const uint8_t* vp = a.c.v + block + head * a.c.v_head + static_cast<uint64_t>(t) * a.c.v_token;
-        if constexpr (F8) {
-          const uint32_t chunk = slot % (S::C / 2);
-          const bool in = ok && mine && chunk * 16 < a.c.dim;
-          held_k[i] = in ? *reinterpret_cast<const u32x4*>(kp + static_cast<uint64_t>(chunk) * a.c.k_chunk) : u32x4{0, 0, 0, 0};
-          if constexpr (!VX) held_v[i] = in ? *reinterpret_cast<const u32x4*>(vp + chunk * 16) : u32x4{0, 0, 0, 0};
+      const uint32_t chunk = k_chunk(i);
+      const uint64_t at = rows_at[n % 4][k_entry(i)];
+      const uint8_t* kp = reinterpret_cast<const uint8_t*>(at) + chunk * a.c.k_chunk;
+      const uint8_t* vp = reinterpret_cast<const uint8_t*>(at) + v_from_k + chunk * 16;  // not x-packed: as far from V's start
+      const bool live = chunk * (F8 ? 16 : 8) < a.c.dim;
+      if constexpr (F8) {
+        held_k[b][i] = at && live ? *reinterpret_cast<const u32x4*>(kp) : u32x4{0, 0, 0, 0};
+        if constexpr (!VX) held_v[b][i] = at && live ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
+      } else if (live) {
+        if (at) {
+          __builtin_amdgcn_global_load_lds((global_u8*)kp, (lds_u8*)(kl + (i * 256 + wave * 64) * 16), 16, 0, 0);
+          if constexpr (!VX)
+            __builtin_amdgcn_global_load_lds((global_u8*)vp, (lds_u8*)(vl + (i * 256 + wave * 64) * 16), 16, 0, 0);
         } else {
-          const uint32_t chunk = (slot % S::C) ^ S::swizzle(k_entry(i));
-          if (chunk * 8 < a.c.dim) {
-            if (ok) {
-              __builtin_amdgcn_global_load_lds((global_u8*)(kp + static_cast<uint64_t>(chunk) * a.c.k_chunk),
-                                               (lds_u8*)(lds[b][0] + (i * 256 + wave * 64) * 16), 16, 0, 0);
-              if constexpr (!VX)
-                __builtin_amdgcn_global_load_lds((global_u8*)(vp + chunk * 16), (lds_u8*)(lds[b][1] + (i * 256 + wave * 64) * 16), 16, 0, 0);
-            } else {
-              *reinterpret_cast<u32x4*>(lds[b][0] + slot * 16) = u32x4{0, 0, 0, 0};
-              if constexpr (!VX) *reinterpret_cast<u32x4*>(lds[b][1] + slot * 16) = u32x4{0, 0, 0, 0};
-            }
-          }
+          const uint32_t slot = i * 256 + threadIdx.x;
+          *reinterpret_cast<u32x4*>(kl + slot * 16) = u32x4{0, 0, 0, 0};
+          if constexpr (!VX) *reinterpret_cast<u32x4*>(vl + slot * 16) = u32x4{0, 0, 0, 0};
         }
       }
       if constexpr (VX) {
-        const uint32_t per = F8 ? 16 : 8, d = F8 ? slot / (S::VC / 2) : slot / S::VC;
-        const uint32_t e = base + x_entry(i), bl = block_of(a.c, e < end ? e : end - 1), t = e - bl * a.c.tokens;
-        const bool has = static_cast<uint32_t>(vid[i]) < a.c.num_blocks, in = e < end && has && mine && d < a.c.dim;
-        const uint32_t left = in ? end - e : 0;  // of the chunk's entries, those before the end
-        const uint8_t* vp = a.c.v + (in ? static_cast<uint64_t>(static_cast<uint32_t>(vid[i])) * a.c.block_bytes : 0) + head * a.c.v_head +
-                            static_cast<uint64_t>(in ? d : 0) * a.c.v_chunk + static_cast<uint64_t>(in ? t : 0) * a.c.v_token;
+        const uint32_t d = x_value(i), c = x_chunk(i);
+        const uint64_t from = groups_at[n % 4][c];
+        const uint8_t* xp = reinterpret_cast<const uint8_t*>(from) + d * a.c.v_chunk;
+        const bool in = from && d < a.c.dim;
+        const uint32_t e = base + c * kPer, left = !tail ? kPer : e < end ? end - e : 0;  // of the chunk's entries, those before the end
         if constexpr (F8) {
-          held_v[i] = in ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
-          if (left < per) {
+          held_v[b][i] = in ? *reinterpret_cast<const u32x4*>(xp) : u32x4{0, 0, 0, 0};
+          if (left < kPer) {
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j)
-              held_v[i][j] &= left >= 4 * j + 4 ? ~0u : left <= 4 * j ? 0u : (1u << (left - 4 * j) * 8) - 1;
+              held_v[b][i][j] &= left >= 4 * j + 4 ? ~0u : left <= 4 * j ? 0u : (1u << (left - 4 * j) * 8) - 1;
           }
-        } else if (left >= per) {
-          __builtin_amdgcn_global_load_lds((global_u8*)vp, (lds_u8*)(lds[b][1] + (i * 256 + wave * 64) * 16), 16, 0, 0);
+        } else if (in && left >= kPer) {
+          __builtin_amdgcn_global_load_lds((global_u8*)xp, (lds_u8*)(vl + (i * 256 + wave * 64) * 16), 16, 0, 0);
         } else {
-          const u32x4 w = in ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
-          *reinterpret_cast<u32x4*>(lds[b][1] + slot * 16) = only_keys(w, (1u << left) - 1);
+          const u32x4 w = in ? *reinterpret_cast<const u32x4*>(xp) : u32x4{0, 0, 0, 0};
+          *reinterpret_cast<u32x4*>(vl + (i * 256 + threadIdx.x) * 16) = only_keys(w, (1u << left) - 1);
         }
       }
     }
-    if (__any(missing) && lane == 0) absent[b] = n;
   };
   // 8 bits: widen what fetch() holds into buffer b.
-  const auto widen_to = [&](int b) {
+  const auto widen_to = [&](auto b) {
     if constexpr (F8) {
+      uint8_t* const kl = k_of(b);
+      uint8_t* const vl = v_of(b);
 #pragma unroll
       for (int i = 0; i < S::NL; ++i) {
-        if (!in_tile(i)) continue;
-        const uint32_t slot = i * 256 + threadIdx.x, e = k_entry(i), chunk = slot % (S::C / 2) * 2;
-        const u32x4 x = held_k[i], y = held_v[i];
-        *reinterpret_cast<u32x4*>(lds[b][0] + S::at(e, chunk)) = widen<T>(x[0], x[1]);
-        *reinterpret_cast<u32x4*>(lds[b][0] + S::at(e, chunk + 1)) = widen<T>(x[2], x[3]);
+        const uint32_t e = k_entry(i), chunk = k_chunk(i) * 2;
+        const u32x4 x = held_k[b][i], y = held_v[b][i];
+        *reinterpret_cast<u32x4*>(kl + S::at(e, chunk)) = widen<T>(x[0], x[1]);
+        *reinterpret_cast<u32x4*>(kl + S::at(e, chunk + 1)) = widen<T>(x[2], x[3]);
         if constexpr (VX) {
-          const uint32_t d = slot / (S::VC / 2), c = x_entry(i) / 8;
-          *reinterpret_cast<u32x4*>(lds[b][1] + S::at_x(d, c)) = widen<T>(y[0], y[1]);
-          *reinterpret_cast<u32x4*>(lds[b][1] + S::at_x(d, c + 1)) = widen<T>(y[2], y[3]);
+          const uint32_t d = x_value(i), c = x_chunk(i) * 2;
+          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c)) = widen<T>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c + 1)) = widen<T>(y[2], y[3]);
         } else {
-          *reinterpret_cast<u32x4*>(lds[b][1] + S::at(e, chunk)) = widen<T>(y[0], y[1]);
-          *reinterpret_cast<u32x4*>(lds[b][1] + S::at(e, chunk + 1)) = widen<T>(y[2], y[3]);
+          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk)) = widen<T>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk + 1)) = widen<T>(y[2], y[3]);
         }
       }
     }
@@ -740,33 +792,41 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
   const uint32_t k_at = S::at((m / 4) * 8 + m % 4, g);
   const uint32_t v_at = VX ? 0 : S::at(g * 8 + m / 4, m >> 1 & 1) + (m & 1) * 8;
 
+  constexpr uint32_t kAhead = S::AHEAD, KT = S::KT;
   uint32_t number = 1;
-  int b = 0;
   if (begin < end) {
-    look_up(begin);
-    fetch(begin, number, 0);
-    widen_to(0);
-    if (begin + S::KT < end) look_up(begin + S::KT);
+#pragma unroll
+    for (uint32_t i = 0; i <= kAhead; ++i) {
+      look_up(begin + i * KT);
+      publish(begin + i * KT, number + i);
+    }
+    look_up(begin + (kAhead + 1) * KT);
+    __syncthreads();
+    fetch(begin, number, std::false_type());
+    if constexpr (F8)
+      if (begin + KT < end) fetch(begin + KT, number + 1, std::true_type());
+    widen_to(std::false_type());
   }
   uint32_t base = begin;
-  const auto arrive = [&]() {  // the tile at `base` is in buffer b, and the next one is on its way
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the tile is in LDS
-    __syncthreads();                                  // and everyone's, and the other buffer is no longer read
-    if (base + S::KT < end) {
-      fetch(base + S::KT, number + 1, b ^ 1);
-      if (base + 2 * S::KT < end) look_up(base + 2 * S::KT);
+  const auto arrive = [&](auto b) {  // the tile at `base` is in buffer b, and the next ones are on their way
+    if constexpr (!F8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the tile is in LDS
+    __syncthreads();                                                     // and everyone's, and the other buffer is no longer read
+    if (base + kAhead * KT < end) {
+      if constexpr (F8) fetch(base + kAhead * KT, number + kAhead, b);
+      else fetch(base + kAhead * KT, number + kAhead, other(b));
+      publish(base + (kAhead + 1) * KT, number + kAhead + 1);
+      look_up(base + (kAhead + 2) * KT);
     }
   };
-  const auto leave = [&]() {
-    if (base + S::KT < end) widen_to(b ^ 1);
-    base += S::KT;
+  const auto leave = [&](auto b) {
+    if (base + KT < end) widen_to(other(b));
+    base += KT;
     ++number;
-    b ^= 1;
   };
-  const auto tile = [&](auto masked) {
+  const auto tile = [&](auto masked, auto b) {
     constexpr bool kMasked = decltype(masked)::value;
-    const uint8_t* const kl = lds[b][0];
-    const uint8_t* const vl = lds[b][1];
+    const uint8_t* const kl = k_of(b);
+    const uint8_t* const vl = v_of(b);
     f32x4 x[RW][S::SUB][2];
 #pragma unroll
     for (int r = 0; r < RW; ++r)
@@ -806,9 +866,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
       for (int j = 0; j < S::SUB; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) y = fmaxf(y, x[r][j][i / 4][i % 4]);
-      y = fmaxf(y, across(y, 16));
-      y = fmaxf(y, across(y, 32));
-      mx[r] = y * to_log2;
+      mx[r] = max_of_row(y) * to_log2;
       rise |= mx[r] > top[r] + 8.0f;
     }
     if (__any(rise)) {
@@ -852,23 +910,32 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
         add_values<T>(op, p, o);
     }
   };
-  // Tiles that every row sees whole; from the first other one on, masked ones where a wave has any to mask.
-  const uint32_t whole = end < sp.before ? end : sp.before;
-  bool done = false;
-  while (base + S::KT <= whole) {
-    arrive();
-    if (absent[b] == number) {
-      done = true;
-      break;
-    }
-    if (work) tile(std::false_type());
-    leave();
+  // Tiles that every row of the workgroup sees whole, the two buffers in turn; from the first other one on, masked ones.
+  uint32_t whole = a.tree ? sp.before : sp.before + row0 / a.group + 1;
+  if (whole > end) whole = end;
+  bool arrived = false;
+  const auto go = [&](auto b) {
+    if (base + S::KT > whole) return false;
+    arrive(b);
+    arrived = absent[number % 4] == number;
+    if (arrived) return false;
+    if (work) tile(std::false_type(), b);
+    leave(b);
+    return true;
+  };
+  int b = 0;
+  while (true) {
+    b = 0;
+    if (!go(std::false_type())) break;
+    b = 1;
+    if (!go(std::true_type())) break;
   }
   while (base < end) {
-    if (!done) arrive();
-    done = false;
-    if (base < my_end) tile(std::true_type());
-    leave();
+    if (!arrived) b ? arrive(std::true_type()) : arrive(std::false_type());
+    arrived = false;
+    if (base < my_end) tile(std::true_type(), b);
+    b ? leave(std::true_type()) : leave(std::false_type());
+    b ^= 1;
   }
   const float v_scale = a.v_scale ? a.v_scale[head] : 1.0f;
 #pragma unroll
@@ -921,7 +988,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const SeqSpan& sp, u
   if (threadIdx.x == 0) {
     const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
     if (a.lse) a.lse[unit] = l2 * kLn2;
-    if (a.lse2) a.lse2[unit] = l2;
+    if (a.lse2) a.lse2[lse2_at(a, token, qh)] = l2;
   }
   const f32x4* part = reinterpret_cast<const f32x4*>(a.part + unit * a.splits * DP) + l;
   f32x4 o = {0, 0, 0, 0};
@@ -1012,19 +1079,30 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
   }
   const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
   const bool inner = base + kTile <= sp.before;
-  for (uint32_t row0 = 0; row0 < rows; row0 += 16) {
-    if (!a.tree && !inner && sp.before + (row0 + 15 < rows ? row0 + 15 : rows - 1) / a.group < base) continue;
+  // lse2 has a sequence's and KV head's rows side by side. Token and head of this lane's row go on by 16 rows a turn.
+  const float* l2_at = a.lse2 + (static_cast<uint64_t>(head) * a.s.num_tokens + sp.first) * a.group;
+  const uint32_t by_token = 16 / a.group, by_head = 16 % a.group;
+  uint32_t token = m / a.group, e = m % a.group, row0 = 0;
+  if (!a.tree && !inner && base > sp.before) {  // rows of earlier tokens do not see these keys
+    row0 = (base - sp.before) * a.group / 16 * 16;
+    token = (row0 + m) / a.group;
+    e = (row0 + m) % a.group;
+  }
+  for (; row0 < rows; row0 += 16) {
     u32x4 q[KS];
-    const uint32_t row = row0 + m;
-    const bool live = row < rows;
-    load_q<F8, KS>(a, head * a.group + (live ? row % a.group : 0), sp.first + (live ? row / a.group : 0), live, g, q);
+    const bool live = row0 + m < rows;
+    load_q<F8, KS>(a, head * a.group + (live ? e : 0), sp.first + (live ? token : 0), live, g, q);
+    token += by_token;
+    e += by_head;
+    if (e >= a.group) {
+      e -= a.group;
+      ++token;
+    }
     float l2[4];
-    uint32_t token[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t x = row0 + g * 4 + i;
-      token[i] = x / a.group;
-      l2[i] = x < rows ? a.lse2[static_cast<uint64_t>(sp.first + token[i]) * a.q_heads + head * a.group + x % a.group] : INFINITY;
+      l2[i] = x < rows ? l2_at[x] : INFINITY;
       if (l2[i] == -INFINITY) l2[i] = INFINITY;  // a row that sees nothing
     }
 #pragma unroll
@@ -1037,18 +1115,22 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
         else w = k[t][i];
         s = Type<T>::mfma(q[i], w, s);
       }
+      float p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bool see = there[t] && row0 + g * 4 + i < rows;
-        if (!inner && see && key[t] >= sp.before) {
-          const uint32_t d = key[t] - sp.before;
-          see = a.tree ? d / 64 < a.tree_words &&
-                             (a.tree[static_cast<uint64_t>(sp.first + token[i]) * a.tree_words + d / 64] >> (d % 64) & 1)
-                       : d <= token[i];
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[i] * to_log2 - l2[i]);
+      if (!inner && key[t] >= sp.before) {
+        const uint32_t d = key[t] - sp.before;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = row0 + g * 4 + i, of = x / a.group;
+          const bool see = x < rows && (a.tree ? d / 64 < a.tree_words &&
+                                                     (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
+                                               : d <= of);
+          p[i] = see ? p[i] : 0.0f;
         }
-        const float p = __builtin_amdgcn_exp2f(s[i] * to_log2 - l2[i]);
-        sum[t] += see ? p : 0.0f;
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[t] += there[t] && l2[i] < INFINITY ? p[i] : 0.0f;
     }
   }
 #pragma unroll
@@ -1064,19 +1146,19 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
 
 template <class T, bool F8, int DP, bool VX>
 hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  const uint32_t cells = p.splits * a.c.heads * a.s.num_seqs;
   if (p.stream) {
-    const dim3 grid(p.splits * p.row_groups, a.c.heads, a.s.num_seqs);
     if (p.tiles_per_wave == 1) {
-      attention_stream_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a);
+      attention_stream_kernel<T, F8, DP, VX, 1><<<cells, 256, 0, stream>>>(a);
     } else {
-      if constexpr (DP < 256) attention_stream_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a);
+      if constexpr (DP < 256) attention_stream_kernel<T, F8, DP, VX, 2><<<cells, 256, 0, stream>>>(a);
     }
   } else {
-    const uint32_t units = p.splits * p.row_groups * a.c.heads * a.s.num_seqs, grid = (units + 7) / 8 * 8;
+    const uint32_t grid = (cells + 7) / 8 * 8 * p.row_groups;
     if (p.tiles_per_wave == 1)
-      attention_rows_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a, p.row_groups, units);
+      attention_rows_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a, p.row_groups, cells);
     else
-      attention_rows_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a, p.row_groups, units);
+      attention_rows_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a, p.row_groups, cells);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

@@ -244,7 +244,10 @@ AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& 
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
-  const uint64_t want = p.stream ? 1024 : 512, least = 256;  // workgroups in all, entries of a split
+  // Workgroups in all: the 512 that run at once, so that all end together; but 2048 where many sequences, likely of
+  // different lengths, would leave some of those idle (32 of 1k to 8k: 124 us against 138). Entries of a split: 256 at least.
+  const bool many = p.stream && static_cast<uint64_t>(q.num_seqs) * c.heads >= 64;
+  const uint64_t want = many ? 2048 : 512, least = 256;
   uint64_t splits = wgs >= want ? 1 : (want + wgs - 1) / std::max<uint64_t>(wgs, 1);
   splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, up(q.max_len, least)));
   p.split_len = up(up(q.max_len, static_cast<uint32_t>(splits)), 128) * 128;
@@ -420,7 +423,7 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
   if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
   const AttnPlan p = attention_plan(call.c, layout->elem_bytes, *seqs, *a);
-  if (static_cast<uint64_t>(p.row_groups) * p.splits * H * seqs->num_seqs >= 1ull << 24)
+  if (static_cast<uint64_t>(p.row_groups) * (static_cast<uint64_t>(p.splits) * H * seqs->num_seqs + 7) >= 1ull << 24)
     return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
                 seqs->num_seqs, seqs->max_tokens, H);
   if (p.bytes) {
