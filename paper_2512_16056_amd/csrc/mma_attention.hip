@@ -221,32 +221,50 @@ __device__ __forceinline__ uint64_t lse2_at(const AttnArgs& a, uint32_t token, u
 }
 
 // What a row's result goes to: the output and lse, or with several splits this split's part of them.
-template <class T, int DP, int NC, class At>
+// SIDE: a lane's 4 sums of an instruction are neighbours (value 16 c + 4 g); else the sums of CE instructions are, for each of the 4.
+template <class T, int DP, int NC, int SIDE>
 __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uint32_t qh, uint32_t split, uint32_t g, float top,
-                                          float sum, float v_scale, const f32x4 (&o)[NC], At value_at) {
+                                          float sum, float v_scale, const f32x4 (&o)[NC]) {
   const uint64_t unit = static_cast<uint64_t>(token) * a.q_heads + qh;
   if (a.part_ml && !g) {
     float* ml = a.part_ml + 2 * (unit * a.splits + split);
     ml[0] = top;
     ml[1] = sum;
   }
+  // The q-th four neighbours of the lane, and the head value of the first.
+  const auto four = [&](int q) -> f32x4 {
+    if constexpr (SIDE) return o[q];
+    constexpr int CE = DP == 64 ? 4 : 8;
+    const int i = q / (CE / 4) % 4, c = q / CE * CE + q % (CE / 4) * 4;
+    return f32x4{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+  };
+  const auto value = [&](int q) -> uint32_t {
+    if constexpr (SIDE) return q * 16 + g * 4;
+    constexpr int CE = DP == 64 ? 4 : 8;
+    return q / CE * 16 * CE + (g * 4 + q / (CE / 4) % 4) * CE + q % (CE / 4) * 4;
+  };
   if (a.splits > 1) {
     float* to = a.part + (unit * a.splits + split) * DP;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) to[value_at(c, g * 4 + i)] = o[c][i] * v_scale;
+    for (int q = 0; q < NC; ++q) *reinterpret_cast<f32x4*>(to + value(q)) = four(q) * v_scale;
     return;
   }
   const float by = sum == 0 ? 0.0f : v_scale / sum;
   T* to = reinterpret_cast<T*>(a.out.data) + token * a.out.token + qh * a.out.head;
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int q = 0; q < NC; ++q) {
+    const f32x4 x = four(q) * by;
+    const uint32_t d = value(q);
+    if (d >= a.c.dim) continue;
+    const u32x2 w = {Type<T>::pack(x[0], x[1]), Type<T>::pack(x[2], x[3])};
+    if (a.wide_out) {
+      *reinterpret_cast<u32x2*>(to + d) = w;
+    } else {
+      uint16_t* h = reinterpret_cast<uint16_t*>(to + d);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t d = value_at(c, g * 4 + i);
-      if (d < a.c.dim) to[d] = static_cast<T>(o[c][i] * by);
+      for (int i = 0; i < 4; ++i) h[i] = static_cast<uint16_t>(w[i / 2] >> (i % 2 * 16));
     }
+  }
   if (!g) {
     const float l2 = sum == 0 ? -INFINITY : top + __builtin_amdgcn_logf(sum);
     if (a.lse) a.lse[unit] = l2 * kLn2;
@@ -272,10 +290,7 @@ struct Stream {
   static constexpr int NC = DP / 16;                  // instructions of 16 head values
   static constexpr int VW = VX ? (F8 ? 2 : 4) : CE / (F8 ? 4 : 2);  // dwords of a load of V
   static constexpr int NV = VX ? NC : NP * 8;                       // loads of V
-  // Head value of V^T row r (0..15) of instruction c.
-  static __device__ __forceinline__ uint32_t value_at(int c, uint32_t r) {
-    return VX ? c * 16 + r : (c / CE) * 16 * CE + r * CE + c % CE;
-  }
+  // Row r (0..15) of V^T of instruction c is head value 16 c + r (VX), else c / CE * 16 CE + r CE + c % CE.
 
   u32x4 k[2][NK];
   uint32_t v[NV][VW];
@@ -325,7 +340,7 @@ struct Stream {
       }
     }
   }
-  // Operand c of V^T: value value_at(c, m) of the lane's 8 keys.
+  // Operand c of V^T: row m of instruction c, of the lane's 8 keys.
   template <class T>
   __device__ __forceinline__ u32x4 value(int c) const {
     if constexpr (VX) {
@@ -539,8 +554,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 #pragma unroll
   for (int r = 0; r < R; ++r)
     if (live[r])
-      store_row<T, DP>(a, sp.first + token[r], head * a.group + (row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r],
-                       S::value_at);
+      store_row<T, DP, S::NC, VX>(a, sp.first + token[r], head * a.group + (row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r]);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -584,6 +598,7 @@ struct Tiles {
 };
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
+constexpr int kMfma = 0x008, kDsRead = 0x100;  // groups of instructions for the scheduler
 typedef __attribute__((address_space(1))) const uint8_t global_u8;
 
 __device__ __forceinline__ u32x2 read_turned(const uint8_t* p) {  // 16 lanes: 4 rows of 16 values, a column to each
@@ -721,6 +736,25 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     uint8_t* const kl = k_of(b);
     uint8_t* const vl = v_of(b);
     const bool tail = base + S::KT > end;
+    if constexpr (!F8 && !VX) {
+      // All of the tile there and no padding, as almost always: nothing but the loads.
+      uint64_t at[S::NL];
+      bool all = a.c.dim == DP;
+#pragma unroll
+      for (int i = 0; i < S::NL; ++i) {
+        at[i] = rows_at[n % 4][k_entry(i)];
+        all = all && at[i];
+      }
+      if (__all(all)) {
+#pragma unroll
+        for (int i = 0; i < S::NL; ++i) {
+          const uint8_t* kp = reinterpret_cast<const uint8_t*>(at[i]) + k_chunk(i) * 16;  // rows: chunks follow each other
+          __builtin_amdgcn_global_load_lds((global_u8*)kp, (lds_u8*)(kl + (i * 256 + wave * 64) * 16), 16, 0, 0);
+          __builtin_amdgcn_global_load_lds((global_u8*)(kp + v_from_k), (lds_u8*)(vl + (i * 256 + wave * 64) * 16), 16, 0, 0);
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < S::NL; ++i) {
       const uint32_t chunk = k_chunk(i);
@@ -812,10 +846,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     if constexpr (!F8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this thread's part of the tile is in LDS
     __syncthreads();                                                     // and everyone's, and the other buffer is no longer read
     if (base + kAhead * KT < end) {
-      if constexpr (F8) fetch(base + kAhead * KT, number + kAhead, b);
-      else fetch(base + kAhead * KT, number + kAhead, other(b));
+      // In this order, so that the block looked up last time is not waited for behind the tile's own loads.
       publish(base + (kAhead + 1) * KT, number + kAhead + 1);
       look_up(base + (kAhead + 2) * KT);
+      if constexpr (F8) fetch(base + kAhead * KT, number + kAhead, b);
+      else fetch(base + kAhead * KT, number + kAhead, other(b));
     }
   };
   const auto leave = [&](auto b) {
@@ -844,6 +879,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
 #pragma unroll
           for (int r = 0; r < RW; ++r) x[r][j][t] = Type<T>::mfma(k, q[r][i], x[r][j][t]);
         }
+    if constexpr (!kMasked) {
+      constexpr int kReads = S::KS * S::SUB * 2;
+      __builtin_amdgcn_sched_group_barrier(kDsRead, kReads / 2, 0);
+#pragma unroll
+      for (int i = 0; i < kReads / 2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, RW, 0);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(kMfma, RW * kReads / 2, 0);
+    }
     uint32_t seen[S::SUB][RW];
     if constexpr (kMasked) {
 #pragma unroll
@@ -943,8 +988,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     sum[r] += across(sum[r], 16);
     sum[r] += across(sum[r], 32);
     if (live[r])
-      store_row<T, DP>(a, sp.first + token[r], head * a.group + (my_row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r],
-                       [](int c, uint32_t i) { return c * 16 + i; });
+      store_row<T, DP, S::NC, 1>(a, sp.first + token[r], head * a.group + (my_row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r]);
   }
 }
 
@@ -1000,9 +1044,15 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const SeqSpan& sp, u
   for (uint32_t i = 1; i < W; ++i) o += lds[i * L + l];
   const float by = sum == 0 ? 0.0f : 1.0f / sum;
   T* to = reinterpret_cast<T*>(a.out.data) + token * a.out.token + qh * a.out.head;
+  if (l * 4 >= a.c.dim) return;
+  const u32x2 y = {Type<T>::pack(o[0] * by, o[1] * by), Type<T>::pack(o[2] * by, o[3] * by)};
+  if (a.wide_out) {
+    *reinterpret_cast<u32x2*>(to + l * 4) = y;
+  } else {
+    uint16_t* h = reinterpret_cast<uint16_t*>(to + l * 4);
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (l * 4 + j < a.c.dim) to[l * 4 + j] = static_cast<T>(o[j] * by);
+    for (int j = 0; j < 4; ++j) h[j] = static_cast<uint16_t>(y[j / 2] >> (j % 2 * 16));
+  }
 }
 
 constexpr uint32_t kWeigh = 1024;  // entries of a workgroup that adds up kept logits
@@ -1048,78 +1098,81 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
 
 // ---------------------------------------------------------------- weights of the entries, many rows
 // With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
-// lane adds up its key's rows. A wave has 32 keys and goes through the rows; each score has one
-// writer, so that the result does not depend on the order of waves.
+// lane adds up its key's rows. A wave has 16 NT keys in registers and goes through the rows, the next 16 of them on their
+// way; each score has one writer, so that the result does not depend on the order of waves.
+template <bool F8, int DP>
+constexpr int kScoreTiles = DP == 256 ? 2 : 4;  // NT: of 16 keys
+
 template <class T, bool F8, int DP>
 __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
-  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS;
+  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, NT = kScoreTiles<F8, DP>;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
-  const uint32_t base = (blockIdx.x * 4 + wave) * kTile;
+  const uint32_t base = (blockIdx.x * 4 + wave) * 16 * NT;
   if (base >= sp.total) return;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
   const uint32_t rows = sp.count * a.group;
-  u32x4 k[2][NK];
-  uint32_t key[2];
-  bool there[2];
-  float sum[2] = {0, 0};
+  u32x4 k[NT][NK];
+  uint32_t there = 0;  // bit t: the lane's t-th key is
+  float sum[NT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < NT; ++t) {
     uint32_t in_block;
-    key[t] = base + t * 16 + m;
-    const int32_t id = block_at(a.c, table, key[t] < sp.total ? key[t] : sp.total - 1, &in_block);
-    there[t] = key[t] < sp.total && id >= 0;
-    const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + static_cast<uint64_t>(in_block) * a.c.k_token;
+    const uint32_t key = base + t * 16 + m;
+    const int32_t id = block_at(a.c, table, key < sp.total ? key : sp.total - 1, &in_block);
+    there |= (key < sp.total && id >= 0 ? 1u : 0u) << t;
+    sum[t] = 0;
+    const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + in_block * a.c.k_token;
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
       const uint32_t chunk = s * 4 + g;
-      k[t][s] = chunk * (F8 ? 16 : 8) < a.c.dim ? *reinterpret_cast<const u32x4*>(p + static_cast<uint64_t>(chunk) * a.c.k_chunk) : u32x4{0, 0, 0, 0};
+      k[t][s] = chunk * (F8 ? 16 : 8) < a.c.dim ? *reinterpret_cast<const u32x4*>(p + chunk * a.c.k_chunk) : u32x4{0, 0, 0, 0};
     }
   }
   const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
-  const bool inner = base + kTile <= sp.before;
+  const bool inner = base + 16 * NT <= sp.before;
   // lse2 has a sequence's and KV head's rows side by side. Token and head of this lane's row go on by 16 rows a turn.
   const float* l2_at = a.lse2 + (static_cast<uint64_t>(head) * a.s.num_tokens + sp.first) * a.group;
   const uint32_t by_token = 16 / a.group, by_head = 16 % a.group;
-  uint32_t token = m / a.group, e = m % a.group, row0 = 0;
-  if (!a.tree && !inner && base > sp.before) {  // rows of earlier tokens do not see these keys
-    row0 = (base - sp.before) * a.group / 16 * 16;
-    token = (row0 + m) / a.group;
-    e = (row0 + m) % a.group;
-  }
-  for (; row0 < rows; row0 += 16) {
-    u32x4 q[KS];
-    const bool live = row0 + m < rows;
-    load_q<F8, KS>(a, head * a.group + (live ? e : 0), sp.first + (live ? token : 0), live, g, q);
+  uint32_t row0 = 0;
+  if (!a.tree && base > sp.before) row0 = (base - sp.before) * a.group / 16 * 16;  // rows of earlier tokens do not see these keys
+  uint32_t token = (row0 + m) / a.group, e = (row0 + m) % a.group;
+  u32x4 q[2][KS];
+  float l2[2][4];
+  const auto load = [&](auto b, uint32_t first) {  // rows first .. first + 15
+    const bool live = first + m < rows;
+    load_q<F8, KS>(a, head * a.group + (live ? e : 0), sp.first + (live ? token : 0), live, g, q[b]);
     token += by_token;
     e += by_head;
     if (e >= a.group) {
       e -= a.group;
       ++token;
     }
-    float l2[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint32_t x = row0 + g * 4 + i;
-      l2[i] = x < rows ? l2_at[x] : INFINITY;
-      if (l2[i] == -INFINITY) l2[i] = INFINITY;  // a row that sees nothing
+      const uint32_t x = first + g * 4 + i;
+      const float l = x < rows ? l2_at[x] : INFINITY;
+      l2[b][i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
     }
+  };
+  const auto add = [&](auto b) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < NT; ++t) {
       f32x4 s = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         u32x4 w;
         if constexpr (F8) w = widen<T>(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1]);
         else w = k[t][i];
-        s = Type<T>::mfma(q[i], w, s);
+        s = Type<T>::mfma(q[b][i], w, s);
       }
       float p[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[i] * to_log2 - l2[i]);
-      if (!inner && key[t] >= sp.before) {
-        const uint32_t d = key[t] - sp.before;
+      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[i] * to_log2 - l2[b][i]);
+      const uint32_t key = base + t * 16 + m;
+      if (!inner && key >= sp.before) {
+        const uint32_t d = key - sp.before;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t x = row0 + g * 4 + i, of = x / a.group;
@@ -1130,16 +1183,26 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum[t] += there[t] && l2[i] < INFINITY ? p[i] : 0.0f;
+      for (int i = 0; i < 4; ++i) sum[t] += (there >> t & 1) && l2[b][i] < INFINITY ? p[i] : 0.0f;
     }
+    row0 += 16;
+  };
+  if (row0 < rows) load(std::false_type(), row0);
+  while (row0 < rows) {
+    if (row0 + 16 < rows) load(std::true_type(), row0 + 16);
+    add(std::false_type());
+    if (row0 >= rows) break;
+    if (row0 + 16 < rows) load(std::false_type(), row0 + 16);
+    add(std::true_type());
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < NT; ++t) {
     sum[t] += across(sum[t], 16);
     sum[t] += across(sum[t], 32);
-    if (g == t && key[t] < sp.total) {
-      const uint64_t at = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key[t];
-      a.scores_out[at] = (a.scores_in && key[t] < sp.before ? a.decay * a.scores_in[at] : 0.0f) + sum[t];
+    const uint32_t key = base + t * 16 + m;
+    if (g == t % 4 && key < sp.total) {
+      const uint64_t at = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
+      a.scores_out[at] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[at] : 0.0f) + sum[t];
     }
   }
 }
@@ -1170,7 +1233,7 @@ hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   }
   if (a.lse2) {
     attention_scores_kernel<T, F8, DP>
-        <<<dim3((a.s.max_len + 4 * kTile - 1) / (4 * kTile), a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
+        <<<dim3((a.s.max_len + 64 * kScoreTiles<F8, DP> - 1) / (64 * kScoreTiles<F8, DP>), a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
     e = hipGetLastError();
   }
   return e;
