@@ -1098,112 +1098,122 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
 
 // ---------------------------------------------------------------- weights of the entries, many rows
 // With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
-// lane adds up its key's rows. A wave has 16 NT keys in registers and goes through the rows, the next 16 of them on their
-// way; each score has one writer, so that the result does not depend on the order of waves.
-template <bool F8, int DP>
-constexpr int kScoreTiles = DP == 256 ? 2 : 4;  // NT: of 16 keys
+// lane adds up its key's rows. A workgroup has up to kScored keys (score_len); each of its waves keeps 32 of every 128 rows in
+// registers and goes through the keys 32 at a time, the next ones on their way: what it waits for at its start (lengths,
+// table, rows) is waited for once. The waves' sums are joined in LDS; each score has one writer and its sum one order.
+constexpr uint32_t kScored = 1024;
 
 template <class T, bool F8, int DP>
 __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
-  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, NT = kScoreTiles<F8, DP>;
+  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, R = DP == 256 ? 1 : 2;
+  __shared__ float sums[4][kScored];
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
-  const uint32_t base = (blockIdx.x * 4 + wave) * 16 * NT;
-  if (base >= sp.total) return;
+  const uint32_t begin = blockIdx.x * a.score_len;
+  if (begin >= sp.total) return;
+  const uint32_t end = begin + a.score_len < sp.total ? begin + a.score_len : sp.total;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
   const uint32_t rows = sp.count * a.group;
-  u32x4 k[NT][NK];
-  uint32_t there = 0;  // bit t: the lane's t-th key is
-  float sum[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    uint32_t in_block;
-    const uint32_t key = base + t * 16 + m;
-    const int32_t id = block_at(a.c, table, key < sp.total ? key : sp.total - 1, &in_block);
-    there |= (key < sp.total && id >= 0 ? 1u : 0u) << t;
-    sum[t] = 0;
-    const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + in_block * a.c.k_token;
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      const uint32_t chunk = s * 4 + g;
-      k[t][s] = chunk * (F8 ? 16 : 8) < a.c.dim ? *reinterpret_cast<const u32x4*>(p + chunk * a.c.k_chunk) : u32x4{0, 0, 0, 0};
-    }
-  }
   const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
-  const bool inner = base + 16 * NT <= sp.before;
-  // lse2 has a sequence's and KV head's rows side by side. Token and head of this lane's row go on by 16 rows a turn.
+  // lse2 has a sequence's and KV head's rows side by side.
   const float* l2_at = a.lse2 + (static_cast<uint64_t>(head) * a.s.num_tokens + sp.first) * a.group;
-  const uint32_t by_token = 16 / a.group, by_head = 16 % a.group;
-  uint32_t row0 = 0;
-  if (!a.tree && base > sp.before) row0 = (base - sp.before) * a.group / 16 * 16;  // rows of earlier tokens do not see these keys
-  uint32_t token = (row0 + m) / a.group, e = (row0 + m) % a.group;
-  u32x4 q[2][KS];
-  float l2[2][4];
-  const auto load = [&](auto b, uint32_t first) {  // rows first .. first + 15
-    const bool live = first + m < rows;
-    load_q<F8, KS>(a, head * a.group + (live ? e : 0), sp.first + (live ? token : 0), live, g, q[b]);
-    token += by_token;
-    e += by_head;
-    if (e >= a.group) {
-      e -= a.group;
-      ++token;
-    }
+  const auto load = [&](uint32_t base, u32x4 (&k)[2][NK], uint32_t* there) {
+    uint32_t have = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = first + g * 4 + i;
-      const float l = x < rows ? l2_at[x] : INFINITY;
-      l2[b][i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
-    }
-  };
-  const auto add = [&](auto b) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      f32x4 s = {0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        u32x4 w;
-        if constexpr (F8) w = widen<T>(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1]);
-        else w = k[t][i];
-        s = Type<T>::mfma(q[b][i], w, s);
-      }
-      float p[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(s[i] * to_log2 - l2[b][i]);
+    for (int t = 0; t < 2; ++t) {
+      uint32_t in_block;
       const uint32_t key = base + t * 16 + m;
-      if (!inner && key >= sp.before) {
-        const uint32_t d = key - sp.before;
+      const int32_t id = block_at(a.c, table, key < end ? key : end - 1, &in_block);
+      have |= (key < end && id >= 0 ? 1u : 0u) << t;
+      const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + in_block * a.c.k_token;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t x = row0 + g * 4 + i, of = x / a.group;
-          const bool see = x < rows && (a.tree ? d / 64 < a.tree_words &&
-                                                     (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
-                                               : d <= of);
-          p[i] = see ? p[i] : 0.0f;
+      for (int s = 0; s < NK; ++s) {
+        const uint32_t chunk = s * 4 + g;
+        k[t][s] = *reinterpret_cast<const u32x4*>(p + (chunk * (F8 ? 16 : 8) < a.c.dim ? chunk * a.c.k_chunk : 0));
+      }
+    }
+    *there = have;
+  };
+  // Rows of tokens before the first key's do not see these keys.
+  const uint32_t start = !a.tree && begin > sp.before ? (begin - sp.before) * a.group / 16 * 16 : 0;
+  bool first = true;
+  for (uint32_t row0 = start; row0 < rows || first; row0 += 64 * R, first = false) {
+    u32x4 q[R][KS];
+    float l2[R][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const uint32_t at = row0 + (wave * R + r) * 16, row = at + m;
+      const bool live = row < rows;
+      load_q<F8, KS>(a, head * a.group + (live ? row % a.group : 0), sp.first + (live ? row / a.group : 0), live, g, q[r]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t x = at + g * 4 + i;
+        const float l = x < rows ? l2_at[x] : INFINITY;
+        l2[r][i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
+      }
+    }
+    u32x4 k[2][2][NK];
+    uint32_t there[2];
+    const auto add = [&](uint32_t base, auto b) {
+#pragma unroll
+      for (int s = 0; s < NK; ++s)
+        if (a.c.dim < DP && (s * 4 + g) * (F8 ? 16 : 8) >= a.c.dim) k[b][0][s] = k[b][1][s] = u32x4{0, 0, 0, 0};
+      f32x4 x[R][2];
+#pragma unroll
+      for (int r = 0; r < R; ++r) x[r][0] = x[r][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          u32x4 w;
+          if constexpr (F8) w = widen<T>(k[b][t][i / 2][i % 2 * 2], k[b][t][i / 2][i % 2 * 2 + 1]);
+          else w = k[b][t][i];
+#pragma unroll
+          for (int r = 0; r < R; ++r) x[r][t] = Type<T>::mfma(q[r][i], w, x[r][t]);
+        }
+      const bool inner = base + kTile <= sp.before;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float sum = 0;
+        const uint32_t key = base + t * 16 + m;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float p = __builtin_amdgcn_exp2f(x[r][t][i] * to_log2 - l2[r][i]);
+            bool see = l2[r][i] < INFINITY;
+            if (!inner && key >= sp.before && see) {
+              const uint32_t d = key - sp.before, of = (row0 + (wave * R + r) * 16 + g * 4 + i) / a.group;
+              see = a.tree ? d / 64 < a.tree_words && (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
+                           : d <= of;
+            }
+            sum += see ? p : 0.0f;
+          }
+        sum = there[b] >> t & 1 ? sum : 0.0f;
+        sum += across(sum, 16);
+        sum += across(sum, 32);
+        if (!g) {
+          float* to = &sums[wave][base - begin + t * 16 + m];
+          *to = first ? sum : *to + sum;
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum[t] += (there >> t & 1) && l2[b][i] < INFINITY ? p[i] : 0.0f;
+    };
+    load(begin, k[0], &there[0]);
+    for (uint32_t base = begin; base < end; base += 2 * kTile) {
+      if (base + kTile < end) load(base + kTile, k[1], &there[1]);
+      add(base, std::false_type());
+      if (base + kTile >= end) break;
+      if (base + 2 * kTile < end) load(base + 2 * kTile, k[0], &there[0]);
+      add(base + kTile, std::true_type());
     }
-    row0 += 16;
-  };
-  if (row0 < rows) load(std::false_type(), row0);
-  while (row0 < rows) {
-    if (row0 + 16 < rows) load(std::true_type(), row0 + 16);
-    add(std::false_type());
-    if (row0 >= rows) break;
-    if (row0 + 16 < rows) load(std::false_type(), row0 + 16);
-    add(std::true_type());
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    sum[t] += across(sum[t], 16);
-    sum[t] += across(sum[t], 32);
-    const uint32_t key = base + t * 16 + m;
-    if (g == t % 4 && key < sp.total) {
-      const uint64_t at = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
-      a.scores_out[at] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[at] : 0.0f) + sum[t];
-    }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; begin + i < end; i += 256) {
+    const uint32_t key = begin + i;
+    const uint64_t at = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
+    const float w = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    a.scores_out[at] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[at] : 0.0f) + w;
   }
 }
 
@@ -1233,7 +1243,7 @@ hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   }
   if (a.lse2) {
     attention_scores_kernel<T, F8, DP>
-        <<<dim3((a.s.max_len + 64 * kScoreTiles<F8, DP> - 1) / (64 * kScoreTiles<F8, DP>), a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
+        <<<dim3((a.s.max_len + a.score_len - 1) / a.score_len, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
     e = hipGetLastError();
   }
   return e;

@@ -115,14 +115,27 @@ template <class T, bool F8>
 __device__ __forceinline__ void append_turned(const AppendArgs& a, uint32_t first, uint32_t head, uint16_t* tile, int32_t* ids,
                                               uint32_t* ats) {
   const uint32_t n = a.s.num_tokens - first < kRun ? a.s.num_tokens - first : kRun, D = a.c.dim;
-  const uint32_t wave = threadIdx.x / kOpsWave;
   constexpr uint32_t S = kRun + 2;  // of a value's row in LDS: an odd number of dwords
-  for (uint32_t t = wave; t < n; t += 4) {  // seq_of is a whole wave's
-    const uint32_t seq = seq_of(a.s, first + t);
-    if (threadIdx.x % kOpsWave == 0) {
+  if (threadIdx.x < kOpsWave) {  // lane t finds token t's place, all at once
+    const uint32_t lane = threadIdx.x;
+    uint32_t seq = 0;
+    if (!a.s.q_start) {
+      seq = (first + lane) / a.s.max_tokens;
+    } else {
+      for (uint32_t s0 = 0; s0 < a.s.num_seqs; s0 += kOpsWave) {
+        const int32_t start = s0 + lane < a.s.num_seqs ? a.s.q_start[s0 + lane] : INT32_MAX;
+#pragma unroll
+        for (uint32_t t = 0; t < kRun; ++t) {
+          const uint32_t before = __popcll(__ballot(start <= static_cast<int32_t>(first + t)));
+          if (lane == t) seq += before;
+        }
+      }
+      seq = seq ? seq - 1 : 0;
+    }
+    if (lane < n) {
       uint32_t at;
-      ids[t] = entry_of(a, seq, first + t, &at);
-      ats[t] = at;
+      ids[lane] = entry_of(a, seq, first + lane, &at);
+      ats[lane] = at;
     }
   }
   const float scale = a.v_scale ? a.v_scale[head] : 1.0f;
@@ -175,25 +188,25 @@ __device__ __forceinline__ void append_turned(const AppendArgs& a, uint32_t firs
 // L lanes have a row of a token: L * 8 >= head_dim values. Rows of a token are its query heads,
 // then its keys, then (but for x-packed values) its values; a workgroup takes `parts`-th parts of
 // them. Where there are many tokens it takes all: what the rows share (position, place in the
-// cache, cosines and sines) is then read once. Workgroups past those turn x-packed values.
+// cache, cosines and sines) is then read once. The first workgroups, whose chain of loads is longest, turn x-packed values.
 template <class T, bool F8, bool VX, int L>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t parts) {
   constexpr uint32_t kRows = 256 / L;
   constexpr uint32_t kTurn = kRows * (L * 8 + 1) * 4, kTile = VX ? L * 8 * (kRun + 2) * 2 : 0;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kTurn > kTile ? kTurn : kTile];
-  const uint32_t row_blocks = a.s.num_tokens * parts;
+  const uint32_t turns = VX ? (a.s.num_tokens + kRun - 1) / kRun * a.c.heads : 0;
   if constexpr (VX) {
     __shared__ int32_t ids[kRun];
     __shared__ uint32_t ats[kRun];
-    if (blockIdx.x >= row_blocks) {
-      const uint32_t u = blockIdx.x - row_blocks;
+    if (blockIdx.x < turns) {
+      const uint32_t u = blockIdx.x;
       append_turned<T, F8>(a, u / a.c.heads * kRun, u % a.c.heads, reinterpret_cast<uint16_t*>(lds), ids, ats);
       return;
     }
   }
   float(*turn)[L * 8 + 1] = reinterpret_cast<float(*)[L * 8 + 1]>(lds);
   const uint32_t lane = threadIdx.x % L, slot = threadIdx.x / L;
-  const uint32_t token = blockIdx.x / parts, part = blockIdx.x % parts;
+  const uint32_t block_row = blockIdx.x - turns, token = block_row / parts, part = block_row % parts;
   const uint32_t heads = a.c.heads, rows = a.q_heads + (VX ? 1 : 2) * heads;
   const uint32_t d0 = lane * 8, D = a.c.dim, R = a.rot_dim, half = R / 2;
   // Pairs a multiple of 8 apart: a lane's 8 partners are another lane's 8 values, its cosines 32 bytes in a row.

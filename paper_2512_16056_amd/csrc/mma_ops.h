@@ -76,6 +76,7 @@ struct AttnArgs {
   float* logits;    // [sequence][KV head][logit_rows][logit_stride], base 2, or NULL
   uint32_t logit_rows, logit_stride;
   uint32_t q_heads, group, tree_words, scores_stride;
+  uint32_t score_len;          // entries of a workgroup of the scores kernel: a multiple of 32, at most 1024
   uint32_t splits, split_len;  // entries of a split: a multiple of the tile
   uint32_t wide_q, wide_out;   // rows start at 16 bytes
   float scale, decay;
