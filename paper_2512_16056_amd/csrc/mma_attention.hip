@@ -575,7 +575,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 template <bool F8, int DP, bool VX>
 struct Tiles {
   static constexpr int KT = DP == 256 || (F8 && DP == 128) ? 32 : 64;  // entries of a tile
-  static constexpr int AHEAD = F8 ? 2 : 1;        // tiles on their way while one is worked on
+  static constexpr int AHEAD = F8 ? 4 : 1;        // tiles on their way while one is worked on
   static constexpr int SUB = KT / 32;
   static constexpr int KS = DP / 32;
   static constexpr int NC = DP / 16;
@@ -627,8 +627,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     if constexpr (std::is_same<decltype(b), int>::value) return b ^ 1;
     else return std::bool_constant<!decltype(b)::value>();
   };
-  __shared__ uint64_t rows_at[4][S::KT], groups_at[4][VX ? S::VC : 1];  // of every four tiles, addresses of their entries, 0 where there is none
-  __shared__ uint32_t absent[4];  // number of the last tile of every four that had entries without a block
+  constexpr uint32_t kRing = F8 ? 8 : 4;  // more than the tiles between a publication and the last use of it
+  __shared__ uint64_t rows_at[kRing][S::KT], groups_at[kRing][VX ? S::VC : 1];  // of the last tiles, addresses of their entries, 0 where there is none
+  __shared__ uint32_t absent[8];  // number of the last tile of every eight that had entries without a block
+  // 8 bits: tiles as they come, 4 in turn; a thread's 16 bytes of K at 16 i of its chunk i, then those of V.
+  constexpr uint32_t kRaw = F8 ? S::NL * 2 * 4096 : 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t raw[F8 ? 4 : 1][kRaw];
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kOpsWave), lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   // Workgroups go to the 8 XCDs in turn. Row groups with the same keys follow each other on one XCD, so that they
   // share its L2; what they belong to (heads and sequences first, then splits) goes round the XCDs.
@@ -685,7 +689,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
       reinterpret_cast<u32x4*>(k0)[i] = u32x4{0, 0, 0, 0};
       reinterpret_cast<u32x4*>(k1)[i] = u32x4{0, 0, 0, 0};
     }
-  if (threadIdx.x < 4) absent[threadIdx.x] = 0;
+  if (threadIdx.x < 8) absent[threadIdx.x] = 0;
   __syncthreads();
 
   // Where a tile's entries (and, x-packed, the 8 or 16 entries of a chunk of values) lie, found once for all threads that
@@ -712,10 +716,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
         p += reinterpret_cast<uint64_t>(a.c.v) + head * a.c.v_head + static_cast<uint64_t>(t) * a.c.v_token;
     }
     if (finds) {
-      rows_at[n % 4][threadIdx.x] = p;
-      if (e < end && !has) absent[n % 4] = n;
+      rows_at[n % kRing][threadIdx.x] = p;
+      if (e < end && !has) absent[n % 8] = n;
     } else {
-      groups_at[n % 4][threadIdx.x - S::KT] = p;
+      groups_at[n % kRing][threadIdx.x - S::KT] = p;
     }
   };
 
@@ -730,11 +734,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     return F8 ? c : c ^ (S::VC == 8 ? d >> 1 & 7 : d >> 2 & 3);
   };
   const uint64_t v_from_k = a.c.v - a.c.k;
-  u32x4 held_k[2][F8 ? S::NL : 1], held_v[2][F8 ? S::NL : 1];
-  // Start bringing tile n, at `base`, to buffer b (8 bits: to the registers that go there).
+  uint32_t in_full = 0;  // 8 bits: how many tiles in a row this wave asked for every chunk of
+  // Start bringing tile n, at `base`, to buffer b (8 bits: to its turn of `raw`).
   const auto fetch = [&](uint32_t base, uint32_t n, auto b) {
     uint8_t* const kl = k_of(b);
     uint8_t* const vl = v_of(b);
+    uint8_t* const rl = raw[F8 ? n % 4 : 0];
+    bool full = true;
     const bool tail = base + S::KT > end;
     if constexpr (!F8 && !VX) {
       // All of the tile there and no padding, as almost always: nothing but the loads.
@@ -742,7 +748,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
       bool all = a.c.dim == DP;
 #pragma unroll
       for (int i = 0; i < S::NL; ++i) {
-        at[i] = rows_at[n % 4][k_entry(i)];
+        at[i] = rows_at[n % kRing][k_entry(i)];
         all = all && at[i];
       }
       if (__all(all)) {
@@ -758,13 +764,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
 #pragma unroll
     for (int i = 0; i < S::NL; ++i) {
       const uint32_t chunk = k_chunk(i);
-      const uint64_t at = rows_at[n % 4][k_entry(i)];
+      const uint64_t at = rows_at[n % kRing][k_entry(i)];
       const uint8_t* kp = reinterpret_cast<const uint8_t*>(at) + chunk * a.c.k_chunk;
       const uint8_t* vp = reinterpret_cast<const uint8_t*>(at) + v_from_k + chunk * 16;  // not x-packed: as far from V's start
       const bool live = chunk * (F8 ? 16 : 8) < a.c.dim;
       if constexpr (F8) {
-        held_k[b][i] = at && live ? *reinterpret_cast<const u32x4*>(kp) : u32x4{0, 0, 0, 0};
-        if constexpr (!VX) held_v[b][i] = at && live ? *reinterpret_cast<const u32x4*>(vp) : u32x4{0, 0, 0, 0};
+        const uint32_t slot = i * 256 + threadIdx.x, to = (i * 256 + wave * 64) * 16;
+        const bool in = at && live;
+        full = full && in;
+        if (in) {
+          __builtin_amdgcn_global_load_lds((global_u8*)kp, (lds_u8*)(rl + to), 16, 0, 0);
+          if constexpr (!VX) __builtin_amdgcn_global_load_lds((global_u8*)vp, (lds_u8*)(rl + S::NL * 4096 + to), 16, 0, 0);
+        } else {
+          *reinterpret_cast<u32x4*>(rl + slot * 16) = u32x4{0, 0, 0, 0};
+          if constexpr (!VX) *reinterpret_cast<u32x4*>(rl + S::NL * 4096 + slot * 16) = u32x4{0, 0, 0, 0};
+        }
       } else if (live) {
         if (at) {
           __builtin_amdgcn_global_load_lds((global_u8*)kp, (lds_u8*)(kl + (i * 256 + wave * 64) * 16), 16, 0, 0);
@@ -778,16 +792,20 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
       }
       if constexpr (VX) {
         const uint32_t d = x_value(i), c = x_chunk(i);
-        const uint64_t from = groups_at[n % 4][c];
+        const uint64_t from = groups_at[n % kRing][c];
         const uint8_t* xp = reinterpret_cast<const uint8_t*>(from) + d * a.c.v_chunk;
         const bool in = from && d < a.c.dim;
         const uint32_t e = base + c * kPer, left = !tail ? kPer : e < end ? end - e : 0;  // of the chunk's entries, those before the end
         if constexpr (F8) {
-          held_v[b][i] = in ? *reinterpret_cast<const u32x4*>(xp) : u32x4{0, 0, 0, 0};
-          if (left < kPer) {
+          const uint32_t slot = i * 256 + threadIdx.x;
+          full = full && in && left >= kPer;
+          if (in && left >= kPer) {
+            __builtin_amdgcn_global_load_lds((global_u8*)xp, (lds_u8*)(rl + S::NL * 4096 + (i * 256 + wave * 64) * 16), 16, 0, 0);
+          } else {
+            u32x4 w = in ? *reinterpret_cast<const u32x4*>(xp) : u32x4{0, 0, 0, 0};
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j)
-              held_v[b][i][j] &= left >= 4 * j + 4 ? ~0u : left <= 4 * j ? 0u : (1u << (left - 4 * j) * 8) - 1;
+            for (uint32_t j = 0; j < 4; ++j) w[j] &= left >= 4 * j + 4 ? ~0u : left <= 4 * j ? 0u : (1u << (left - 4 * j) * 8) - 1;
+            *reinterpret_cast<u32x4*>(rl + S::NL * 4096 + slot * 16) = w;
           }
         } else if (in && left >= kPer) {
           __builtin_amdgcn_global_load_lds((global_u8*)xp, (lds_u8*)(vl + (i * 256 + wave * 64) * 16), 16, 0, 0);
@@ -797,16 +815,28 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
         }
       }
     }
+    if constexpr (F8) in_full = __all(full) ? in_full + 1 : 0;
   };
-  // 8 bits: widen what fetch() holds into buffer b.
-  const auto widen_to = [&](auto b) {
+  // 8 bits: widen tile n from its turn of `raw` into buffer b, for all waves once. A thread widens what it asked for, so it
+  // waits for its own loads alone, and not for those of the `later` tiles asked for since where their number is sure.
+  // (The reads are written out, with their wait: the compiler would wait for all loads that are on their way to `raw`.)
+  const auto widen_to = [&](auto b, uint32_t n, bool later) {
     if constexpr (F8) {
       uint8_t* const kl = k_of(b);
       uint8_t* const vl = v_of(b);
+      if (later && in_full >= S::AHEAD - 1)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::AHEAD - 1) * 2 * S::NL) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_u8*)raw[n % 4])) + threadIdx.x * 16;
 #pragma unroll
       for (int i = 0; i < S::NL; ++i) {
         const uint32_t e = k_entry(i), chunk = k_chunk(i) * 2;
-        const u32x4 x = held_k[b][i], y = held_v[b][i];
+        u32x4 x, y;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\tds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(x), "=&v"(y)
+                     : "v"(at + i * 4096), "v"(at + (S::NL + i) * 4096)
+                     : "memory");
         *reinterpret_cast<u32x4*>(kl + S::at(e, chunk)) = widen<T>(x[0], x[1]);
         *reinterpret_cast<u32x4*>(kl + S::at(e, chunk + 1)) = widen<T>(x[2], x[3]);
         if constexpr (VX) {
@@ -836,10 +866,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     }
     look_up(begin + (kAhead + 1) * KT);
     __syncthreads();
-    fetch(begin, number, std::false_type());
-    if constexpr (F8)
-      if (begin + KT < end) fetch(begin + KT, number + 1, std::true_type());
-    widen_to(std::false_type());
+#pragma unroll
+    for (uint32_t i = 0; i < (F8 ? kAhead : 1); ++i)
+      if (begin + i * KT < end) fetch(begin + i * KT, number + i, std::false_type());
+    widen_to(std::false_type(), number, false);
   }
   uint32_t base = begin;
   const auto arrive = [&](auto b) {  // the tile at `base` is in buffer b, and the next ones are on their way
@@ -849,12 +879,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
       // In this order, so that the block looked up last time is not waited for behind the tile's own loads.
       publish(base + (kAhead + 1) * KT, number + kAhead + 1);
       look_up(base + (kAhead + 2) * KT);
-      if constexpr (F8) fetch(base + kAhead * KT, number + kAhead, b);
-      else fetch(base + kAhead * KT, number + kAhead, other(b));
+      fetch(base + kAhead * KT, number + kAhead, other(b));
     }
   };
   const auto leave = [&](auto b) {
-    if (base + KT < end) widen_to(other(b));
+    if (base + KT < end) widen_to(other(b), number + 1, base + kAhead * KT < end);
     base += KT;
     ++number;
   };
@@ -962,7 +991,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
   const auto go = [&](auto b) {
     if (base + S::KT > whole) return false;
     arrive(b);
-    arrived = absent[number % 4] == number;
+    arrived = absent[number % 8] == number;
     if (arrived) return false;
     if (work) tile(std::false_type(), b);
     leave(b);
@@ -1098,15 +1127,16 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
 
 // ---------------------------------------------------------------- weights of the entries, many rows
 // With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
-// lane adds up its key's rows. A workgroup has up to kScored keys (score_len); each of its waves keeps 32 of every 128 rows in
-// registers and goes through the keys 32 at a time, the next ones on their way: what it waits for at its start (lengths,
-// table, rows) is waited for once. The waves' sums are joined in LDS; each score has one writer and its sum one order.
+// lane adds up its key's rows. A workgroup has up to kScored keys (score_len) and 128 rows at a time (64 with heads above 128),
+// in LDS with their lse; its waves take the keys, 32 at a time, in turn, the next ones on their way: what bounds it is how
+// many different keys are on their way at once. Each score has one writer and its sum one order.
 constexpr uint32_t kScored = 1024;
 
 template <class T, bool F8, int DP>
 __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
-  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, R = DP == 256 ? 1 : 2;
-  __shared__ float sums[4][kScored];
+  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, C = DP / 8, kRows = DP == 256 ? 64 : 128;
+  __shared__ __attribute__((aligned(16))) uint8_t ql[kRows * C * 16];
+  __shared__ float sums[kScored], ll[kRows];
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
@@ -1118,6 +1148,8 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
   const float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
   // lse2 has a sequence's and KV head's rows side by side.
   const float* l2_at = a.lse2 + (static_cast<uint64_t>(head) * a.s.num_tokens + sp.first) * a.group;
+  // 16 bytes of a row in LDS: chunks exchanged by the row's number, so that 16 rows' do not meet in a bank.
+  const auto at = [&](uint32_t row, uint32_t chunk) { return (row * C + (chunk ^ (C == 8 ? row >> 1 & 7 : row & 15))) * 16; };
   const auto load = [&](uint32_t base, u32x4 (&k)[2][NK], uint32_t* there) {
     uint32_t have = 0;
 #pragma unroll
@@ -1137,83 +1169,90 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
   };
   // Rows of tokens before the first key's do not see these keys.
   const uint32_t start = !a.tree && begin > sp.before ? (begin - sp.before) * a.group / 16 * 16 : 0;
+  const uint32_t step = 4 * kTile;
   bool first = true;
-  for (uint32_t row0 = start; row0 < rows || first; row0 += 64 * R, first = false) {
-    u32x4 q[R][KS];
-    float l2[R][4];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const uint32_t at = row0 + (wave * R + r) * 16, row = at + m;
-      const bool live = row < rows;
-      load_q<F8, KS>(a, head * a.group + (live ? row % a.group : 0), sp.first + (live ? row / a.group : 0), live, g, q[r]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = at + g * 4 + i;
-        const float l = x < rows ? l2_at[x] : INFINITY;
-        l2[r][i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
-      }
+  for (uint32_t row0 = start; row0 < rows || first; row0 += kRows, first = false) {
+    if (!first) __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kRows * C; i += 256) {
+      const uint32_t r = i / C, chunk = i % C, row = row0 + r, d = chunk * 8;
+      u32x4 w = {0, 0, 0, 0};
+      if (row < rows && d < a.c.dim)
+        w = load_row8(a.q.data + 2 * ((sp.first + row / a.group) * a.q.token + (head * a.group + row % a.group) * a.q.head + d), a.wide_q);
+      *reinterpret_cast<u32x4*>(ql + at(r, chunk)) = w;
     }
+    for (uint32_t i = threadIdx.x; i < kRows; i += 256) {
+      const float l = row0 + i < rows ? l2_at[row0 + i] : INFINITY;
+      ll[i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
+    }
+    __syncthreads();
+    const uint32_t some = row0 < rows ? (rows - row0 < kRows ? rows - row0 : kRows) : 0;
     u32x4 k[2][2][NK];
     uint32_t there[2];
     const auto add = [&](uint32_t base, auto b) {
+      u32x4 kw[2][KS];
 #pragma unroll
-      for (int s = 0; s < NK; ++s)
-        if (a.c.dim < DP && (s * 4 + g) * (F8 ? 16 : 8) >= a.c.dim) k[b][0][s] = k[b][1][s] = u32x4{0, 0, 0, 0};
-      f32x4 x[R][2];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < R; ++r) x[r][0] = x[r][1] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < KS; ++i)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          u32x4 w;
-          if constexpr (F8) w = widen<T>(k[b][t][i / 2][i % 2 * 2], k[b][t][i / 2][i % 2 * 2 + 1]);
-          else w = k[b][t][i];
-#pragma unroll
-          for (int r = 0; r < R; ++r) x[r][t] = Type<T>::mfma(q[r][i], w, x[r][t]);
+        for (int i = 0; i < KS; ++i) {
+          const bool live = F8 ? ((i / 2) * 4 + g) * 16 < a.c.dim : (i * 4 + g) * 8 < a.c.dim;
+          if constexpr (F8) kw[t][i] = widen<T>(k[b][t][i / 2][i % 2 * 2], k[b][t][i / 2][i % 2 * 2 + 1]);
+          else kw[t][i] = k[b][t][i];
+          if (a.c.dim < DP && !live) kw[t][i] = u32x4{0, 0, 0, 0};
         }
       const bool inner = base + kTile <= sp.before;
+      float sum[2] = {0, 0};
+      for (uint32_t r0 = 0; r0 < some; r0 += 16) {
+        f32x4 x[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float sum = 0;
-        const uint32_t key = base + t * 16 + m;
+        for (int i = 0; i < KS; ++i) {
+          const u32x4 q = *reinterpret_cast<const u32x4*>(ql + at(r0 + m, F8 ? i / 2 * 8 + g * 2 + i % 2 : i * 4 + g));
+          x[0] = Type<T>::mfma(q, kw[0][i], x[0]);
+          x[1] = Type<T>::mfma(q, kw[1][i], x[1]);
+        }
+        const f32x4 l2 = *reinterpret_cast<const f32x4*>(ll + r0 + g * 4);
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float p = __builtin_amdgcn_exp2f(x[r][t][i] * to_log2 - l2[r][i]);
-            bool see = l2[r][i] < INFINITY;
-            if (!inner && key >= sp.before && see) {
-              const uint32_t d = key - sp.before, of = (row0 + (wave * R + r) * 16 + g * 4 + i) / a.group;
-              see = a.tree ? d / 64 < a.tree_words && (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
-                           : d <= of;
+            const float p = __builtin_amdgcn_exp2f(x[t][i] * to_log2 - l2[i]);
+            bool see = l2[i] < INFINITY;
+            if (!inner) {
+              const uint32_t key = base + t * 16 + m;
+              if (key >= sp.before && see) {
+                const uint32_t d = key - sp.before, of = (row0 + r0 + g * 4 + i) / a.group;
+                see = a.tree ? d / 64 < a.tree_words && (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
+                             : d <= of;
+              }
             }
-            sum += see ? p : 0.0f;
+            sum[t] += see ? p : 0.0f;
           }
-        sum = there[b] >> t & 1 ? sum : 0.0f;
-        sum += across(sum, 16);
-        sum += across(sum, 32);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float w = there[b] >> t & 1 ? sum[t] : 0.0f;
+        w += across(w, 16);
+        w += across(w, 32);
         if (!g) {
-          float* to = &sums[wave][base - begin + t * 16 + m];
-          *to = first ? sum : *to + sum;
+          float* to = &sums[base - begin + t * 16 + m];
+          *to = first ? w : *to + w;
         }
       }
     };
-    load(begin, k[0], &there[0]);
-    for (uint32_t base = begin; base < end; base += 2 * kTile) {
-      if (base + kTile < end) load(base + kTile, k[1], &there[1]);
+    uint32_t base = begin + wave * kTile;
+    if (base < end) load(base, k[0], &there[0]);
+    for (; base < end; base += 2 * step) {
+      if (base + step < end) load(base + step, k[1], &there[1]);
       add(base, std::false_type());
-      if (base + kTile >= end) break;
-      if (base + 2 * kTile < end) load(base + 2 * kTile, k[0], &there[0]);
-      add(base + kTile, std::true_type());
+      if (base + step >= end) break;
+      if (base + 2 * step < end) load(base + 2 * step, k[0], &there[0]);
+      add(base + step, std::true_type());
     }
   }
   __syncthreads();
   for (uint32_t i = threadIdx.x; begin + i < end; i += 256) {
     const uint32_t key = begin + i;
-    const uint64_t at = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
-    const float w = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
-    a.scores_out[at] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[at] : 0.0f) + w;
+    const uint64_t to = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
+    a.scores_out[to] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[to] : 0.0f) + sums[i];
   }
 }
 

@@ -456,9 +456,9 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.group = a->q_heads / H;
   k.tree_words = a->tree_words;
   k.scores_stride = a->scores_stride;
-  // Some 2000 workgroups, of 64 to 1024 entries: a workgroup's start is a few loads one after the other.
-  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / 2048;
-  k.score_len = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(up_to(per, 32), 64), 1024));
+  // Some 1000 workgroups, of 128 to 1024 entries: a workgroup's start is a few loads one after the other.
+  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / 1024;
+  k.score_len = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(up_to(per, 128), 128), 1024));
   k.splits = p.splits;
   k.split_len = p.split_len;
   k.wide_q = rows_wide(k.q);
