@@ -625,3 +625,144 @@ def test_nothing_to_do():
     assert mma.mma_kv_attention(c.layout(), layer, c.seqs(), q).shape == (0, 8, 128)
     assert mma.mma_kv_append(c.layout(), layer, c.seqs(), q, q[:, :2], q[:, :2]).shape == (0, 8, 128)
     assert same_bits(layer.cpu(), c.flat[0])
+
+
+# ------------------------------------------------------------------ many rows, long rows, large caches, together
+@pytest.mark.parametrize("layout,cache,dim,tokens,group,lens,counts", [
+    ("piece", BF16, 128, 16, 4, [300, 0, 65], [40, 9, 12]),      # 128 rows of a workgroup
+    ("hnd", F16, 128, 24, 4, [130], [13]),                       # 64 rows
+    ("xpacked", F8, 128, 16, 4, [500, 64, 31], [33, 32, 1]),
+    ("hnd", F8, 80, 16, 4, [260, 700], [20, 34]),
+    ("piece", F8, 64, 16, 2, [520, 3], [70, 33]),
+    ("xpacked", BF16, 256, 16, 2, [150, 33], [30, 50]),
+    ("piece", F8, 256, 5, 3, [99], [40]),
+    ("xpacked", F16, 64, 32, 8, [400], [12]),
+    ("hnd", BF16, 40, 3, 5, [77, 10], [30, 11]),
+])
+def test_attention_many_rows(layout, cache, dim, tokens, group, lens, counts):
+    log(f"attention rows {layout} {cache} dim {dim}")
+    dtype = F16 if cache is F16 else BF16
+    check_attention(Case(layout, cache, lens, counts, dim, 1, group, tokens, dtype), None, True)
+    c = Case(layout, cache, lens, counts, dim, 1, group, tokens, dtype, seed=3)
+    check_attention(c, tree_bits(counts, c.g, empty=True), True)
+
+
+@pytest.mark.parametrize("layout,cache", [("piece", BF16), ("xpacked", F8), ("hnd", F8), ("xpacked", F16)])
+def test_attention_many_rows_over_splits_and_missing_blocks(layout, cache):
+    """Hundreds of tiles, split and joined, with blocks that are not there at the start, inside and at the end."""
+    c = Case(layout, cache, [1500, 0, 700], [20, 17, 3], dim=64, heads=1, group=4, dtype=F16 if cache is F16 else BF16)
+    check_attention(c, None, True)
+    for b in (0, 3, 50, 93):
+        c.table[0, b] = -1
+    c.table[1, :] = -1
+    c.table[2, 43] = c.c.blocks
+    check_attention(c, tree_bits(c.counts, c.g), True)
+
+
+def test_attention_chunk_without_context():
+    """A whole prompt: every row sees its own part of the call's tokens and nothing else."""
+    c = Case("hnd", BF16, [0, 0], [300, 37], dim=64, heads=1, group=1)
+    check_attention(c, None, True)
+
+
+@pytest.mark.parametrize("n,keep", [(20000, 7000), (70000, 30000), (70001, 3)])
+def test_evict_rows_past_the_registers(n, keep):
+    """Rows listed by a launch of their own, and rows that are read anew in each pass, with ties across them."""
+    c = evict_case("hnd", F8, [n, n - 4100], keep, dim=16, heads=1)
+    s = torch.exp(3 * normal(c.g, 2, 1, n))
+    s[1] = torch.randint(0, 3, (1, n), generator=c.g).float()
+    check_evict(c, keep, 1, 2, s)
+
+
+def test_caches_past_32_bits():
+    """Blocks whose bytes lie more than 4 GiB into a layer give what the same blocks give in a small one."""
+    small = Case("hnd", BF16, [200], [3], heads=8)
+    blocks = 80_000  # of 32 KiB, twice: 4.9 GiB
+    layer = torch.empty(2 * blocks * small.c.piece, dtype=BF16, device="cuda")
+    big = mma.kv_layout(1, 16, 8, 128, 2, blocks, 1, LAYOUTS["hnd"])
+    shift = blocks - small.c.blocks
+    lay, flat = small.layout(), small.flat[0].cuda()
+    view = layer.view(2, blocks, -1)
+    view[:, shift:] = flat.view(2, small.c.blocks, -1)
+    far = mma.kv_seqs((small.table + shift).cuda(), torch.tensor(small.lens, dtype=torch.int32).cuda(), small.q_start.cuda(),
+                      max_tokens=3, max_len=small.max_len)
+    near = small.seqs()
+    q = normal(small.g, 3, 32, 128).to(BF16).cuda()
+    for l, x, s in ((lay, flat, near), (big, layer, far)):
+        mma.mma_kv_append(l, x, s, q, q[:, :8], q[:, 8:16])
+    a, b = (mma.mma_kv_attention(l, x, s, q) for l, x, s in ((lay, flat, near), (big, layer, far)))
+    wide = q.repeat(1, 4, 1)
+    c, d = (mma.mma_kv_attention(l, x, s, wide) for l, x, s in ((lay, flat, near), (big, layer, far)))
+    acc, one = torch.tensor([[1, 2]], dtype=torch.int32, device="cuda"), torch.tensor([2], dtype=torch.int32, device="cuda")
+    for l, x, s in ((lay, flat, near), (big, layer, far)):
+        mma.mma_kv_commit(l, [x], s, acc, one)
+    assert same_bits(a.cpu(), b.cpu()) and same_bits(c.cpu(), d.cpu())
+    assert same_bits(view[:, shift:].contiguous().cpu(), flat.view(2, small.c.blocks, -1).cpu())
+    sc = torch.rand(1, 8, small.max_len, device="cuda")
+    dst = small.spare[:2].view(1, 2).cuda()
+    mma.mma_kv_evict(big, layer, far, dst + shift, sc, 20)
+    mma.mma_kv_evict(lay, flat, near, dst, sc, 20)
+    assert same_bits(view[:, shift:].contiguous().cpu(), flat.view(2, small.c.blocks, -1).cpu())
+
+
+def test_all_on_another_stream_and_captured():
+    """A decode step (append, attention with scores, commit, evict) on a stream of its own and in a graph, replayed
+    with other work between the replays, gives the bits of the eager calls."""
+    c = Case("xpacked", F8, [700, 90], [5, 3], heads=2, layers=2)
+    extra = ok.Cache("xpacked", F8, c.c.blocks + 6, 16, 2, 128)
+    c.c, c.flat = extra, to_cache(normal(c.g, 2, 2 * extra.blocks * extra.piece), F8)
+    dst = (torch.arange(6, dtype=torch.int32).view(2, 3) + extra.blocks - 6).cuda()
+    lay, seqs, sc = c.layout(), c.seqs(), c.scales()
+    q = normal(c.g, 8, 8, 128).to(BF16).cuda()
+    k, v = q[:, :2].contiguous(), q[:, 2:4].contiguous()
+    scores = torch.rand(2, 2, c.max_len, generator=c.g).cuda()
+    other = scores.clone()  # the second layer's
+    acc, cnt = torch.tensor([[0, 2, 4], [1, 2, 0]], dtype=torch.int32).cuda(), torch.tensor([3, 2], dtype=torch.int32).cuda()
+    ws = torch.empty(max(mma.kv_attention_workspace(lay, seqs, 8, 8, BF16, True), mma.kv_evict_workspace(lay, seqs)),
+                     dtype=torch.uint8, device="cuda")
+
+    def step(layers, s_out, stream=None):
+        qo = mma.mma_kv_append(lay, layers[0], seqs, q, k, v, **sc, stream=stream)
+        out = mma.mma_kv_attention(lay, layers[0], seqs, qo, scores_in=scores, scores_out=s_out, workspace=ws, **sc, stream=stream)
+        lens = mma.mma_kv_commit(lay, layers, seqs, acc, cnt, scores=[s_out, other], stream=stream)
+        got = mma.mma_kv_evict(lay, layers[1], seqs, dst, s_out, 40, sinks=2, recent=3, workspace=ws, stream=stream)
+        return (out, lens, *got)
+
+    def fresh():
+        return [x.clone().cuda() for x in c.flat], scores.clone()
+
+    layers, s_out = fresh()
+    want = [x.cpu() for x in step(layers, s_out)] + [x.cpu() for x in layers] + [s_out.cpu()]
+    side = torch.cuda.Stream()
+    layers, s_out = fresh()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(layers, s_out, side)
+    side.synchronize()
+    assert all(same_bits(a.cpu(), b) for a, b in zip([*got, *layers, s_out], want))
+    layers, s_out = fresh()
+    keep = [x.clone() for x in layers], s_out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(layers, s_out)
+    for i in range(3):
+        for x, y in zip(layers, keep[0]):
+            x.copy_(y)
+        s_out.copy_(keep[1])
+        ws.random_()
+        (torch.randn(512, 512, device="cuda") @ torch.randn(512, 512, device="cuda")).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(same_bits(a.cpu(), b) for a, b in zip([*got, *layers, s_out], want)), f"replay {i}"
+
+
+@pytest.mark.parametrize("layout,cache", [("hnd", "bf16"), ("xpacked", "f8")])
+def test_example(layout, cache):
+    """The example, in its own process (it initialises the library itself)."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "kv_decode.py"), "--layers", "2", "--prompt", "700", "--keep",
+                        "128", "--steps", "3", "--layout", layout, "--cache", cache], capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "evicted 700 -> 128 entries" in r.stdout and "140 entries, position 712" in r.stdout, r.stdout
