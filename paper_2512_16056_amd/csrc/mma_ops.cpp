@@ -231,15 +231,24 @@ uint64_t up_to(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
 // How an attention call is cut. Rows of one sequence and KV head (a token and a head of
 // the group each) go in tiles of 16; the entries go in splits, joined afterwards, where
 // sequences, heads and rows alone are too few workgroups for 256 CUs.
-AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& q, const mma_kv_attention_t& a) {
+AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const mma_kv_seqs_t& q,
+                        const mma_kv_attention_t& a) {
   AttnPlan p{};
   const uint32_t group = a.q_heads / c.heads;
   const uint64_t tokens = std::min(q.max_tokens, a.num_tokens);
   p.rows = static_cast<uint32_t>(tokens * group);
   p.dim_pad = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-  // Up to two tiles of rows have their keys in registers (one with heads above 128: the second would
-  // not fit them), if a lane's 8 keys share a block.
+  // Up to two tiles of rows have their keys in registers (one with heads above 128: the second would not fit
+  // them), if a lane's 8 keys share a block. 8-bit and x-packed entries are best there throughout (32 rows, 4 trees
+  // over 15k entries, 8 bits: 32 us, through LDS 49; 4 rows, 32 sequences of up to 8k, x-packed: 122 against 151).
+  // Of 16-bit entries with heads of 65 to 128 V costs registers to be turned in, and from 17 rows on LDS is better
+  // (32 rows, 4 x 15k: 52 against 41), with fewer from some thousands of entries on, unless their logits are kept
+  // (4 rows, 4 x 15k: 45 against 38, 64k: 61 against 57; but 6 x 900: 12.1 against 14.2, 64k and scores: 70 against
+  // 92). Below 65 the two are within 5 %, above 128 the registers win (32 x 8k: 248 against 379).
   p.stream = p.rows <= (p.dim_pad == 256 ? 16u : 32u) && c.tokens % 8 == 0;
+  if (p.dim_pad == 128 && layout.elem_bytes == 2 && layout.gpu_layout != MMA_KV_LAYOUT_XPACKED &&
+      (p.rows > 16 || (q.max_len > 4096 && !a.scores_out)))
+    p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
@@ -255,8 +264,9 @@ AttnPlan attention_plan(const CacheArgs& c, uint32_t elem, const mma_kv_seqs_t& 
   const uint64_t units = static_cast<uint64_t>(a.num_tokens) * a.q_heads;
   if (p.splits > 1) p.part_bytes = up_to(units * p.splits * p.dim_pad * 4, 256);
   if (a.scores_out) {
-    // Keeping a row's logit writes and reads 8 bytes an entry; doing its products again reads the entry's key.
-    p.logits = p.stream && p.tiles_per_wave == 1 && 8ull * p.rows <= c.dim * elem / 2;
+    // One tile's logits are kept: 8 bytes a row and entry there and back, against reading the keys again (64k entries:
+    // 4 rows of 16 bits 70 us against 94, 16 rows of 8 bits 61 against 69).
+    p.logits = p.stream && p.tiles_per_wave == 1;
     p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
     if (p.logits)
       p.logit_bytes = up_to(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows * p.logit_stride * 4, 256);
@@ -391,7 +401,7 @@ mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma
   if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
   Call call;
   if (mma_status_t s = check_attention_sizes(layout, seqs, a, &call)) return s;
-  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, layout->elem_bytes, *seqs, *a).bytes : 0;
+  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, *layout, *seqs, *a).bytes : 0;
   return MMA_OK;
 } catch (...) {
   return ops_boundary_error("mma_kv_attention_workspace");
@@ -422,7 +432,7 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
   if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
   if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
-  const AttnPlan p = attention_plan(call.c, layout->elem_bytes, *seqs, *a);
+  const AttnPlan p = attention_plan(call.c, *layout, *seqs, *a);
   if (static_cast<uint64_t>(p.row_groups) * (static_cast<uint64_t>(p.splits) * H * seqs->num_seqs + 7) >= 1ull << 24)
     return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
                 seqs->num_seqs, seqs->max_tokens, H);
@@ -456,8 +466,10 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.group = a->q_heads / H;
   k.tree_words = a->tree_words;
   k.scores_stride = a->scores_stride;
-  // Some 1000 workgroups, of 128 to 1024 entries: a workgroup's start is a few loads one after the other.
-  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / 1024;
+  // Entries of a workgroup, 128 to 1024, its start being a few loads one after the other: the 512 workgroups that run
+  // at once for one sequence, twice as many for several, whose lengths differ (128 rows: one sequence of 64k entries
+  // 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
+  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / (seqs->num_seqs == 1 ? 512 : 1024);
   k.score_len = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(up_to(per, 128), 128), 1024));
   k.splits = p.splits;
   k.split_len = p.split_len;

@@ -766,3 +766,24 @@ def test_example(layout, cache):
                         "128", "--steps", "3", "--layout", layout, "--cache", cache], capture_output=True, text=True, timeout=110)
     assert r.returncode == 0, r.stderr[-2000:]
     assert "evicted 700 -> 128 entries" in r.stdout and "140 entries, position 712" in r.stdout, r.stdout
+
+
+@pytest.mark.parametrize("layout,cache,dim,counts", [("piece", BF16, 128, [1, 2]), ("hnd", F16, 120, [4, 1]), ("xpacked", BF16, 128, [1, 2]),
+                                                     ("hnd", F8, 96, [1, 3])])
+def test_attention_few_rows_over_thousands_of_entries(layout, cache, dim, counts):
+    """With and without the weights of the entries, which take different ways from some length on."""
+    for scores in (False, True):
+        c = Case(layout, cache, [4300, 0 if layout == "hnd" else 70], counts, dim, 1, 4, dtype=F16 if cache is F16 else BF16)
+        c.table[0, 200] = -1
+        check_attention(c, tree_bits(c.counts, c.g), scores)
+
+
+@pytest.mark.parametrize("cache", [BF16, F8])
+def test_attention_kept_logits_of_a_whole_tile(cache):
+    c = Case("piece", cache, [900, 40], [4, 3], heads=2)
+    check_attention(c, tree_bits(c.counts, c.g), True)
+
+
+def test_append_in_one_part_and_in_several():
+    for n in (511, 512):
+        check_append(Case("xpacked", BF16, [3], [n], dim=64, heads=1, group=2), 64, False, True)
