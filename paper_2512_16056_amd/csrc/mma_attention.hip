@@ -17,8 +17,9 @@
 //
 // Two kernels share that arithmetic. attention_stream_kernel, for up to 32 rows, reads keys
 // and values from memory straight into the registers of the instructions; its waves split the
-// entries. attention_rows_kernel, for more rows, brings tiles to LDS once for the
-// workgroup's 128 rows; its waves split the rows.
+// entries. attention_rows_kernel, for more rows and for long 16-bit contexts, brings tiles to
+// LDS once for the workgroup's 64 or 128 rows; its waves split the rows. Which of them takes a
+// call, and in how many splits, is attention_plan's choice (mma_ops.cpp).
 #include "mma_ops.h"
 
 #include <algorithm>
@@ -281,6 +282,10 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uin
 // layout, where 8 tokens of a value are contiguous, as it stands. Blocks hold a multiple of 8
 // tokens here: a lane's keys of a tile and its values' keys are in one block each, whose
 // table entries are read two tiles ahead, keys one tile ahead, values in the tile.
+// Bound by the bytes in flight: its registers let two waves on a SIMD (a bound of three spilled: 223
+// us instead of 123 for 32 sequences of 1k to 8k). 4 rows, one sequence of 64k entries, bf16, heads
+// of 128: 63 us, 4.3 TB/s; the same entries of 8 bits 33 us; 100 entries 7 us, the chain of loads
+// from the length over the table to the entry.
 template <bool F8, int DP, bool VX>
 struct Stream {
   static constexpr int KS = DP / 32;                  // instructions of 32 head values
@@ -368,8 +373,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   typedef Stream<F8, DP, VX> S;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   // Workgroups go to the 8 XCDs in turn: heads and sequences first, so that each XCD has early and late splits alike
-  // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 141 us instead of 120
-  // for 32 sequences of up to 8k).
+  // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 141 us and more
+  // instead of 123 for 32 sequences of 1k to 8k).
   const uint32_t pairs = a.c.heads * a.s.num_seqs, pair = blockIdx.x % pairs, split = blockIdx.x / pairs;
   const uint32_t head = pair % a.c.heads, seq = pair / a.c.heads;
   const SeqSpan sp = span_of(a.s, seq);
@@ -572,6 +577,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 //
 // The maximum that probabilities are taken from follows the row's own only where it would
 // be passed by more than 2^8: the factor is 1 otherwise and nothing is scaled.
+//
+// 2048 tokens of 32 heads behind 6144 entries (8 KV heads, 128 values, bf16): 281 us, 0.85
+// PFLOP/s, where a plain matrix product of the library reaches 1.09. Without the fetches a tile
+// takes 12 % less, without the exponentials the same, without the reads of V 10 %: no one of
+// them bounds it, the chain through a tile of few waves does. 4 trees of 24 tokens over 15k 8-bit
+// x-packed entries: 58 us, as many workgroups as run at once and their widening; 4 rows over 32
+// sequences of 1k to 8k, bf16: 112 us, 5.5 TB/s.
 template <bool F8, int DP, bool VX>
 struct Tiles {
   static constexpr int KT = DP == 256 || (F8 && DP == 128) ? 32 : 64;  // entries of a tile
@@ -1048,7 +1060,8 @@ __device__ __forceinline__ void join_ml(const float* ml, uint32_t n, float* top,
 }
 
 // A row: out = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i over its splits. A workgroup has one
-// row; DP / 4 lanes read a split, and 1024 / DP splits are read at once.
+// row; DP / 4 lanes read a split, and 1024 / DP splits are read at once. 6 us for 32 rows of 64
+// splits and the weights of 64k entries: a launch and two dependent reads.
 template <class T, int DP>
 __device__ __forceinline__ void join_row(const AttnArgs& a, const SeqSpan& sp, uint32_t row, uint32_t head, f32x4* lds) {
   constexpr uint32_t L = DP / 4, W = 256 / L;
@@ -1127,16 +1140,24 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
 
 // ---------------------------------------------------------------- weights of the entries, many rows
 // With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
-// lane adds up its key's rows. A workgroup has up to kScored keys (score_len) and 128 rows at a time (64 with heads above 128),
-// in LDS with their lse; its waves take the keys, 32 at a time, in turn, the next ones on their way: what bounds it is how
-// many different keys are on their way at once. Each score has one writer and its sum one order.
+// lane adds up its key's rows. Rows come to LDS with their lse. Each score has one writer and its
+// sum one order.
+//
+// Up to some hundred rows a workgroup has up to kScored keys (score_len) and brings kRows rows at
+// a time; its waves take the keys, 32 at a time, in turn, the next ones on their way: what bounds
+// it is how many different keys are on their way at once. With more rows (STAY) a wave's 32 keys
+// stay in its registers and the rows pass by in two buffers, the next ones on their way to
+// registers: bound by the exponentials and LDS, about 300 us for 8192 rows and 8192 entries of
+// 8 KV heads.
 constexpr uint32_t kScored = 1024;
 
-template <class T, bool F8, int DP>
+template <class T, bool F8, int DP, bool STAY>
 __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
-  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, C = DP / 8, kRows = DP == 256 ? 64 : 128;
-  __shared__ __attribute__((aligned(16))) uint8_t ql[kRows * C * 16];
-  __shared__ float sums[kScored], ll[kRows];
+  constexpr int KS = DP / 32, NK = F8 ? KS / 2 : KS, C = DP / 8, kRows = STAY || DP == 256 ? 64 : 128;
+  constexpr int kChunks = kRows * C / 256;  // 16-byte chunks of the rows that a thread brings
+  __shared__ __attribute__((aligned(16))) uint8_t ql[(STAY ? 2 : 1) * kRows * C * 16];
+  __shared__ __attribute__((aligned(16))) float ll[(STAY ? 2 : 1) * kRows];
+  __shared__ float sums[kScored];
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
@@ -1149,7 +1170,9 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
   // lse2 has a sequence's and KV head's rows side by side.
   const float* l2_at = a.lse2 + (static_cast<uint64_t>(head) * a.s.num_tokens + sp.first) * a.group;
   // 16 bytes of a row in LDS: chunks exchanged by the row's number, so that 16 rows' do not meet in a bank.
-  const auto at = [&](uint32_t row, uint32_t chunk) { return (row * C + (chunk ^ (C == 8 ? row >> 1 & 7 : row & 15))) * 16; };
+  const auto at = [&](uint32_t row, uint32_t chunk) {
+    return (row * C + (chunk ^ (C == 8 ? row >> 1 & 7 : row & 15))) * 16;
+  };
   const auto load = [&](uint32_t base, u32x4 (&k)[2][NK], uint32_t* there) {
     uint32_t have = 0;
 #pragma unroll
@@ -1158,7 +1181,8 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
       const uint32_t key = base + t * 16 + m;
       const int32_t id = block_at(a.c, table, key < end ? key : end - 1, &in_block);
       have |= (key < end && id >= 0 ? 1u : 0u) << t;
-      const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head + in_block * a.c.k_token;
+      const uint8_t* p = a.c.k + static_cast<uint64_t>(id < 0 ? 0 : id) * a.c.block_bytes + head * a.c.k_head +
+                         in_block * a.c.k_token;
 #pragma unroll
       for (int s = 0; s < NK; ++s) {
         const uint32_t chunk = s * 4 + g;
@@ -1167,85 +1191,150 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
     }
     *there = have;
   };
-  // Rows of tokens before the first key's do not see these keys.
-  const uint32_t start = !a.tree && begin > sp.before ? (begin - sp.before) * a.group / 16 * 16 : 0;
-  const uint32_t step = 4 * kTile;
-  bool first = true;
-  for (uint32_t row0 = start; row0 < rows || first; row0 += kRows, first = false) {
-    if (!first) __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kRows * C; i += 256) {
-      const uint32_t r = i / C, chunk = i % C, row = row0 + r, d = chunk * 8;
-      u32x4 w = {0, 0, 0, 0};
-      if (row < rows && d < a.c.dim)
-        w = load_row8(a.q.data + 2 * ((sp.first + row / a.group) * a.q.token + (head * a.group + row % a.group) * a.q.head + d), a.wide_q);
-      *reinterpret_cast<u32x4*>(ql + at(r, chunk)) = w;
-    }
-    for (uint32_t i = threadIdx.x; i < kRows; i += 256) {
-      const float l = row0 + i < rows ? l2_at[row0 + i] : INFINITY;
-      ll[i] = l == -INFINITY ? INFINITY : l;  // a row that sees nothing
-    }
-    __syncthreads();
-    const uint32_t some = row0 < rows ? (rows - row0 < kRows ? rows - row0 : kRows) : 0;
-    u32x4 k[2][2][NK];
-    uint32_t there[2];
-    const auto add = [&](uint32_t base, auto b) {
-      u32x4 kw[2][KS];
+  const auto operands = [&](const u32x4 (&k)[2][NK], u32x4 (&kw)[2][KS]) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          const bool live = F8 ? ((i / 2) * 4 + g) * 16 < a.c.dim : (i * 4 + g) * 8 < a.c.dim;
-          if constexpr (F8) kw[t][i] = widen<T>(k[b][t][i / 2][i % 2 * 2], k[b][t][i / 2][i % 2 * 2 + 1]);
-          else kw[t][i] = k[b][t][i];
-          if (a.c.dim < DP && !live) kw[t][i] = u32x4{0, 0, 0, 0};
-        }
-      const bool inner = base + kTile <= sp.before;
-      float sum[2] = {0, 0};
+      for (int i = 0; i < KS; ++i) {
+        const bool live = F8 ? ((i / 2) * 4 + g) * 16 < a.c.dim : (i * 4 + g) * 8 < a.c.dim;
+        if constexpr (F8) kw[t][i] = widen<T>(k[t][i / 2][i % 2 * 2], k[t][i / 2][i % 2 * 2 + 1]);
+        else kw[t][i] = k[t][i];
+        if (a.c.dim < DP && !live) kw[t][i] = u32x4{0, 0, 0, 0};
+      }
+  };
+  const auto row_chunk = [&](uint32_t row0, uint32_t i) {
+    const uint32_t row = row0 + i / C, d = i % C * 8;
+    u32x4 w = {0, 0, 0, 0};
+    if (row < rows && d < a.c.dim)
+      w = load_row8(a.q.data + 2 * ((sp.first + row / a.group) * a.q.token + (head * a.group + row % a.group) * a.q.head + d),
+                    a.wide_q);
+    return w;
+  };
+  const auto row_lse = [&](uint32_t row) {
+    const float l = row < rows ? l2_at[row] : INFINITY;
+    return l == -INFINITY ? INFINITY : l;  // a row that sees nothing
+  };
+  // Adds to a lane's two keys' sums what `some` rows from row0 on, in LDS at q_at and l_at, give them. A loop of its own
+  // for keys that every row sees, for drafted ones of a chain, seen from row `from` on, and for those of a tree.
+  const auto weigh = [&](uint32_t base, const u32x4 (&kw)[2][KS], const uint8_t* q_at, const float* l_at, uint32_t row0,
+                         uint32_t some, float (&sum)[2]) {
+    const auto run = [&](auto mode) {
+      constexpr int kMode = decltype(mode)::value;
+      uint32_t from[2], draft[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t key = base + t * 16 + m;
+        draft[t] = key < sp.before ? 0 : key - sp.before;
+        from[t] = draft[t] * a.group;
+      }
       for (uint32_t r0 = 0; r0 < some; r0 += 16) {
         f32x4 x[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
-          const u32x4 q = *reinterpret_cast<const u32x4*>(ql + at(r0 + m, F8 ? i / 2 * 8 + g * 2 + i % 2 : i * 4 + g));
+          const u32x4 q = *reinterpret_cast<const u32x4*>(q_at + at(r0 + m, F8 ? i / 2 * 8 + g * 2 + i % 2 : i * 4 + g));
           x[0] = Type<T>::mfma(q, kw[0][i], x[0]);
           x[1] = Type<T>::mfma(q, kw[1][i], x[1]);
         }
-        const f32x4 l2 = *reinterpret_cast<const f32x4*>(ll + r0 + g * 4);
+        const f32x4 l2 = *reinterpret_cast<const f32x4*>(l_at + r0 + g * 4);
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float p = __builtin_amdgcn_exp2f(x[t][i] * to_log2 - l2[i]);
+            const uint32_t row = row0 + r0 + g * 4 + i;
             bool see = l2[i] < INFINITY;
-            if (!inner) {
-              const uint32_t key = base + t * 16 + m;
-              if (key >= sp.before && see) {
-                const uint32_t d = key - sp.before, of = (row0 + r0 + g * 4 + i) / a.group;
-                see = a.tree ? d / 64 < a.tree_words && (a.tree[static_cast<uint64_t>(sp.first + of) * a.tree_words + d / 64] >> (d % 64) & 1)
-                             : d <= of;
+            if constexpr (kMode == 1) see = see && row >= from[t];
+            if constexpr (kMode == 2)
+              if (see && base + t * 16 + m >= sp.before) {
+                const uint32_t d = draft[t];
+                see = d / 64 < a.tree_words &&
+                      (a.tree[static_cast<uint64_t>(sp.first + row / a.group) * a.tree_words + d / 64] >> (d % 64) & 1);
               }
-            }
             sum[t] += see ? p : 0.0f;
           }
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float w = there[b] >> t & 1 ? sum[t] : 0.0f;
-        w += across(w, 16);
-        w += across(w, 32);
-        if (!g) {
-          float* to = &sums[base - begin + t * 16 + m];
-          *to = first ? w : *to + w;
-        }
-      }
     };
-    uint32_t base = begin + wave * kTile;
-    if (base < end) load(base, k[0], &there[0]);
-    for (; base < end; base += 2 * step) {
-      if (base + step < end) load(base + step, k[1], &there[1]);
-      add(base, std::false_type());
-      if (base + step >= end) break;
-      if (base + 2 * step < end) load(base + 2 * step, k[0], &there[0]);
-      add(base + step, std::true_type());
+    if (base + kTile <= sp.before)
+      run(std::integral_constant<int, 0>());
+    else if (!a.tree)
+      run(std::integral_constant<int, 1>());
+    else
+      run(std::integral_constant<int, 2>());
+  };
+  // A key's rows are in the lanes 16 apart.
+  const auto joined = [&](const float (&sum)[2], uint32_t there, int t) {
+    float w = there >> t & 1 ? sum[t] : 0.0f;
+    w += across(w, 16);
+    return w + across(w, 32);
+  };
+  // Rows of tokens before the first key's do not see these keys.
+  const uint32_t start = !a.tree && begin > sp.before ? (begin - sp.before) * a.group / 16 * 16 : 0;
+  if constexpr (STAY) {
+    const uint32_t base = begin + wave * kTile;
+    u32x4 k[2][NK], kw[2][KS], next[kChunks];
+    uint32_t there = 0;
+    float next_lse = 0, sum[2] = {0, 0};
+    const auto fetch = [&](uint32_t row0) {
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) next[i] = row_chunk(row0, i * 256 + threadIdx.x);
+      if (threadIdx.x < kRows) next_lse = row_lse(row0 + threadIdx.x);
+    };
+    if (start < rows) fetch(start);
+    load(base, k, &there);
+    operands(k, kw);
+    uint32_t b = 0;
+    for (uint32_t row0 = start; row0 < rows; row0 += kRows, b ^= 1) {
+      uint8_t* q_at = ql + b * kRows * C * 16;
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        const uint32_t n = i * 256 + threadIdx.x;
+        *reinterpret_cast<u32x4*>(q_at + at(n / C, n % C)) = next[i];
+      }
+      if (threadIdx.x < kRows) ll[b * kRows + threadIdx.x] = next_lse;
+      __syncthreads();
+      if (row0 + kRows < rows) fetch(row0 + kRows);
+      if (base < end) weigh(base, kw, q_at, ll + b * kRows, row0, rows - row0 < kRows ? rows - row0 : kRows, sum);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float w = joined(sum, there, t);
+      if (!g) sums[wave * kTile + t * 16 + m] = w;
+    }
+  } else {
+    const uint32_t step = 4 * kTile;
+    bool first = true;
+    for (uint32_t row0 = start; row0 < rows || first; row0 += kRows, first = false) {
+      if (!first) __syncthreads();
+      for (uint32_t i = threadIdx.x; i < kRows * C; i += 256)
+        *reinterpret_cast<u32x4*>(ql + at(i / C, i % C)) = row_chunk(row0, i);
+      for (uint32_t i = threadIdx.x; i < kRows; i += 256) ll[i] = row_lse(row0 + i);
+      __syncthreads();
+      const uint32_t some = row0 < rows ? (rows - row0 < kRows ? rows - row0 : kRows) : 0;
+      u32x4 k[2][2][NK];
+      uint32_t there[2];
+      const auto add = [&](uint32_t base, auto b) {
+        u32x4 kw[2][KS];
+        float sum[2] = {0, 0};
+        operands(k[b], kw);
+        weigh(base, kw, ql, ll, row0, some, sum);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const float w = joined(sum, there[b], t);
+          if (!g) {
+            float* to = &sums[base - begin + t * 16 + m];
+            *to = first ? w : *to + w;
+          }
+        }
+      };
+      uint32_t base = begin + wave * kTile;
+      if (base < end) load(base, k[0], &there[0]);
+      for (; base < end; base += 2 * step) {
+        if (base + step < end) load(base + step, k[1], &there[1]);
+        add(base, std::false_type());
+        if (base + step >= end) break;
+        if (base + 2 * step < end) load(base + 2 * step, k[0], &there[0]);
+        add(base + step, std::true_type());
+      }
     }
   }
   __syncthreads();
@@ -1281,8 +1370,11 @@ hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.lse2) {
-    attention_scores_kernel<T, F8, DP>
-        <<<dim3((a.s.max_len + a.score_len - 1) / a.score_len, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
+    const dim3 grid((a.s.max_len + a.score_len - 1) / a.score_len, a.c.heads, a.s.num_seqs);
+    if (p.keys_stay)
+      attention_scores_kernel<T, F8, DP, true><<<grid, 256, 0, stream>>>(a);
+    else
+      attention_scores_kernel<T, F8, DP, false><<<grid, 256, 0, stream>>>(a);
     e = hipGetLastError();
   }
   return e;

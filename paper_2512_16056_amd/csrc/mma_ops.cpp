@@ -130,7 +130,8 @@ mma_status_t check_layout(const mma_kv_layout_t* lay, Call* call) {
   c.tokens = B;
   c.heads = H;
   c.dim = D;
-  // entry / B for entries below 2^31: with 2^(s-1) < B <= 2^s, m = 2^(31+s) / B + 1 errs by at most B / 2^(31+s) <= 2^-31 per entry.
+  // entry / B for entries below 2^31: with 2^(s-1) < B <= 2^s, m = 2^(31+s) / B + 1 errs by at most
+  // B / 2^(31+s) <= 2^-31 per entry.
   uint32_t s = 0;
   while ((1ull << s) < B) ++s;
   c.div_mul = static_cast<uint32_t>((1ull << (31 + s)) / B + 1);
@@ -254,10 +255,11 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
   // Workgroups in all: the 512 that run at once, so that all end together; but 2048 where many sequences, likely of
-  // different lengths, would leave some of those idle (32 of 1k to 8k: 124 us against 138). Entries of a split: 256 at least.
+  // different lengths, would leave some of those idle (32 of 1k to 8k: 124 us against 138). Entries of a split: 256 at
+  // least (4 rows over 1000 or 4096 entries: 128 the same, 512 14.3 and 15.2 us against 12.0 and 12.5).
   const bool many = p.stream && static_cast<uint64_t>(q.num_seqs) * c.heads >= 64;
   const uint64_t want = many ? 2048 : 512, least = 256;
-  uint64_t splits = wgs >= want ? 1 : (want + wgs - 1) / std::max<uint64_t>(wgs, 1);
+  uint64_t splits = wgs >= want ? 1 : up(want, std::max<uint64_t>(wgs, 1));
   splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, up(q.max_len, least)));
   p.split_len = up(up(q.max_len, static_cast<uint32_t>(splits)), 128) * 128;
   p.splits = up(q.max_len, p.split_len);
@@ -267,6 +269,10 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
     // One tile's logits are kept: 8 bytes a row and entry there and back, against reading the keys again (64k entries:
     // 4 rows of 16 bits 70 us against 94, 16 rows of 8 bits 61 against 69).
     p.logits = p.stream && p.tiles_per_wave == 1;
+    // Scores of many rows: keys stay in registers from 257 rows on (8192 rows over 8k entries, with the attention, 588 us
+    // against 758), of several sequences from 65 on (192 rows, 4 x 15k: 173 against 190); 128 rows over one sequence
+    // of 64k take 147 so and 136 with the rows staying.
+    p.keys_stay = p.rows > (q.num_seqs > 1 ? 64u : 256u);
     p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
     if (p.logits)
       p.logit_bytes = up_to(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows * p.logit_stride * 4, 256);
@@ -466,11 +472,11 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.group = a->q_heads / H;
   k.tree_words = a->tree_words;
   k.scores_stride = a->scores_stride;
-  // Entries of a workgroup, 128 to 1024, its start being a few loads one after the other: the 512 workgroups that run
-  // at once for one sequence, twice as many for several, whose lengths differ (128 rows: one sequence of 64k entries
-  // 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
+  // Entries of a workgroup: 32 for each of its waves where these stay, else 128 to 1024, its start being a few loads one
+  // after the other: the 512 workgroups that run at once for one sequence, twice as many for several, whose lengths
+  // differ (128 rows over 64k entries 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
   const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / (seqs->num_seqs == 1 ? 512 : 1024);
-  k.score_len = static_cast<uint32_t>(std::min<uint64_t>(std::max<uint64_t>(up_to(per, 128), 128), 1024));
+  k.score_len = p.keys_stay ? 128 : static_cast<uint32_t>(std::clamp<uint64_t>(up_to(per, 128), 128, 1024));
   k.splits = p.splits;
   k.split_len = p.split_len;
   k.wide_q = rows_wide(k.q);

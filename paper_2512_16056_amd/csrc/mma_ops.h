@@ -121,6 +121,7 @@ struct AttnPlan {
   uint32_t splits, split_len;
   uint32_t dim_pad;
   bool logits;              // scores from logits that the main kernel keeps
+  bool keys_stay;           // else: attention_scores_kernel keeps a wave's keys, or the rows
   uint32_t logit_stride;
   uint64_t part_bytes, ml_bytes, lse_bytes, logit_bytes, bytes;
 };

@@ -787,3 +787,12 @@ def test_attention_kept_logits_of_a_whole_tile(cache):
 def test_append_in_one_part_and_in_several():
     for n in (511, 512):
         check_append(Case("xpacked", BF16, [3], [n], dim=64, heads=1, group=2), 64, False, True)
+
+
+@pytest.mark.parametrize("layout,cache,dim,lens,counts", [("piece", BF16, 128, [200], [90]), ("hnd", F8, 80, [70, 0], [70, 40]),
+                                                          ("xpacked", F16, 256, [130], [70]), ("xpacked", F8, 64, [300, 5], [20, 90])])
+def test_attention_scores_of_hundreds_of_rows(layout, cache, dim, lens, counts):
+    for tree in (False, True):
+        c = Case(layout, cache, lens, counts, dim, 2, 4, dtype=F16 if cache is F16 else BF16)
+        c.table[0, 2] = -1
+        check_attention(c, tree_bits(c.counts, c.g, empty=True) if tree else None, True)
