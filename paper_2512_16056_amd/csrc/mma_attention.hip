@@ -222,7 +222,8 @@ __device__ __forceinline__ uint64_t lse2_at(const AttnArgs& a, uint32_t token, u
 }
 
 // What a row's result goes to: the output and lse, or with several splits this split's part of them.
-// SIDE: a lane's 4 sums of an instruction are neighbours (value 16 c + 4 g); else the sums of CE instructions are, for each of the 4.
+// SIDE: a lane's 4 sums of an instruction are neighbours (value 16 c + 4 g); else the sums of CE instructions are, for
+// each of the 4.
 template <class T, int DP, int NC, int SIDE>
 __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uint32_t qh, uint32_t split, uint32_t g, float top,
                                           float sum, float v_scale, const f32x4 (&o)[NC]) {
@@ -501,7 +502,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
       add_values<T>(op, p, o);
     base += step;
   };
-  // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not there), masked ones.
+  // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not
+  // there), masked ones.
   uint32_t whole = a.tree ? sp.before : sp.before + row0 / a.group + 1;
   if (whole > end) whole = end;
   bool have = there(vid);
