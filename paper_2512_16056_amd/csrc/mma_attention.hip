@@ -1140,6 +1140,16 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
     if (key + j < sp.total) a.scores_out[at + j] = (a.scores_in && key + j < sp.before ? a.decay * a.scores_in[at + j] : 0.0f) + w[j];
 }
 
+// The queries kept for the weights where the output is written over them: 8 values a thread.
+__global__ __launch_bounds__(256) void attention_keep_queries_kernel(AttnArgs a) {
+  const uint32_t chunks = a.c.dim / 8;
+  const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x, row = i / chunks;
+  if (row >= static_cast<uint64_t>(a.s.num_tokens) * a.q_heads) return;
+  const uint64_t token = row / a.q_heads, head = row % a.q_heads, d = i % chunks * 8;
+  const u32x4 w = load_row8(a.q.data + 2 * (token * a.q.token + head * a.q.head + d), a.wide_q);
+  *reinterpret_cast<u32x4*>(a.score_q.data + 2 * (token * a.score_q.token + head * a.score_q.head + d)) = w;
+}
+
 // ---------------------------------------------------------------- weights of the entries, many rows
 // With every row's sum known, Q K^T once more, this time rows down and keys across, so that a
 // lane adds up its key's rows. Rows come to LDS with their lse. Each score has one writer and its
@@ -1208,8 +1218,8 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
     const uint32_t row = row0 + i / C, d = i % C * 8;
     u32x4 w = {0, 0, 0, 0};
     if (row < rows && d < a.c.dim)
-      w = load_row8(a.q.data + 2 * ((sp.first + row / a.group) * a.q.token + (head * a.group + row % a.group) * a.q.head + d),
-                    a.wide_q);
+      w = load_row8(a.score_q.data + 2 * ((sp.first + row / a.group) * a.score_q.token +
+                                          (head * a.group + row % a.group) * a.score_q.head + d), a.wide_score_q);
     return w;
   };
   const auto row_lse = [&](uint32_t row) {
@@ -1350,6 +1360,11 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
 template <class T, bool F8, int DP, bool VX>
 hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   const uint32_t cells = p.splits * a.c.heads * a.s.num_seqs;
+  if (a.score_q.data != a.q.data) {
+    const uint64_t chunks = static_cast<uint64_t>(a.s.num_tokens) * a.q_heads * (a.c.dim / 8);
+    attention_keep_queries_kernel<<<static_cast<uint32_t>((chunks + 255) / 256), 256, 0, stream>>>(a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   if (p.stream) {
     if (p.tiles_per_wave == 1) {
       attention_stream_kernel<T, F8, DP, VX, 1><<<cells, 256, 0, stream>>>(a);

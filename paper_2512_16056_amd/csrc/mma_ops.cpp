@@ -99,6 +99,12 @@ mma_status_t rows(Call* call, const char* what, const mma_rows_t& r, uint32_t to
   return MMA_OK;
 }
 
+// Whether the memory from the first to the last value of two [tokens][heads][dim] rows meets.
+bool rows_meet(const RowArgs& x, const RowArgs& y, uint32_t tokens, uint32_t heads, uint32_t dim) {
+  const auto end = [&](const RowArgs& r) { return r.data + 2 * ((tokens - 1) * r.token + (heads - 1) * r.head + dim); };
+  return x.data < end(y) && y.data < end(x);
+}
+
 bool rows_wide(const RowArgs& r) { return aligned(r.data, 16) && r.token % 8 == 0 && r.head % 8 == 0; }
 
 mma_status_t check_types(uint32_t type, uint32_t cache_type, uint32_t elem_bytes) {
@@ -276,11 +282,13 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
     p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
     if (p.logits)
       p.logit_bytes = up_to(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows * p.logit_stride * 4, 256);
-    else
+    else {
       p.lse_bytes = up_to(units * 4, 256);
+      p.q_bytes = up_to(units * c.dim * 2, 256);  // of queries that `out` replaces before the weights are formed
+    }
   }
   if (p.splits > 1 || p.logits) p.ml_bytes = up_to(units * p.splits * 8, 256);
-  p.bytes = p.part_bytes + p.ml_bytes + p.lse_bytes + p.logit_bytes;
+  p.bytes = p.part_bytes + p.ml_bytes + p.lse_bytes + p.q_bytes + p.logit_bytes;
   return p;
 }
 
@@ -465,6 +473,9 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.part = take(p.part_bytes);
   k.part_ml = take(p.ml_bytes);
   k.lse2 = take(p.lse_bytes);
+  k.score_q = k.q;
+  if (float* copy = take(p.q_bytes); copy && rows_meet(k.q, k.out, n, a->q_heads, D))
+    k.score_q = RowArgs{reinterpret_cast<uint8_t*>(copy), static_cast<uint64_t>(a->q_heads) * D, D};
   k.logits = take(p.logit_bytes);
   k.logit_rows = p.rows;
   k.logit_stride = p.logit_stride;
@@ -481,6 +492,7 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.split_len = p.split_len;
   k.wide_q = rows_wide(k.q);
   k.wide_out = rows_wide(k.out);
+  k.wide_score_q = rows_wide(k.score_q);
   k.scale = a->scale;
   k.decay = a->decay;
   return launched(launch_attention(k, p, {a->type, a->cache_type, layout->gpu_layout}, static_cast<hipStream_t>(stream)),

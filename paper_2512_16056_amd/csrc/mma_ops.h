@@ -64,6 +64,7 @@ struct AttnArgs {
   CacheArgs c;
   SeqArgs s;
   RowArgs q, out;
+  RowArgs score_q;  // the queries as the weights kernel reads them: q, or its copy where `out` takes q's place
   const uint64_t* tree;
   float* lse;
   const float* scores_in;
@@ -78,7 +79,7 @@ struct AttnArgs {
   uint32_t q_heads, group, tree_words, scores_stride;
   uint32_t score_len;          // entries of a workgroup of the scores kernel: a multiple of 32, at most 1024
   uint32_t splits, split_len;  // entries of a split: a multiple of the tile
-  uint32_t wide_q, wide_out;   // rows start at 16 bytes
+  uint32_t wide_q, wide_out, wide_score_q;  // rows start at 16 bytes
   float scale, decay;
 };
 
@@ -123,7 +124,7 @@ struct AttnPlan {
   bool logits;              // scores from logits that the main kernel keeps
   bool keys_stay;           // else: attention_scores_kernel keeps a wave's keys, or the rows
   uint32_t logit_stride;
-  uint64_t part_bytes, ml_bytes, lse_bytes, logit_bytes, bytes;
+  uint64_t part_bytes, ml_bytes, lse_bytes, q_bytes, logit_bytes, bytes;
 };
 
 hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stream);

@@ -796,3 +796,30 @@ def test_attention_scores_of_hundreds_of_rows(layout, cache, dim, lens, counts):
         c = Case(layout, cache, lens, counts, dim, 2, 4, dtype=F16 if cache is F16 else BF16)
         c.table[0, 2] = -1
         check_attention(c, tree_bits(c.counts, c.g, empty=True) if tree else None, True)
+
+
+def odd_rows(x):
+    """The rows of x at any 2 bytes, heads outermost."""
+    n, h, d = x.shape
+    view = torch.zeros(h, n, d + 3, dtype=x.dtype, device="cuda")[:, :, 1: 1 + d].permute(1, 0, 2)
+    view.copy_(x)
+    return view
+
+
+@pytest.mark.parametrize("layout,cache,dim,tokens,group,lens,counts", [
+    ("piece", F8, 128, 16, 4, [300], [6]),           # 24 rows, entries from memory to registers
+    ("piece", BF16, 128, 16, 4, [300, 40], [6, 5]),  # 24 rows through LDS
+    ("hnd", F16, 64, 5, 4, [90], [3]),               # blocks of any number of tokens
+    ("piece", BF16, 64, 16, 4, [40], [40]),          # 160 rows, one split
+    ("xpacked", F8, 64, 16, 2, [1500], [70]),        # 140 rows, several splits
+    ("hnd", BF16, 128, 16, 4, [60], [70]),           # 280 rows, past those whose keys stay
+    ("hnd", BF16, 256, 16, 2, [600, 9], [20, 40]),
+])
+def test_attention_in_place_with_scores(layout, cache, dim, tokens, group, lens, counts):
+    """The weights of the entries are the queries' though the output takes their place."""
+    dtype = F16 if cache is F16 else BF16
+    for view in (None, odd_rows):
+        c = Case(layout, cache, lens, counts, dim, 2, group, tokens, dtype)
+        check_attention(c, tree_bits(counts, c.g), True, q_view=view, in_place=True)
+        c = Case(layout, cache, lens, counts, dim, 2, group, tokens, dtype)
+        check_attention(c, None, True, q_view=view, in_place=True)
