@@ -569,7 +569,7 @@ typedef struct mma_kv_commit {
 /* Entry lens[s] + accepted[s][i] moves to lens[s] + i, in place, for i < counts[s]: K and V
  * of every layer, and its scores. A list ends where an index is negative, not above the
  * one before, or not below the sequence's tokens in the call, and counts past
- * accepted_stride end there; lens_out counts what was moved. gpu_layers: num_layers device pointers, copied before return. */
+ * accepted_stride (which may be 0) end there; lens_out counts what was moved. gpu_layers: num_layers device pointers, copied before return. */
 mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_seqs_t* seqs,
                            const mma_kv_commit_t* args, void* stream);
 

@@ -512,10 +512,10 @@ mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layer
   if (a->scores && a->scores_stride < seqs->max_len)
     return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
   if (a->lens_out && a->lens_out == seqs->lens) return fail(MMA_ERR_INVALID_ARG, "lens_out is seqs->lens");
-  if (!seqs->num_seqs || !a->accepted_stride) return MMA_OK;
+  if (!seqs->num_seqs || (!a->accepted_stride && !a->lens_out)) return MMA_OK;  // lists of no places still give lens_out
   Device dev(call.device);
   if ((s = check_seqs(seqs, layout->block_tokens, INT32_MAX, &call))) return s;
-  if ((s = array(&call, "accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4), 4))) return s;
+  if ((s = array(&call, "accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4), 4, !a->accepted_stride))) return s;
   if ((s = array(&call, "counts", a->counts, 4ull * seqs->num_seqs, 4))) return s;
   if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads, a->scores_stride, 4);

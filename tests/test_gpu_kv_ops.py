@@ -823,3 +823,17 @@ def test_attention_in_place_with_scores(layout, cache, dim, tokens, group, lens,
         check_attention(c, tree_bits(counts, c.g), True, q_view=view, in_place=True)
         c = Case(layout, cache, lens, counts, dim, 2, group, tokens, dtype)
         check_attention(c, None, True, q_view=view, in_place=True)
+
+
+@pytest.mark.parametrize("layers", [1, 200])
+def test_commit_of_empty_lists(layers):
+    """Lists without places: nothing moves, and the new lengths are the old ones."""
+    c = Case("piece", BF16, [7, 0, 30, -4], [3, 2, 5, 0], 16, 2, 1, 8, layers=1)
+    layer, scores = c.flat[0].cuda(), torch.rand(4, 2, c.max_len).cuda()
+    none, counts = torch.zeros(4, 0, dtype=torch.int32).cuda(), torch.tensor([0, 5, -1, 2], dtype=torch.int32).cuda()
+    lay = mma.kv_layout(layers, 8, 2, 16, 2, c.c.blocks, 1, 0)
+    torch.full((4,), 77, dtype=torch.int32, device="cuda")  # what the new lengths' memory may hold
+    want = scores.clone()
+    got = mma.mma_kv_commit(lay, [layer] * layers, c.seqs(), none, counts, scores=[scores] * layers)
+    assert got.tolist() == [7, 0, 30, 0]
+    assert same_bits(layer.cpu(), c.flat[0]) and torch.equal(scores, want)
