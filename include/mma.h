@@ -547,7 +547,8 @@ typedef struct mma_kv_attention {
  * not see, infinities and NaN among it, does not reach the row.
  * scores_out[s][h][j] = decay * scores_in[s][h][j], for j < lens[s], plus the p of entry
  * j summed over the call's tokens and the heads of KV head h; for the entries that the
- * sequence has, the call's tokens included, and unwritten past them. */
+ * sequence has, the call's tokens included, and unwritten past them. A call without tokens
+ * (num_tokens or max_tokens 0) does this too, and reads and writes nothing else. */
 mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
                               const mma_kv_attention_t* args, void* stream);
 

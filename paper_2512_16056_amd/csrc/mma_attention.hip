@@ -1101,8 +1101,8 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const SeqSpan& sp, u
 
 constexpr uint32_t kWeigh = 1024;  // entries of a workgroup that adds up kept logits
 
-// Rows of the call first (`joins` of them), then, where logits were kept, the weights of the entries:
-// scores_out = decay scores_in + sum over the rows of 2^(logit - lse).
+// Rows of the call first (`joins` of them), then, where logits were kept or the call has no rows, the weights of the
+// entries: scores_out = decay scores_in + sum over the rows of 2^(logit - lse).
 template <class T, int DP>
 __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint32_t joins) {
   __shared__ f32x4 lds[256];
@@ -1116,7 +1116,7 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
   const uint32_t first = (blockIdx.x - joins) * kWeigh;
   if (first >= sp.total) return;
   float* l2 = reinterpret_cast<float*>(lds);  // of the rows: at most 16
-  const uint32_t n = splits_of(a, sp.total);
+  const uint32_t n = rows ? splits_of(a, sp.total) : 0;
   for (uint32_t r = threadIdx.x / kOpsWave; r < rows; r += 4) {
     const uint64_t unit = static_cast<uint64_t>(sp.first + r / a.group) * a.q_heads + head * a.group + r % a.group;
     float top, sum;
@@ -1364,6 +1364,11 @@ hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
     const uint64_t chunks = static_cast<uint64_t>(a.s.num_tokens) * a.q_heads * (a.c.dim / 8);
     attention_keep_queries_kernel<<<static_cast<uint32_t>((chunks + 255) / 256), 256, 0, stream>>>(a);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (!p.rows) {  // the weights fade, that is all
+    const dim3 grid((a.s.max_len + kWeigh - 1) / kWeigh, a.c.heads, a.s.num_seqs);
+    attention_finish_kernel<T, DP><<<grid, 256, 0, stream>>>(a, 0);
+    return hipGetLastError();
   }
   if (p.stream) {
     if (p.tiles_per_wave == 1) {

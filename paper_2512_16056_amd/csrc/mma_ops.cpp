@@ -432,18 +432,28 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   if (a->scores_in && !a->scores_out) return fail(MMA_ERR_INVALID_ARG, "scores_in without scores_out");
   if (a->scores_out && a->scores_stride < seqs->max_len)
     return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
-  if (!n || !seqs->num_seqs || !seqs->max_tokens) return MMA_OK;
+  const bool rows_too = n && seqs->max_tokens;  // else the entries' weights fade and no more
+  if (!seqs->num_seqs || (!rows_too && !a->scores_out)) return MMA_OK;
   Device dev(call.device);
-  if ((s = check_layer(layer, &call))) return s;
+  if (rows_too && (s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
   AttnArgs k{};
+  const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
+  if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
+  k.c = call.c;
+  k.s = call.s;
+  k.scores_in = a->scores_in;
+  k.scores_out = a->scores_out;
+  k.scores_stride = a->scores_stride;
+  k.decay = a->decay;
+  const OpsKind kind{a->type, a->cache_type, layout->gpu_layout};
+  if (!rows_too)
+    return launched(launch_attention(k, AttnPlan{}, kind, static_cast<hipStream_t>(stream)), "KV attention");
   if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
   if ((s = rows(&call, "out", a->out, n, a->q_heads, D, true, &k.out))) return s;
   if ((s = array(&call, "tree", a->tree, extent(n, a->tree_words, 8), 8, true))) return s;
   if ((s = array(&call, "lse", a->lse, extent(n, a->q_heads, 4), 4, true))) return s;
-  const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
-  if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
-  if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
   if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
   if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
   const AttnPlan p = attention_plan(call.c, *layout, *seqs, *a);
@@ -456,12 +466,8 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
                   static_cast<unsigned long long>(a->workspace_bytes), static_cast<unsigned long long>(p.bytes));
     if ((s = array(&call, "workspace", a->workspace, p.bytes, 256))) return s;
   }
-  k.c = call.c;
-  k.s = call.s;
   k.tree = a->tree;
   k.lse = a->lse;
-  k.scores_in = a->scores_in;
-  k.scores_out = a->scores_out;
   k.k_scale = a->cache_type == MMA_TYPE_F8 ? a->k_scale : nullptr;
   k.v_scale = a->cache_type == MMA_TYPE_F8 ? a->v_scale : nullptr;
   char* ws = static_cast<char*>(a->workspace);
@@ -482,7 +488,6 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.q_heads = a->q_heads;
   k.group = a->q_heads / H;
   k.tree_words = a->tree_words;
-  k.scores_stride = a->scores_stride;
   // Entries of a workgroup: 32 for each of its waves where these stay, else 128 to 1024, its start being a few loads one
   // after the other: the 512 workgroups that run at once for one sequence, twice as many for several, whose lengths
   // differ (128 rows over 64k entries 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
@@ -494,9 +499,7 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   k.wide_out = rows_wide(k.out);
   k.wide_score_q = rows_wide(k.score_q);
   k.scale = a->scale;
-  k.decay = a->decay;
-  return launched(launch_attention(k, p, {a->type, a->cache_type, layout->gpu_layout}, static_cast<hipStream_t>(stream)),
-                  "KV attention");
+  return launched(launch_attention(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
 } catch (...) {
   return ops_boundary_error("mma_kv_attention");
 }

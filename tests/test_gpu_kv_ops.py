@@ -837,3 +837,24 @@ def test_commit_of_empty_lists(layers):
     got = mma.mma_kv_commit(lay, [layer] * layers, c.seqs(), none, counts, scores=[scores] * layers)
     assert got.tolist() == [7, 0, 30, 0]
     assert same_bits(layer.cpu(), c.flat[0]) and torch.equal(scores, want)
+
+
+@pytest.mark.parametrize("how", ["no tokens", "tokens of no sequence"])
+@pytest.mark.parametrize("layout,cache,group,tokens", [("piece", BF16, 4, 16), ("xpacked", F8, 8, 16), ("hnd", F16, 1, 3)])
+def test_attention_scores_without_tokens(layout, cache, group, tokens, how):
+    """The entries' weights fade all the same, and those past a sequence's entries stay."""
+    c = Case(layout, cache, [40, 0, 2100, -3], [0, 0, 0, 0], 64, 2, group, tokens, F16 if cache is F16 else BF16)
+    n = 0 if how == "no tokens" else 2
+    q = torch.full((n, 2 * group, 64), 3.0, dtype=c.dtype, device="cuda")
+    old = torch.rand(4, 2, c.max_len + 3, generator=c.g).cuda()
+    new, out = torch.full_like(old, -3.0), torch.full_like(q, 5.0)
+    mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(max_tokens=0 if n else 1), q, out=out, scores_in=old,
+                         scores_out=new, decay=0.5, **c.scales())
+    want = torch.full_like(old, -3.0)
+    for s, m in enumerate(c.lens):
+        want[s, :, :max(m, 0)] = 0.5 * old[s, :, :max(m, 0)]
+    assert torch.equal(new, want) and (out == 5).all()
+    mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(max_tokens=0 if n else 1), q, out=out, scores_out=new, **c.scales())
+    for s, m in enumerate(c.lens):
+        want[s, :, :max(m, 0)] = 0
+    assert torch.equal(new, want)
