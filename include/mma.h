@@ -514,7 +514,8 @@ typedef struct mma_kv_append {
 
 /* Of every token: q and k of each head times 1 / sqrt(mean of squares + eps) and the
  * weight, then each pair (a, b) turned to (a cos - b sin, b cos + a sin); q to q_out,
- * k and v to their entry of the cache (those of a token of no sequence nowhere). One rounding, at the store. 8-bit entries past
+ * k and v to their entry of the cache (those of a token of no sequence nowhere; so all,
+ * where num_seqs or max_tokens is 0). One rounding, at the store. 8-bit entries past
  * 448 are stored as 448 of their sign, NaN as NaN. */
 mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma_kv_seqs_t* seqs,
                            const mma_kv_append_t* args, void* stream);

@@ -372,10 +372,15 @@ mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma
                 a->rope_rows);
   if ((a->q_weight || a->k_weight) && !(a->eps >= 0)) return fail(MMA_ERR_INVALID_ARG, "eps has to be 0 or more");
   if ((s = check_seqs_sizes(seqs, layout->block_tokens))) return s;
-  if (!n || !seqs->num_seqs || !seqs->max_tokens) return MMA_OK;
+  if (!n) return MMA_OK;
   Device dev(call.device);
-  if ((s = check_layer(layer, &call))) return s;
-  if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
+  if (seqs->num_seqs && seqs->max_tokens) {
+    if ((s = check_layer(layer, &call))) return s;
+    if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
+  } else {  // tokens of no sequence: their queries are wanted all the same
+    call.s.max_tokens = 1;
+    call.s.num_tokens = n;
+  }
   AppendArgs k{};
   if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
   if ((s = rows(&call, "k", a->k, n, H, D, false, &k.k))) return s;

@@ -858,3 +858,23 @@ def test_attention_scores_without_tokens(layout, cache, group, tokens, how):
     for s, m in enumerate(c.lens):
         want[s, :, :max(m, 0)] = 0
     assert torch.equal(new, want)
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+@pytest.mark.parametrize("seqs,starts", [(0, True), (0, False), (2, True), (2, False)])
+def test_append_of_tokens_of_no_sequence(layout, seqs, starts):
+    """No sequences, or none that may have tokens: the queries come all the same, and nothing is written to the cache."""
+    c = Case(layout, BF16, [7, 5], [17, 3])
+    q = normal(c.g, c.total, 8, 128).to(BF16)
+    pos = torch.arange(c.total, dtype=torch.int32)
+    table = torch.from_numpy(mma.mma_rope_table(30, 128))
+    w = (1 + normal(c.g, 128, std=0.2)).to(BF16)
+    want, _, _ = ok.append(q, q[:, :2], q[:, :2], pos, table, False, w, w, 1e-6)
+    layer, x = c.flat[0].cuda(), q.cuda()
+    none = mma.kv_seqs(c.table[:seqs].cuda(), torch.tensor(c.lens[:seqs], dtype=torch.int32).cuda(),
+                       c.q_start[:seqs + 1].cuda() if starts else None, max_tokens=0 if seqs else 20, max_len=c.max_len)
+    out = torch.full_like(x, 9.0)
+    mma.mma_kv_append(c.layout(), layer, none, x, x[:, :2], x[:, :2], pos.cuda(), table.cuda(), q_out=out, q_weight=w.cuda(),
+                      k_weight=w.cuda())
+    rounded_close(out.cpu(), want, BF16, (128 + 16) * EPS * want.abs().amax(-1, keepdim=True))
+    assert same_bits(layer.cpu(), c.flat[0])
