@@ -1132,7 +1132,7 @@ __global__ __launch_bounds__(256) void attention_finish_kernel(AttnArgs a, uint3
   for (uint32_t r = 0; r < rows; ++r) {
     const f32x4 y = *reinterpret_cast<const f32x4*>(x + static_cast<uint64_t>(r) * a.logit_stride);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] += __builtin_amdgcn_exp2f(y[j] - l2[r]);
+    for (int j = 0; j < 4; ++j) w[j] += y[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y[j] - l2[r]);  // 0 though l2 be NaN
   }
   const uint64_t at = pair * a.scores_stride + key;
 #pragma unroll
@@ -1254,7 +1254,7 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
           for (int i = 0; i < 4; ++i) {
             const float p = __builtin_amdgcn_exp2f(x[t][i] * to_log2 - l2[i]);
             const uint32_t row = row0 + r0 + g * 4 + i;
-            bool see = l2[i] < INFINITY;
+            bool see = l2[i] != INFINITY;  // NaN does: its entries' weights are no numbers
             if constexpr (kMode == 1) see = see && row >= from[t];
             if constexpr (kMode == 2)
               if (see && base + t * 16 + m >= sp.before) {

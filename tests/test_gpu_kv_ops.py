@@ -878,3 +878,32 @@ def test_append_of_tokens_of_no_sequence(layout, seqs, starts):
                       k_weight=w.cuda())
     rounded_close(out.cpu(), want, BF16, (128 + 16) * EPS * want.abs().amax(-1, keepdim=True))
     assert same_bits(layer.cpu(), c.flat[0])
+
+
+@pytest.mark.parametrize("layout,cache,group,tokens,counts", [
+    ("piece", BF16, 2, 16, [4, 3]),      # kept logits
+    ("hnd", F8, 1, 16, [8, 3]),
+    ("hnd", F16, 2, 5, [4, 3]),          # few rows, their keys read again
+    ("piece", BF16, 4, 16, [40, 3]),     # many rows, one sequence's past a wave's
+    ("xpacked", BF16, 4, 16, [90, 30]),
+])
+def test_attention_scores_of_rows_that_are_not_numbers(layout, cache, group, tokens, counts):
+    """A row that sees a NaN gives NaN to the entries that it sees, and nothing to the others."""
+    c = Case(layout, cache, [70, 20], counts, 64, 1, group, tokens, F16 if cache is F16 else BF16)
+    tree = tree_bits(counts, c.g)
+    tree[:] &= ~4
+    tree[1, 0] |= 4  # drafted token 2 is seen by token 1 of its sequence alone
+    bad = to_cache(torch.full((64,), math.nan), cache) if cache is not F8 else torch.full((64,), 0x7F, dtype=torch.uint8)
+    c.flat[0][c.c.index(0, *c.c.entry(c.table[0], 72), 0)] = bad
+    if tokens == 16:
+        c.table[0, 1] = -1
+    q = normal(c.g, c.total, group, 64).to(c.dtype)
+    want = ok.attention(c.c, c.flat[0], c.table, c.spans(), q, group, 0.125, tree, c.k_scale, c.v_scale)
+    got = torch.full((2, 1, c.max_len), -3.0, device="cuda")
+    mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q.cuda(), tree=tree.cuda(), scores_out=got, **c.scales())
+    for s, (_, _, _, m) in enumerate(c.spans()):
+        a, b = got[s, 0, :m].cpu().double(), want["scores"][s, 0, :m]
+        assert s or (torch.isnan(b).any() and not torch.isnan(b).all())
+        assert torch.equal(torch.isnan(a), torch.isnan(b)), (torch.isnan(a).sum(), torch.isnan(b).sum())
+        rel = 2 * 64 * EPS * want["big"][torch.isfinite(want["big"])].max() + 64 * EPS
+        assert ((a - b).abs() / (rel * (1 + b.abs())))[~torch.isnan(b)].max() <= 1
