@@ -59,6 +59,7 @@ struct Type<__bf16> {
                 : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
   }
   static constexpr uint32_t kExponent = 0x7f80;
+  static constexpr float kLift = 0, kRowsLift = 0, kRowsRoom = 8;
 };
 template <>
 struct Type<_Float16> {
@@ -75,6 +76,9 @@ struct Type<_Float16> {
                 : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
   }
   static constexpr uint32_t kExponent = 0x7c00;
+  // f16 has normal numbers from 2^-14 on and nothing below 2^-25, and the many small weights of a long context beside a
+  // few large ones are smaller. So p is held (and summed) times 2^kLift, below the largest number, 2^16.
+  static constexpr float kLift = 15, kRowsLift = 11, kRowsRoom = 15;
 };
 
 template <class T>
@@ -479,12 +483,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 #pragma unroll
       for (int j = 0; j < 8; ++j) mx = fmaxf(mx, y[j]);
       mx = max_of_row(mx);
-      const float fade = __builtin_amdgcn_exp2f(top[r] - mx);
+      const float fade = __builtin_amdgcn_exp2f(top[r] - mx), from = mx - Type<T>::kLift;
       top[r] = mx;
       float add = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        y[j] = __builtin_amdgcn_exp2f(y[j] - mx);
+        y[j] = __builtin_amdgcn_exp2f(y[j] - from);
         add += y[j];
       }
       sum[r] = sum[r] * fade + add;  // this lane's keys; its 4 lanes are joined at the end
@@ -519,6 +523,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   for (int r = 0; r < R; ++r) {
     sum[r] += across(sum[r], 16);
     sum[r] += across(sum[r], 32);
+    top[r] -= Type<T>::kLift;  // what the sums are taken from
   }
 
   // Waves 2, 3 to 0, 1, then 1 to 0. A value's lane and register are the same in every wave.
@@ -577,8 +582,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 // nor the transposing 8-byte reads of V (ds_read_b64_tr_b16: of 4 entries' 16 values each lane of
 // 16 gets one value of the 4) meet in a bank. x-packed values are V^T already.
 //
-// The maximum that probabilities are taken from follows the row's own only where it would
-// be passed by more than 2^8: the factor is 1 otherwise and nothing is scaled.
+// What probabilities are taken from follows the row's maximum only where one would pass
+// 2^kRowsRoom (2^8 in bf16): the factor is 1 otherwise and nothing is scaled.
 //
 // 2048 tokens of 32 heads behind 6144 entries (8 KV heads, 128 values, bf16): 281 us, 0.85
 // PFLOP/s, where a plain matrix product of the library reaches 1.09. Without the fetches a tile
@@ -955,12 +960,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 8; ++i) y = fmaxf(y, x[r][j][i / 4][i % 4]);
       mx[r] = max_of_row(y) * to_log2;
-      rise |= mx[r] > top[r] + 8.0f;
+      rise |= mx[r] > top[r] + Type<T>::kRowsRoom;
     }
     if (__any(rise)) {
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
-        const float y = fmaxf(top[r], mx[r]);
+        const float y = fmaxf(top[r], mx[r] - Type<T>::kRowsLift);
         const float fade = __builtin_amdgcn_exp2f(top[r] - y);
         top[r] = y;
         sum[r] *= fade;

@@ -907,3 +907,22 @@ def test_attention_scores_of_rows_that_are_not_numbers(layout, cache, group, tok
         assert torch.equal(torch.isnan(a), torch.isnan(b)), (torch.isnan(a).sum(), torch.isnan(b).sum())
         rel = 2 * 64 * EPS * want["big"][torch.isfinite(want["big"])].max() + 64 * EPS
         assert ((a - b).abs() / (rel * (1 + b.abs())))[~torch.isnan(b)].max() <= 1
+
+
+@pytest.mark.parametrize("layout,tokens,count", [("piece", 16, 1), ("xpacked", 16, 3), ("hnd", 5, 1), ("hnd", 16, 12)])
+@pytest.mark.parametrize("far", [18.0, 23.5])
+def test_attention_of_small_weights_in_half_precision(layout, tokens, count, far):
+    """Entries with a weight 2^far times that of each of the others and nothing in their values, as first tokens
+    have: the output is the others' alone."""
+    n = 3000
+    c = Case(layout, F16, [n], [count], 64, 1, 4, tokens, F16)
+    for j in range(n + count):
+        at = c.c.entry(c.table[0], j)
+        k, v = torch.zeros(64), torch.rand(64, generator=c.g) + 0.5
+        k[0] = -far / 8 + float(torch.rand(1, generator=c.g)) / 8
+        if j % 32 == 5:
+            k[0], v = 0, torch.zeros(64)
+        c.flat[0][c.c.index(0, *at, 0)], c.flat[0][c.c.index(1, *at, 0)] = k.half(), v.half()
+    q = torch.zeros(count, 4, 64)
+    q[..., 0] = 8
+    check_attention(c, q=q.half(), scale=math.log(2))
