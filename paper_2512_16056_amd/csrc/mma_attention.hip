@@ -672,9 +672,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
 
   float to_log2 = a.scale * kLog2e * (a.k_scale ? a.k_scale[head] : 1.0f);
-  // A negative factor goes into Q, so that the largest product is the largest logit; 0 to a number that keeps -infinity.
+  // A negative factor goes into Q, so that the largest product is the largest logit; 0 becomes a number that keeps -infinity.
   const uint32_t flip = to_log2 < 0 ? 0x80008000u : 0u;
-  to_log2 = fmaxf(fabsf(to_log2), 1e-30f);
+  to_log2 = fabsf(to_log2);
+  if (to_log2 < 1e-30f) to_log2 = 1e-30f;  // not a maximum, which would drop NaN
   u32x4 q[RW][S::KS];
   uint32_t token[RW];
   bool live[RW];

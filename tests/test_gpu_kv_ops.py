@@ -926,3 +926,15 @@ def test_attention_of_small_weights_in_half_precision(layout, tokens, count, far
     q = torch.zeros(count, 4, 64)
     q[..., 0] = 8
     check_attention(c, q=q.half(), scale=math.log(2))
+
+
+@pytest.mark.parametrize("count", [1, 30])
+@pytest.mark.parametrize("layout", ["piece", "xpacked"])
+def test_attention_scales_that_are_not_numbers(layout, count):
+    c = Case(layout, F8, [50], [count], 64)
+    q = normal(c.g, count, 8, 64).to(BF16).cuda()
+    c.k_scale[1] = math.nan
+    out = mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q, **c.scales())
+    assert torch.isfinite(out[:, :4]).all() and torch.isnan(out[:, 4:]).all()
+    out = mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q, scale=math.nan)
+    assert torch.isnan(out).all()
