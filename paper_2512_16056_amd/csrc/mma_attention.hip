@@ -1366,44 +1366,38 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
 template <class T, bool F8, int DP, bool VX>
 hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   const uint32_t cells = p.splits * a.c.heads * a.s.num_seqs;
+  hipError_t e = hipSuccess;
   if (a.score_q.data != a.q.data) {
     const uint64_t chunks = static_cast<uint64_t>(a.s.num_tokens) * a.q_heads * (a.c.dim / 8);
-    attention_keep_queries_kernel<<<static_cast<uint32_t>((chunks + 255) / 256), 256, 0, stream>>>(a);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    e = launch(attention_keep_queries_kernel, static_cast<uint32_t>((chunks + 255) / 256), 256, stream, a);
+    if (e != hipSuccess) return e;
   }
   if (!p.rows) {  // the weights fade, that is all
     const dim3 grid((a.s.max_len + kWeigh - 1) / kWeigh, a.c.heads, a.s.num_seqs);
-    attention_finish_kernel<T, DP><<<grid, 256, 0, stream>>>(a, 0);
-    return hipGetLastError();
+    return launch(attention_finish_kernel<T, DP>, grid, 256, stream, a, 0);
   }
   if (p.stream) {
     if (p.tiles_per_wave == 1) {
-      attention_stream_kernel<T, F8, DP, VX, 1><<<cells, 256, 0, stream>>>(a);
+      e = launch(attention_stream_kernel<T, F8, DP, VX, 1>, cells, 256, stream, a);
     } else {
-      if constexpr (DP == 64 || (DP == 128 && (F8 || VX))) attention_stream_kernel<T, F8, DP, VX, 2><<<cells, 256, 0, stream>>>(a);
+      if constexpr (DP == 64 || (DP == 128 && (F8 || VX))) e = launch(attention_stream_kernel<T, F8, DP, VX, 2>, cells, 256, stream, a);
     }
   } else {
     const uint32_t grid = (cells + 7) / 8 * 8 * p.row_groups;
-    if (p.tiles_per_wave == 1)
-      attention_rows_kernel<T, F8, DP, VX, 1><<<grid, 256, 0, stream>>>(a, p.row_groups, cells);
-    else
-      attention_rows_kernel<T, F8, DP, VX, 2><<<grid, 256, 0, stream>>>(a, p.row_groups, cells);
+    e = p.tiles_per_wave == 1 ? launch(attention_rows_kernel<T, F8, DP, VX, 1>, grid, 256, stream, a, p.row_groups, cells)
+                              : launch(attention_rows_kernel<T, F8, DP, VX, 2>, grid, 256, stream, a, p.row_groups, cells);
   }
-  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint32_t joins = p.splits > 1 ? p.rows : 0;
   const uint32_t weighs = a.logits ? (a.s.max_len + kWeigh - 1) / kWeigh : 0;
   if (joins + weighs) {
-    attention_finish_kernel<T, DP><<<dim3(joins + weighs, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a, joins);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = launch(attention_finish_kernel<T, DP>, dim3(joins + weighs, a.c.heads, a.s.num_seqs), 256, stream, a, joins);
+    if (e != hipSuccess) return e;
   }
   if (a.lse2) {
     const dim3 grid((a.s.max_len + a.score_len - 1) / a.score_len, a.c.heads, a.s.num_seqs);
-    if (p.keys_stay)
-      attention_scores_kernel<T, F8, DP, true><<<grid, 256, 0, stream>>>(a);
-    else
-      attention_scores_kernel<T, F8, DP, false><<<grid, 256, 0, stream>>>(a);
-    e = hipGetLastError();
+    e = p.keys_stay ? launch(attention_scores_kernel<T, F8, DP, true>, grid, 256, stream, a)
+                    : launch(attention_scores_kernel<T, F8, DP, false>, grid, 256, stream, a);
   }
   return e;
 }

@@ -771,13 +771,9 @@ hipError_t append_of(const AppendArgs& a, hipStream_t stream) {
   // rows: 19 us, in parts 27; 256 to 700 tokens: the same within 0.5 us).
   const uint32_t parts = n >= 512 ? 1 : all;
   const uint32_t grid = n * parts + (VX ? (n + kRun - 1) / kRun * a.c.heads : 0);
-  if (lanes == 8)
-    append_kernel<T, F8, VX, 8><<<grid, 256, 0, stream>>>(a, parts);
-  else if (lanes == 16)
-    append_kernel<T, F8, VX, 16><<<grid, 256, 0, stream>>>(a, parts);
-  else
-    append_kernel<T, F8, VX, 32><<<grid, 256, 0, stream>>>(a, parts);
-  return hipGetLastError();
+  if (lanes == 8) return launch(append_kernel<T, F8, VX, 8>, grid, 256, stream, a, parts);
+  if (lanes == 16) return launch(append_kernel<T, F8, VX, 16>, grid, 256, stream, a, parts);
+  return launch(append_kernel<T, F8, VX, 32>, grid, 256, stream, a, parts);
 }
 
 template <class T>
@@ -797,43 +793,25 @@ hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stre
   const bool f8 = k.cache_type == MMA_TYPE_F8, vx = k.layout == MMA_KV_LAYOUT_XPACKED;
   const uint32_t chunks = a.c.dim * (f8 ? 1 : 2) / 16, units = a.c.heads * (chunks + (vx ? a.c.dim : chunks));
   const dim3 grid((units + 255) / 256, a.layers, a.s.num_seqs);
-  if (f8 && vx)
-    commit_kernel<true, true><<<grid, 256, 0, stream>>>(a);
-  else if (f8)
-    commit_kernel<true, false><<<grid, 256, 0, stream>>>(a);
-  else if (vx)
-    commit_kernel<false, true><<<grid, 256, 0, stream>>>(a);
-  else
-    commit_kernel<false, false><<<grid, 256, 0, stream>>>(a);
-  return hipGetLastError();
+  return f8 ? vx ? launch(commit_kernel<true, true>, grid, 256, stream, a) : launch(commit_kernel<true, false>, grid, 256, stream, a)
+            : vx ? launch(commit_kernel<false, true>, grid, 256, stream, a) : launch(commit_kernel<false, false>, grid, 256, stream, a);
 }
 
 hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream) {
   const bool f8 = k.cache_type == MMA_TYPE_F8, vx = k.layout == MMA_KV_LAYOUT_XPACKED;
   const dim3 pairs(a.c.heads, a.s.num_seqs);
   const bool listed = a.s.max_len <= kListed * kSelect;
-  if (a.s.max_len <= 8 * kSelect)
-    evict_select_kernel<8><<<pairs, kSelect, 0, stream>>>(a);
-  else if (listed)
-    evict_select_kernel<kListed><<<pairs, kSelect, 0, stream>>>(a);
-  else
-    evict_select_kernel<64><<<pairs, kSelect, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = a.s.max_len <= 8 * kSelect ? launch(evict_select_kernel<8>, pairs, kSelect, stream, a)
+                 : listed                   ? launch(evict_select_kernel<kListed>, pairs, kSelect, stream, a)
+                                            : launch(evict_select_kernel<64>, pairs, kSelect, stream, a);
   if (e != hipSuccess) return e;
   if (!listed) {
-    evict_list_kernel<<<dim3((a.s.max_len + kSelect - 1) / kSelect, a.c.heads, a.s.num_seqs), 256, 0, stream>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = launch(evict_list_kernel, dim3((a.s.max_len + kSelect - 1) / kSelect, a.c.heads, a.s.num_seqs), 256, stream, a);
+    if (e != hipSuccess) return e;
   }
   const dim3 grid((std::min(a.keep, a.s.max_len) + kMoved - 1) / kMoved, a.c.heads, a.s.num_seqs);
-  if (f8 && vx)
-    evict_move_kernel<true, true><<<grid, 256, 0, stream>>>(a);
-  else if (f8)
-    evict_move_kernel<true, false><<<grid, 256, 0, stream>>>(a);
-  else if (vx)
-    evict_move_kernel<false, true><<<grid, 256, 0, stream>>>(a);
-  else
-    evict_move_kernel<false, false><<<grid, 256, 0, stream>>>(a);
-  return hipGetLastError();
+  return f8 ? vx ? launch(evict_move_kernel<true, true>, grid, 256, stream, a) : launch(evict_move_kernel<true, false>, grid, 256, stream, a)
+            : vx ? launch(evict_move_kernel<false, true>, grid, 256, stream, a) : launch(evict_move_kernel<false, false>, grid, 256, stream, a);
 }
 
 }  // namespace mma

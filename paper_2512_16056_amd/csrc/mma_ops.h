@@ -136,6 +136,18 @@ hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream
 #ifdef __HIPCC__
 constexpr int kOpsWave = 64;
 
+// A launch and its own status: an error that an earlier call left in the runtime is neither taken for this launch's nor
+// taken away.
+template <class T>
+struct AsIs {
+  typedef T type;
+};
+template <class... P>
+hipError_t launch(void (*kernel)(P...), dim3 grid, uint32_t block, hipStream_t stream, const typename AsIs<P>::type&... args) {
+  void* params[] = {const_cast<P*>(&args)...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(block), params, 0, stream);
+}
+
 __device__ __forceinline__ uint32_t block_of(const CacheArgs& c, uint32_t entry) {
   return static_cast<uint32_t>((static_cast<uint64_t>(entry) * c.div_mul) >> c.div_shift);
 }

@@ -938,3 +938,29 @@ def test_attention_scales_that_are_not_numbers(layout, count):
     assert torch.isfinite(out[:, :4]).all() and torch.isnan(out[:, 4:]).all()
     out = mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q, scale=math.nan)
     assert torch.isnan(out).all()
+
+
+def test_an_earlier_error_is_not_a_call_s():
+    """An error that another call left in the runtime is neither reported as these calls' nor taken away."""
+    import ctypes
+    hip = ctypes.CDLL("libamdhip64.so.7")
+    c = Case("piece", BF16, [40], [3], layers=1)
+    lay, seqs, layer = c.layout(), c.seqs(), c.flat[0].cuda()
+    q = torch.ones(3, 8, 128, dtype=BF16, device="cuda")
+    acc = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    one = torch.ones(1, dtype=torch.int32, device="cuda")
+    dst, sc = c.spare[:1].view(1, 1).cuda(), torch.rand(1, 2, c.max_len, device="cuda")
+    for call in (lambda: mma.mma_kv_append(lay, layer, seqs, q, q[:, :2], q[:, :2]),
+                 lambda: mma.mma_kv_attention(lay, layer, seqs, q, scores_out=sc),
+                 lambda: mma.mma_kv_commit(lay, [layer], seqs, acc, one),
+                 lambda: mma.mma_kv_evict(lay, layer, seqs, dst, sc, 10)):
+        call()
+        torch.cuda.synchronize()
+        try:
+            left = hip.hipSetDevice(99)
+            assert left != 0
+            call()
+        finally:
+            found = hip.hipGetLastError()
+        assert found == left
+    torch.cuda.synchronize()
