@@ -540,11 +540,26 @@ def kv_attention_workspace(layout: mma_kv_layout_t, seqs: KVSeqs, num_tokens: in
     return need.value
 
 
+def _moved_layer(t, layout: mma_kv_layout_t) -> None:
+    """A layer whose entries are moved as they are: bytes (an integer type) or a type that caches hold, contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        return
+    held = (torch.float8_e4m3fn,) if layout.elem_bytes == 1 else (torch.bfloat16, torch.float16)
+    if not t.is_contiguous() or not (t.dtype in held or not (t.dtype.is_floating_point or t.dtype.is_complex)):
+        raise ValueError(f"layer: a contiguous tensor of {held} or of bytes is wanted, got {t.dtype}, strides {t.stride()}")
+
+
 def mma_kv_commit(layout: mma_kv_layout_t, layers, seqs: KVSeqs, accepted: torch.Tensor, counts: torch.Tensor, *,
                   scores=None, scores_stride: Optional[int] = None, stream=None) -> torch.Tensor:
     """Move the accepted drafted entries together in every layer (in place); returns the new lengths. `layers`,
     `scores`: tensors, or a layer_table (then scores_stride is needed)."""
+    if not isinstance(layers, ctypes.Array):
+        layers = list(layers)
+        for t in layers:
+            _moved_layer(t, layout)
     if scores is not None and not isinstance(scores, ctypes.Array):
+        if not len(scores):
+            raise ValueError("scores: a tensor of each layer is wanted")
         shape = tuple(scores[0].shape)
         if len(shape) != 3 or shape[:2] != (seqs.num_seqs, layout.kv_heads):
             raise ValueError(f"scores: [{seqs.num_seqs}][{layout.kv_heads}][entries] is wanted, got {shape}")
@@ -573,6 +588,7 @@ def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.
     """Keep the `keep` entries of each sequence and KV head that attention went to, moved into the blocks of
     dst_table; returns (entries kept, their scores, new lengths). `workspace`: a uint8 tensor of kv_evict_workspace()
     bytes or more; a new one of the stream's unless given."""
+    _moved_layer(layer, layout)
     entries = kept = lens = None
     if stream is not None:
         shape = (seqs.num_seqs, layout.kv_heads, keep)

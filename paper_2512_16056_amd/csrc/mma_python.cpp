@@ -91,6 +91,17 @@ void* address(PyObject* o) {
   return p;
 }
 
+// A cache layer: raw bytes (an integer type) or the type that the cache holds, contiguous. What is no GPU tensor is the
+// library's to refuse.
+void* layer(PyObject* o, at::ScalarType type) {
+  if (!THPVariable_Check(o)) return address(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.is_cuda() && !(t.is_contiguous() && (c10::isIntegralType(t.scalar_type(), false) || t.scalar_type() == type)))
+    REFUSE("layer: a contiguous tensor of %s or of bytes is wanted, got %s%s", c10::toString(type), c10::toString(t.scalar_type()),
+           t.is_contiguous() ? "" : ", not contiguous");
+  return t.data_ptr();
+}
+
 std::string text(at::IntArrayRef v) {
   std::string s = "[";
   for (size_t i = 0; i < v.size(); ++i) s += (i ? ", " : "") + std::to_string(v[i]);
@@ -136,12 +147,14 @@ struct Queries {
   const at::Tensor& t;
   at::ScalarType type;
   uint32_t kind, cache;
+  at::ScalarType cache_type;
   int64_t n, heads;
   Queries(PyObject* q, const mma_kv_layout_t* l) : t(tensor(q, "q")), type(t.scalar_type()) {
     if ((type != at::kBFloat16 && type != at::kHalf) || t.dim() != 3 || t.size(2) != l->head_dim)
       REFUSE("q: [tokens][heads][%u] of bfloat16 or float16 is wanted, got %s %s", l->head_dim, c10::toString(type), text(t.sizes()).c_str());
     kind = type == at::kBFloat16 ? MMA_TYPE_BF16 : MMA_TYPE_F16;
     cache = l->elem_bytes == 1 ? MMA_TYPE_F8 : kind;
+    cache_type = l->elem_bytes == 1 ? at::kFloat8_e4m3fn : type;
     n = t.size(0);
     heads = t.size(1);
   }
@@ -181,7 +194,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   x.q_heads = size32(q.heads, "q");
   x.type = q.kind;
   x.cache_type = q.cache;
-  check(g_append(c.layout, address(a[1]), c.seqs, &x, reinterpret_cast<void*>(number(a[15]))), "mma_kv_append");
+  check(g_append(c.layout, layer(a[1], q.cache_type), c.seqs, &x, reinterpret_cast<void*>(number(a[15]))), "mma_kv_append");
   return THPVariable_Wrap(out);
   } catch (const Refused&) {
     return nullptr;
@@ -232,7 +245,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
       x.workspace = own.data_ptr();
     }
   }
-  check(g_attention(c.layout, address(a[1]), c.seqs, &x, reinterpret_cast<void*>(number(a[14]))), "mma_kv_attention");
+  check(g_attention(c.layout, layer(a[1], q.cache_type), c.seqs, &x, reinterpret_cast<void*>(number(a[14]))), "mma_kv_attention");
   return THPVariable_Wrap(out);
   } catch (const Refused&) {
     return nullptr;

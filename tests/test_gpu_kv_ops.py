@@ -964,3 +964,38 @@ def test_an_earlier_error_is_not_a_call_s():
             found = hip.hipGetLastError()
         assert found == left
     torch.cuda.synchronize()
+
+
+def test_layers_of_another_type_or_order_are_refused():
+    c = Case("hnd", BF16, [40], [3])
+    lay, seqs, layer = c.layout(), c.seqs(), c.flat[0].cuda()
+    q = torch.ones(3, 8, 128, dtype=BF16, device="cuda")
+    f8 = Case("hnd", F8, [40], [3])
+    small = f8.flat[0].cuda()
+    acc, one = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    dst, sc = c.spare[:1].view(1, 1).cuda(), torch.rand(1, 2, c.max_len, device="cuda")
+    append = lambda x, l=lay: mma.mma_kv_append(l, x, seqs, q, q[:, :2], q[:, :2])  # noqa: E731
+    attend = lambda x, l=lay: mma.mma_kv_attention(l, x, seqs, q)  # noqa: E731
+    commit = lambda x: mma.mma_kv_commit(lay, [x], seqs, acc, one)  # noqa: E731
+    evict = lambda x: mma.mma_kv_evict(lay, x, seqs, dst, sc, 10)  # noqa: E731
+    for call in (append, attend):
+        for x in (layer.half(), layer.float(), layer.half().view(2, -1)):
+            with pytest.raises(ValueError, match="layer"):
+                call(x)
+        for t in (torch.float8_e5m2, torch.float8_e4m3fnuz):
+            with pytest.raises(ValueError, match="layer"):
+                call(small.view(t), f8.layout())
+        for x in (small, small.view(F8)):
+            call(x, f8.layout())
+    strided = torch.zeros(layer.numel(), 2, dtype=BF16, device="cuda")[:, 0]
+    for call in (append, attend, commit, evict):
+        with pytest.raises(ValueError, match="layer"):
+            call(strided)
+        for x in (layer, layer.view(torch.uint8), layer.view(2, c.c.blocks, -1), layer.data_ptr()):
+            call(x)
+    for call in (commit, evict):
+        with pytest.raises(ValueError, match="layer"):
+            call(layer.float())
+    with pytest.raises(ValueError, match="scores"):
+        mma.mma_kv_commit(lay, [layer], seqs, acc, one, scores=[])
+    assert mma.mma_kv_commit(lay, (x for x in [layer]), seqs, acc, one).tolist() == [41]
