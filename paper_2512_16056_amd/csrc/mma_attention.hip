@@ -703,11 +703,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     for (int c = 0; c < S::NC; ++c) o[r][c] = f32x4{0, 0, 0, 0};
   }
 
-  // Chunks past head_dim are never written: K's count as 0.
+  // Chunks past head_dim that no tile brings count as 0: K's in the products, and V's would be looked through for
+  // infinities, as whatever the last kernel left there (8-bit and x-packed tiles bring zeros themselves).
   if (a.c.dim < DP)
     for (uint32_t i = threadIdx.x; i < S::kBytes / 16; i += 256) {
       reinterpret_cast<u32x4*>(k0)[i] = u32x4{0, 0, 0, 0};
       reinterpret_cast<u32x4*>(k1)[i] = u32x4{0, 0, 0, 0};
+      if constexpr (!F8 && !VX) {
+        reinterpret_cast<u32x4*>(v0)[i] = u32x4{0, 0, 0, 0};
+        reinterpret_cast<u32x4*>(v1)[i] = u32x4{0, 0, 0, 0};
+      }
     }
   if (threadIdx.x < 8) absent[threadIdx.x] = 0;
   __syncthreads();

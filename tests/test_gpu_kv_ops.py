@@ -999,3 +999,29 @@ def test_layers_of_another_type_or_order_are_refused():
     with pytest.raises(ValueError, match="scores"):
         mma.mma_kv_commit(lay, [layer], seqs, acc, one, scores=[])
     assert mma.mma_kv_commit(lay, (x for x in [layer]), seqs, acc, one).tolist() == [41]
+
+
+def test_attention_padded_heads_take_the_same_time_whatever_ran_before():
+    """Heads of 96 are padded to 128 on the chip; what an earlier kernel left in the padding (NaN, here) is not looked
+    at. It costs 3.6 times as much if it is; 1.5 leaves room for noise."""
+    c = Case("piece", BF16, [0] * 16, [512] * 16, 96, 8, 4)
+    layer, seqs, lay = c.flat[0].cuda(), c.seqs(), c.layout()
+    q = torch.randn(c.total, 32, 96, device="cuda").to(BF16)
+    out = torch.empty_like(q)
+    before = Case("piece", BF16, [2000] * 16, [64] * 16, 128, 8, 4)
+    other = torch.zeros(before.total, 32, 128, dtype=BF16, device="cuda")
+    times = []
+    for fill in (0.0, math.nan):
+        left = torch.full_like(before.flat[0], fill).cuda()
+        took = []
+        for _ in range(15):
+            mma.mma_kv_attention(before.layout(), left, before.seqs(), other)
+            a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+            a.record()
+            mma.mma_kv_attention(lay, layer, seqs, q, out=out)
+            b.record()
+            torch.cuda.synchronize()
+            took.append(a.elapsed_time(b))
+        times.append(sorted(took)[7])
+    log(f"padded heads: {times}")
+    assert times[1] < 1.5 * times[0], times
