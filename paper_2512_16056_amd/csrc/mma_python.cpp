@@ -64,6 +64,12 @@ double real(PyObject* o) {
   return v;
 }
 
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Refused();
+  return v != 0;
+}
+
 uint32_t count(PyObject* o, const char* name) {
   const long long v = PyLong_AsLongLong(o);
   if (v == -1 && PyErr_Occurred()) throw Refused();
@@ -184,7 +190,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     x.rope_rows = size32(t.size(0), "rope");
     x.rot_dim = size32(t.size(1), "rope");
   }
-  x.interleaved = PyObject_IsTrue(a[9]) == 1;
+  x.interleaved = truth(a[9]);
   x.q_weight = flat_ptr<void>(a[10], "q_weight", q.type, {D});
   x.k_weight = flat_ptr<void>(a[11], "k_weight", q.type, {D});
   x.eps = static_cast<float>(real(a[12]));

@@ -1025,3 +1025,13 @@ def test_attention_padded_heads_take_the_same_time_whatever_ran_before():
         times.append(sorted(took)[7])
     log(f"padded heads: {times}")
     assert times[1] < 1.5 * times[0], times
+
+
+def test_an_object_without_a_truth_value_is_refused():
+    class Neither:
+        def __bool__(self):
+            raise RuntimeError("neither")
+    c = Case("hnd", BF16, [40], [3])
+    q = torch.ones(3, 8, 128, dtype=BF16, device="cuda")
+    with pytest.raises(RuntimeError, match="neither"):
+        mma.mma_kv_append(c.layout(), c.flat[0].cuda(), c.seqs(), q, q[:, :2], q[:, :2], interleaved=Neither())
