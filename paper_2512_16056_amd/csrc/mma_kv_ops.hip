@@ -381,7 +381,9 @@ __global__ __launch_bounds__(256) void commit_kernel(CommitArgs a) {
       const uint32_t at = first + lane;
       const int32_t j = at < a.accepted_stride ? acc[at] : -1, before = at && at < a.accepted_stride ? acc[at - 1] : -1;
       const int32_t c = a.counts[seq];
-      const SeqSpan sp = span_of(a.s, seq);
+      SeqSpan sp = span_of(a.s, seq);
+      if (!a.s.q_start)  // no token tensors here, whose rows would bound it
+        sp.total = sp.before + (a.s.max_tokens < a.s.max_len - sp.before ? a.s.max_tokens : a.s.max_len - sp.before);
       const uint32_t n = c < 0 ? 0 : static_cast<uint32_t>(c) > a.accepted_stride ? a.accepted_stride : static_cast<uint32_t>(c);
       const bool good = at < n && j >= 0 && static_cast<uint32_t>(j) < sp.total - sp.before && j > before;
       const uint64_t bad = ~__ballot(good);

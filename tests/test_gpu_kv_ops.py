@@ -1035,3 +1035,18 @@ def test_an_object_without_a_truth_value_is_refused():
     q = torch.ones(3, 8, 128, dtype=BF16, device="cuda")
     with pytest.raises(RuntimeError, match="neither"):
         mma.mma_kv_append(c.layout(), c.flat[0].cuda(), c.seqs(), q, q[:, :2], q[:, :2], interleaved=Neither())
+
+
+def test_commit_with_a_bound_far_above_the_tokens():
+    """Without starts each sequence has max_tokens tokens, whatever the product with the sequences before it."""
+    c = Case("piece", BF16, [7, 0, 30], [5, 5, 5], 16, 2, 1, 8, layers=1)
+    layer = c.flat[0].cuda()
+    acc = torch.tensor([[0, 2, 3], [1, 2, 4], [0, 3, 4]], dtype=torch.int32)
+    counts = torch.tensor([3, 2, 3], dtype=torch.int32)
+    seqs = mma.kv_seqs(c.table.cuda(), torch.tensor(c.lens, dtype=torch.int32).cuda(), max_tokens=1 << 30, max_len=c.max_len)
+    moves, lens = ok.commit_moves(acc, counts, [(0, 5, n, n + 5) for n in c.lens])
+    assert mma.mma_kv_commit(c.layout(), [layer], seqs, acc.cuda(), counts.cuda()).tolist() == lens == [10, 2, 33]
+    want = c.flat[0]
+    for s in range(3):
+        want = ok.move_entries(c.c, want, c.table[s], c.table[s], moves[s])
+    assert same_bits(layer.cpu(), want)
