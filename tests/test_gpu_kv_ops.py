@@ -1050,3 +1050,13 @@ def test_commit_with_a_bound_far_above_the_tokens():
     for s in range(3):
         want = ok.move_entries(c.c, want, c.table[s], c.table[s], moves[s])
     assert same_bits(layer.cpu(), want)
+
+
+def test_attention_starts_that_descend():
+    """Starts that go back, of ranges that do not meet, and a length above the call's bound."""
+    c = Case("piece", BF16, [10, 40, 20, 7], [3, 4, 2, 3], heads=1)
+    c.q_start = torch.tensor([6, 9, 3, 6, 1], dtype=torch.int32)  # rows 6-8, none, 3-5, none
+    check_attention(c)
+    c = Case("piece", BF16, [40, 40, 1000], [3, 4, 2], heads=1)
+    c.max_len = 300
+    check_attention(c, None, True)
