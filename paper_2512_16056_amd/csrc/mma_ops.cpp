@@ -272,17 +272,21 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   const uint64_t units = static_cast<uint64_t>(a.num_tokens) * a.q_heads;
   if (p.splits > 1) p.part_bytes = up_to(units * p.splits * p.dim_pad * 4, 256);
   if (a.scores_out) {
-    // One tile's logits are kept: 8 bytes a row and entry there and back, against reading the keys again (64k entries:
-    // 4 rows of 16 bits 70 us against 94, 16 rows of 8 bits 61 against 69).
-    p.logits = p.stream && p.tiles_per_wave == 1;
+    // One tile's logits are kept: 8 bytes a row and entry there and back, against reading the keys again. With the keys
+    // read again, 32 sequences of 1k to 8k entries of 8 KV heads, head-major, take this much (kept logits in brackets):
+    // 4 rows: heads of 64 in 8 bits 77 us (56), of 128 in bf16 235 (162), of 256 in bf16 474 (300); 8 rows of 64 in 8 bits
+    // 79 (73); 16 rows: of 64 in 8 bits 83 (93), in bf16 141 (137), of 128 in 8 bits 163 (143), in bf16 249 (214). So they
+    // are kept up to one and a half times a key's bytes; and up to 1 GiB, for the workspace's sake.
+    p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
+    const uint64_t kept = extent(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows, p.logit_stride, 4);
+    p.logits = p.stream && p.tiles_per_wave == 1 && 16 * p.rows <= 3 * c.dim * layout.elem_bytes && kept <= 1u << 30;
     // Scores of many rows: keys stay in registers from 257 rows on (8192 rows over 8k entries, with the attention, 588 us
     // against 758), of several sequences from 65 on (192 rows, 4 x 15k: 173 against 190); 128 rows over one sequence
     // of 64k take 147 so and 136 with the rows staying.
     p.keys_stay = p.rows > (q.num_seqs > 1 ? 64u : 256u);
-    p.logit_stride = static_cast<uint32_t>(up_to(q.max_len, 32));
-    if (p.logits)
-      p.logit_bytes = up_to(static_cast<uint64_t>(q.num_seqs) * c.heads * p.rows * p.logit_stride * 4, 256);
-    else {
+    if (p.logits) {
+      p.logit_bytes = up_to(kept, 256);
+    } else {
       p.lse_bytes = up_to(units * 4, 256);
       p.q_bytes = up_to(units * c.dim * 2, 256);  // of queries that `out` replaces before the weights are formed
     }

@@ -1060,3 +1060,11 @@ def test_attention_starts_that_descend():
     c = Case("piece", BF16, [40, 40, 1000], [3, 4, 2], heads=1)
     c.max_len = 300
     check_attention(c, None, True)
+
+
+@pytest.mark.parametrize("layout,cache,dim", [("hnd", F8, 64), ("piece", BF16, 32), ("xpacked", F8, 128)])
+def test_attention_scores_of_12_13_and_16_rows(layout, cache, dim):
+    """Rows whose logits are kept up to some number, depending on the keys' bytes, and whose keys are read again above it."""
+    for group in (12, 13, 16):
+        c = Case(layout, cache, [900, 40], [1, 1], dim, 2, group)
+        check_attention(c, tree_bits(c.counts, c.g), True)

@@ -127,3 +127,17 @@ def test_reference_selection_by_hand():
     assert ok.evict_select([nan, -math.inf, 0.0, -0.0], 4, 2, 0, 0) == [2, 3]
     assert ok.evict_select([nan, -math.inf, nan], 3, 2, 0, 0) == [0, 1]
     assert ok.evict_select([1, 2], 2, 5, 0, 0) == [0, 1]
+
+
+@pytest.mark.parametrize("dim,elem,rows", [(64, 1, 16), (64, 2, 16), (128, 2, 4), (128, 1, 16), (256, 2, 16)])
+@pytest.mark.parametrize("seqs,length", [(64, 131072), (1024, 131072), (65535, 1 << 24), (65535, (1 << 31) - 8192)])
+def test_workspace_of_weights_is_bounded(dim, elem, rows, seqs, length):
+    """Weights of the entries need 1 GiB at most beside the rows' own sums, however long the sequences may be: of a row
+    its lse and a copy of its queries, and parts of a row for each of its splits, of which there are 2048 workgroups' or one."""
+    lay = mma.kv_layout(1, 16, 8, dim, elem, 5000, 1, 0)
+    c = mma.mma_kv_seqs_t(0, 0, 0, seqs, length // 16, 1, length)
+    need = ctypes.c_uint64()
+    a = mma.mma_kv_attention_t(num_tokens=seqs, q_heads=8 * rows, scores_out=1, cache_type=2 if elem == 1 else 0)
+    assert mma.lib.mma_kv_attention_workspace(lay, c, a, need) == mma.MMA_OK
+    own, parts = seqs * 8 * rows * (4 + 2 * dim), (2048 + 8 * seqs) * rows * (dim + 2) * 4
+    assert seqs * 8 * rows * 4 <= need.value <= max(1 << 30, own) + parts + 1024
