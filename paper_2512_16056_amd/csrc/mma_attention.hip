@@ -1385,7 +1385,8 @@ hipError_t launch_of(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
     if (p.tiles_per_wave == 1) {
       e = launch(attention_stream_kernel<T, F8, DP, VX, 1>, cells, 256, stream, a);
     } else {
-      if constexpr (DP == 64 || (DP == 128 && (F8 || VX))) e = launch(attention_stream_kernel<T, F8, DP, VX, 2>, cells, 256, stream, a);
+      e = hipErrorInvalidValue;  // no plan has it
+      if constexpr (stream_two_tiles(DP, F8, VX)) e = launch(attention_stream_kernel<T, F8, DP, VX, 2>, cells, 256, stream, a);
     }
   } else {
     const uint32_t grid = (cells + 7) / 8 * 8 * p.row_groups;

@@ -252,10 +252,9 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   // (32 rows, 4 x 15k: 52 against 41), with fewer from some thousands of entries on, unless their logits are kept
   // (4 rows, 4 x 15k: 45 against 38, 64k: 61 against 57; but 6 x 900: 12.1 against 14.2, 64k and scores: 70 against
   // 92). Below 65 the two are within 5 %, above 128 the registers win (32 x 8k: 248 against 379).
-  p.stream = p.rows <= (p.dim_pad == 256 ? 16u : 32u) && c.tokens % 8 == 0;
-  if (p.dim_pad == 128 && layout.elem_bytes == 2 && layout.gpu_layout != MMA_KV_LAYOUT_XPACKED &&
-      (p.rows > 16 || (q.max_len > 4096 && !a.scores_out)))
-    p.stream = false;
+  const bool two = stream_two_tiles(p.dim_pad, layout.elem_bytes == 1, layout.gpu_layout == MMA_KV_LAYOUT_XPACKED);
+  p.stream = p.rows <= (two ? 32u : 16u) && c.tokens % 8 == 0;
+  if (p.dim_pad == 128 && !two && q.max_len > 4096 && !a.scores_out) p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);

@@ -127,6 +127,12 @@ struct AttnPlan {
   uint64_t part_bytes, ml_bytes, lse_bytes, q_bytes, logit_bytes, bytes;
 };
 
+// Whether attention_stream_kernel is there for two tiles of rows, with their keys and values in registers: not with heads
+// above 128, and of 65 to 128 not where V is turned in registers.
+constexpr bool stream_two_tiles(uint32_t dim_pad, bool f8, bool xpacked) {
+  return dim_pad == 64 || (dim_pad == 128 && (f8 || xpacked));
+}
+
 hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stream);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stream);
