@@ -384,12 +384,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   const uint32_t head = pair % a.c.heads, seq = pair / a.c.heads;
   const SeqSpan sp = span_of(a.s, seq);
   const uint32_t rows = sp.count * a.group;
-  constexpr uint32_t row0 = 0;
   if (!rows) return;
   const uint32_t begin = split * a.split_len;
   if (begin >= sp.total && split) return;  // the first split also writes the rows that have no entries
   // Without a tree no row of the workgroup sees entries past its last token's.
-  const uint32_t last_token = (row0 + R * 16 < rows ? row0 + R * 16 - 1 : rows - 1) / a.group;
+  const uint32_t last_token = (R * 16 < rows ? R * 16 - 1 : rows - 1) / a.group;
   uint32_t end = begin + a.split_len < sp.total ? begin + a.split_len : sp.total;
   if (!a.tree && end > sp.before + last_token + 1) end = sp.before + last_token + 1;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
@@ -399,7 +398,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   bool live[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const uint32_t row = row0 + r * 16 + m;
+    const uint32_t row = r * 16 + m;
     live[r] = row < rows;
     token[r] = live[r] ? row / a.group : 0;
     load_q<F8, S::KS>(a, head * a.group + (live[r] ? row % a.group : 0), sp.first + token[r], live[r], g, q[r]);
@@ -435,7 +434,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   float* logits[R];
 #pragma unroll
   for (int r = 0; r < R; ++r)
-    logits[r] = a.logits && live[r] ? a.logits + ((static_cast<uint64_t>(seq) * a.c.heads + head) * a.logit_rows + row0 + r * 16 + m) * a.logit_stride + g * 8
+    logits[r] = a.logits && live[r] ? a.logits + ((static_cast<uint64_t>(seq) * a.c.heads + head) * a.logit_rows + r * 16 + m) * a.logit_stride + g * 8
                                     : nullptr;
   const auto tile = [&](auto masked, bool have) {
     constexpr bool kMasked = decltype(masked)::value;
@@ -508,7 +507,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   };
   // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not
   // there), masked ones.
-  uint32_t whole = a.tree ? sp.before : sp.before + row0 / a.group + 1;
+  uint32_t whole = a.tree ? sp.before : sp.before + 1;
   if (whole > end) whole = end;
   bool have = there(vid);
   while (base + kTile <= whole && __all(have)) {
@@ -566,7 +565,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 #pragma unroll
   for (int r = 0; r < R; ++r)
     if (live[r])
-      store_row<T, DP, S::NC, VX>(a, sp.first + token[r], head * a.group + (row0 + r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r]);
+      store_row<T, DP, S::NC, VX>(a, sp.first + token[r], head * a.group + (r * 16 + m) % a.group, split, g, top[r], sum[r], v_scale, o[r]);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -1180,7 +1179,7 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(AttnArgs a) {
   constexpr int kChunks = kRows * C / 256;  // 16-byte chunks of the rows that a thread brings
   __shared__ __attribute__((aligned(16))) uint8_t ql[(STAY ? 2 : 1) * kRows * C * 16];
   __shared__ __attribute__((aligned(16))) float ll[(STAY ? 2 : 1) * kRows];
-  __shared__ float sums[kScored];
+  __shared__ float sums[STAY ? 4 * kTile : kScored];
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
