@@ -54,6 +54,14 @@ struct Type<__bf16> {
     const f32x2 v = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
   }
+  // Numbers from 0 on as the sum of two of 16 bits: the first cut off, the second what is left, and above 0 with the
+  // number, so that an infinity times the two is no NaN.
+  static __device__ __forceinline__ uint32_t split(float a, float b, uint32_t* rest) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+    *rest = pack(fmaxf(a - __builtin_bit_cast(float, x & 0xffff0000u), a * 0x1p-24f),
+                 fmaxf(b - __builtin_bit_cast(float, y & 0xffff0000u), b * 0x1p-24f));
+    return __builtin_amdgcn_perm(y, x, 0x07060302u);
+  }
   static __device__ __forceinline__ uint32_t from_f8(uint32_t w, bool high) {  // exact
     return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true))
                 : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
@@ -70,6 +78,12 @@ struct Type<_Float16> {
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
     const f32x2 v = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+  }
+  static __device__ __forceinline__ uint32_t split(float a, float b, uint32_t* rest) {
+    const auto cut = __builtin_amdgcn_cvt_pkrtz(a, b);
+    *rest = pack(fmaxf(a - static_cast<float>(cut[0]), fminf(a, 0x1p-24f)),  // the least that there is
+                 fmaxf(b - static_cast<float>(cut[1]), fminf(b, 0x1p-24f)));
+    return __builtin_bit_cast(uint32_t, cut);
   }
   static __device__ __forceinline__ uint32_t from_f8(uint32_t w, bool high) {
     return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true))
@@ -171,14 +185,35 @@ __device__ __forceinline__ uint32_t nonfinite_keys(u32x4 w) {
   return bad;
 }
 
-// O^T += V^T P^T over 32 keys: operand c of V^T from op(c).
-template <class T, int R, int NC, class Op>
-__device__ __forceinline__ void add_values(Op op, const u32x4 (&p)[R], f32x4 (&o)[R][NC]) {
+// O^T += V^T P^T over 32 keys: operand c of V^T from op(c); P in one term or two.
+template <class T, int R, int NC, int TERMS, class Op>
+__device__ __forceinline__ void add_values(Op op, const u32x4 (&p)[TERMS][R], f32x4 (&o)[R][NC]) {
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const u32x4 v = op(c);
 #pragma unroll
-    for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[r], o[r][c]);
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[t][r], o[r][c]);
+  }
+}
+
+// Probabilities y of 8 keys as the operand, in TERMS terms of 16 bits. Where a wave has one tile of rows, two: memory
+// bounds it, and an error below 2^-15 of p (f16: 2^-21) costs 2 % at most (4 rows, 32 sequences of up to 8k, bf16, head-major: 124.5 us
+// with one term, 125.6 with two). With two tiles one, rounded to nearest: an error of the size of the output's own
+// rounding. A second one would take a prompt of 2048 tokens behind 6144 entries, bf16, from 282 us to 369, and 32 rows
+// over 4 x 15k 8-bit x-packed entries, for lack of registers, from 32 to 38. The sum of p is of unrounded ones.
+template <class T, int R, int TERMS>
+__device__ __forceinline__ void operand_of(const float (&y)[8], u32x4 (&p)[TERMS][R], int r) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TERMS == 2) {
+      uint32_t rest;
+      p[0][r][i] = Type<T>::split(y[2 * i], y[2 * i + 1], &rest);
+      p[1][r][i] = rest;
+    } else {
+      p[0][r][i] = Type<T>::pack(y[2 * i], y[2 * i + 1]);
+    }
   }
 }
 
@@ -186,8 +221,8 @@ __device__ __forceinline__ void add_values(Op op, const u32x4 (&p)[R], f32x4 (&o
 // as 0, and an infinite or NaN value of a key reaches the rows that see the key, no others,
 // though a product with a probability of 0 would bring NaN to all. Such keys are left out of the
 // joint product and added one by one to the rows that see them.
-template <class T, int R, int NC, class Op>
-__device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[R], const uint32_t (&seen)[R], uint32_t ok,
+template <class T, int R, int NC, int TERMS, class Op>
+__device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[TERMS][R], const uint32_t (&seen)[R], uint32_t ok,
                                                   uint32_t g, uint32_t m, f32x4 (&o)[R][NC]) {
   uint32_t bad = 0;
 #pragma unroll
@@ -197,7 +232,9 @@ __device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[R], co
     bad |= n;
     v = only_keys(v, ~n);
 #pragma unroll
-    for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[r], o[r][c]);
+    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+      for (int r = 0; r < R; ++r) o[r][c] = Type<T>::mfma(v, p[t][r], o[r][c]);
   }
   if (!__any(bad)) return;
   for (uint32_t j = 0; j < kTile; ++j) {
@@ -212,7 +249,7 @@ __device__ __forceinline__ void add_values_masked(Op op, const u32x4 (&p)[R], co
       v = only_keys(v, nonfinite_keys<T>(v));
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const f32x4 d = Type<T>::mfma(v, only_keys(p[r], mine), f32x4{0, 0, 0, 0});
+        const f32x4 d = Type<T>::mfma(v, only_keys(p[0][r], mine), f32x4{0, 0, 0, 0});
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[r][c][i] = sees[r] ? o[r][c][i] + d[i] : o[r][c][i];
       }
@@ -463,7 +500,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
       const uint32_t first = base + g * 8;
       okay = !have || first >= end ? 0 : end - first >= 8 ? 0xffu : (1u << (end - first)) - 1;
     }
-    u32x4 p[R];
+    u32x4 p[R == 1 ? 2 : 1][R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float y[8];
@@ -491,10 +528,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
         add += y[j];
       }
       sum[r] = sum[r] * fade + add;  // this lane's keys; its 4 lanes are joined at the end
-      // The probabilities are rounded to the type's 16 bits for the product with V, as the
-      // output is: an error of the same size as the output's own. Their sum is not rounded.
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[r][i] = Type<T>::pack(y[2 * i], y[2 * i + 1]);
+      operand_of<T>(y, p, r);
 #pragma unroll
       for (int c = 0; c < S::NC; ++c) o[r][c] *= fade;
     }
@@ -980,7 +1014,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     }
 #pragma unroll
     for (int j = 0; j < S::SUB; ++j) {
-      u32x4 p[RW];
+      u32x4 p[RW == 1 ? 2 : 1][RW];
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
         float y[8];
@@ -989,9 +1023,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
           y[i] = __builtin_amdgcn_exp2f(fmaf(x[r][j][i / 4][i % 4], to_log2, -top[r]));
           sum[r] += y[i];
         }
-        // Rounded to 16 bits for the product with V (an error of the size of the output's own rounding), not in the sum.
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[r][i] = Type<T>::pack(y[2 * i], y[2 * i + 1]);
+        operand_of<T>(y, p, r);
       }
       const auto op = [&](int c) {
         if constexpr (VX) {

@@ -1068,3 +1068,52 @@ def test_attention_scores_of_12_13_and_16_rows(layout, cache, dim):
     for group in (12, 13, 16):
         c = Case(layout, cache, [900, 40], [1, 1], dim, 2, group)
         check_attention(c, tree_bits(c.counts, c.g), True)
+
+
+FEW_ROWS = [
+    # layout, cache, dim, tokens, group, lens, counts
+    ("piece", BF16, 128, 16, 4, [700, 33], [1, 3]),     # memory to registers, a tile of rows
+    ("xpacked", F8, 128, 16, 4, [700], [4]),
+    ("hnd", F16, 64, 16, 8, [300, 90], [2, 2]),
+    ("xpacked", F16, 256, 16, 2, [500], [5]),
+    ("hnd", BF16, 128, 16, 4, [4400], [1]),             # through LDS, 64 rows of a workgroup
+    ("piece", F8, 80, 5, 4, [400], [9]),
+    ("xpacked", BF16, 256, 8, 4, [300], [12]),
+]
+
+
+@pytest.mark.parametrize("layout,cache,dim,tokens,group,lens,counts", FEW_ROWS)
+def test_attention_of_few_rows_holds_weights_in_two_terms(layout, cache, dim, tokens, group, lens, counts):
+    """Where memory bounds a call the products with V lose no more than 2^-15 of a weight (cut to 8 bits, below 2^-7 is
+    left, and rounding that to 8 loses 2^-8 of it), and the output's own rounding is what is left of the error."""
+    dtype = F16 if cache is F16 else BF16
+    c = Case(layout, cache, lens, counts, dim, 1, group, tokens, dtype)
+    q = normal(c.g, c.total, group, dim, std=1.0).to(dtype)
+    want = ok.attention(c.c, c.flat[0], c.table, c.spans(), q, group, dim ** -0.5, None, c.k_scale, c.v_scale)
+    out = mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q.cuda(), **c.scales()).cpu().double()
+    u = 2.0 ** -(BITS[dtype] + 1)
+    p_err = (2 * dim * EPS * want["big"] + 64 * EPS)[..., None]
+    tol = u * want["out"].abs() * (1 + 2 * u) + (2.0 ** -15 + p_err) * want["mag"] * (1 + 2 * u) + STEP[dtype]
+    worst = ((out - want["out"]).abs() / tol).max().item()
+    assert worst <= 1, f"{worst:.3g} of the tolerance"
+
+
+@pytest.mark.parametrize("layout,cache,dim,tokens,group,lens,counts", FEW_ROWS)
+def test_attention_of_few_rows_and_the_ends_of_the_range(layout, cache, dim, tokens, group, lens, counts):
+    """An infinite value that all rows see, with weights that one term holds whole, makes infinite outputs; the largest
+    finite one that a row does not see does not reach it."""
+    dtype = F16 if cache is F16 else BF16
+    c = Case(layout, cache, lens, counts, dim, 1, group, tokens, dtype)
+    q = torch.zeros(c.total, group, dim, dtype=dtype)
+    top = 448.0 if cache is F8 else torch.finfo(cache).max
+    at = c.c.index(1, *c.c.entry(c.table[0], lens[0] + counts[0] - 1), 0)
+    c.flat[0][at] = to_cache(torch.full((dim,), top), cache)
+    out = check_attention(c, q=q)
+    if counts[0] > 1:
+        assert out[: counts[0] - 1].abs().max() < 16
+    if cache is F8:
+        return
+    c.flat[0][c.c.index(1, *c.c.entry(c.table[0], 9), 0)[0]] = math.inf
+    c.flat[0][c.c.index(1, *c.c.entry(c.table[0], 70), 0)[1]] = -math.inf
+    out = check_attention(c, q=q)
+    assert (out[: counts[0], :, 0] == math.inf).all() and (out[: counts[0], :, 1] == -math.inf).all()
