@@ -545,9 +545,10 @@ typedef struct mma_kv_attention {
  * out = sum of p V; lse = log of the sum of exp (rows of no sequence are left alone). It sees its sequence's lens[s] entries
  * and of the call's own tokens (which mma_kv_append has written) those that `tree` says.
  * Logits, maxima and sums are 32-bit. For the product with V p is held in two 16-bit terms
- * (an error below 2^-15 of p, in f16 2^-21) where a sequence has up to 16 rows (tokens x
- * query heads of a KV head) in the call, with up to 64 in some layouts, and in one (2^-8,
- * in f16 2^-11: as the output is rounded) where it has more.
+ * (an error below 2^-15 of p; in f16, and over 8-bit caches, 2^-21) where a sequence has up
+ * to 16 rows (tokens x query heads of a KV head) in the call, with up to 64 in some layouts,
+ * and in one (2^-8, as the output is rounded; in f16, and over 8-bit caches, 2^-11) where it
+ * has more.
  * A row that sees nothing is 0 with lse -infinity. What lies in entries that a row does
  * not see, infinities and NaN among it, does not reach the row.
  * scores_out[s][h][j] = decay * scores_in[s][h][j], for j < lens[s], plus the p of entry

@@ -95,6 +95,10 @@ struct Type<_Float16> {
   static constexpr float kLift = 15, kRowsLift = 11, kRowsRoom = 15;
 };
 
+// What V and the probabilities are multiplied in: 8-bit values are exact in f16, whose 11 bits lose less of p than bf16's 8.
+template <class T, bool F8>
+using ValueType = typename std::conditional<F8, _Float16, T>::type;
+
 template <class T>
 __device__ __forceinline__ float to_float(uint32_t bits16) {
   return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(bits16)));
@@ -200,9 +204,9 @@ __device__ __forceinline__ void add_values(Op op, const u32x4 (&p)[TERMS][R], f3
 
 // Probabilities y of 8 keys as the operand, in TERMS terms of 16 bits. Where a wave has one tile of rows, two: memory
 // bounds it, and an error below 2^-15 of p (f16: 2^-21) costs 2 % at most (4 rows, 32 sequences of up to 8k, bf16, head-major: 124.5 us
-// with one term, 125.6 with two). With two tiles one, rounded to nearest: an error of the size of the output's own
-// rounding. A second one would take a prompt of 2048 tokens behind 6144 entries, bf16, from 282 us to 369, and 32 rows
-// over 4 x 15k 8-bit x-packed entries, for lack of registers, from 32 to 38. The sum of p is of unrounded ones.
+// with one term, 125.6 with two). With two tiles one, rounded to nearest: 2^-8 of p in bf16, as the output is rounded,
+// 2^-11 in f16 and over 8-bit caches. A second one would take a prompt of 2048 tokens behind 6144 entries, bf16, from 282
+// us to 369, and 32 rows over 4 x 15k 8-bit x-packed entries, for lack of registers, from 32 to 38. The sum of p is of unrounded ones.
 template <class T, int R, int TERMS>
 __device__ __forceinline__ void operand_of(const float (&y)[8], u32x4 (&p)[TERMS][R], int r) {
 #pragma unroll
@@ -413,6 +417,7 @@ struct Stream {
 template <class T, bool F8, int DP, bool VX, int R>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kernel(AttnArgs a) {
   typedef Stream<F8, DP, VX> S;
+  typedef ValueType<T, F8> TV;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   // Workgroups go to the 8 XCDs in turn: heads and sequences first, so that each XCD has early and late splits alike
   // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 141 us and more
@@ -519,7 +524,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 #pragma unroll
       for (int j = 0; j < 8; ++j) mx = fmaxf(mx, y[j]);
       mx = max_of_row(mx);
-      const float fade = __builtin_amdgcn_exp2f(top[r] - mx), from = mx - Type<T>::kLift;
+      const float fade = __builtin_amdgcn_exp2f(top[r] - mx), from = mx - Type<TV>::kLift;
       top[r] = mx;
       float add = 0;
 #pragma unroll
@@ -528,15 +533,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
         add += y[j];
       }
       sum[r] = sum[r] * fade + add;  // this lane's keys; its 4 lanes are joined at the end
-      operand_of<T>(y, p, r);
+      operand_of<TV>(y, p, r);
 #pragma unroll
       for (int c = 0; c < S::NC; ++c) o[r][c] *= fade;
     }
-    const auto op = [&](int c) { return s.template value<T>(c); };
+    const auto op = [&](int c) { return s.template value<TV>(c); };
     if constexpr (kMasked)
-      add_values_masked<T>(op, p, seen, okay, g, m, o);
+      add_values_masked<TV>(op, p, seen, okay, g, m, o);
     else
-      add_values<T>(op, p, o);
+      add_values<TV>(op, p, o);
     base += step;
   };
   // Tiles that every row sees whole; from the first other one on (drafted tokens, the end, or a block that is not
@@ -556,7 +561,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   for (int r = 0; r < R; ++r) {
     sum[r] += across(sum[r], 16);
     sum[r] += across(sum[r], 32);
-    top[r] -= Type<T>::kLift;  // what the sums are taken from
+    top[r] -= Type<TV>::kLift;  // what the sums are taken from
   }
 
   // Waves 2, 3 to 0, 1, then 1 to 0. A value's lane and register are the same in every wave.
@@ -662,6 +667,7 @@ __device__ __forceinline__ u32x2 read_turned(const uint8_t* p) {  // 16 lanes: 4
 template <class T, bool F8, int DP, bool VX, int RW>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(AttnArgs a, uint32_t row_groups, uint32_t cells) {
   typedef Tiles<F8, DP, VX> S;
+  typedef ValueType<T, F8> TV;
   // Two buffers, each of its own so that the compiler can tell reads of one from loads on their way to the other and
   // does not wait for those: code that knows its buffer takes it as a constant B.
   __shared__ __attribute__((aligned(1024))) uint8_t k0[S::kBytes], v0[S::kBytes], k1[S::kBytes], v1[S::kBytes];
@@ -899,11 +905,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
         *reinterpret_cast<u32x4*>(kl + S::at(e, chunk + 1)) = widen<T>(x[2], x[3]);
         if constexpr (VX) {
           const uint32_t d = x_value(i), c = x_chunk(i) * 2;
-          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c)) = widen<T>(y[0], y[1]);
-          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c + 1)) = widen<T>(y[2], y[3]);
+          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c)) = widen<TV>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(vl + S::at_x(d, c + 1)) = widen<TV>(y[2], y[3]);
         } else {
-          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk)) = widen<T>(y[0], y[1]);
-          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk + 1)) = widen<T>(y[2], y[3]);
+          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk)) = widen<TV>(y[0], y[1]);
+          *reinterpret_cast<u32x4*>(vl + S::at(e, chunk + 1)) = widen<TV>(y[2], y[3]);
         }
       }
     }
@@ -999,12 +1005,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 8; ++i) y = fmaxf(y, x[r][j][i / 4][i % 4]);
       mx[r] = max_of_row(y) * to_log2;
-      rise |= mx[r] > top[r] + Type<T>::kRowsRoom;
+      rise |= mx[r] > top[r] + Type<TV>::kRowsRoom;
     }
     if (__any(rise)) {
 #pragma unroll
       for (int r = 0; r < RW; ++r) {
-        const float y = fmaxf(top[r], mx[r] - Type<T>::kRowsLift);
+        const float y = fmaxf(top[r], mx[r] - Type<TV>::kRowsLift);
         const float fade = __builtin_amdgcn_exp2f(top[r] - y);
         top[r] = y;
         sum[r] *= fade;
@@ -1023,7 +1029,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
           y[i] = __builtin_amdgcn_exp2f(fmaf(x[r][j][i / 4][i % 4], to_log2, -top[r]));
           sum[r] += y[i];
         }
-        operand_of<T>(y, p, r);
+        operand_of<TV>(y, p, r);
       }
       const auto op = [&](int c) {
         if constexpr (VX) {
@@ -1035,9 +1041,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
         }
       };
       if constexpr (kMasked)
-        add_values_masked<T>(op, p, seen[j], 0xff, g, m, o);  // entries that are not there are 0 in LDS
+        add_values_masked<TV>(op, p, seen[j], 0xff, g, m, o);  // entries that are not there are 0 in LDS
       else
-        add_values<T>(op, p, o);
+        add_values<TV>(op, p, o);
     }
   };
   // Tiles that every row of the workgroup sees whole, the two buffers in turn; from the first other one on, masked ones.

@@ -1117,3 +1117,18 @@ def test_attention_of_few_rows_and_the_ends_of_the_range(layout, cache, dim, tok
     c.flat[0][c.c.index(1, *c.c.entry(c.table[0], 70), 0)[1]] = -math.inf
     out = check_attention(c, q=q)
     assert (out[: counts[0], :, 0] == math.inf).all() and (out[: counts[0], :, 1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("layout,dim,tokens,lens,counts", [("xpacked", 128, 16, [900], [8]), ("hnd", 128, 16, [300, 70], [24, 9]),
+                                                           ("xpacked", 64, 16, [700], [40]), ("piece", 256, 5, [300], [30])])
+def test_attention_over_8_bits_loses_no_bits_of_bf16(layout, dim, tokens, lens, counts):
+    """8-bit values are exact in f16, so that weights of many rows lose 2^-11 and not bf16's 2^-8."""
+    c = Case(layout, F8, lens, counts, dim, 1, 4, tokens)
+    q = normal(c.g, c.total, 4, dim, std=0.3).to(BF16)
+    want = ok.attention(c.c, c.flat[0], c.table, c.spans(), q, 4, dim ** -0.5, None, c.k_scale, c.v_scale)
+    out = mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q.cuda(), **c.scales()).cpu().double()
+    u = 2.0 ** -8
+    p_err = (2 * dim * EPS * want["big"] + 64 * EPS)[..., None]
+    tol = u * want["out"].abs() * (1 + 2 * u) + (2.0 ** -11 + p_err) * want["mag"] * (1 + 2 * u) + STEP[BF16]
+    worst = ((out - want["out"]).abs() / tol).max().item()
+    assert worst <= 1, f"{worst:.3g} of the tolerance"
