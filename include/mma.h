@@ -526,7 +526,7 @@ typedef struct mma_kv_attention {
                                sequence's tokens in this call; NULL: token i sees 0 .. i */
   float* lse;               /* [num_tokens][q_heads] or NULL */
   const float* scores_in;   /* [num_seqs][kv_heads][scores_stride] or NULL (0) */
-  float* scores_out;        /* the same shape; may be scores_in; NULL: no scores */
+  float* scores_out;        /* the same shape; may be scores_in, else apart from it; NULL: no scores */
   const float* k_scale;
   const float* v_scale;
   void* workspace;          /* mma_kv_attention_workspace bytes of device memory, 256-byte aligned, the
@@ -566,7 +566,7 @@ mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma
 typedef struct mma_kv_commit {
   const int32_t* accepted;  /* [num_seqs][accepted_stride]: drafted tokens, ascending */
   const int32_t* counts;    /* [num_seqs]: how many of a row */
-  int32_t* lens_out;        /* [num_seqs] or NULL: lens + counts; not seqs->lens */
+  int32_t* lens_out;        /* [num_seqs] or NULL: lens + counts; apart from lens, counts and accepted */
   float* const* scores;     /* host array of num_layers device pointers, each to
                                [num_seqs][kv_heads][scores_stride], or NULL */
   uint32_t accepted_stride;
@@ -585,7 +585,7 @@ typedef struct mma_kv_evict {
   const float* scores;      /* [num_seqs][kv_heads][scores_stride] */
   int32_t* entries;         /* [num_seqs][kv_heads][keep]: the entries kept, ascending, -1 behind them */
   float* scores_out;        /* [num_seqs][kv_heads][keep] or NULL: their scores, 0 behind them */
-  int32_t* lens_out;        /* [num_seqs] or NULL; not seqs->lens */
+  int32_t* lens_out;        /* [num_seqs] or NULL; apart from seqs->lens, as entries and scores_out from scores */
   void* workspace;          /* mma_kv_evict_workspace bytes of device memory, 8-byte aligned, as for attention */
   uint64_t workspace_bytes;
   uint32_t dst_stride;      /* at least keep / block_tokens, rounded up */

@@ -56,6 +56,13 @@ uint64_t extent(uint64_t n, uint64_t m, uint64_t bytes) {
   return r;
 }
 
+// An output and an input that the kernels read while others of the same launch write: they may not share memory.
+mma_status_t apart(const char* out, const void* p, uint64_t n, const char* in, const void* q, uint64_t m) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p), b = reinterpret_cast<uint64_t>(q);
+  if (!p || !q || !n || !m || (a < b ? b - a >= n : a - b >= m)) return MMA_OK;
+  return fail(MMA_ERR_INVALID_ARG, "%s overlaps %s", out, in);
+}
+
 mma_status_t device_range(Call* call, const void* p, uint64_t bytes) {
   const uint64_t at = reinterpret_cast<uint64_t>(p);
   for (const Known& k : call->known)
@@ -449,6 +456,8 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
   if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
   if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
+  if (a->scores_in != a->scores_out && (s = apart("scores_out", a->scores_out, score_bytes, "scores_in", a->scores_in, score_bytes)))
+    return s;
   k.c = call.c;
   k.s = call.s;
   k.scores_in = a->scores_in;
@@ -522,13 +531,16 @@ mma_status_t mma_kv_commit(const mma_kv_layout_t* layout, void* const* gpu_layer
   if ((s = check_seqs_sizes(seqs, layout->block_tokens))) return s;
   if (a->scores && a->scores_stride < seqs->max_len)
     return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
-  if (a->lens_out && a->lens_out == seqs->lens) return fail(MMA_ERR_INVALID_ARG, "lens_out is seqs->lens");
+  const uint64_t each = 4ull * seqs->num_seqs;
+  if ((s = apart("lens_out", a->lens_out, each, "seqs->lens", seqs->lens, each))) return s;
+  if ((s = apart("lens_out", a->lens_out, each, "counts", a->counts, each))) return s;
+  if ((s = apart("lens_out", a->lens_out, each, "accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4)))) return s;
   if (!seqs->num_seqs || (!a->accepted_stride && !a->lens_out)) return MMA_OK;  // lists of no places still give lens_out
   Device dev(call.device);
   if ((s = check_seqs(seqs, layout->block_tokens, INT32_MAX, &call))) return s;
   if ((s = array(&call, "accepted", a->accepted, extent(seqs->num_seqs, a->accepted_stride, 4), 4, !a->accepted_stride))) return s;
-  if ((s = array(&call, "counts", a->counts, 4ull * seqs->num_seqs, 4))) return s;
-  if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
+  if ((s = array(&call, "counts", a->counts, each, 4))) return s;
+  if ((s = array(&call, "lens_out", a->lens_out, each, 4, true))) return s;
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads, a->scores_stride, 4);
   for (uint32_t l = 0; l < layout->num_layers; ++l) {
     if ((s = array(&call, "a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
@@ -584,17 +596,20 @@ mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_
     return fail(MMA_ERR_INVALID_ARG, "dst_stride %u blocks do not hold %u entries", a->dst_stride, a->keep);
   if (a->scores_stride < seqs->max_len)
     return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
-  if (a->lens_out && a->lens_out == seqs->lens) return fail(MMA_ERR_INVALID_ARG, "lens_out is seqs->lens");
+  const uint64_t each = 4ull * seqs->num_seqs, heads = static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads;
+  const uint64_t score_bytes = extent(heads, a->scores_stride, 4), kept_bytes = extent(heads, a->keep, 4);
+  if ((s = apart("lens_out", a->lens_out, each, "seqs->lens", seqs->lens, each))) return s;
+  if ((s = apart("scores_out", a->scores_out, kept_bytes, "scores", a->scores, score_bytes))) return s;
+  if ((s = apart("entries", a->entries, kept_bytes, "scores", a->scores, score_bytes))) return s;
   if (!seqs->num_seqs) return MMA_OK;
   Device dev(call.device);
   if ((s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, 0, &call))) return s;
-  const uint64_t heads = static_cast<uint64_t>(seqs->num_seqs) * layout->kv_heads;
   if ((s = array(&call, "dst_table", a->dst_table, extent(seqs->num_seqs, a->dst_stride, 4), 4))) return s;
-  if ((s = array(&call, "scores", a->scores, extent(heads, a->scores_stride, 4), 4))) return s;
-  if ((s = array(&call, "entries", a->entries, extent(heads, a->keep, 4), 4))) return s;
-  if ((s = array(&call, "scores_out", a->scores_out, extent(heads, a->keep, 4), 4, true))) return s;
-  if ((s = array(&call, "lens_out", a->lens_out, 4ull * seqs->num_seqs, 4, true))) return s;
+  if ((s = array(&call, "scores", a->scores, score_bytes, 4))) return s;
+  if ((s = array(&call, "entries", a->entries, kept_bytes, 4))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, kept_bytes, 4, true))) return s;
+  if ((s = array(&call, "lens_out", a->lens_out, each, 4, true))) return s;
   const uint64_t need = evict_workspace(seqs, layout->kv_heads);
   if (a->workspace_bytes < need)
     return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",

@@ -1132,3 +1132,34 @@ def test_attention_over_8_bits_loses_no_bits_of_bf16(layout, dim, tokens, lens, 
     tol = u * want["out"].abs() * (1 + 2 * u) + (2.0 ** -11 + p_err) * want["mag"] * (1 + 2 * u) + STEP[BF16]
     worst = ((out - want["out"]).abs() / tol).max().item()
     assert worst <= 1, f"{worst:.3g} of the tolerance"
+
+
+def test_outputs_that_share_memory_with_inputs_are_refused():
+    """Lengths, lists and scores that some workgroups read while others write: refused before a launch."""
+    c = Case("piece", BF16, [40, 20], [3, 3], heads=2)
+    lay, seqs, layer = c.layout(), c.seqs(), c.flat[0].cuda()
+    keep = [layer.clone(), seqs.tensors[1].clone()]
+    x = torch.zeros(64, dtype=torch.int32, device="cuda")
+    at = lambda i: x.data_ptr() + 4 * i  # noqa: E731
+    layers = mma.layer_table([layer])
+    call = lambda acc, cnt, out: mma.lib.mma_kv_commit(lay, layers, seqs.c, mma.mma_kv_commit_t(acc, cnt, out, 0, 4, 0), 0)  # noqa: E731
+    lens = seqs.tensors[1].data_ptr()
+    for out in (at(8), at(9), at(7), at(0), at(6), lens, lens + 4):  # accepted is 0 .. 7, counts 8 and 9
+        assert call(at(0), at(8), out) == mma.MMA_ERR_INVALID_ARG
+        assert "overlaps" in mma.lib.mma_last_error().decode()
+    assert call(at(0), at(8), at(10)) == mma.MMA_OK
+    s = torch.rand(2, 2, 64, device="cuda")
+    dst = c.spare[:2].view(2, 1).cuda()
+    ws = torch.empty(mma.kv_evict_workspace(lay, seqs), dtype=torch.uint8, device="cuda")
+    ent = torch.empty(2, 2, 10, dtype=torch.int32, device="cuda")
+    ev = lambda entries, out, lens_out: mma.lib.mma_kv_evict(lay, layer.data_ptr(), seqs.c, mma.mma_kv_evict_t(  # noqa: E731
+        dst.data_ptr(), s.data_ptr(), entries, out, lens_out, ws.data_ptr(), ws.numel(), 1, 64, 10, 0, 0), 0)
+    for bad in ((ent.data_ptr(), s.data_ptr(), 0), (ent.data_ptr(), s.data_ptr() + 4 * 255, 0), (s.data_ptr() + 40, 0, 0),
+                (ent.data_ptr(), 0, lens)):
+        assert ev(*bad) == mma.MMA_ERR_INVALID_ARG
+    q = torch.zeros(6, 8, 128, dtype=BF16, device="cuda")
+    more = torch.rand(2 * 2 * 64 + 8, device="cuda")
+    a, b = more[:256].view(2, 2, 64), more[8:].view(2, 2, 64)
+    refused(lambda: mma.mma_kv_attention(lay, layer, seqs, q, scores_in=a, scores_out=b))
+    torch.cuda.synchronize()
+    assert same_bits(layer, keep[0]) and torch.equal(seqs.tensors[1], keep[1])
