@@ -328,10 +328,10 @@ __device__ __forceinline__ void store_row(const AttnArgs& a, uint32_t token, uin
 // layout, where 8 tokens of a value are contiguous, as it stands. Blocks hold a multiple of 8
 // tokens here: a lane's keys of a tile and its values' keys are in one block each, whose
 // table entries are read two tiles ahead, keys one tile ahead, values in the tile.
-// Bound by the bytes in flight: its registers let two waves on a SIMD (a bound of three spilled: 223
-// us instead of 123 for 32 sequences of 1k to 8k). 4 rows, one sequence of 64k entries, bf16, heads
-// of 128: 63 us, 4.3 TB/s; the same entries of 8 bits 33 us; 100 entries 7 us, the chain of loads
-// from the length over the table to the entry.
+// Bound by the bytes in flight: its registers let two waves on a SIMD (a bound of three spilled: 32 sequences of 1k to 8k,
+// 4 rows, heads of 128, x-packed, 179 us instead of 128 in bf16, 112 instead of 74 in 8 bits). 4 rows, one sequence of 64k
+// entries, bf16, heads of 128, piece layout, logits kept: 63 us, 4.3 TB/s; the same entries of 8 bits, none kept, 32
+// us with the join; 100 entries 7 us, the chain of loads from the length over the table to the entry.
 template <bool F8, int DP, bool VX>
 struct Stream {
   static constexpr int KS = DP / 32;                  // instructions of 32 head values
@@ -420,8 +420,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
   typedef ValueType<T, F8> TV;
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   // Workgroups go to the 8 XCDs in turn: heads and sequences first, so that each XCD has early and late splits alike
-  // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 141 us and more
-  // instead of 123 for 32 sequences of 1k to 8k).
+  // (late ones exist of long sequences only; with splits first, counts of 4 and 8 left XCDs idle: 147 us instead of 128
+  // for 32 sequences of 1k to 8k, 4 rows, x-packed bf16, and 86 instead of 74 in 8 bits).
   const uint32_t pairs = a.c.heads * a.s.num_seqs, pair = blockIdx.x % pairs, split = blockIdx.x / pairs;
   const uint32_t head = pair % a.c.heads, seq = pair / a.c.heads;
   const SeqSpan sp = span_of(a.s, seq);
@@ -623,12 +623,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
 // What probabilities are taken from follows the row's maximum only where one would pass
 // 2^kRowsRoom (2^8 in bf16): the factor is 1 otherwise and nothing is scaled.
 //
-// 2048 tokens of 32 heads behind 6144 entries (8 KV heads, 128 values, bf16): 281 us, 0.85
-// PFLOP/s, where a plain matrix product of the library reaches 1.09. Without the fetches a tile
+// 2048 tokens of 32 heads behind 6144 entries (8 KV heads, 128 values, bf16, head-major): 284 us, 0.85
+// PFLOP/s, where a plain matrix product of the library reaches 1.37 (8192^3, both over hundreds of
+// passes; over 40 after a rest of the GPU, 331 us, 0.73 PFLOP/s, and 1.29). Without the fetches a tile
 // takes 12 % less, without the exponentials the same, without the reads of V 10 %: no one of
-// them bounds it, the chain through a tile of few waves does. 4 trees of 24 tokens over 15k 8-bit
-// x-packed entries: 58 us, as many workgroups as run at once and their widening; 4 rows over 32
-// sequences of 1k to 8k, bf16: 112 us, 5.5 TB/s.
+// them bounds it, the chain through a tile of few waves does. 4 trees of 13 to 24 tokens over 3k to 15k 8-bit
+// x-packed entries: 56 us; splits are cut for the longest, so that 248 of 480 workgroups have entries, up to 1024 each,
+// and pass a widened tile every 1.7 us. 4 rows over 32 sequences of 1k to 8k, bf16, head-major: 114 us, 5.4 TB/s.
 template <bool F8, int DP, bool VX>
 struct Tiles {
   static constexpr int KT = DP == 256 || (F8 && DP == 128) ? 32 : 64;  // entries of a tile

@@ -190,7 +190,8 @@ __device__ __forceinline__ void append_turned(const AppendArgs& a, uint32_t firs
 // them. Where there are many tokens it takes all: what the rows share (position, place in the
 // cache, cosines and sines) is then read once. The first workgroups, whose chain of loads is longest, turn x-packed
 // values. One token: 4.3 us, a launch and that chain; 4095 tokens of 48 rows of 128 f16 values (86 MB): 17.9 us, 4.8
-// TB/s, memory; 680 tokens to x-packed 8 bits (12 MB): 9.8 us, the chain.
+// TB/s, memory; 680 tokens to x-packed 8 bits (12 MB): 9.8 us, the chain and then single bytes, as a draft's run seldom fills
+// 16 aligned tokens of a value, from as many threads as a head has values.
 template <class T, bool F8, bool VX, int L>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t parts) {
   constexpr uint32_t kRows = 256 / L;

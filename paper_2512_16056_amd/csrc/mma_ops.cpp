@@ -253,12 +253,13 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   p.rows = static_cast<uint32_t>(tokens * group);
   p.dim_pad = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
   // Up to two tiles of rows have their keys in registers (one with heads above 128: the second would not fit
-  // them), if a lane's 8 keys share a block. 8-bit and x-packed entries are best there throughout (32 rows, 4 trees
-  // over 15k entries, 8 bits: 32 us, through LDS 49; 4 rows, 32 sequences of up to 8k, x-packed: 122 against 151).
-  // Of 16-bit entries with heads of 65 to 128 V costs registers to be turned in, and from 17 rows on LDS is better
-  // (32 rows, 4 x 15k: 52 against 41), with fewer from some thousands of entries on, unless their logits are kept
-  // (4 rows, 4 x 15k: 45 against 38, 64k: 61 against 57; but 6 x 900: 12.1 against 14.2, 64k and scores: 70 against
-  // 92). Below 65 the two are within 5 %, above 128 the registers win (32 x 8k: 248 against 379).
+  // them), if a lane's 8 keys share a block. 8 KV heads of 128 unless said. 8-bit and x-packed entries are best there
+  // throughout (32 rows, 4 sequences of 3k to 15k, 8-bit x-packed: 32 us, through LDS 56; 4 rows, 32 sequences of 1k to 8k,
+  // x-packed bf16: 128 against 153, 8-bit head-major 77 against 154). Of 16-bit entries with heads of 65 to 128 V costs
+  // registers to be turned in, and from 17 rows on LDS is better, with fewer from some thousands of entries on, unless
+  // their logits are kept (4 rows, bf16: 4 of 3k to 15k, head-major, 38.6 against 34.7, 32 of 1k to 8k 130 against 125, 64k in
+  // pieces 59 against 55; but 6 x 900, head-major, 12.7 against 14.4, 64k with weights 70 against 83). Below 65 the two are
+  // within 8 % (70 against 76), above 128 the registers win (4 heads of 256: 164 against 215).
   const bool two = stream_two_tiles(p.dim_pad, layout.elem_bytes == 1, layout.gpu_layout == MMA_KV_LAYOUT_XPACKED);
   p.stream = p.rows <= (two ? 32u : 16u) && c.tokens % 8 == 0;
   if (p.dim_pad == 128 && !two && q.max_len > 4096 && !a.scores_out) p.stream = false;
@@ -267,8 +268,10 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
   // Workgroups in all: the 512 that run at once, so that all end together; but 2048 where many sequences, likely of
-  // different lengths, would leave some of those idle (32 of 1k to 8k: 124 us against 138). Entries of a split: 256 at
-  // least (4 rows over 1000 or 4096 entries: 128 the same, 512 14.3 and 15.2 us against 12.0 and 12.5).
+  // different lengths, would leave some of those idle (4 rows, 8 heads of 128, x-packed bf16: 32 of 1k to 8k 126 us against
+  // 133, 8 heads of 64 in pieces 78 against 98). Where they are alike, or short, it costs: 32 of 4095 104 against 99, 64 of up
+  // to 2k 67 against 59, in 8 bits 42 against 35. Entries of a split: 256 at least (4 rows over 1000 or 4096 entries: 128 the
+  // same, 512 14.3 and 15.2 us against 12.0 and 12.5).
   const bool many = p.stream && static_cast<uint64_t>(q.num_seqs) * c.heads >= 64;
   const uint64_t want = many ? 2048 : 512, least = 256;
   uint64_t splits = wgs >= want ? 1 : up(want, std::max<uint64_t>(wgs, 1));
