@@ -465,7 +465,9 @@ def _empty_on(stream, shape, dtype, device) -> torch.Tensor:
 
 class KVSeqs:
     """The sequences of a call (``mma_kv_seqs_t``) and the tensors that it points to. Built once per step, or
-    kept while its tensors' addresses and the two bounds stay: what the tensors hold may change between calls."""
+    kept while its tensors' addresses and the two bounds stay: what the tensors hold may change between calls. Tokens
+    of a sequence past max_tokens (1 unless given to kv_seqs) are left out of a call, their rows of an attention's output
+    unwritten; max_len also sets how attention cuts its work, so it is best near the longest sequence."""
 
     def __init__(self, block_table: torch.Tensor, lens: torch.Tensor, q_start: Optional[torch.Tensor] = None, *,
                  max_tokens: int, max_len: int):
