@@ -568,6 +568,31 @@ mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, 
 mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs,
                                         const mma_kv_attention_t* args, uint64_t* bytes);
 
+/* What a model makes of a score before the softmax, and which entries its tokens see. The token of entry
+ * i and entry j (lens[s] + t is token t's entry): x = scale * q . K; with a cap c > 0, c tanh(x / c); then
+ * less slopes[head] * |i - j|. It sees j < prefix[s] (in both directions: an image, a document read as
+ * a whole, or with a window the first entries that stay in sight), and of the others those with j <= i
+ * and, with a window, i - j < window. Entries that a call's tokens do not see are not read.
+ * The cap goes with a tree; the others do not, as a tree does not tell a drafted token's distance. */
+typedef struct mma_kv_shape {
+  const float* slopes;      /* [q_heads] or NULL (0); -infinity, infinity and NaN make rows that are not numbers */
+  const int32_t* prefix;    /* [num_seqs] or NULL (0); below 0: 0; entries that the sequence has not yet are not seen */
+  uint32_t max_prefix;      /* no sequence has a longer prefix (further entries are left out of it); with a window the
+                               work is cut by it, as by max_len */
+  uint32_t window;          /* 0: none */
+  float softcap;            /* 0: none; else from 1e-6 to 1e6 */
+} mma_kv_shape_t;
+
+/* mma_kv_attention with such scores; lse and the weights of the entries are of the shaped ones. NULL, or a
+ * shape of nothing: mma_kv_attention. The cap's tanh is within 2^-22 of the cap. */
+mma_status_t mma_kv_attention_shaped(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
+                                     const mma_kv_attention_t* args, const mma_kv_shape_t* shape, void* stream);
+
+/* Host only: the workspace of that call; of the shape's pointers only whether they are NULL matters. */
+mma_status_t mma_kv_attention_shaped_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs,
+                                               const mma_kv_attention_t* args, const mma_kv_shape_t* shape,
+                                               uint64_t* bytes);
+
 typedef struct mma_kv_commit {
   const int32_t* accepted;  /* [num_seqs][accepted_stride]: drafted tokens, ascending */
   const int32_t* counts;    /* [num_seqs]: how many of a row */

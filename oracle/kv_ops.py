@@ -97,9 +97,10 @@ def spans(c: Cache, table, lens, q_start, num_tokens, max_tokens, max_len):
 
 
 def attention(c: Cache, flat, table, span, q, group, scale, tree=None, k_scale=None, v_scale=None, scores_in=None,
-              decay=1.0):
+              decay=1.0, cap=0.0, slopes=None, window=0, prefix=None, max_prefix=None):
     """out, lse, scores [sequences][heads][...] (NaN where nothing is written) and, for error bounds, sum p |V|
-    and the largest |logit| of each row."""
+    and the largest |logit| of each row. cap, slopes (of each query head), window and prefix (of each sequence) shape the
+    logits and what is seen."""
     total, heads_q, dim = q.shape
     out = torch.zeros(total, heads_q, dim, dtype=torch.float64)
     mag = torch.zeros_like(out)
@@ -122,7 +123,14 @@ def attention(c: Cache, flat, table, span, q, group, scale, tree=None, k_scale=N
             mass = torch.zeros(m, dtype=torch.float64)
             for i in range(t):
                 sees = there.clone()
+                if tree is None and (window or prefix is not None):
+                    j = torch.arange(m)
+                    ahead = 0 if prefix is None else max(0, int(prefix[s]))
+                    ahead = ahead if max_prefix is None else min(ahead, max_prefix)
+                    sees &= (j < ahead) | ((j <= n + i) & ((n + i - j < window) if window else True))
                 for d in range(m - n):
+                    if tree is None and (window or prefix is not None):
+                        break
                     if tree is None:
                         sees[n + d] &= d <= i
                     else:
@@ -132,6 +140,10 @@ def attention(c: Cache, flat, table, span, q, group, scale, tree=None, k_scale=N
                     if not bool(sees.any()):
                         continue
                     x = (k[sees] @ q[a + i, e].double()) * scale
+                    if cap:
+                        x = cap * torch.tanh(x / cap)
+                    if slopes is not None:
+                        x = x - float(slopes[e]) * (n + i - torch.arange(m)[sees]).abs()
                     w = torch.logsumexp(x, 0)
                     p = torch.exp(x - w)
                     out[a + i, e] = p @ v[sees]

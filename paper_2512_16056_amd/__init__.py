@@ -174,6 +174,11 @@ class mma_kv_attention_t(ctypes.Structure):
                 ("scale", ctypes.c_float), ("decay", ctypes.c_float)]
 
 
+class mma_kv_shape_t(ctypes.Structure):
+    _fields_ = [("slopes", ctypes.c_void_p), ("prefix", ctypes.c_void_p), ("max_prefix", ctypes.c_uint32),
+                ("window", ctypes.c_uint32), ("softcap", ctypes.c_float)]
+
+
 class mma_kv_commit_t(ctypes.Structure):
     _fields_ = [("accepted", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("lens_out", ctypes.c_void_p),
                 ("scores", ctypes.c_void_p), ("accepted_stride", ctypes.c_uint32), ("scores_stride", ctypes.c_uint32)]
@@ -219,6 +224,11 @@ _SIGNATURES = {
                           ctypes.POINTER(mma_kv_attention_t), _P], _S),
     "mma_kv_attention_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(mma_kv_seqs_t),
                                     ctypes.POINTER(mma_kv_attention_t), ctypes.POINTER(_U64)], _S),
+    "mma_kv_attention_shaped": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
+                                 ctypes.POINTER(mma_kv_attention_t), ctypes.POINTER(mma_kv_shape_t), _P], _S),
+    "mma_kv_attention_shaped_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(mma_kv_seqs_t),
+                                           ctypes.POINTER(mma_kv_attention_t), ctypes.POINTER(mma_kv_shape_t),
+                                           ctypes.POINTER(_U64)], _S),
     "mma_kv_commit": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
                        ctypes.POINTER(mma_kv_commit_t), _P], _S),
     "mma_kv_evict": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
@@ -515,30 +525,40 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
                      scores_in: Optional[torch.Tensor] = None, scores_out: Optional[torch.Tensor] = None,
                      decay: float = 1.0, k_scale: Optional[torch.Tensor] = None,
                      v_scale: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     softcap: float = 0.0, window: int = 0, slopes: Optional[torch.Tensor] = None,
+                     prefix: Optional[torch.Tensor] = None, max_prefix: Optional[int] = None,
                      stream=None) -> torch.Tensor:
     """Attention of the call's tokens over their sequences' entries; returns `out` (or a new tensor). `tree`: int64
     [tokens][words] bits. `scale`: 1 / sqrt(head_dim) unless given. `workspace`: a uint8 tensor of
-    kv_attention_workspace() bytes or more; a new one of the stream's unless given."""
+    kv_attention_workspace() bytes or more; a new one of the stream's unless given.
+
+    Scores have the shape of ``mma_kv_shape_t``: capped (`softcap`), less `slopes` (float32 [heads]) times the distance, seen
+    within `window` entries up to the token's own, and in both directions within `prefix` (int32 [sequences]) entries, of
+    which no sequence has more than `max_prefix` (max_len unless given)."""
     if stream is not None:
         if out is None:
             out = _empty_on(stream, q.shape, q.dtype, q.device)
         if workspace is None:
-            need = kv_attention_workspace(layout, seqs, q.shape[0], q.shape[1], q.dtype, scores_out is not None)
+            need = kv_attention_workspace(layout, seqs, q.shape[0], q.shape[1], q.dtype, scores_out is not None, window=window,
+                                          prefix=prefix is not None, max_prefix=max_prefix)
             workspace = _empty_on(stream, (need,), torch.uint8, q.device)
     return _kv_ops.attention(layout, layer, seqs.address, q, out, scale, tree, lse, scores_in, scores_out, decay, k_scale,
-                             v_scale, workspace, _stream(stream))
+                             v_scale, workspace, _stream(stream), softcap, window, slopes, prefix, max_prefix)
 
 
 def kv_attention_workspace(layout: mma_kv_layout_t, seqs: KVSeqs, num_tokens: int, q_heads: int, dtype: torch.dtype,
-                           scores: bool = False) -> int:
-    """Bytes of workspace of an attention call of these sizes."""
+                           scores: bool = False, *, window: int = 0, prefix: bool = False,
+                           max_prefix: Optional[int] = None) -> int:
+    """Bytes of workspace of an attention call of these sizes; with a window a call needs fewer."""
     kind = _TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"queries of {dtype}: bfloat16 or float16 is wanted")
     a = mma_kv_attention_t(num_tokens=num_tokens, q_heads=q_heads, type=kind, scores_out=1 if scores else None,
                            cache_type=MMA_TYPE_F8 if layout.elem_bytes == 1 else kind)
     need = _U64()
-    _check(lib.mma_kv_attention_workspace(layout, seqs.c, a, need), "mma_kv_attention_workspace")
+    shape = mma_kv_shape_t(prefix=1 if prefix else None, max_prefix=seqs.max_len if max_prefix is None else max_prefix,
+                           window=window)
+    _check(lib.mma_kv_attention_shaped_workspace(layout, seqs.c, a, shape, need), "mma_kv_attention_shaped_workspace")
     return need.value
 
 
@@ -610,7 +630,8 @@ def _load_kv_ops():
     spec = importlib.util.spec_from_file_location("_kv_ops", path)
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
-    names = ("append", "attention", "attention_workspace", "commit", "evict", "evict_workspace")
+    names = ("append", "attention", "attention_workspace", "commit", "evict", "evict_workspace", "attention_shaped",
+             "attention_shaped_workspace")
     m.attach(*(ctypes.cast(getattr(lib, "mma_kv_" + x), _P).value for x in names), _check, _ptr)
     return m
 

@@ -33,6 +33,7 @@ SOURCES = {
     "mma_plan.cpp": ["-x", "c++"],
     "mma_ops.cpp": ["-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{os.path.join(ROCM, 'include')}"],
     "mma_attention.hip": DEVICE,
+    "mma_attention_shaped.hip": DEVICE,
     "mma_kv_ops.hip": DEVICE,
 }
 

@@ -246,7 +246,7 @@ uint64_t up_to(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
 // the group each) go in tiles of 16; the entries go in splits, joined afterwards, where
 // sequences, heads and rows alone are too few workgroups for 256 CUs.
 AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const mma_kv_seqs_t& q,
-                        const mma_kv_attention_t& a) {
+                        const mma_kv_attention_t& a, const mma_kv_shape_t* shape) {
   AttnPlan p{};
   const uint32_t group = a.q_heads / c.heads;
   const uint64_t tokens = std::min(q.max_tokens, a.num_tokens);
@@ -262,10 +262,20 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   // within 8 % (70 against 76), above 128 the registers win (4 heads of 256: 164 against 215).
   const bool two = stream_two_tiles(p.dim_pad, layout.elem_bytes == 1, layout.gpu_layout == MMA_KV_LAYOUT_XPACKED);
   p.stream = p.rows <= (two ? 32u : 16u) && c.tokens % 8 == 0;
-  if (p.dim_pad == 128 && !two && q.max_len > 4096 && !a.scores_out) p.stream = false;
+  // Entries that a workgroup's rows walk over: with a window those of the prefix and of its tokens' windows, each to a
+  // multiple of 64, and no more than there are.
+  const auto walked = [&](uint32_t wg_rows) -> uint32_t {
+    if (!shape || !shape->window) return q.max_len;
+    const uint64_t prefix = shape->prefix ? std::min(shape->max_prefix, q.max_len) : 0;
+    const uint64_t most = up_to(prefix, 64) + std::min<uint64_t>(tokens, wg_rows / group + 2) + shape->window + 64;
+    return static_cast<uint32_t>(std::min<uint64_t>(most, q.max_len));
+  };
+  if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out) p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
-  p.row_groups = up(p.rows, per_tile * p.tiles_per_wave);
+  p.wg_rows = per_tile * p.tiles_per_wave;
+  p.row_groups = up(p.rows, p.wg_rows);
+  const uint32_t most = walked(p.wg_rows);
   const uint64_t wgs = static_cast<uint64_t>(q.num_seqs) * c.heads * p.row_groups;
   // Workgroups in all: the 512 that run at once, so that all end together; but 2048 where many sequences, likely of
   // different lengths, would leave some of those idle (4 rows, 8 heads of 128, x-packed bf16: 32 of 1k to 8k 126 us against
@@ -275,9 +285,9 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
   const bool many = p.stream && static_cast<uint64_t>(q.num_seqs) * c.heads >= 64;
   const uint64_t want = many ? 2048 : 512, least = 256;
   uint64_t splits = wgs >= want ? 1 : up(want, std::max<uint64_t>(wgs, 1));
-  splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, up(q.max_len, least)));
-  p.split_len = up(up(q.max_len, static_cast<uint32_t>(splits)), 128) * 128;
-  p.splits = up(q.max_len, p.split_len);
+  splits = std::max<uint64_t>(1, std::min<uint64_t>(splits, up(most, least)));
+  p.split_len = up(up(most, static_cast<uint32_t>(splits)), 128) * 128;
+  p.splits = up(most, p.split_len);
   const uint64_t units = static_cast<uint64_t>(a.num_tokens) * a.q_heads;
   if (p.splits > 1) p.part_bytes = up_to(units * p.splits * p.dim_pad * 4, 256);
   if (a.scores_out) {
@@ -309,15 +319,123 @@ uint64_t evict_workspace(const mma_kv_seqs_t* q, uint32_t kv_heads) {
   return static_cast<uint64_t>(q->num_seqs) * kv_heads * 8 * (1 + up(q->max_len, 1024));
 }
 
-// What the split goes by, checked where no pointer is needed.
+// What the split goes by, checked where no pointer is needed. A shape that shapes nothing becomes NULL.
 mma_status_t check_attention_sizes(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, const mma_kv_attention_t* a,
-                                   Call* call) {
+                                   const mma_kv_shape_t** shape, Call* call) {
   mma_status_t s;
   if (!a) return fail(MMA_ERR_INVALID_ARG, "NULL arguments");
+  if (const mma_kv_shape_t* x = *shape) {
+    if (x->softcap != 0 && !(x->softcap >= 1e-6f && x->softcap <= 1e6f))
+      return fail(MMA_ERR_INVALID_ARG, "softcap has to be 0, or from 1e-6 to 1e6");
+    if (a->tree && (x->slopes || x->prefix || x->window))
+      return fail(MMA_ERR_INVALID_ARG, "a drafted token's distance is not told by its tree: no slopes, prefix or window with one");
+    if (x->softcap == 0 && !x->slopes && !x->prefix && !x->window) *shape = nullptr;
+  }
   if ((s = check_layout(layout, call))) return s;
   if ((s = check_types(a->type, a->cache_type, layout->elem_bytes))) return s;
   if ((s = check_heads(a->q_heads, layout->kv_heads, a->num_tokens))) return s;
   return check_seqs_sizes(seqs, layout->block_tokens);
+}
+
+mma_status_t attention_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, const mma_kv_attention_t* a,
+                                 const mma_kv_shape_t* shape, uint64_t* bytes) {
+  if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  Call call;
+  if (mma_status_t s = check_attention_sizes(layout, seqs, a, &shape, &call)) return s;
+  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, *layout, *seqs, *a, shape).bytes : 0;
+  return MMA_OK;
+}
+
+mma_status_t attention(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
+                       const mma_kv_attention_t* a, const mma_kv_shape_t* shape, void* stream) {
+  mma_status_t s;
+  Call call;
+  if ((s = begin(&call))) return s;
+  if ((s = check_attention_sizes(layout, seqs, a, &shape, &call))) return s;
+  const uint32_t D = layout->head_dim, H = layout->kv_heads, n = a->num_tokens;
+  if (a->tree && !a->tree_words) return fail(MMA_ERR_INVALID_ARG, "a tree needs tree_words");
+  if (a->scores_in && !a->scores_out) return fail(MMA_ERR_INVALID_ARG, "scores_in without scores_out");
+  if (a->scores_out && a->scores_stride < seqs->max_len)
+    return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
+  const bool rows_too = n && seqs->max_tokens;  // else the entries' weights fade and no more
+  if (!seqs->num_seqs || (!rows_too && !a->scores_out)) return MMA_OK;
+  Device dev(call.device);
+  if (rows_too && (s = check_layer(layer, &call))) return s;
+  if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
+  ShapedArgs k{};
+  const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
+  if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
+  if (a->scores_in != a->scores_out && (s = apart("scores_out", a->scores_out, score_bytes, "scores_in", a->scores_in, score_bytes)))
+    return s;
+  k.c = call.c;
+  k.s = call.s;
+  k.scores_in = a->scores_in;
+  k.scores_out = a->scores_out;
+  k.scores_stride = a->scores_stride;
+  k.decay = a->decay;
+  const OpsKind kind{a->type, a->cache_type, layout->gpu_layout};
+  if (!rows_too)
+    return launched(launch_attention(k, AttnPlan{}, kind, static_cast<hipStream_t>(stream)), "KV attention");
+  if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
+  if ((s = rows(&call, "out", a->out, n, a->q_heads, D, true, &k.out))) return s;
+  if ((s = array(&call, "tree", a->tree, extent(n, a->tree_words, 8), 8, true))) return s;
+  if ((s = array(&call, "lse", a->lse, extent(n, a->q_heads, 4), 4, true))) return s;
+  if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
+  if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
+  const AttnPlan p = attention_plan(call.c, *layout, *seqs, *a, shape);
+  if (static_cast<uint64_t>(p.row_groups) * (static_cast<uint64_t>(p.splits) * H * seqs->num_seqs + 7) >= 1ull << 24)
+    return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
+                seqs->num_seqs, seqs->max_tokens, H);
+  if (p.bytes) {
+    if (a->workspace_bytes < p.bytes)
+      return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
+                  static_cast<unsigned long long>(a->workspace_bytes), static_cast<unsigned long long>(p.bytes));
+    if ((s = array(&call, "workspace", a->workspace, p.bytes, 256))) return s;
+  }
+  k.tree = a->tree;
+  k.lse = a->lse;
+  k.k_scale = a->cache_type == MMA_TYPE_F8 ? a->k_scale : nullptr;
+  k.v_scale = a->cache_type == MMA_TYPE_F8 ? a->v_scale : nullptr;
+  char* ws = static_cast<char*>(a->workspace);
+  const auto take = [&](uint64_t bytes) {
+    float* at = bytes ? reinterpret_cast<float*>(ws) : nullptr;
+    ws += bytes;
+    return at;
+  };
+  k.part = take(p.part_bytes);
+  k.part_ml = take(p.ml_bytes);
+  k.lse2 = take(p.lse_bytes);
+  k.score_q = k.q;
+  if (float* copy = take(p.q_bytes); copy && rows_meet(k.q, k.out, n, a->q_heads, D))
+    k.score_q = RowArgs{reinterpret_cast<uint8_t*>(copy), static_cast<uint64_t>(a->q_heads) * D, D};
+  k.logits = take(p.logit_bytes);
+  k.logit_rows = p.rows;
+  k.logit_stride = p.logit_stride;
+  k.q_heads = a->q_heads;
+  k.group = a->q_heads / H;
+  k.tree_words = a->tree_words;
+  // Entries of a workgroup: 32 for each of its waves where these stay, else 128 to 1024, its start being a few loads one
+  // after the other: the 512 workgroups that run at once for one sequence, twice as many for several, whose lengths
+  // differ (128 rows over 64k entries 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
+  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / (seqs->num_seqs == 1 ? 512 : 1024);
+  k.score_len = p.keys_stay ? 128 : static_cast<uint32_t>(std::clamp<uint64_t>(up_to(per, 128), 128, 1024));
+  k.splits = p.splits;
+  k.split_len = p.split_len;
+  k.wide_q = rows_wide(k.q);
+  k.wide_out = rows_wide(k.out);
+  k.wide_score_q = rows_wide(k.score_q);
+  k.scale = a->scale;
+  if (!shape) return launched(launch_attention(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
+  if ((s = array(&call, "slopes", shape->slopes, 4ull * a->q_heads, 4, true))) return s;
+  if ((s = array(&call, "prefix", shape->prefix, 4ull * seqs->num_seqs, 4, true))) return s;
+  k.slopes = shape->slopes;
+  k.prefix = shape->prefix;
+  k.max_prefix = shape->max_prefix;
+  k.window = std::min<uint32_t>(shape->window, INT32_MAX);
+  k.cap2 = shape->softcap * 1.44269504088896340736f;
+  k.wg_rows = p.wg_rows;
+  return launched(launch_attention_shaped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
 }
 
 }  // namespace
@@ -428,98 +546,30 @@ mma_status_t mma_kv_append(const mma_kv_layout_t* layout, void* layer, const mma
   return ops_boundary_error("mma_kv_append");
 }
 
+mma_status_t mma_kv_attention_shaped_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs,
+                                               const mma_kv_attention_t* a, const mma_kv_shape_t* shape, uint64_t* bytes) try {
+  return attention_workspace(layout, seqs, a, shape, bytes);
+} catch (...) {
+  return ops_boundary_error("mma_kv_attention_shaped_workspace");
+}
+
 mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs,
                                         const mma_kv_attention_t* a, uint64_t* bytes) try {
-  if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
-  Call call;
-  if (mma_status_t s = check_attention_sizes(layout, seqs, a, &call)) return s;
-  *bytes = a->num_tokens && seqs->num_seqs && seqs->max_tokens ? attention_plan(call.c, *layout, *seqs, *a).bytes : 0;
-  return MMA_OK;
+  return attention_workspace(layout, seqs, a, nullptr, bytes);
 } catch (...) {
   return ops_boundary_error("mma_kv_attention_workspace");
 }
 
+mma_status_t mma_kv_attention_shaped(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
+                                     const mma_kv_attention_t* a, const mma_kv_shape_t* shape, void* stream) try {
+  return attention(layout, layer, seqs, a, shape, stream);
+} catch (...) {
+  return ops_boundary_error("mma_kv_attention_shaped");
+}
+
 mma_status_t mma_kv_attention(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
                               const mma_kv_attention_t* a, void* stream) try {
-  mma_status_t s;
-  Call call;
-  if ((s = begin(&call))) return s;
-  if ((s = check_attention_sizes(layout, seqs, a, &call))) return s;
-  const uint32_t D = layout->head_dim, H = layout->kv_heads, n = a->num_tokens;
-  if (a->tree && !a->tree_words) return fail(MMA_ERR_INVALID_ARG, "a tree needs tree_words");
-  if (a->scores_in && !a->scores_out) return fail(MMA_ERR_INVALID_ARG, "scores_in without scores_out");
-  if (a->scores_out && a->scores_stride < seqs->max_len)
-    return fail(MMA_ERR_INVALID_ARG, "scores_stride %u is below max_len %u", a->scores_stride, seqs->max_len);
-  const bool rows_too = n && seqs->max_tokens;  // else the entries' weights fade and no more
-  if (!seqs->num_seqs || (!rows_too && !a->scores_out)) return MMA_OK;
-  Device dev(call.device);
-  if (rows_too && (s = check_layer(layer, &call))) return s;
-  if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
-  AttnArgs k{};
-  const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
-  if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
-  if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
-  if (a->scores_in != a->scores_out && (s = apart("scores_out", a->scores_out, score_bytes, "scores_in", a->scores_in, score_bytes)))
-    return s;
-  k.c = call.c;
-  k.s = call.s;
-  k.scores_in = a->scores_in;
-  k.scores_out = a->scores_out;
-  k.scores_stride = a->scores_stride;
-  k.decay = a->decay;
-  const OpsKind kind{a->type, a->cache_type, layout->gpu_layout};
-  if (!rows_too)
-    return launched(launch_attention(k, AttnPlan{}, kind, static_cast<hipStream_t>(stream)), "KV attention");
-  if ((s = rows(&call, "q", a->q, n, a->q_heads, D, false, &k.q))) return s;
-  if ((s = rows(&call, "out", a->out, n, a->q_heads, D, true, &k.out))) return s;
-  if ((s = array(&call, "tree", a->tree, extent(n, a->tree_words, 8), 8, true))) return s;
-  if ((s = array(&call, "lse", a->lse, extent(n, a->q_heads, 4), 4, true))) return s;
-  if ((s = array(&call, "k_scale", a->k_scale, 4ull * H, 4, true))) return s;
-  if ((s = array(&call, "v_scale", a->v_scale, 4ull * H, 4, true))) return s;
-  const AttnPlan p = attention_plan(call.c, *layout, *seqs, *a);
-  if (static_cast<uint64_t>(p.row_groups) * (static_cast<uint64_t>(p.splits) * H * seqs->num_seqs + 7) >= 1ull << 24)
-    return fail(MMA_ERR_INVALID_ARG, "%u sequences of up to %u tokens and %u KV heads are more workgroups than a launch takes",
-                seqs->num_seqs, seqs->max_tokens, H);
-  if (p.bytes) {
-    if (a->workspace_bytes < p.bytes)
-      return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
-                  static_cast<unsigned long long>(a->workspace_bytes), static_cast<unsigned long long>(p.bytes));
-    if ((s = array(&call, "workspace", a->workspace, p.bytes, 256))) return s;
-  }
-  k.tree = a->tree;
-  k.lse = a->lse;
-  k.k_scale = a->cache_type == MMA_TYPE_F8 ? a->k_scale : nullptr;
-  k.v_scale = a->cache_type == MMA_TYPE_F8 ? a->v_scale : nullptr;
-  char* ws = static_cast<char*>(a->workspace);
-  const auto take = [&](uint64_t bytes) {
-    float* at = bytes ? reinterpret_cast<float*>(ws) : nullptr;
-    ws += bytes;
-    return at;
-  };
-  k.part = take(p.part_bytes);
-  k.part_ml = take(p.ml_bytes);
-  k.lse2 = take(p.lse_bytes);
-  k.score_q = k.q;
-  if (float* copy = take(p.q_bytes); copy && rows_meet(k.q, k.out, n, a->q_heads, D))
-    k.score_q = RowArgs{reinterpret_cast<uint8_t*>(copy), static_cast<uint64_t>(a->q_heads) * D, D};
-  k.logits = take(p.logit_bytes);
-  k.logit_rows = p.rows;
-  k.logit_stride = p.logit_stride;
-  k.q_heads = a->q_heads;
-  k.group = a->q_heads / H;
-  k.tree_words = a->tree_words;
-  // Entries of a workgroup: 32 for each of its waves where these stay, else 128 to 1024, its start being a few loads one
-  // after the other: the 512 workgroups that run at once for one sequence, twice as many for several, whose lengths
-  // differ (128 rows over 64k entries 151 us, with 1024 workgroups 172; 96 rows over 4 x 15k: 104 and 88).
-  const uint64_t per = static_cast<uint64_t>(seqs->max_len) * seqs->num_seqs * H / (seqs->num_seqs == 1 ? 512 : 1024);
-  k.score_len = p.keys_stay ? 128 : static_cast<uint32_t>(std::clamp<uint64_t>(up_to(per, 128), 128, 1024));
-  k.splits = p.splits;
-  k.split_len = p.split_len;
-  k.wide_q = rows_wide(k.q);
-  k.wide_out = rows_wide(k.out);
-  k.wide_score_q = rows_wide(k.score_q);
-  k.scale = a->scale;
-  return launched(launch_attention(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
+  return attention(layout, layer, seqs, a, nullptr, stream);
 } catch (...) {
   return ops_boundary_error("mma_kv_attention");
 }

@@ -81,6 +81,18 @@ struct AttnArgs {
   uint32_t splits, split_len;  // entries of a split: a multiple of the tile
   uint32_t wide_q, wide_out, wide_score_q;  // rows start at 16 bytes
   float scale, decay;
+  static constexpr bool kShaped = false;
+};
+
+// Attention whose scores have a shape (mma_kv_shape_t).
+struct ShapedArgs : AttnArgs {
+  const float* slopes;    // [q_heads] or NULL
+  const int32_t* prefix;  // [num_seqs] or NULL
+  uint32_t max_prefix;
+  uint32_t window;        // entries up to a token's own, at most 2^31 - 1; 0: all
+  float cap2;             // the cap, base 2; 0: none
+  uint32_t wg_rows;       // rows of a workgroup
+  static constexpr bool kShaped = true;
 };
 
 struct CommitArgs {
@@ -118,6 +130,7 @@ struct AttnPlan {
   bool stream;              // attention_stream_kernel, else attention_rows_kernel
   uint32_t rows;            // most rows (token, head of a group) of one sequence and KV head
   uint32_t tiles_per_wave;  // of 16 rows
+  uint32_t wg_rows;         // rows of a workgroup
   uint32_t row_groups;      // workgroups that the rows take
   uint32_t splits, split_len;
   uint32_t dim_pad;
@@ -135,6 +148,7 @@ constexpr bool stream_two_tiles(uint32_t dim_pad, bool f8, bool xpacked) {
 
 hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stream);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
+hipError_t launch_attention_shaped(const ShapedArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream);
 

@@ -19,6 +19,8 @@ namespace {
 decltype(&mma_kv_append) g_append;
 decltype(&mma_kv_attention) g_attention;
 decltype(&mma_kv_attention_workspace) g_attention_workspace;
+decltype(&mma_kv_attention_shaped) g_attention_shaped;
+decltype(&mma_kv_attention_shaped_workspace) g_attention_shaped_workspace;
 decltype(&mma_kv_commit) g_commit;
 decltype(&mma_kv_evict) g_evict;
 decltype(&mma_kv_evict_workspace) g_evict_workspace;
@@ -209,7 +211,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  if (nargs != 15) REFUSE("15 arguments");
+  if (nargs != 20) REFUSE("20 arguments");
   const Common c(a[0], a[2]);
   const Queries q(a[3], c.layout);
   const int64_t H = c.layout->kv_heads, D = c.layout->head_dim;
@@ -239,19 +241,33 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   x.q_heads = size32(q.heads, "q");
   x.type = q.kind;
   x.cache_type = q.cache;
+  mma_kv_shape_t shape{};
+  shape.softcap = static_cast<float>(real(a[15]));
+  shape.window = count(a[16], "window");
+  shape.slopes = flat_ptr<float>(a[17], "slopes", at::kFloat, {q.heads});
+  shape.prefix = flat_ptr<int32_t>(a[18], "prefix", at::kInt, {c.seqs->num_seqs});
+  shape.max_prefix = a[19] == Py_None ? c.seqs->max_len : count(a[19], "max_prefix");
+  const bool shaped = shape.softcap != 0 || shape.window || a[17] != Py_None || a[18] != Py_None;
   at::Tensor own;
   if (a[13] != Py_None) {
     const at::Tensor& t = flat(a[13], "workspace", at::kByte, {-1});
     x.workspace = t.data_ptr();
     x.workspace_bytes = t.numel();
   } else {
-    check(g_attention_workspace(c.layout, c.seqs, &x, &x.workspace_bytes), "mma_kv_attention_workspace");
+    if (shaped)
+      check(g_attention_shaped_workspace(c.layout, c.seqs, &x, &shape, &x.workspace_bytes), "mma_kv_attention_shaped_workspace");
+    else
+      check(g_attention_workspace(c.layout, c.seqs, &x, &x.workspace_bytes), "mma_kv_attention_workspace");
     if (x.workspace_bytes) {
       own = fresh({static_cast<int64_t>(x.workspace_bytes)}, at::kByte, q.t);
       x.workspace = own.data_ptr();
     }
   }
-  check(g_attention(c.layout, layer(a[1], q.cache_type), c.seqs, &x, reinterpret_cast<void*>(number(a[14]))), "mma_kv_attention");
+  void* const stream = reinterpret_cast<void*>(number(a[14]));
+  if (shaped)
+    check(g_attention_shaped(c.layout, layer(a[1], q.cache_type), c.seqs, &x, &shape, stream), "mma_kv_attention_shaped");
+  else
+    check(g_attention(c.layout, layer(a[1], q.cache_type), c.seqs, &x, stream), "mma_kv_attention");
   return THPVariable_Wrap(out);
   } catch (const Refused&) {
     return nullptr;
@@ -329,12 +345,13 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 
 // The library's entry points and the two Python helpers.
 PyObject* attach(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  if (nargs != 8) {
-    PyErr_SetString(PyExc_ValueError, "8 arguments");
+  constexpr int kEntries = 8;
+  if (nargs != kEntries + 2) {
+    PyErr_SetString(PyExc_ValueError, "the entry points and two helpers");
     return nullptr;
   }
-  void* p[6];
-  for (int i = 0; i < 6; ++i) {
+  void* p[kEntries];
+  for (int i = 0; i < kEntries; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "NULL entry point"), nullptr);
   }
@@ -344,10 +361,12 @@ PyObject* attach(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   g_commit = reinterpret_cast<decltype(g_commit)>(p[3]);
   g_evict = reinterpret_cast<decltype(g_evict)>(p[4]);
   g_evict_workspace = reinterpret_cast<decltype(g_evict_workspace)>(p[5]);
-  Py_INCREF(a[6]);
-  g_check = a[6];
-  Py_INCREF(a[7]);
-  g_address = a[7];
+  g_attention_shaped = reinterpret_cast<decltype(g_attention_shaped)>(p[6]);
+  g_attention_shaped_workspace = reinterpret_cast<decltype(g_attention_shaped_workspace)>(p[7]);
+  Py_INCREF(a[kEntries]);
+  g_check = a[kEntries];
+  Py_INCREF(a[kEntries + 1]);
+  g_address = a[kEntries + 1];
   Py_RETURN_NONE;
 }
 

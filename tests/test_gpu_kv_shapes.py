@@ -1,0 +1,292 @@
+"""Attention whose scores are capped, biased by distance, kept to a window or seen both ways in a prefix, against the 64-bit
+reference (oracle.kv_ops).
+
+Tolerances are those of the plain scores (test_gpu_kv_ops), and of the shape, before any run: c tanh(x / c) is formed as
+c (1 - 2 / (1 + 2^y)), whose reciprocal has an error of one unit in its last place, 2^-23 of at most 1, and whose
+power's error of 2^-23 counts for half at most: below 2^-21 c. slope * |i - j| is a product and a sum, each rounded
+to 2^-24 of at most the logit and the bias. p carries an error in its logit and in the row's sum.
+"""
+import math
+
+import pytest
+import torch
+
+from oracle import kv_ops as ok
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+import paper_2512_16056_amd as mma  # noqa: E402
+from gpu_helpers import session  # noqa: E402
+from test_gpu_kv_ops import BF16, BITS, EPS, F8, F16, LAYOUTS, STEP, Case, normal, refused, same_bits, to_cache, tree_bits  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    with session():
+        yield
+
+
+def i32(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32)
+
+
+def check(c, cap=0.0, slopes=None, window=0, prefix=None, max_prefix=None, tree=None, scores=False, std=2.0, scale=None, q=None,
+          in_place=False, stream=None):
+    D = c.c.dim
+    q = normal(c.g, c.total, c.heads_q, D, std=std).to(c.dtype) if q is None else q
+    scale = D ** -0.5 if scale is None else scale
+    span = c.spans()
+    s_in = torch.rand(len(c.lens), c.c.heads, c.max_len + 5, generator=c.g) if scores else None
+    shape = dict(slopes=slopes, window=window, prefix=i32(prefix), max_prefix=max_prefix)
+    want = ok.attention(c.c, c.flat[0], c.table, span, q, c.group, scale, tree, c.k_scale, c.v_scale, s_in, 0.5, cap, **shape)
+    more = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in shape.items()}
+    if scores:
+        s_out = torch.full_like(s_in, -3.0).cuda()
+        more.update(scores_in=s_in.cuda(), scores_out=s_out, decay=0.5)
+    lse = torch.full((c.total, c.heads_q), 7.0, device="cuda")
+    layer, dev = c.flat[0].cuda(), q.cuda()
+    out = mma.mma_kv_attention(c.layout(), layer, c.seqs(), dev, out=dev if in_place else None, scale=scale, softcap=cap,
+                               tree=None if tree is None else tree.cuda(), lse=lse, **c.scales(), **more)
+    torch.cuda.synchronize()
+    assert same_bits(layer.cpu(), c.flat[0])
+    covered = torch.zeros(c.total, dtype=torch.bool)
+    for a, t, _, _ in span:
+        covered[a: a + t] = True
+    out, lse = out.cpu()[covered].double(), lse.cpu()[covered].double()
+    w = {x: want[x][covered] for x in ("out", "lse", "mag", "big")}
+    assert torch.equal(torch.isnan(w["out"]), torch.isnan(out))
+    finite = torch.isfinite(w["out"]) & torch.isfinite(w["mag"])
+    u = 2.0 ** -(BITS[c.dtype] + 1)
+    bias = 0.0 if slopes is None else slopes.abs().max().item() * c.max_len
+    x_err = 2 * D * EPS * w["big"] + 64 * EPS + 2 * (4 * EPS * cap + 4 * EPS * bias)
+    tol = u * w["out"].abs() * (1 + 2 * u) + (u + x_err[..., None]) * w["mag"] * (1 + 2 * u) + STEP[c.dtype]
+    worst = ((out - w["out"]).abs() / tol)[finite].max().item() if finite.any() else 0.0
+    assert worst <= 1, f"out: {worst:.3g} of the tolerance"
+    empty = w["lse"] == -math.inf
+    assert torch.equal(lse == -math.inf, empty) and not out[empty].any()
+    seen = ~empty & torch.isfinite(w["lse"])
+    err = (lse - w["lse"]).abs() / (x_err + 64 * EPS * w["lse"].abs())
+    assert not seen.any() or err[seen].max().item() <= 1, f"lse: {err[seen].max().item():.3g}"
+    if scores:
+        got = more["scores_out"].cpu().double()
+        written = torch.zeros(got.shape, dtype=torch.bool)
+        for s, (_, _, _, m) in enumerate(span):
+            written[s, :, :m] = True
+        assert (got[~written] == -3).all(), "scores past the entries changed"
+        exact = torch.zeros_like(got)
+        exact[:, :, : want["scores"].shape[2]] = want["scores"]
+        err = ((got - exact).abs() / (x_err.max() * (1 + exact.abs())))[written]
+        assert not err.numel() or err.max().item() <= 1, f"scores: {err.max().item():.3g} of the tolerance"
+    return out
+
+
+def alibi(heads):
+    return torch.tensor([2.0 ** (-8.0 * (h + 1) / heads) for h in range(heads)])
+
+
+CASES = [
+    # layout, cache, dim, tokens, heads, group, lens, counts: few rows and many, short contexts and split ones
+    ("piece", BF16, 128, 16, 2, 4, [101], [1]),
+    ("hnd", F16, 128, 16, 2, 4, [0, 1, 31, 32, 33, 700], [1, 1, 1, 1, 1, 1]),
+    ("xpacked", F8, 128, 16, 2, 4, [63, 0, 250], [24, 3, 70]),
+    ("xpacked", BF16, 64, 8, 1, 8, [5, 129], [2, 33]),
+    ("piece", F8, 80, 24, 1, 7, [77, 20], [9, 1]),
+    ("hnd", BF16, 96, 1, 2, 1, [40, 3], [5, 2]),
+    ("xpacked", F16, 256, 32, 1, 2, [300, 17], [3, 40]),
+    ("piece", F16, 256, 7, 1, 3, [90], [20]),
+    ("piece", BF16, 8, 3, 3, 2, [50, 0], [4, 1]),
+    ("hnd", F8, 64, 16, 2, 16, [500], [5]),
+    ("hnd", BF16, 72, 24, 1, 5, [200, 64, 65], [1, 13, 0]),
+    ("piece", BF16, 128, 16, 2, 4, [300, 0, 65], [40, 9, 12]),
+    ("xpacked", F8, 64, 16, 1, 4, [1500, 30], [4, 2]),
+    ("hnd", BF16, 64, 16, 1, 2, [10, 0], [200, 130]),
+    ("piece", BF16, 64, 16, 1, 2, [3000, 7], [1, 1]),
+]
+SHAPES = {
+    "cap": dict(cap=5.0),
+    "slopes": dict(slopes=True),
+    "window": dict(window=17),
+    "window_1": dict(window=1),
+    "window_long": dict(window=200, scores=True),
+    "prefix": dict(prefix=45),
+    "window_prefix": dict(window=33, prefix=5, scores=True),
+    "all": dict(cap=30.0, slopes=True, window=50, prefix=90, scores=True),
+}
+
+
+@pytest.mark.parametrize("shape", list(SHAPES))
+@pytest.mark.parametrize("layout,cache,dim,tokens,heads,group,lens,counts", CASES)
+def test_shapes(layout, cache, dim, tokens, heads, group, lens, counts, shape):
+    c = Case(layout, cache, lens, counts, dim, heads, group, tokens, F16 if cache is F16 else BF16)
+    kw = dict(SHAPES[shape])
+    if "slopes" in kw:
+        kw["slopes"] = alibi(c.heads_q)
+    if "prefix" in kw:  # the longest, one, none, and one past the end
+        kw["prefix"] = [(kw["prefix"], 1, 0, 10 ** 6)[s % 4] for s in range(len(lens))]
+        kw["max_prefix"] = max(kw["prefix"][0], 60)
+    check(c, **kw)
+
+
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_window_over_many_splits(layout):
+    """A window and a prefix that each take several splits, the gap between them passed over."""
+    for count in (1, 3, 40):
+        c = Case(layout, BF16, [5000, 10, 0, 1025], [count, 1, 1, count], heads=1, group=2, dim=64)
+        check(c, window=1100, prefix=[700, 3, 5, 1000], scores=True)
+
+
+@pytest.mark.parametrize("cache", [BF16, F8])
+def test_edges_of_window_and_prefix(cache):
+    """Every place of the window's and the prefix's ends in a tile and a block, one token and some."""
+    for n, edge in ((127, 0), (128, 1), (129, 31), (191, 32), (200, 33), (193, 63), (260, 64), (261, 65)):
+        for count in (1, 20):
+            c = Case("hnd", cache, [n], [count], heads=1, group=4, dim=64, seed=n)
+            check(c, window=1 + edge, prefix=[edge], scores=True)
+            check(c, window=n - edge, prefix=[n + count - edge])
+
+
+def test_prefix_is_bounded_and_may_be_of_nothing():
+    c = Case("piece", BF16, [100, 40], [30, 5], heads=1)
+    check(c, prefix=[-3, 0], window=7)
+    check(c, prefix=[90, 90], max_prefix=13, window=7, scores=True)
+    check(c, prefix=[90, 90], max_prefix=0)
+    check(c, prefix=[2 ** 31 - 1, 2 ** 31 - 1], max_prefix=2 ** 32 - 1)
+    check(c, window=2 ** 32 - 1)
+
+
+def test_cap_with_a_tree_and_negative_scale():
+    for layout in LAYOUTS:
+        c = Case(layout, BF16, [70, 0], [24, 5], heads=1)
+        check(c, cap=8.0, tree=tree_bits(c.counts, c.g, empty=True), scores=True)
+    c = Case("hnd", BF16, [300], [40], heads=1)
+    check(c, cap=8.0, scale=-0.3)
+    check(c, slopes=-alibi(c.heads_q) * 0.1, scale=-0.3)
+
+
+def test_cap_at_both_ends():
+    """Logits far past the cap are the cap; infinite ones too, where plain ones would be no numbers."""
+    for counts in ([1], [40]):
+        c = Case("hnd", BF16, [100], counts, heads=1)
+        check(c, cap=3.0, std=300.0)
+        c.flat[0][c.c.index(0, *c.c.entry(c.table[0], 7), 0)] = torch.tensor([math.inf] + [0.0] * 127, dtype=BF16)
+        q = normal(c.g, c.total, 4, 128).to(BF16)
+        q[:, :, 0] = 1.0
+        out = check(c, cap=3.0, q=q)
+        assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("cache", [BF16, F16, F8])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_infinities_behind_the_window(layout, cache):
+    """NaN and infinities in entries out of the window, K and V, reach no row."""
+    for counts in ([1, 2], [30, 21]):
+        c = Case(layout, cache, [300, 77], counts, heads=1, group=4, dtype=F16 if cache is F16 else BF16)
+        bad = torch.full((128,), 0x7F, dtype=torch.uint8) if cache is F8 else \
+            to_cache(torch.tensor([math.nan, math.inf, -math.inf, math.nan] * 32), cache)
+        for s, n in enumerate(c.lens):
+            for j in range(4, n - 40 + 1):
+                for which in (0, 1):
+                    c.flat[0][c.c.index(which, *c.c.entry(c.table[s], j), 0)] = bad
+        out = check(c, window=40, prefix=[4, 4], cap=20.0)
+        assert torch.isfinite(out).all()
+
+
+def test_missing_blocks_and_long_rows_of_tokens():
+    for layout in LAYOUTS:
+        c = Case(layout, BF16, [170, 33], [50, 2], heads=1)
+        c.table[0, 1] = -1
+        c.table[0, 8] = c.c.blocks + 7
+        c.table[1, :] = -1  # nothing there at all
+        check(c, window=60, prefix=[20, 20], cap=9.0, slopes=alibi(4), scores=True)
+
+
+def test_bounds_of_the_call():
+    """Tokens past max_len see what is left of their window; a window that ends before every entry leaves nothing."""
+    c = Case("piece", BF16, [10, 40, 20], [3, 40, 2], heads=1)
+    c.max_tokens, c.max_len = 30, 30
+    check(c, window=4)
+    check(c, window=4, prefix=[2, 3, 4])
+    c = Case("hnd", BF16, [-5, 40, 20], [3, 4, 2], heads=1)
+    c.lens[0] = -5
+    check(c, window=4, cap=3.0)
+
+
+def test_in_place_other_stream_and_captured():
+    c = Case("hnd", BF16, [3000, 70], [9, 3], heads=2)
+    check(c, cap=9.0, window=900, in_place=True, scores=True)
+    q = normal(c.g, c.total, c.heads_q, 128).to(BF16).cuda()
+    layer, seqs, lay = c.flat[0].cuda(), c.seqs(), c.layout()
+    kw = dict(softcap=9.0, window=900, slopes=alibi(c.heads_q).cuda(), prefix=i32([5, 80]).cuda(), max_prefix=80)
+    want = mma.mma_kv_attention(lay, layer, seqs, q, **kw)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = mma.mma_kv_attention(lay, layer, seqs, q, stream=side, **kw)
+    side.synchronize()
+    assert same_bits(got, want)
+    out = torch.empty_like(q)
+    need = mma.kv_attention_workspace(lay, seqs, q.shape[0], q.shape[1], q.dtype, window=900, prefix=True, max_prefix=80)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mma.mma_kv_attention(lay, layer, seqs, q, out=out, workspace=ws, **kw)
+    for _ in range(3):
+        out.zero_()
+        ws.random_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same_bits(out, want)
+
+
+def test_a_shape_of_nothing_is_the_plain_call():
+    c = Case("piece", BF16, [500], [3], heads=2)
+    q = normal(c.g, c.total, c.heads_q, 128).to(BF16).cuda()
+    layer = c.flat[0].cuda()
+    want = mma.mma_kv_attention(c.layout(), layer, c.seqs(), q)
+    assert same_bits(mma.mma_kv_attention(c.layout(), layer, c.seqs(), q, softcap=0.0, window=0, max_prefix=3), want)
+
+
+def test_caches_past_32_bits():
+    """A window at the end of a cache whose blocks lie beyond 4 GiB."""
+    tokens, heads, dim = 16, 8, 128
+    blocks = (5 << 30) // (tokens * heads * dim * 2)
+    lay = mma.kv_layout(1, tokens, heads, dim, 2, blocks, 1, mma.MMA_KV_LAYOUT_HND)
+    layer = torch.zeros(2 * blocks * tokens * heads * dim, dtype=BF16, device="cuda")
+    table = torch.arange(blocks - 20, blocks, dtype=torch.int32, device="cuda")[None].contiguous()
+    k = torch.randn(320, heads, dim, device="cuda").to(BF16)
+    v = torch.randn(320, heads, dim, device="cuda").to(BF16)
+    view = layer.view(2, blocks, heads, tokens, dim)
+    view[0, blocks - 20:] = k.view(20, tokens, heads, dim).transpose(1, 2)
+    view[1, blocks - 20:] = v.view(20, tokens, heads, dim).transpose(1, 2)
+    q = torch.randn(1, heads * 2, dim, device="cuda").to(BF16)
+    seqs = mma.kv_seqs(table, torch.tensor([319], dtype=torch.int32, device="cuda"), max_len=320)
+    out = mma.mma_kv_attention(lay, layer, seqs, q, window=100)
+    kk, vv, qq = k[220:].cpu().double(), v[220:].cpu().double(), q[0].cpu().double().view(heads, 2, dim)
+    p = torch.softmax(torch.einsum("hgd,jhd->hgj", qq, kk) * dim ** -0.5, -1)
+    want = torch.einsum("hgj,jhd->hgd", p, vv).reshape(1, heads * 2, dim)
+    # one rounding of the output and of p, and sums of 128 products in 32 bits
+    assert (out.cpu().double() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 2.0 ** -8 * vv.abs().max()
+
+
+def test_refusals():
+    c = Case("piece", BF16, [40], [3], heads=2)
+    lay, seqs, layer = c.layout(), c.seqs(), c.flat[0].cuda()
+    q = torch.zeros(3, 8, 128, dtype=BF16, device="cuda")
+    att = lambda **kw: mma.mma_kv_attention(lay, layer, seqs, q, **kw)  # noqa: E731
+    tree = torch.ones(3, 1, dtype=torch.int64, device="cuda")
+    one, pre = torch.ones(8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for kw in (dict(softcap=-1.0), dict(softcap=math.nan), dict(softcap=math.inf), dict(softcap=1e-30),
+               dict(tree=tree, window=3), dict(tree=tree, slopes=one), dict(tree=tree, prefix=pre)):
+        refused(lambda: att(**kw))
+    for kw in (dict(window=-1), dict(window=2 ** 32), dict(slopes=one[:7]), dict(slopes=one.double()), dict(slopes=one.cpu()),
+               dict(prefix=pre.long()), dict(prefix=torch.zeros(2, dtype=torch.int32, device="cuda")), dict(prefix=pre, max_prefix=-1)):
+        with pytest.raises(ValueError):
+            att(**kw)
+    with pytest.raises(TypeError):
+        att(softcap="3")
+    need = mma.kv_attention_workspace(c.layout(), c.seqs(), 3, 8, BF16, True, window=5)
+    ws = torch.empty(max(need - 1, 1), dtype=torch.uint8, device="cuda")
+    refused(lambda: att(window=5, scores_out=torch.zeros(1, 2, 64, device="cuda"), workspace=ws), "MMA_ERR_BUFFER_TOO_SMALL")
