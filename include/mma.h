@@ -442,6 +442,7 @@ mma_status_t mma_digest_u32(const void* dev_ptr, uint64_t bytes, uint64_t* dev_o
 #define MMA_TYPE_BF16 0u
 #define MMA_TYPE_F16 1u
 #define MMA_TYPE_F8 2u
+#define MMA_TYPE_F32 3u /* logits only */
 
 /* The sequences of a call. Entry j of sequence s lies in block
  * block_table[s * table_stride + j / block_tokens], at token j % block_tokens. The
@@ -635,6 +636,91 @@ mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_
 /* Host only: the workspace of that call: 8 bytes and 8 for every 1024 of max_len, for each
  * sequence and KV head. */
 mma_status_t mma_kv_evict_workspace(const mma_kv_layout_t* layout, const mma_kv_seqs_t* seqs, uint64_t* bytes);
+
+/* Beam search: of each request the best continuations over its beams and the vocabulary. Rows of
+ * `logits` are [batch][beams]. */
+typedef struct mma_beam_select {
+  const void* logits;       /* rows of vocab values of `type`, row_stride elements apart */
+  const float* scores;      /* [batch][beams]: the beams' log-probabilities so far */
+  const uint8_t* done;      /* [batch][beams] or NULL: not 0 for a beam that has ended */
+  int32_t* tokens;          /* [batch][keep] */
+  int32_t* parents;         /* [batch][keep]: the row of the beam that a candidate goes on from */
+  float* scores_out;        /* [batch][keep]; like the others apart from the inputs */
+  void* workspace;          /* mma_beam_select_workspace bytes of device memory, 8-byte aligned, as for attention */
+  uint64_t workspace_bytes;
+  uint64_t row_stride;
+  uint32_t batch;
+  uint32_t beams;           /* at most 64 */
+  uint32_t vocab;
+  uint32_t keep;            /* at most 128, and times (vocab + 7) / 8192, rounded up, at most 16384 */
+  uint32_t type;            /* MMA_TYPE_BF16, MMA_TYPE_F16 or MMA_TYPE_F32 */
+  int32_t done_token;       /* with `done`: from 0 to vocab - 1 */
+} mma_beam_select_t;
+
+/* v = score + (logit - lse), lse the log of the sum of exp of the beam's logits; of each request the `keep`
+ * largest, in order, ties to the lower beam, then the lower token. lse and v are 64-bit (lse within
+ * 2^-39), v rounded at the store. Within a beam candidates go by their logits. A beam that has ended has
+ * one candidate: done_token, with its score as it is. Logits of -infinity are no candidates; a beam
+ * whose score or lse is not finite (a logit that is NaN or +infinity) has none. Where there are fewer than
+ * `keep`, the rest have token and parent -1 and a score of -infinity. */
+mma_status_t mma_beam_select(const mma_beam_select_t* args, void* stream);
+
+/* Host only: the workspace of that call; pointers of args do not matter. */
+mma_status_t mma_beam_select_workspace(const mma_beam_select_t* args, uint64_t* bytes);
+
+/* Sequences that go on from others, on the GPU's side of a pool whose blocks are shared by count:
+ * refs[b] says how many places of tables hold block b, 0 that it is free. */
+typedef struct mma_kv_fork {
+  const int32_t* parents;   /* [num_children]: the sequence it goes on from; outside [0, num_seqs): it has no entries */
+  const int32_t* grow;      /* [num_children] or NULL (0): tokens to come that it is to have blocks for */
+  const int32_t* refs;      /* [gpu_num_blocks] */
+  int32_t* refs_out;        /* the same; may be refs */
+  int32_t* table_out;       /* [num_children][out_stride], -1 where there is no block */
+  int32_t* lens_out;        /* [num_children] */
+  int32_t* free_out;        /* [1]: free blocks afterwards; below 0: how many places found none */
+  void* workspace;          /* 12 bytes a child of device memory (mma_kv_fork_workspace), 4-byte aligned, as for attention */
+  uint64_t workspace_bytes;
+  uint32_t num_children;
+  uint32_t out_stride;      /* at least max_len / block_tokens, rounded up */
+} mma_kv_fork_t;
+
+/* Every sequence gives back its places (all of its row of the table, max_tokens and q_start are not used),
+ * and each child takes over its parent's entries: whole blocks are shared; the last, partly
+ * filled one is the child's own. It is the same block for the first child (by number) that has it as its
+ * last, if nothing else holds it; else, for the others, a new one into which the block is copied,
+ * in every layer. Behind it come new blocks for `grow` tokens more, as far as out_stride goes. New blocks are
+ * those with a count of 0, the lowest first, given to the children in their order and to a
+ * child's places in theirs; where none is left a place is -1 (free_out tells; what the block would have held is
+ * not in the child). A sequence without children so frees its blocks; a child without a parent is
+ * a new, empty sequence. Outputs but refs_out are apart from inputs. A block that a table holds is to be counted
+ * in refs at least as often. gpu_layers: num_layers device pointers, copied before return. */
+mma_status_t mma_kv_fork(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_seqs_t* seqs,
+                         const mma_kv_fork_t* args, void* stream);
+
+/* Host only: the workspace of that call; of args num_children matters. */
+mma_status_t mma_kv_fork_workspace(const mma_kv_fork_t* args, uint64_t* bytes);
+
+typedef struct mma_kv_compact {
+  const int32_t* block_table; /* [num_seqs][table_stride] */
+  int32_t* table_out;       /* the same; may be block_table */
+  const int32_t* refs;      /* [gpu_num_blocks]: 0: the block is free */
+  int32_t* refs_out;        /* the same; may be refs */
+  int32_t* moved;           /* [gpu_num_blocks]: where a block is now, -1 of a free one: for tables kept elsewhere */
+  int32_t* held_out;        /* [1]: blocks held, which are now 0 .. held - 1 */
+  void* workspace;          /* mma_kv_compact_workspace bytes of device memory, 8-byte aligned, as for attention */
+  uint64_t workspace_bytes;
+  uint32_t num_seqs;
+  uint32_t table_stride;
+} mma_kv_compact_t;
+
+/* Moves the held blocks of a pool together: with n of them, the k-th held block from n on goes to the k-th
+ * free one below n, K and V of every layer; counts and the table's places follow. Blocks below n stay.
+ * Places of the table without a block, or with a free one, stay as they are. */
+mma_status_t mma_kv_compact(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_compact_t* args,
+                            void* stream);
+
+/* Host only: the workspace of that call. */
+mma_status_t mma_kv_compact_workspace(const mma_kv_layout_t* layout, uint64_t* bytes);
 
 /* ------------------------------------------------------------------- status */
 

@@ -55,6 +55,7 @@ MMA_TASK_SDMA_ONLY = 2
 MMA_TYPE_BF16 = 0
 MMA_TYPE_F16 = 1
 MMA_TYPE_F8 = 2
+MMA_TYPE_F32 = 3
 MMA_ROPE_NONE = 0
 MMA_ROPE_LINEAR = 1
 MMA_ROPE_BASE = 2
@@ -192,6 +193,28 @@ class mma_kv_evict_t(ctypes.Structure):
                 ("recent", ctypes.c_uint32)]
 
 
+class mma_beam_select_t(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("scores", ctypes.c_void_p), ("done", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("parents", ctypes.c_void_p), ("scores_out", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64), ("row_stride", ctypes.c_uint64),
+                ("batch", ctypes.c_uint32), ("beams", ctypes.c_uint32), ("vocab", ctypes.c_uint32),
+                ("keep", ctypes.c_uint32), ("type", ctypes.c_uint32), ("done_token", ctypes.c_int32)]
+
+
+class mma_kv_fork_t(ctypes.Structure):
+    _fields_ = [("parents", ctypes.c_void_p), ("grow", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("refs_out", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("lens_out", ctypes.c_void_p),
+                ("free_out", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+                ("num_children", ctypes.c_uint32), ("out_stride", ctypes.c_uint32)]
+
+
+class mma_kv_compact_t(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("refs_out", ctypes.c_void_p), ("moved", ctypes.c_void_p), ("held_out", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64), ("num_seqs", ctypes.c_uint32),
+                ("table_stride", ctypes.c_uint32)]
+
+
 _P = ctypes.c_void_p
 _U64 = ctypes.c_uint64
 _I32 = ctypes.c_int32
@@ -234,6 +257,13 @@ _SIGNATURES = {
     "mma_kv_evict": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t),
                       ctypes.POINTER(mma_kv_evict_t), _P], _S),
     "mma_kv_evict_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(mma_kv_seqs_t), ctypes.POINTER(_U64)], _S),
+    "mma_beam_select": ([ctypes.POINTER(mma_beam_select_t), _P], _S),
+    "mma_beam_select_workspace": ([ctypes.POINTER(mma_beam_select_t), ctypes.POINTER(_U64)], _S),
+    "mma_kv_fork": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_seqs_t), ctypes.POINTER(mma_kv_fork_t), _P],
+                    _S),
+    "mma_kv_fork_workspace": ([ctypes.POINTER(mma_kv_fork_t), ctypes.POINTER(_U64)], _S),
+    "mma_kv_compact": ([ctypes.POINTER(mma_kv_layout_t), _P, ctypes.POINTER(mma_kv_compact_t), _P], _S),
+    "mma_kv_compact_workspace": ([ctypes.POINTER(mma_kv_layout_t), ctypes.POINTER(_U64)], _S),
     "mma_get_stats": ([ctypes.POINTER(mma_stats_t)], _S),
     "mma_reset_stats": ([], _S),
     "mma_status_str": ([_S], ctypes.c_char_p),
@@ -622,6 +652,86 @@ def mma_kv_evict(layout: mma_kv_layout_t, layer, seqs: KVSeqs, dst_table: torch.
                          workspace, _stream(stream))
 
 
+def beam_select_workspace(batch: int, beams: int, vocab: int, keep: int, dtype: torch.dtype) -> int:
+    """Bytes of workspace of a selection of these sizes."""
+    kind = {**_TYPES, torch.float32: MMA_TYPE_F32}.get(dtype)
+    if kind is None:
+        raise ValueError(f"logits of {dtype}: bfloat16, float16 or float32 is wanted")
+    need = _U64()
+    a = mma_beam_select_t(batch=batch, beams=beams, vocab=vocab, keep=keep, type=kind)
+    _check(lib.mma_beam_select_workspace(a, need), "mma_beam_select_workspace")
+    return need.value
+
+
+def mma_beam_select(logits: torch.Tensor, scores: torch.Tensor, keep: int, *, done: Optional[torch.Tensor] = None,
+                    done_token: int = 0, out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None,
+                    workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The `keep` best continuations of each request over its beams and the vocabulary: (tokens, parents, scores), each
+    [requests][keep]. `logits`: [requests * beams][vocabulary] or [requests][beams][vocabulary]; `scores`: float32
+    [requests][beams]; `done`: uint8 or bool of that shape, beams that have ended and stay as they are with `done_token`;
+    `out`: the three results' tensors. Parents are rows of `logits`: what mma_kv_fork takes."""
+    tokens, parents, best = (None, None, None) if out is None else out
+    if stream is not None:
+        shape = (scores.shape[0], keep)
+        if out is None:
+            tokens, parents, best = (_empty_on(stream, shape, t, scores.device) for t in (torch.int32, torch.int32, torch.float32))
+        if workspace is None:
+            need = beam_select_workspace(*scores.shape, logits.shape[-1], keep, logits.dtype)
+            workspace = _empty_on(stream, (need,), torch.uint8, scores.device)
+    return _kv_ops.beam_select(logits, scores, keep, done, done_token, tokens, parents, best, workspace, _stream(stream))
+
+
+def _moved_layers(layers, layout: mma_kv_layout_t) -> ctypes.Array:
+    if isinstance(layers, ctypes.Array):
+        return layers
+    layers = list(layers)
+    for t in layers:
+        _moved_layer(t, layout)
+    return layer_table(layers)
+
+
+def mma_kv_fork(layout: mma_kv_layout_t, layers, seqs: KVSeqs, parents: torch.Tensor, refs: torch.Tensor, *,
+                grow: Optional[torch.Tensor] = None, width: Optional[int] = None,
+                out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]] = None,
+                workspace: Optional[torch.Tensor] = None,
+                stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Children that go on from `parents` (int32, sequences of the call; -1: none): whole blocks shared by count, the open one
+    kept or copied in every layer, blocks for `grow` (int32) tokens more; sequences without children give theirs
+    back. Returns (block table [children][width], lengths, counts of the blocks, [1]: blocks that are free). `refs`: int32
+    [blocks], how often tables hold each. `out`: the four results' tensors, of which the counts may be `refs`."""
+    table, lens, counts, left = (None,) * 4 if out is None else out
+    if stream is not None:
+        n = parents.shape[0]
+        if out is None:
+            wide = seqs.c.table_stride if width is None else width
+            table, lens, counts, left = (_empty_on(stream, s, torch.int32, refs.device) for s in ((n, wide), (n,), refs.shape, (1,)))
+        if workspace is None:
+            workspace = _empty_on(stream, (12 * n,), torch.uint8, refs.device)
+    return _kv_ops.fork(layout, _moved_layers(layers, layout), seqs.address, parents, refs, grow, width, table, lens, counts, left,
+                        workspace, _stream(stream))
+
+
+def mma_kv_compact(layout: mma_kv_layout_t, layers, table: torch.Tensor, refs: torch.Tensor, *,
+                   out: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]] = None,
+                   workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Held blocks (those that `refs` counts) moved to the lowest places of the pool, in every layer. Returns (the block
+    table, the counts, where each block is now, [1]: how many are held). `out`: the four results' tensors, of which
+    the first two may be `table` and `refs`."""
+    new, counts, moved, held = (None,) * 4 if out is None else out
+    if stream is not None:
+        if out is None:
+            new, counts, moved, held = (_empty_on(stream, s, torch.int32, refs.device)
+                                        for s in (table.shape, refs.shape, refs.shape, (1,)))
+        if workspace is None:
+            need = _U64()
+            _check(lib.mma_kv_compact_workspace(layout, need), "mma_kv_compact_workspace")
+            workspace = _empty_on(stream, (need.value,), torch.uint8, refs.device)
+    return _kv_ops.compact(layout, _moved_layers(layers, layout), table, refs, new, counts, moved, held, workspace,
+                           _stream(stream))
+
+
 def _load_kv_ops():
     """The operators' binding, a compiled module next to libmma.so, given the library's entry points."""
     path = os.path.join(_HERE, "_kv_ops.so")
@@ -630,9 +740,10 @@ def _load_kv_ops():
     spec = importlib.util.spec_from_file_location("_kv_ops", path)
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
-    names = ("append", "attention", "attention_workspace", "commit", "evict", "evict_workspace", "attention_shaped",
-             "attention_shaped_workspace")
-    m.attach(*(ctypes.cast(getattr(lib, "mma_kv_" + x), _P).value for x in names), _check, _ptr)
+    names = ("kv_append", "kv_attention", "kv_attention_workspace", "kv_commit", "kv_evict", "kv_evict_workspace",
+             "kv_attention_shaped", "kv_attention_shaped_workspace", "beam_select", "beam_select_workspace", "kv_fork",
+             "kv_fork_workspace", "kv_compact", "kv_compact_workspace")
+    m.attach(*(ctypes.cast(getattr(lib, "mma_" + x), _P).value for x in names), _check, _ptr)
     return m
 
 

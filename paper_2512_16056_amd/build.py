@@ -35,6 +35,8 @@ SOURCES = {
     "mma_attention.hip": DEVICE,
     "mma_attention_shaped.hip": DEVICE,
     "mma_kv_ops.hip": DEVICE,
+    "mma_beam.hip": DEVICE,
+    "mma_pages.hip": DEVICE,
 }
 
 

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "mma_engine.h"
 #include "mma_plan.h"
@@ -438,6 +439,84 @@ mma_status_t attention(const mma_kv_layout_t* layout, const void* layer, const m
   return launched(launch_attention_shaped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
 }
 
+// Memory of a call that its kernels read or write.
+struct Part {
+  const char* name;
+  const void* p;
+  uint64_t bytes;
+};
+
+// Outputs apart from the inputs and from each other.
+mma_status_t all_apart(std::initializer_list<Part> outs, std::initializer_list<Part> ins) {
+  for (const Part* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Part& i : ins)
+      if (mma_status_t s = apart(o->name, o->p, o->bytes, i.name, i.p, i.bytes)) return s;
+    for (const Part* q = outs.begin(); q != o; ++q)
+      if (mma_status_t s = apart(o->name, o->p, o->bytes, q->name, q->p, q->bytes)) return s;
+  }
+  return MMA_OK;
+}
+
+mma_status_t workspace(Call* call, void* p, uint64_t bytes, uint64_t need, uintptr_t align) {
+  if (bytes < need)
+    return fail(MMA_ERR_BUFFER_TOO_SMALL, "the workspace has %llu bytes, %llu are needed",
+                static_cast<unsigned long long>(bytes), static_cast<unsigned long long>(need));
+  return need ? array(call, "workspace", p, need, align) : MMA_OK;
+}
+
+struct BeamPlan {
+  uint32_t splits;
+  bool joined;  // each row's parts before the request's
+  uint64_t sum_bytes, list_bytes, row_bytes, max_bytes, bytes;
+};
+
+mma_status_t check_beam_sizes(const mma_beam_select_t* a, BeamPlan* p) {
+  if (!a) return fail(MMA_ERR_INVALID_ARG, "NULL arguments");
+  if (a->type != MMA_TYPE_BF16 && a->type != MMA_TYPE_F16 && a->type != MMA_TYPE_F32)
+    return fail(MMA_ERR_INVALID_ARG, "unknown type %u of logits", a->type);
+  if (!a->beams || a->beams > kBeamMost) return fail(MMA_ERR_INVALID_ARG, "%u beams: from 1 to %u", a->beams, kBeamMost);
+  if (!a->keep || a->keep > kBeamKeep) return fail(MMA_ERR_INVALID_ARG, "keep %u: from 1 to %u", a->keep, kBeamKeep);
+  if (!a->vocab || a->vocab > INT32_MAX) return fail(MMA_ERR_INVALID_ARG, "a vocabulary of %u: from 1 to 2^31 - 1", a->vocab);
+  // Rows start anywhere in 16 bytes: up to 7 elements more.
+  const uint64_t splits = up(static_cast<uint64_t>(a->vocab) + 7, kBeamChunk), rows = static_cast<uint64_t>(a->batch) * a->beams;
+  if (splits * a->keep > kBeamMerge)
+    return fail(MMA_ERR_INVALID_ARG, "the %u best of a vocabulary of %u: keep times its parts of %u may not pass %u", a->keep,
+                a->vocab, kBeamChunk, kBeamMerge);
+  if (rows * splits >= 1u << 22)
+    return fail(MMA_ERR_INVALID_ARG, "%u requests of %u beams are more workgroups than a launch takes", a->batch, a->beams);
+  p->splits = static_cast<uint32_t>(splits);
+  p->joined = splits * a->keep * a->beams > kBeamMerge;
+  p->sum_bytes = rows * splits * 8;
+  p->list_bytes = rows * splits * a->keep * 8;
+  p->row_bytes = p->joined ? rows * a->keep * 8 : 0;
+  p->max_bytes = up_to(rows * splits * 4, 8);
+  p->bytes = p->sum_bytes + p->list_bytes + p->row_bytes + p->max_bytes;
+  return MMA_OK;
+}
+
+// Pages from[k] to to[k] of every layer.
+mma_status_t move_pages(const Call& call, const mma_kv_layout_t* layout, void* const* layers, const int32_t* from, const int32_t* to,
+                        const uint32_t* moves, uint32_t most, hipStream_t stream) {
+  if (!most) return MMA_OK;
+  static thread_local MoveArgs k;
+  k.from = from;
+  k.to = to;
+  k.moves = moves;
+  k.piece = call.piece;
+  k.v_offset = call.piece * call.c.num_blocks;
+  k.most = most;
+  for (uint32_t first = 0; first < layout->num_layers; first += MoveArgs::kMaxLayers) {
+    k.layers = std::min(layout->num_layers - first, MoveArgs::kMaxLayers);
+    for (uint32_t l = 0; l < k.layers; ++l) k.layer[l] = reinterpret_cast<uint64_t>(layers[first + l]);
+    if (mma_status_t s = launched(launch_moves(k, stream), "KV page move")) return s;
+  }
+  return MMA_OK;
+}
+
+uint64_t fork_workspace(uint32_t num_children) { return 12ull * num_children; }
+
+uint64_t compact_workspace(uint32_t num_blocks) { return 8 + 8ull * num_blocks; }
+
 }  // namespace
 }  // namespace mma
 
@@ -686,6 +765,198 @@ mma_status_t mma_kv_evict(const mma_kv_layout_t* layout, void* layer, const mma_
   return launched(launch_evict(k, kind, static_cast<hipStream_t>(stream)), "KV evict");
 } catch (...) {
   return ops_boundary_error("mma_kv_evict");
+}
+
+mma_status_t mma_beam_select_workspace(const mma_beam_select_t* a, uint64_t* bytes) try {
+  if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  BeamPlan p{};
+  if (mma_status_t s = check_beam_sizes(a, &p)) return s;
+  *bytes = p.bytes;
+  return MMA_OK;
+} catch (...) {
+  return ops_boundary_error("mma_beam_select_workspace");
+}
+
+mma_status_t mma_beam_select(const mma_beam_select_t* a, void* stream) try {
+  mma_status_t s;
+  Call call;
+  BeamPlan p{};
+  if ((s = begin(&call))) return s;
+  if ((s = check_beam_sizes(a, &p))) return s;
+  if (a->done && (a->done_token < 0 || static_cast<uint32_t>(a->done_token) >= a->vocab))
+    return fail(MMA_ERR_INVALID_ARG, "done_token %d is not in a vocabulary of %u", a->done_token, a->vocab);
+  if (!a->batch) return MMA_OK;
+  const uint64_t rows = static_cast<uint64_t>(a->batch) * a->beams, size = a->type == MMA_TYPE_F32 ? 4 : 2;
+  const uint64_t kept = 4ull * a->batch * a->keep;
+  uint64_t reach;
+  if (__builtin_mul_overflow(rows - 1, a->row_stride, &reach) || reach > UINT64_MAX / 8)
+    return fail(MMA_ERR_INVALID_ARG, "logits: their extent is beyond 64 bits");
+  reach = (reach + a->vocab) * size;
+  if ((s = all_apart({{"tokens", a->tokens, kept}, {"parents", a->parents, kept}, {"scores_out", a->scores_out, kept}},
+                     {{"logits", a->logits, reach}, {"scores", a->scores, 4 * rows}, {"done", a->done, rows}})))
+    return s;
+  Device dev(call.device);
+  if ((s = array(&call, "logits", a->logits, reach, size))) return s;
+  if ((s = array(&call, "scores", a->scores, 4 * rows, 4))) return s;
+  if ((s = array(&call, "done", a->done, rows, 1, true))) return s;
+  if ((s = array(&call, "tokens", a->tokens, kept, 4))) return s;
+  if ((s = array(&call, "parents", a->parents, kept, 4))) return s;
+  if ((s = array(&call, "scores_out", a->scores_out, kept, 4))) return s;
+  if ((s = workspace(&call, a->workspace, a->workspace_bytes, p.bytes, 8))) return s;
+  BeamArgs k{};
+  k.logits = static_cast<const uint8_t*>(a->logits);
+  k.row_bytes = a->row_stride * size;
+  k.scores = a->scores;
+  k.done = a->done;
+  k.tokens = a->tokens;
+  k.parents = a->parents;
+  k.scores_out = a->scores_out;
+  char* ws = static_cast<char*>(a->workspace);
+  k.part_sum = reinterpret_cast<double*>(ws);
+  k.lists = reinterpret_cast<uint64_t*>(ws + p.sum_bytes);
+  k.rows = p.joined ? k.lists + p.list_bytes / 8 : nullptr;
+  k.part_max = reinterpret_cast<float*>(ws + p.sum_bytes + p.list_bytes + p.row_bytes);
+  k.batch = a->batch;
+  k.beams = a->beams;
+  k.vocab = a->vocab;
+  k.keep = a->keep;
+  k.splits = p.splits;
+  k.done_token = a->done_token;
+  return launched(launch_beam(k, a->type, static_cast<hipStream_t>(stream)), "beam selection");
+} catch (...) {
+  return ops_boundary_error("mma_beam_select");
+}
+
+mma_status_t mma_kv_fork_workspace(const mma_kv_fork_t* a, uint64_t* bytes) try {
+  if (!a || !bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  *bytes = fork_workspace(a->num_children);
+  return MMA_OK;
+} catch (...) {
+  return ops_boundary_error("mma_kv_fork_workspace");
+}
+
+mma_status_t mma_kv_fork(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_seqs_t* seqs,
+                         const mma_kv_fork_t* a, void* stream) try {
+  mma_status_t s;
+  Call call;
+  if ((s = begin(&call))) return s;
+  if (!a || !gpu_layers) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  if ((s = check_layout(layout, &call))) return s;
+  if ((s = check_seqs_sizes(seqs, layout->block_tokens))) return s;
+  if (a->num_children > kMaxGrid) return fail(MMA_ERR_INVALID_ARG, "%u children, at most %u", a->num_children, kMaxGrid);
+  if (static_cast<uint64_t>(a->out_stride) * layout->block_tokens < seqs->max_len)
+    return fail(MMA_ERR_INVALID_ARG, "out_stride %u blocks do not hold %u entries", a->out_stride, seqs->max_len);
+  const uint64_t places = static_cast<uint64_t>(a->num_children) * a->out_stride;
+  if (places > 1u << 30) return fail(MMA_ERR_INVALID_ARG, "more than 2^30 places in table_out");
+  const uint64_t counts = 4ull * layout->gpu_num_blocks, each = 4ull * a->num_children, lens = 4ull * seqs->num_seqs;
+  const uint64_t table = extent(seqs->num_seqs, seqs->table_stride, 4);
+  if ((s = all_apart({{"refs_out", a->refs_out, counts}, {"table_out", a->table_out, 4 * places}, {"lens_out", a->lens_out, each},
+                      {"free_out", a->free_out, 4}},
+                     {{"block_table", seqs->block_table, table}, {"lens", seqs->lens, lens}, {"parents", a->parents, each},
+                      {"grow", a->grow, each}})))
+    return s;
+  for (const Part& o : {Part{"table_out", a->table_out, 4 * places}, Part{"lens_out", a->lens_out, each}, Part{"free_out", a->free_out, 4}})
+    if ((s = apart(o.name, o.p, o.bytes, "refs", a->refs, counts))) return s;
+  if (a->refs_out != a->refs && (s = apart("refs_out", a->refs_out, counts, "refs", a->refs, counts))) return s;
+  Device dev(call.device);
+  if (seqs->num_seqs) {
+    if ((s = check_seqs(seqs, layout->block_tokens, 0, &call))) return s;
+  }
+  if (a->num_children) {
+    if ((s = array(&call, "parents", a->parents, each, 4))) return s;
+    if ((s = array(&call, "grow", a->grow, each, 4, true))) return s;
+    if ((s = array(&call, "table_out", a->table_out, 4 * places, 4))) return s;
+    if ((s = array(&call, "lens_out", a->lens_out, each, 4))) return s;
+  }
+  if ((s = array(&call, "refs", a->refs, counts, 4))) return s;
+  if ((s = array(&call, "refs_out", a->refs_out, counts, 4))) return s;
+  if ((s = array(&call, "free_out", a->free_out, 4, 4))) return s;
+  if ((s = workspace(&call, a->workspace, a->workspace_bytes, fork_workspace(a->num_children), 4))) return s;
+  for (uint32_t l = 0; l < layout->num_layers; ++l)
+    if ((s = array(&call, "a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
+  ForkArgs k{};
+  k.table = seqs->block_table;
+  k.lens = seqs->lens;
+  k.parents = a->parents;
+  k.grow = a->grow;
+  k.refs = a->refs;
+  k.refs_out = a->refs_out;
+  k.table_out = a->table_out;
+  k.lens_out = a->lens_out;
+  k.free_out = a->free_out;
+  k.from = static_cast<int32_t*>(a->workspace);
+  k.to = k.from + a->num_children;
+  k.wants = reinterpret_cast<uint32_t*>(k.to + a->num_children);
+  k.num_seqs = seqs->num_seqs;
+  k.table_stride = seqs->table_stride;
+  k.num_children = a->num_children;
+  k.out_stride = a->out_stride;
+  k.num_blocks = layout->gpu_num_blocks;
+  k.tokens = layout->block_tokens;
+  k.max_len = seqs->max_len;
+  const hipStream_t on = static_cast<hipStream_t>(stream);
+  if ((s = launched(launch_fork(k, on), "KV fork"))) return s;
+  return move_pages(call, layout, gpu_layers, k.from, k.to, nullptr, a->num_children, on);
+} catch (...) {
+  return ops_boundary_error("mma_kv_fork");
+}
+
+mma_status_t mma_kv_compact_workspace(const mma_kv_layout_t* layout, uint64_t* bytes) try {
+  if (!bytes) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  Call call;
+  if (mma_status_t s = check_layout(layout, &call)) return s;
+  *bytes = compact_workspace(layout->gpu_num_blocks);
+  return MMA_OK;
+} catch (...) {
+  return ops_boundary_error("mma_kv_compact_workspace");
+}
+
+mma_status_t mma_kv_compact(const mma_kv_layout_t* layout, void* const* gpu_layers, const mma_kv_compact_t* a, void* stream) try {
+  mma_status_t s;
+  Call call;
+  if ((s = begin(&call))) return s;
+  if (!a || !gpu_layers) return fail(MMA_ERR_INVALID_ARG, "NULL argument");
+  if ((s = check_layout(layout, &call))) return s;
+  const uint64_t places = static_cast<uint64_t>(a->num_seqs) * a->table_stride, counts = 4ull * layout->gpu_num_blocks;
+  if (places > 1u << 30) return fail(MMA_ERR_INVALID_ARG, "more than 2^30 places in the table");
+  if ((s = all_apart({{"table_out", a->table_out, 4 * places}, {"refs_out", a->refs_out, counts}, {"moved", a->moved, counts},
+                      {"held_out", a->held_out, 4}}, {})))
+    return s;
+  for (const Part& o : {Part{"refs_out", a->refs_out, counts}, Part{"moved", a->moved, counts}, Part{"held_out", a->held_out, 4}})
+    if ((s = apart(o.name, o.p, o.bytes, "block_table", a->block_table, 4 * places))) return s;
+  for (const Part& o : {Part{"table_out", a->table_out, 4 * places}, Part{"moved", a->moved, counts}, Part{"held_out", a->held_out, 4}})
+    if ((s = apart(o.name, o.p, o.bytes, "refs", a->refs, counts))) return s;
+  if (a->refs_out != a->refs && (s = apart("refs_out", a->refs_out, counts, "refs", a->refs, counts))) return s;
+  if (a->table_out != a->block_table && (s = apart("table_out", a->table_out, 4 * places, "block_table", a->block_table, 4 * places))) return s;
+  Device dev(call.device);
+  if (places) {
+    if ((s = array(&call, "block_table", a->block_table, 4 * places, 4))) return s;
+    if ((s = array(&call, "table_out", a->table_out, 4 * places, 4))) return s;
+  }
+  if ((s = array(&call, "refs", a->refs, counts, 4))) return s;
+  if ((s = array(&call, "refs_out", a->refs_out, counts, 4))) return s;
+  if ((s = array(&call, "moved", a->moved, counts, 4))) return s;
+  if ((s = array(&call, "held_out", a->held_out, 4, 4))) return s;
+  if ((s = workspace(&call, a->workspace, a->workspace_bytes, compact_workspace(layout->gpu_num_blocks), 8))) return s;
+  for (uint32_t l = 0; l < layout->num_layers; ++l)
+    if ((s = array(&call, "a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
+  CompactArgs k{};
+  k.table = a->block_table;
+  k.table_out = a->table_out;
+  k.refs = a->refs;
+  k.refs_out = a->refs_out;
+  k.moved = a->moved;
+  k.held_out = a->held_out;
+  k.moves = static_cast<uint32_t*>(a->workspace);
+  k.from = reinterpret_cast<int32_t*>(k.moves + 2);
+  k.to = k.from + layout->gpu_num_blocks;
+  k.places = places;
+  k.num_blocks = layout->gpu_num_blocks;
+  const hipStream_t on = static_cast<hipStream_t>(stream);
+  if ((s = launched(launch_compact(k, on), "KV compaction"))) return s;
+  return move_pages(call, layout, gpu_layers, k.from, k.to, k.moves, layout->gpu_num_blocks / 2, on);
+} catch (...) {
+  return ops_boundary_error("mma_kv_compact");
 }
 
 }  // extern "C"

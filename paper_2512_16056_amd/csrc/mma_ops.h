@@ -120,6 +120,69 @@ struct EvictArgs {
   uint32_t dst_stride, scores_stride, keep, sinks, recent;
 };
 
+// Beam search's selection. Parts of rows: [row][split], lists of `keep` keys each (mma_beam.hip).
+constexpr uint32_t kBeamChunk = 8192;   // logits of a part
+constexpr uint32_t kBeamMerge = 16384;  // keys that a merge takes
+constexpr uint32_t kBeamMost = 64;      // beams of a request
+constexpr uint32_t kBeamKeep = 128;
+
+struct BeamArgs {
+  const uint8_t* logits;
+  uint64_t row_bytes;
+  const float* scores;
+  const uint8_t* done;
+  int32_t* tokens;
+  int32_t* parents;
+  float* scores_out;
+  double* part_sum;
+  uint64_t* lists;
+  uint64_t* rows;  // each row's parts joined, or NULL where a request's parts are few enough
+  float* part_max;
+  uint32_t batch, beams, vocab, keep, splits;
+  int32_t done_token;
+};
+
+struct ForkArgs {
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* parents;
+  const int32_t* grow;
+  const int32_t* refs;
+  int32_t* refs_out;
+  int32_t* table_out;
+  int32_t* lens_out;
+  int32_t* free_out;
+  int32_t* from;    // of each child: the block that is copied for it, or -1
+  int32_t* to;      // and where, or -1
+  uint32_t* wants;  // new blocks of the children before it
+  uint32_t num_seqs, table_stride, num_children, out_stride, num_blocks, tokens, max_len;
+};
+
+struct CompactArgs {
+  const int32_t* table;
+  int32_t* table_out;
+  const int32_t* refs;
+  int32_t* refs_out;
+  int32_t* moved;
+  int32_t* held_out;
+  int32_t* from;  // the moves
+  int32_t* to;
+  uint32_t* moves;  // how many
+  uint64_t places;
+  uint32_t num_blocks;
+};
+
+struct MoveArgs {
+  const int32_t* from;
+  const int32_t* to;
+  const uint32_t* moves;  // how many, or NULL: `most`
+  uint64_t piece;         // bytes of a block's K or V
+  uint64_t v_offset;      // of V of block 0 from the layer's start
+  uint32_t most, layers;
+  static constexpr uint32_t kMaxLayers = 192;
+  uint64_t layer[kMaxLayers];
+};
+
 // What a kernel is compiled for.
 struct OpsKind {
   uint32_t type, cache_type, layout;
@@ -150,6 +213,10 @@ hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stre
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_attention_shaped(const ShapedArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stream);
+hipError_t launch_beam(const BeamArgs& a, uint32_t type, hipStream_t stream);
+hipError_t launch_fork(const ForkArgs& a, hipStream_t stream);
+hipError_t launch_compact(const CompactArgs& a, hipStream_t stream);
+hipError_t launch_moves(const MoveArgs& a, hipStream_t stream);
 hipError_t launch_evict(const EvictArgs& a, const OpsKind& k, hipStream_t stream);
 
 // ------------------------------------------------------------ device helpers

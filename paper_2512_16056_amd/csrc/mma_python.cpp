@@ -24,6 +24,12 @@ decltype(&mma_kv_attention_shaped_workspace) g_attention_shaped_workspace;
 decltype(&mma_kv_commit) g_commit;
 decltype(&mma_kv_evict) g_evict;
 decltype(&mma_kv_evict_workspace) g_evict_workspace;
+decltype(&mma_beam_select) g_beam_select;
+decltype(&mma_beam_select_workspace) g_beam_select_workspace;
+decltype(&mma_kv_fork) g_fork;
+decltype(&mma_kv_fork_workspace) g_fork_workspace;
+decltype(&mma_kv_compact) g_compact;
+decltype(&mma_kv_compact_workspace) g_compact_workspace;
 PyObject* g_check;    // (status, name): raises the library's error
 PyObject* g_address;  // (object): its address
 
@@ -343,9 +349,170 @@ PyObject* evict(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// A workspace that was given, or a new one.
+struct Space {
+  at::Tensor own;
+  void* p = nullptr;
+  uint64_t bytes = 0;
+  template <class Need>
+  Space(PyObject* given, const at::Tensor& like, Need need) {
+    if (given != Py_None) {
+      const at::Tensor& t = flat(given, "workspace", at::kByte, {-1});
+      p = t.data_ptr();
+      bytes = t.numel();
+      return;
+    }
+    bytes = need();
+    if (!bytes) return;
+    own = fresh({static_cast<int64_t>(bytes)}, at::kByte, like);
+    p = own.data_ptr();
+  }
+};
+
+at::Tensor given_or(PyObject* o, const char* name, at::ScalarType type, std::initializer_list<int64_t> sizes, const at::Tensor& like) {
+  return o == Py_None ? fresh(at::IntArrayRef(sizes), type, like) : flat(o, name, type, sizes);
+}
+
+PyObject* tuple_of(std::initializer_list<at::Tensor> tensors) {
+  PyObject* r = PyTuple_New(static_cast<Py_ssize_t>(tensors.size()));
+  if (!r) throw Refused();
+  Py_ssize_t i = 0;
+  for (const at::Tensor& t : tensors) PyTuple_SET_ITEM(r, i++, THPVariable_Wrap(t));
+  return r;
+}
+
+PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 10) REFUSE("10 arguments");
+  const at::Tensor& x = tensor(a[0], "logits");
+  const at::Tensor& scores = flat(a[1], "scores", at::kFloat, {-1, -1});
+  const int64_t batch = scores.size(0), beams = scores.size(1);
+  mma_beam_select_t b{};
+  if (x.scalar_type() == at::kBFloat16) b.type = MMA_TYPE_BF16;
+  else if (x.scalar_type() == at::kHalf) b.type = MMA_TYPE_F16;
+  else if (x.scalar_type() == at::kFloat) b.type = MMA_TYPE_F32;
+  else REFUSE("logits: bfloat16, float16 or float32 is wanted, got %s", c10::toString(x.scalar_type()));
+  const bool rows = x.dim() == 2 && x.size(0) == batch * beams;
+  const bool items = x.dim() == 3 && x.size(0) == batch && x.size(1) == beams;
+  if (!x.is_cuda() || !(rows || items))
+    REFUSE("logits: [%lld, vocabulary] or [%lld, %lld, vocabulary] on the GPU is wanted, got %s on %s", static_cast<long long>(batch * beams),
+           static_cast<long long>(batch), static_cast<long long>(beams), text(x.sizes()).c_str(), x.device().str().c_str());
+  const int64_t vocab = x.size(x.dim() - 1);
+  if (vocab > 1 && x.stride(x.dim() - 1) != 1) REFUSE("logits: a row's values have to be contiguous, strides %s", text(x.strides()).c_str());
+  if (items && batch > 1 && beams > 1 && x.stride(0) != x.stride(1) * beams)
+    REFUSE("logits: rows at one distance are wanted, strides %s", text(x.strides()).c_str());
+  b.row_stride = static_cast<uint64_t>(rows ? x.stride(0) : beams > 1 ? x.stride(1) : x.stride(0));
+  b.keep = count(a[2], "keep");
+  if (!b.keep) REFUSE("keep: at least 1");
+  if (a[3] != Py_None) {
+    const at::Tensor& d = tensor(a[3], "done");
+    b.done = static_cast<const uint8_t*>(flat(a[3], "done", d.scalar_type() == at::kBool ? at::kBool : at::kByte, {batch, beams}).data_ptr());
+  }
+  const double token = real(a[4]);
+  if (!(token >= -2147483648.0 && token <= 2147483647.0)) REFUSE("done_token: a token is wanted");
+  b.done_token = static_cast<int32_t>(token);
+  b.logits = x.data_ptr();
+  b.scores = static_cast<const float*>(scores.data_ptr());
+  b.batch = size32(batch, "scores");
+  b.beams = size32(beams, "scores");
+  b.vocab = size32(vocab, "logits");
+  const int64_t keep = b.keep;
+  const at::Tensor tokens = given_or(a[5], "tokens", at::kInt, {batch, keep}, scores);
+  const at::Tensor parents = given_or(a[6], "parents", at::kInt, {batch, keep}, scores);
+  const at::Tensor best = given_or(a[7], "scores_out", at::kFloat, {batch, keep}, scores);
+  b.tokens = static_cast<int32_t*>(tokens.data_ptr());
+  b.parents = static_cast<int32_t*>(parents.data_ptr());
+  b.scores_out = static_cast<float*>(best.data_ptr());
+  const Space space(a[8], scores, [&] {
+    uint64_t need = 0;
+    check(g_beam_select_workspace(&b, &need), "mma_beam_select_workspace");
+    return need;
+  });
+  b.workspace = space.p;
+  b.workspace_bytes = space.bytes;
+  check(g_beam_select(&b, reinterpret_cast<void*>(number(a[9]))), "mma_beam_select");
+  return tuple_of({tokens, parents, best});
+  } catch (const Refused&) {
+    return nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 13) REFUSE("13 arguments");
+  const Common c(a[0], a[2]);
+  const Py_ssize_t table = static_cast<Py_ssize_t>(sizeof(void*)) * c.layout->num_layers;
+  const at::Tensor& parents = flat(a[3], "parents", at::kInt, {-1});
+  const int64_t n = parents.size(0), blocks = c.layout->gpu_num_blocks;
+  const at::Tensor& refs = flat(a[4], "refs", at::kInt, {blocks});
+  const int64_t width = a[6] == Py_None ? static_cast<int64_t>(c.seqs->table_stride) : count(a[6], "width");
+  mma_kv_fork_t x{};
+  x.parents = static_cast<const int32_t*>(parents.data_ptr());
+  x.grow = flat_ptr<int32_t>(a[5], "grow", at::kInt, {n});
+  x.refs = static_cast<const int32_t*>(refs.data_ptr());
+  x.num_children = size32(n, "parents");
+  x.out_stride = static_cast<uint32_t>(width);
+  const at::Tensor out = given_or(a[7], "table", at::kInt, {n, width}, refs);
+  const at::Tensor lens = given_or(a[8], "lens", at::kInt, {n}, refs);
+  const at::Tensor counts = given_or(a[9], "refs_out", at::kInt, {blocks}, refs);
+  const at::Tensor left = given_or(a[10], "free", at::kInt, {1}, refs);
+  x.table_out = static_cast<int32_t*>(out.data_ptr());
+  x.lens_out = static_cast<int32_t*>(lens.data_ptr());
+  x.refs_out = static_cast<int32_t*>(counts.data_ptr());
+  x.free_out = static_cast<int32_t*>(left.data_ptr());
+  const Space space(a[11], refs, [&] {
+    uint64_t need = 0;
+    check(g_fork_workspace(&x, &need), "mma_kv_fork_workspace");
+    return need;
+  });
+  x.workspace = space.p;
+  x.workspace_bytes = space.bytes;
+  void* const* layers = static_cast<void* const*>(bytes_of(a[1], table, "layers"));
+  check(g_fork(c.layout, layers, c.seqs, &x, reinterpret_cast<void*>(number(a[12]))), "mma_kv_fork");
+  return tuple_of({out, lens, counts, left});
+  } catch (const Refused&) {
+    return nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 10) REFUSE("10 arguments");
+  const mma_kv_layout_t* layout = static_cast<const mma_kv_layout_t*>(bytes_of(a[0], sizeof(mma_kv_layout_t), "layout"));
+  const at::Tensor& table = flat(a[2], "table", at::kInt, {-1, -1});
+  const int64_t blocks = layout->gpu_num_blocks;
+  const at::Tensor& refs = flat(a[3], "refs", at::kInt, {blocks});
+  mma_kv_compact_t x{};
+  x.block_table = static_cast<const int32_t*>(table.data_ptr());
+  x.num_seqs = size32(table.size(0), "table");
+  x.table_stride = size32(table.size(1), "table");
+  x.refs = static_cast<const int32_t*>(refs.data_ptr());
+  const at::Tensor out = given_or(a[4], "table_out", at::kInt, {table.size(0), table.size(1)}, refs);
+  const at::Tensor counts = given_or(a[5], "refs_out", at::kInt, {blocks}, refs);
+  const at::Tensor moved = given_or(a[6], "moved", at::kInt, {blocks}, refs);
+  const at::Tensor held = given_or(a[7], "held", at::kInt, {1}, refs);
+  x.table_out = static_cast<int32_t*>(out.data_ptr());
+  x.refs_out = static_cast<int32_t*>(counts.data_ptr());
+  x.moved = static_cast<int32_t*>(moved.data_ptr());
+  x.held_out = static_cast<int32_t*>(held.data_ptr());
+  const Space space(a[8], refs, [&] {
+    uint64_t need = 0;
+    check(g_compact_workspace(layout, &need), "mma_kv_compact_workspace");
+    return need;
+  });
+  x.workspace = space.p;
+  x.workspace_bytes = space.bytes;
+  void* const* layers = static_cast<void* const*>(bytes_of(a[1], static_cast<Py_ssize_t>(sizeof(void*)) * layout->num_layers, "layers"));
+  check(g_compact(layout, layers, &x, reinterpret_cast<void*>(number(a[9]))), "mma_kv_compact");
+  return tuple_of({out, counts, moved, held});
+  } catch (const Refused&) {
+    return nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
 // The library's entry points and the two Python helpers.
 PyObject* attach(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
-  constexpr int kEntries = 8;
+  constexpr int kEntries = 14;
   if (nargs != kEntries + 2) {
     PyErr_SetString(PyExc_ValueError, "the entry points and two helpers");
     return nullptr;
@@ -363,6 +530,12 @@ PyObject* attach(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   g_evict_workspace = reinterpret_cast<decltype(g_evict_workspace)>(p[5]);
   g_attention_shaped = reinterpret_cast<decltype(g_attention_shaped)>(p[6]);
   g_attention_shaped_workspace = reinterpret_cast<decltype(g_attention_shaped_workspace)>(p[7]);
+  g_beam_select = reinterpret_cast<decltype(g_beam_select)>(p[8]);
+  g_beam_select_workspace = reinterpret_cast<decltype(g_beam_select_workspace)>(p[9]);
+  g_fork = reinterpret_cast<decltype(g_fork)>(p[10]);
+  g_fork_workspace = reinterpret_cast<decltype(g_fork_workspace)>(p[11]);
+  g_compact = reinterpret_cast<decltype(g_compact)>(p[12]);
+  g_compact_workspace = reinterpret_cast<decltype(g_compact_workspace)>(p[13]);
   Py_INCREF(a[kEntries]);
   g_check = a[kEntries];
   Py_INCREF(a[kEntries + 1]);
@@ -371,7 +544,8 @@ PyObject* attach(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
-PyMethodDef g_methods[] = {METHOD(attach), METHOD(append), METHOD(attention), METHOD(commit), METHOD(evict), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_methods[] = {METHOD(attach), METHOD(append), METHOD(attention), METHOD(commit), METHOD(evict),
+                          METHOD(beam_select), METHOD(fork), METHOD(compact), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_kv_ops", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
