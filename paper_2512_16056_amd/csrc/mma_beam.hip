@@ -61,8 +61,9 @@ __device__ __forceinline__ double exp_of(double d) {
   p = fma(p, f, 0.24022650695821055);
   p = fma(p, f, 0.6931471805459343);
   p = fma(p, f, 0.9999999999999997);
-  const uint64_t b = __builtin_bit_cast(uint64_t, p) + (__builtin_bit_cast(uint64_t, t) << 52);  // times 2^n
-  return __builtin_bit_cast(double, b);
+  const uint64_t b = __builtin_bit_cast(uint64_t, p);  // times 2^n: into the exponent
+  const uint32_t high = static_cast<uint32_t>(b >> 32) + (static_cast<uint32_t>(__builtin_bit_cast(uint64_t, t)) << 20);
+  return __builtin_bit_cast(double, static_cast<uint64_t>(high) << 32 | static_cast<uint32_t>(b));
 }
 
 __device__ __forceinline__ float max_of_wave(float v) {
@@ -90,19 +91,55 @@ __device__ __forceinline__ uint32_t count_of(uint32_t* waves, F is) {
   return n;
 }
 
-// The value of rank `keep` - 1 of 256 in LDS, the largest first: as many different threads hold one at least as large.
-template <class H>
-__device__ __forceinline__ void bound_of(const H* h, uint32_t keep, H* bound) {
-  if (threadIdx.x < 256) {
-    const H mine = h[threadIdx.x];
-    uint32_t rank = 0;
-#pragma unroll 16
-    for (uint32_t i = 0; i < 256; ++i) {
-      const H x = h[i];
-      rank += x > mine || (x == mine && i < threadIdx.x) ? 1 : 0;
-    }
-    if (rank == keep - 1) *bound = mine;
+// A number that at least `keep` of 256 in LDS reach, and hardly more: by one wave, bit by bit from the top until exactly as
+// many do. (Each of 256 threads ranking its own number against the others took 17 us, waiting on LDS.)
+__device__ __forceinline__ uint32_t bound_of(const uint32_t* numbers, uint32_t keep) {
+  const u32x4 x = *reinterpret_cast<const u32x4*>(numbers + threadIdx.x % kOpsWave * 4);
+  uint32_t bound = 0;
+  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+    const uint32_t next = bound | bit;
+    const uint32_t n = __popcll(__ballot(x[0] >= next)) + __popcll(__ballot(x[1] >= next)) + __popcll(__ballot(x[2] >= next)) +
+                       __popcll(__ballot(x[3] >= next));
+    if (n >= keep) bound = next;
+    if (n == keep) break;
   }
+  return bound;
+}
+
+// Candidates of a list in LDS: larger values first, equal ones by place (PLACES; else there are no equal ones).
+struct List {
+  uint64_t value[kList + 8];
+  uint32_t rank[kList];
+  uint32_t n;
+};
+
+// Ranks of the list's n candidates, counted by all of THREADS threads: of few candidates several threads have one, each
+// against its share of the others. The list is filled up with zeros to a multiple of 8.
+template <int THREADS, bool PLACES>
+__device__ __forceinline__ void rank_list(List& l, const uint32_t* places, uint32_t n) {
+  const uint32_t t = threadIdx.x, filled = (n + 7) & ~7u;
+  if (t < 8 && n + t < filled) l.value[n + t] = 0;
+  for (uint32_t i = t; i < n; i += THREADS) l.rank[i] = 0;
+  __syncthreads();
+  const uint32_t waves = (n + kOpsWave - 1) / kOpsWave;  // that the candidates fill
+  const uint32_t parts = waves ? (THREADS / kOpsWave + waves - 1) / waves : 0, len = parts ? ((filled / 8 + parts - 1) / parts) * 8 : 0;
+  for (uint32_t w = t / kOpsWave; w < waves * parts; w += THREADS / kOpsWave) {
+    const uint32_t i = w % waves * kOpsWave + t % kOpsWave, begin = w / waves * len;
+    const uint32_t end = begin + len < filled ? begin + len : filled;
+    const uint64_t mine = i < n ? l.value[i] : ~0ull;
+    const uint32_t place = PLACES && i < n ? places[i] : 0;
+    uint32_t rank = 0;
+    for (uint32_t j = begin; j < end; j += 8) {
+#pragma unroll
+      for (uint32_t x = 0; x < 8; ++x) {
+        const uint64_t other = l.value[j + x];
+        rank += other > mine ? 1 : 0;
+        if constexpr (PLACES) rank += static_cast<uint32_t>(other == mine) & static_cast<uint32_t>(places[j + x] < place);  // those past n are 0, mine is not
+      }
+    }
+    if (i < n && rank) atomicAdd(&l.rank[i], rank);
+  }
+  __syncthreads();
 }
 
 // A beam whose candidates come from its logits.
@@ -118,74 +155,91 @@ __device__ __forceinline__ float to_float(const u32x4& w, uint32_t j) {
 }
 
 // 8192 logits of a row. Rows start at any multiple of an element: reads go from the 16 bytes that the row's start lies in.
-// The `keep` best: the keep-th largest of the threads' maxima bounds them from below, since as many threads hold one
-// as large; what reaches it (few more than keep) goes to a list, whose entries rank themselves. Where more reach it
-// than the list holds, as of many equal logits, the bound is found bit by bit instead.
+// The `keep` best: as many of the threads' maxima reach a bound, so the keep-th best logit does. What reaches it (few
+// more than keep) goes to a list and is ranked there. Where more reach it than the list holds, as of many equal
+// logits, the bound is found bit by bit over all logits instead. One wave looks for the bound while the others form
+// their sums.
 template <class T>
-__global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
   constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC;
-  __shared__ uint64_t list[kList];
-  __shared__ float maxima[kThreads], bound;
+  __shared__ List l;
+  __shared__ __attribute__((aligned(16))) uint32_t maxima[kThreads];
+  __shared__ float tops[kThreads / kOpsWave];
   __shared__ double sums[kThreads / kOpsWave];
-  __shared__ uint32_t waves[kThreads / kOpsWave], listed;
+  __shared__ uint32_t waves[kThreads / kOpsWave], bound;
   const uint32_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, t = threadIdx.x;
-  if (!grows(a, row)) return;  // the merge does not read its part
   const uint64_t start = reinterpret_cast<uint64_t>(a.logits) + row * a.row_bytes;
   const uint32_t ahead = static_cast<uint32_t>(start % 16) / sizeof(T);  // elements between there and the row's start
-  const T* const from = reinterpret_cast<const T*>(start & ~15ull);
   const uint64_t first = static_cast<uint64_t>(split) * kBeamChunk, end = static_cast<uint64_t>(a.vocab) + ahead;
-  u32x4 w[NC];
-#pragma unroll
-  for (uint32_t i = 0; i < NC; ++i) {
-    const uint64_t v = first + (i * kThreads + t) * VEC;
-    w[i] = v < end ? *reinterpret_cast<const u32x4*>(from + v) : u32x4{0, 0, 0, 0};
-  }
+  const T* const from = reinterpret_cast<const T*>(start & ~15ull) + first;
+  const uint32_t here = end <= first ? 0 : end - first < kBeamChunk ? static_cast<uint32_t>(end - first) : kBeamChunk;  // 0: a part
+  // that only rows with another start have
+  if (!grows(a, row)) return;  // the merge does not read its part
   float x[kPer], top = -INFINITY;
   bool bad = false;
+  if ((first || !ahead) && here == kBeamChunk) {
+    u32x4 w[NC];
+#pragma unroll
+    for (uint32_t i = 0; i < NC; ++i) w[i] = *reinterpret_cast<const u32x4*>(from + (i * kThreads + t) * VEC);
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) x[i] = to_float<T>(w[i / VEC], i % VEC) + 0.0f;
+  } else {
+    const uint32_t low = first ? 0 : ahead;
+    u32x4 w[NC];
+#pragma unroll
+    for (uint32_t i = 0; i < NC; ++i) {
+      const uint32_t v = (i * kThreads + t) * VEC;
+      w[i] = v < here ? *reinterpret_cast<const u32x4*>(from + v) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) {
+      const uint32_t v = (i / VEC * kThreads + t) * VEC + i % VEC;
+      const float y = to_float<T>(w[i / VEC], i % VEC) + 0.0f;
+      x[i] = v >= low && v < here ? y : -INFINITY;
+    }
+  }
 #pragma unroll
   for (uint32_t i = 0; i < kPer; ++i) {
-    const uint64_t v = first + (i / VEC * kThreads + t) * VEC + i % VEC;
-    const float y = to_float<T>(w[i / VEC], i % VEC) + 0.0f;
-    x[i] = v >= ahead && v < end ? y : -INFINITY;
-    bad = bad || x[i] != x[i] || x[i] == INFINITY;
+    bad = bad || !(x[i] < INFINITY);
     top = fmaxf(top, x[i]);
   }
   const auto token_of = [&](uint32_t i) {
-    return static_cast<uint32_t>(first + (i / VEC * kThreads + t) * VEC + i % VEC - ahead);
+    return static_cast<uint32_t>(first - ahead) + (i / VEC * kThreads + t) * VEC + i % VEC;
   };
-  maxima[t] = top;
-  if (!t) listed = 0;
-  __syncthreads();
-  float all = top;
+  maxima[t] = ordered(top);
   {
-    float m = max_of_wave(top);
-    if (t % kOpsWave == 0) sums[t / kOpsWave] = m;
-    bound_of(maxima, a.keep, &bound);
-    __syncthreads();
-    all = fmaxf(fmaxf(sums[0], sums[1]), fmaxf(sums[2], sums[3]));
+    const float m = max_of_wave(top);
+    if (t % kOpsWave == 0) tops[t / kOpsWave] = m;
   }
-  const float least = bound;
+  if (!t) l.n = 0;
   __syncthreads();
+  const float all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  if (t / kOpsWave == split % (kThreads / kOpsWave)) {
+    const uint32_t b = bound_of(maxima, a.keep);
+    if (t % kOpsWave == 0) bound = b;
+  }
 
   // The sum, from the chunk's maximum. Logits far below it count for e^-600, nothing.
-  double sum = 0;
+  double sum[2] = {0, 0};
   if (all > -INFINITY) {
     const float floor = all - 600.0f;
     const double from_top = all;
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) sum += exp_of(static_cast<double>(fmaxf(x[i], floor)) - from_top);
+    for (uint32_t i = 0; i < kPer; ++i) sum[i % 2] += exp_of(static_cast<double>(fmaxf(x[i], floor)) - from_top);
   }
-  if (bad) sum = NAN;
-  sum = sum_of_wave(sum);
-  if (t % kOpsWave == 0) sums[t / kOpsWave] = sum;
+  if (bad) sum[0] = NAN;
+  sum[0] = sum_of_wave(sum[0] + sum[1]);
+  if (t % kOpsWave == 0) sums[t / kOpsWave] = sum[0];
+  __syncthreads();
 
-  // The candidates.
-  if (top >= least && top > -INFINITY) {
+  // The candidates: no -infinity among them.
+  const float least = bound > ordered(-3.4028234664e38f) ? unordered(bound) : -3.4028234664e38f;
+  if (top >= least) {
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i)
-      if (x[i] >= least && x[i] > -INFINITY) {
-        const uint32_t at = atomicAdd(&listed, 1u);
-        if (at < kList) list[at] = key_of(x[i], token_of(i));
+      if (x[i] >= least) {
+        const uint32_t at = atomicAdd(&l.n, 1u);
+        if (at < kList) l.value[at] = key_of(x[i], token_of(i));
       }
   }
   __syncthreads();
@@ -194,95 +248,98 @@ __global__ __launch_bounds__(kThreads) void beam_chunk_kernel(BeamArgs a) {
     a.part_max[part] = all;
     a.part_sum[part] = sums[0] + sums[1] + sums[2] + sums[3];
   }
-  uint32_t n = listed;
+  uint32_t n = l.n;
   if (n > kList) {  // the largest key that at least `keep` candidates reach, which are then exactly so many
     uint64_t key = 0;
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t next = key | 1ull << bit;
       if (count_of<kPer>(waves, [&](int i) { return x[i] > -INFINITY && key_of(x[i], token_of(i)) >= next; }) >= a.keep) key = next;
     }
     __syncthreads();
-    if (!t) listed = 0;
+    if (!t) l.n = 0;
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i)
-      if (x[i] > -INFINITY && key_of(x[i], token_of(i)) >= key) list[atomicAdd(&listed, 1u)] = key_of(x[i], token_of(i));
+      if (x[i] > -INFINITY && key_of(x[i], token_of(i)) >= key) l.value[atomicAdd(&l.n, 1u)] = key_of(x[i], token_of(i));
     __syncthreads();
-    n = listed;
+    n = l.n;
   }
+  rank_list<kThreads, false>(l, nullptr, n);
   uint64_t* const out = a.lists + part * a.keep;
-  for (uint32_t i = t; i < n; i += kThreads) {
-    const uint64_t mine = list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine ? 1 : 0;
-    if (rank < a.keep) out[rank] = mine;
-  }
+  for (uint32_t i = t; i < n; i += kThreads)
+    if (l.rank[i] < a.keep) out[l.rank[i]] = l.value[i];
   for (uint32_t i = n + t; i < a.keep; i += kThreads) out[i] = 0;
 }
 
-// The `keep` best of up to 16 values of each of 1024 threads (0: none), ties to the lower place i * 1024 + thread: found as
-// in beam_chunk_kernel, with the maxima of four threads each. give(rank, value, place); returns how many there are.
+// The `keep` best of up to 16 values of each of 1024 threads (0: none), ties to the lower place i * 1024 + thread; values past
+// `total` are none. Found as in beam_chunk_kernel, with the maxima of four threads each. give(rank, value, place); returns
+// how many there are.
 template <class F>
-__device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint32_t keep, F give) {
-  __shared__ uint64_t list[kList];
-  __shared__ uint32_t places[kList], maxima[256], waves[kMerge / kOpsWave], bound, listed;
+__device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint32_t total, uint32_t keep, F give) {
+  __shared__ List l;
+  __shared__ __attribute__((aligned(16))) uint32_t maxima[256];
+  __shared__ uint32_t places[kList + 8], waves[kMerge / kOpsWave], bound;
   const uint32_t t = threadIdx.x;
-  uint64_t top = 0;
+  if (!t) l.n = 0;
+  if (total > 256) {  // else all go to the list
+    uint64_t top = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) top = v[i] > top ? v[i] : top;
-  uint32_t high = static_cast<uint32_t>(top >> 32);
+    for (uint32_t i = 0; i < kMergePer; ++i) top = v[i] > top ? v[i] : top;
+    uint32_t high = static_cast<uint32_t>(top >> 32);
 #pragma unroll
-  for (int x = 1; x < 4; x *= 2) {
-    const uint32_t y = __shfl_xor(high, x, kOpsWave);
-    high = y > high ? y : high;
+    for (int x = 1; x < 4; x *= 2) {
+      const uint32_t y = __shfl_xor(high, x, kOpsWave);
+      high = y > high ? y : high;
+    }
+    if (t % 4 == 0) maxima[t / 4] = high;
+    __syncthreads();
+    if (t < kOpsWave) {
+      const uint32_t b = bound_of(maxima, keep);
+      if (!t) bound = b;
+    }
   }
-  if (t % 4 == 0) maxima[t / 4] = high;
-  if (!t) listed = 0;
   __syncthreads();
-  bound_of(maxima, keep, &bound);
-  __syncthreads();
-  uint64_t least = static_cast<uint64_t>(bound) << 32;
+  uint64_t least = total > 256 ? static_cast<uint64_t>(bound) << 32 : 1;
   if (!least) least = 1;
 #pragma unroll
   for (uint32_t i = 0; i < kMergePer; ++i)
     if (v[i] >= least) {
-      const uint32_t at = atomicAdd(&listed, 1u);
-      if (at < kList) list[at] = v[i], places[at] = i * kMerge + t;
+      const uint32_t at = atomicAdd(&l.n, 1u);
+      if (at < kList) l.value[at] = v[i], places[at] = i * kMerge + t;
     }
   __syncthreads();
-  uint32_t n = listed;
+  uint32_t n = l.n;
   if (n > kList) {
     uint64_t key = 0;
+#pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t next = key | 1ull << bit;
       if (count_of<kMergePer>(waves, [&](int i) { return v[i] >= next; }) >= keep) key = next;
     }
-    // All above it, and of those that equal it the lowest places: below the smallest `until` that leaves enough of them.
+    // All above it, and of those that equal it the lowest places, up to `until`.
     const uint32_t more = keep - count_of<kMergePer>(waves, [&](int i) { return v[i] > key; });
     uint32_t until = 0;
+#pragma unroll 1
     for (uint32_t bit = kBeamMerge; bit; bit /= 2) {
       const uint32_t next = until + bit;
       if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return v[i] == key && i * kMerge + t < next; }) < more) until = next;
     }
     __syncthreads();
-    if (!t) listed = 0;
+    if (!t) l.n = 0;
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < kMergePer; ++i)
       if (v[i] > key || (v[i] == key && i * kMerge + t <= until)) {
-        const uint32_t at = atomicAdd(&listed, 1u);
-        if (at < kList) list[at] = v[i], places[at] = i * kMerge + t;
+        const uint32_t at = atomicAdd(&l.n, 1u);
+        if (at < kList) l.value[at] = v[i], places[at] = i * kMerge + t;
       }
     __syncthreads();
-    n = listed;
+    n = l.n;
   }
-  for (uint32_t i = t; i < n; i += kMerge) {
-    const uint64_t mine = list[i];
-    const uint32_t place = places[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < n; ++j) rank += list[j] > mine || (list[j] == mine && places[j] < place) ? 1 : 0;
-    if (rank < keep) give(rank, mine, place);
-  }
+  rank_list<kMerge, true>(l, places, n);
+  for (uint32_t i = t; i < n; i += kMerge)
+    if (l.rank[i] < keep) give(l.rank[i], l.value[i], places[i]);
   return n < keep ? n : keep;
 }
 
@@ -293,9 +350,12 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
   const uint64_t* from = a.lists + static_cast<uint64_t>(row) * n;
   uint64_t v[kMergePer];
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) v[i] = i * kMerge + t < n ? from[i * kMerge + t] : 0;
+  for (uint32_t i = 0; i < kMergePer; ++i) {
+    v[i] = 0;
+    if (i * kMerge + t < n) v[i] = from[i * kMerge + t];
+  }
   uint64_t* const out = a.rows + static_cast<uint64_t>(row) * a.keep;
-  const uint32_t found = best_of(v, a.keep, [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
+  const uint32_t found = best_of(v, n, a.keep, [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) out[i] = 0;
 }
 
@@ -303,52 +363,56 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
 __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
   __shared__ double scores[kBeamMost], lses[kBeamMost];
   __shared__ uint8_t state[kBeamMost];  // 0: no candidates, 1: from its logits, 2: done
-  const uint32_t item = blockIdx.x, t = threadIdx.x, lane = t % kOpsWave;
-  for (uint32_t beam = t / kOpsWave; beam < a.beams; beam += kMerge / kOpsWave) {
-    const uint32_t row = item * a.beams + beam;
-    uint8_t is = !finite(a.scores[row]) ? 0 : a.done && a.done[row] ? 2 : 1;
-    double lse = 0;
-    if (is == 1) {
-      const float* m = a.part_max + static_cast<uint64_t>(row) * a.splits;
-      const double* s = a.part_sum + static_cast<uint64_t>(row) * a.splits;
-      float top = -INFINITY;
-      for (uint32_t i = lane; i < a.splits; i += kOpsWave) top = fmaxf(top, m[i]);
-      top = max_of_wave(top);
-      double sum = 0;
-      for (uint32_t i = lane; i < a.splits; i += kOpsWave) {
-        const double from_top = static_cast<double>(m[i]) - top;
-        sum += s[i] * (m[i] > -INFINITY ? exp(from_top) : 0.0);
-      }
-      sum = sum_of_wave(sum);
-      if (!(sum > 0)) is = 0;  // no logit above -infinity, or one that is no number or +infinity
-      lse = top + log(sum);
-    }
-    if (!lane) {
-      scores[beam] = a.scores[row];
-      lses[beam] = lse;
-      state[beam] = is;
-    }
-  }
-  __syncthreads();
+  const uint32_t item = blockIdx.x, t = threadIdx.x;
+  constexpr uint32_t kLanes = kMerge / kBeamMost;  // of a beam
   const uint64_t* const lists = a.rows ? a.rows : a.lists;
   const uint32_t per = a.rows ? a.keep : a.splits * a.keep, n = a.beams * per;  // candidates of a beam, of all
   const uint64_t* const from = lists + static_cast<uint64_t>(item) * n;
   uint64_t v[kMergePer];
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) {
-    const uint32_t at = i * kMerge + t;
+  for (uint32_t i = 0; i < kMergePer; ++i) {  // the keys first; lists of beams that have none hold anything
     v[i] = 0;
-    if (at >= n) continue;
-    const uint32_t beam = at / per;
-    if (state[beam] == 1) {
-      const uint64_t key = from[at];
-      if (key) v[i] = ordered(scores[beam] + (unordered(static_cast<uint32_t>(key >> 32)) - lses[beam]) + 0.0);
-    } else if (state[beam] == 2 && at % per == 0) {
-      v[i] = ordered(scores[beam] + 0.0);
+    if (i * kMerge + t < n) v[i] = from[i * kMerge + t];
+  }
+  if (t / kLanes < a.beams) {
+    const uint32_t beam = t / kLanes, lane = t % kLanes, row = item * a.beams + beam;
+    const float score = a.scores[row];
+    uint8_t is = !finite(score) ? 0 : a.done && a.done[row] ? 2 : 1;
+    double lse = 0;
+    if (is == 1) {
+      const float* m = a.part_max + static_cast<uint64_t>(row) * a.splits;
+      const double* s = a.part_sum + static_cast<uint64_t>(row) * a.splits;
+      float top = -INFINITY;
+      for (uint32_t i = lane; i < a.splits; i += kLanes) top = fmaxf(top, m[i]);
+#pragma unroll
+      for (uint32_t x = 1; x < kLanes; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kLanes));
+      double sum = 0;
+      for (uint32_t i = lane; i < a.splits; i += kLanes)
+        sum += s[i] * (m[i] > -INFINITY ? exp_of(static_cast<double>(fmaxf(m[i], top - 600.0f)) - top) : 0.0);
+#pragma unroll
+      for (uint32_t x = 1; x < kLanes; x *= 2) sum += __shfl_xor(sum, x, kLanes);
+      if (!(sum > 0)) is = 0;  // no logit above -infinity, or one that is no number or +infinity
+      lse = top + log(sum);
+    }
+    if (!lane) {
+      scores[beam] = score;
+      lses[beam] = lse;
+      state[beam] = is;
     }
   }
+  __syncthreads();
+#pragma unroll
+  for (uint32_t i = 0; i < kMergePer; ++i) {
+    const uint32_t at = i * kMerge + t;
+    if (at >= n) break;
+    const uint32_t beam = at / per, is = state[beam];
+    const uint64_t key = v[i];
+    v[i] = 0;
+    if (is == 1 && key) v[i] = ordered(scores[beam] + (unordered(static_cast<uint32_t>(key >> 32)) - lses[beam]) + 0.0);
+    if (is == 2 && at == beam * per) v[i] = ordered(scores[beam] + 0.0);
+  }
   const uint64_t to = static_cast<uint64_t>(item) * a.keep;
-  const uint32_t found = best_of(v, a.keep, [&](uint32_t rank, uint64_t value, uint32_t at) {
+  const uint32_t found = best_of(v, n, a.keep, [&](uint32_t rank, uint64_t value, uint32_t at) {
     const uint32_t beam = at / per;
     a.tokens[to + rank] = state[beam] == 2 ? a.done_token : static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(from[at]));
     a.parents[to + rank] = static_cast<int32_t>(item * a.beams + beam);
