@@ -18,7 +18,7 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr uint32_t kThreads = 256;
+constexpr uint32_t kThreads = 512;
 constexpr uint32_t kPer = kBeamChunk / kThreads;  // logits of a thread
 constexpr uint32_t kList = 1024;                  // candidates that a workgroup ranks
 constexpr uint32_t kMerge = 1024;                 // threads of a merge
@@ -91,19 +91,27 @@ __device__ __forceinline__ uint32_t count_of(uint32_t* waves, F is) {
   return n;
 }
 
-// A number that at least `keep` of 256 in LDS reach, and hardly more: by one wave, bit by bit from the top until exactly as
-// many do. (Each of 256 threads ranking its own number against the others took 17 us, waiting on LDS.)
+// A number that at least `keep` of 256 in LDS reach, and a quarter more at most where they differ: by one wave, bit by bit
+// from the top. (Each of 256 threads ranking its own number against the others took 17 us, waiting on LDS.)
 __device__ __forceinline__ uint32_t bound_of(const uint32_t* numbers, uint32_t keep) {
   const u32x4 x = *reinterpret_cast<const u32x4*>(numbers + threadIdx.x % kOpsWave * 4);
+  const uint32_t enough = keep + keep / 4;
   uint32_t bound = 0;
   for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
     const uint32_t next = bound | bit;
     const uint32_t n = __popcll(__ballot(x[0] >= next)) + __popcll(__ballot(x[1] >= next)) + __popcll(__ballot(x[2] >= next)) +
                        __popcll(__ballot(x[3] >= next));
     if (n >= keep) bound = next;
-    if (n == keep) break;
+    if (n >= keep && n <= enough) break;
   }
   return bound;
+}
+
+// Places in a list for the lanes whose bits `is` has, after those of `*at`, which moves on by as many.
+__device__ __forceinline__ uint32_t place_of(uint64_t is, uint32_t* at) {
+  const uint32_t mine = *at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(is >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(is), 0));
+  *at += __popcll(is);
+  return mine;
 }
 
 // Candidates of a list in LDS: larger values first, equal ones by place (PLACES; else there are no equal ones).
@@ -163,7 +171,7 @@ template <class T>
 __global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
   constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC;
   __shared__ List l;
-  __shared__ __attribute__((aligned(16))) uint32_t maxima[kThreads];
+  __shared__ __attribute__((aligned(16))) uint32_t maxima[kThreads / 2];
   __shared__ float tops[kThreads / kOpsWave];
   __shared__ double sums[kThreads / kOpsWave];
   __shared__ uint32_t waves[kThreads / kOpsWave], bound;
@@ -206,14 +214,15 @@ __global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
   const auto token_of = [&](uint32_t i) {
     return static_cast<uint32_t>(first - ahead) + (i / VEC * kThreads + t) * VEC + i % VEC;
   };
-  maxima[t] = ordered(top);
-  {
-    const float m = max_of_wave(top);
-    if (t % kOpsWave == 0) tops[t / kOpsWave] = m;
-  }
+  float high = fmaxf(top, __shfl_xor(top, 1, kOpsWave));
+  if (t % 2 == 0) maxima[t / 2] = ordered(high);
+  high = max_of_wave(high);
+  if (t % kOpsWave == 0) tops[t / kOpsWave] = high;
   if (!t) l.n = 0;
   __syncthreads();
-  const float all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float all = tops[0];
+#pragma unroll
+  for (uint32_t i = 1; i < kThreads / kOpsWave; ++i) all = fmaxf(all, tops[i]);
   if (t / kOpsWave == split % (kThreads / kOpsWave)) {
     const uint32_t b = bound_of(maxima, a.keep);
     if (t % kOpsWave == 0) bound = b;
@@ -234,19 +243,28 @@ __global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
 
   // The candidates: no -infinity among them.
   const float least = bound > ordered(-3.4028234664e38f) ? unordered(bound) : -3.4028234664e38f;
-  if (top >= least) {
+  if (__any(top >= least)) {
+    uint32_t mine = 0, at = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i)
-      if (x[i] >= least) {
-        const uint32_t at = atomicAdd(&l.n, 1u);
-        if (at < kList) l.value[at] = key_of(x[i], token_of(i));
-      }
+    for (uint32_t i = 0; i < kPer; ++i) mine += __popcll(__ballot(x[i] >= least));
+    if (t % kOpsWave == 0) at = atomicAdd(&l.n, mine);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; ++i) {
+      const uint64_t is = __ballot(x[i] >= least);
+      if (!is) continue;
+      const uint32_t to = place_of(is, &at);
+      if (x[i] >= least && to < kList) l.value[to] = key_of(x[i], token_of(i));
+    }
   }
   __syncthreads();
   const uint64_t part = static_cast<uint64_t>(row) * a.splits + split;
   if (!t) {
     a.part_max[part] = all;
-    a.part_sum[part] = sums[0] + sums[1] + sums[2] + sums[3];
+    double add = sums[0];
+#pragma unroll
+    for (uint32_t i = 1; i < kThreads / kOpsWave; ++i) add += sums[i];
+    a.part_sum[part] = add;
   }
   uint32_t n = l.n;
   if (n > kList) {  // the largest key that at least `keep` candidates reach, which are then exactly so many
@@ -272,11 +290,12 @@ __global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
   for (uint32_t i = n + t; i < a.keep; i += kThreads) out[i] = 0;
 }
 
-// The `keep` best of up to 16 values of each of 1024 threads (0: none), ties to the lower place i * 1024 + thread; values past
-// `total` are none. Found as in beam_chunk_kernel, with the maxima of four threads each. give(rank, value, place); returns
-// how many there are.
+// The `keep` best of `total` values, `per` of each of 1024 threads side by side (0: none), ties to the lower place thread *
+// per + i. Found as in beam_chunk_kernel, with the maxima of four threads each: values come in descending lists, and
+// these are the lists' first ones. (With values 1024 apart a thread has one rank of many lists, the bound was so low that the
+// list overflowed: 32 beams of 8 parts of 64, 42 us.) give(rank, value, place); returns how many there are.
 template <class F>
-__device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint32_t total, uint32_t keep, F give) {
+__device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint32_t total, uint32_t per, uint32_t keep, F give) {
   __shared__ List l;
   __shared__ __attribute__((aligned(16))) uint32_t maxima[256];
   __shared__ uint32_t places[kList + 8], waves[kMerge / kOpsWave], bound;
@@ -302,12 +321,18 @@ __device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint
   __syncthreads();
   uint64_t least = total > 256 ? static_cast<uint64_t>(bound) << 32 : 1;
   if (!least) least = 1;
+  uint32_t mine = 0, at = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i)
-    if (v[i] >= least) {
-      const uint32_t at = atomicAdd(&l.n, 1u);
-      if (at < kList) l.value[at] = v[i], places[at] = i * kMerge + t;
-    }
+  for (uint32_t i = 0; i < kMergePer; ++i) mine += __popcll(__ballot(v[i] >= least));
+  if (mine && t % kOpsWave == 0) at = atomicAdd(&l.n, mine);
+  at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+  for (uint32_t i = 0; i < kMergePer; ++i) {
+    const uint64_t is = __ballot(v[i] >= least);
+    if (!is) continue;
+    const uint32_t to = place_of(is, &at);
+    if (v[i] >= least && to < kList) l.value[to] = v[i], places[to] = t * per + i;
+  }
   __syncthreads();
   uint32_t n = l.n;
   if (n > kList) {
@@ -323,16 +348,16 @@ __device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint
 #pragma unroll 1
     for (uint32_t bit = kBeamMerge; bit; bit /= 2) {
       const uint32_t next = until + bit;
-      if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return v[i] == key && i * kMerge + t < next; }) < more) until = next;
+      if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return v[i] == key && t * per + i < next; }) < more) until = next;
     }
     __syncthreads();
     if (!t) l.n = 0;
     __syncthreads();
 #pragma unroll
     for (uint32_t i = 0; i < kMergePer; ++i)
-      if (v[i] > key || (v[i] == key && i * kMerge + t <= until)) {
+      if (v[i] > key || (v[i] == key && t * per + i <= until)) {
         const uint32_t at = atomicAdd(&l.n, 1u);
-        if (at < kList) l.value[at] = v[i], places[at] = i * kMerge + t;
+        if (at < kList) l.value[at] = v[i], places[at] = t * per + i;
       }
     __syncthreads();
     n = l.n;
@@ -349,13 +374,14 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
   if (!grows(a, row)) return;
   const uint64_t* from = a.lists + static_cast<uint64_t>(row) * n;
   uint64_t v[kMergePer];
+  const uint32_t each = (n + kMerge - 1) / kMerge;
 #pragma unroll
   for (uint32_t i = 0; i < kMergePer; ++i) {
     v[i] = 0;
-    if (i * kMerge + t < n) v[i] = from[i * kMerge + t];
+    if (i < each && t * each + i < n) v[i] = from[t * each + i];
   }
   uint64_t* const out = a.rows + static_cast<uint64_t>(row) * a.keep;
-  const uint32_t found = best_of(v, n, a.keep, [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
+  const uint32_t found = best_of(v, n, each, a.keep, [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) out[i] = 0;
 }
 
@@ -369,26 +395,33 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
   const uint32_t per = a.rows ? a.keep : a.splits * a.keep, n = a.beams * per;  // candidates of a beam, of all
   const uint64_t* const from = lists + static_cast<uint64_t>(item) * n;
   uint64_t v[kMergePer];
+  const uint32_t each = (n + kMerge - 1) / kMerge;
 #pragma unroll
   for (uint32_t i = 0; i < kMergePer; ++i) {  // the keys first; lists of beams that have none hold anything
     v[i] = 0;
-    if (i * kMerge + t < n) v[i] = from[i * kMerge + t];
+    if (i < each && t * each + i < n) v[i] = from[t * each + i];
   }
   if (t / kLanes < a.beams) {
     const uint32_t beam = t / kLanes, lane = t % kLanes, row = item * a.beams + beam;
+    const float* m = a.part_max + static_cast<uint64_t>(row) * a.splits;
+    const double* s = a.part_sum + static_cast<uint64_t>(row) * a.splits;
+    // Asked for at once: of a beam without candidates they are anything.
     const float score = a.scores[row];
-    uint8_t is = !finite(score) ? 0 : a.done && a.done[row] ? 2 : 1;
+    const uint8_t over = a.done ? a.done[row] : 0;
+    const float m0 = lane < a.splits ? m[lane] : -INFINITY;
+    const double s0 = lane < a.splits ? s[lane] : 0.0;
+    uint8_t is = !finite(score) ? 0 : over ? 2 : 1;
     double lse = 0;
     if (is == 1) {
-      const float* m = a.part_max + static_cast<uint64_t>(row) * a.splits;
-      const double* s = a.part_sum + static_cast<uint64_t>(row) * a.splits;
-      float top = -INFINITY;
-      for (uint32_t i = lane; i < a.splits; i += kLanes) top = fmaxf(top, m[i]);
+      float top = m0;
+      for (uint32_t i = lane + kLanes; i < a.splits; i += kLanes) top = fmaxf(top, m[i]);
 #pragma unroll
       for (uint32_t x = 1; x < kLanes; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kLanes));
-      double sum = 0;
-      for (uint32_t i = lane; i < a.splits; i += kLanes)
-        sum += s[i] * (m[i] > -INFINITY ? exp_of(static_cast<double>(fmaxf(m[i], top - 600.0f)) - top) : 0.0);
+      const auto part = [&](float max, double sum) {
+        return sum * (max > -INFINITY ? exp_of(static_cast<double>(fmaxf(max, top - 600.0f)) - top) : 0.0);
+      };
+      double sum = part(m0, s0);
+      for (uint32_t i = lane + kLanes; i < a.splits; i += kLanes) sum += part(m[i], s[i]);
 #pragma unroll
       for (uint32_t x = 1; x < kLanes; x *= 2) sum += __shfl_xor(sum, x, kLanes);
       if (!(sum > 0)) is = 0;  // no logit above -infinity, or one that is no number or +infinity
@@ -401,18 +434,24 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
     }
   }
   __syncthreads();
+  {
+    uint32_t beam = t * each / per, in = t * each - beam * per, is = 0;  // of the thread's first value, then of the next
+    double score = 0, lse = 0;
+    bool fresh = true;
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) {
-    const uint32_t at = i * kMerge + t;
-    if (at >= n) break;
-    const uint32_t beam = at / per, is = state[beam];
-    const uint64_t key = v[i];
-    v[i] = 0;
-    if (is == 1 && key) v[i] = ordered(scores[beam] + (unordered(static_cast<uint32_t>(key >> 32)) - lses[beam]) + 0.0);
-    if (is == 2 && at == beam * per) v[i] = ordered(scores[beam] + 0.0);
+    for (uint32_t i = 0; i < kMergePer; ++i) {
+      if (i >= each || t * each + i >= n) break;
+      if (fresh) is = state[beam], score = scores[beam], lse = lses[beam];
+      const uint64_t key = v[i];
+      v[i] = 0;
+      if (is == 1 && key) v[i] = ordered(score + (unordered(static_cast<uint32_t>(key >> 32)) - lse) + 0.0);
+      if (is == 2 && !in) v[i] = ordered(score + 0.0);
+      fresh = ++in == per;
+      if (fresh) in = 0, ++beam;
+    }
   }
   const uint64_t to = static_cast<uint64_t>(item) * a.keep;
-  const uint32_t found = best_of(v, n, a.keep, [&](uint32_t rank, uint64_t value, uint32_t at) {
+  const uint32_t found = best_of(v, n, each, a.keep, [&](uint32_t rank, uint64_t value, uint32_t at) {
     const uint32_t beam = at / per;
     a.tokens[to + rank] = state[beam] == 2 ? a.done_token : static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(from[at]));
     a.parents[to + rank] = static_cast<int32_t>(item * a.beams + beam);
