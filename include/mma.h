@@ -652,7 +652,7 @@ typedef struct mma_beam_select {
   uint32_t batch;
   uint32_t beams;           /* at most 64 */
   uint32_t vocab;
-  uint32_t keep;            /* at most 128, and times (vocab + 7) / 8192, rounded up, at most 16384 */
+  uint32_t keep;            /* at most 128 */
   uint32_t type;            /* MMA_TYPE_BF16, MMA_TYPE_F16 or MMA_TYPE_F32 */
   int32_t done_token;       /* with `done`: from 0 to vocab - 1 */
 } mma_beam_select_t;

@@ -3,26 +3,29 @@
 //
 // v = s + (x - lse), lse = log of the sum of exp x over the row. Within a row v is ordered as x is, so a row's best are
 // found from its logits alone while its sum is formed; only across beams the sums enter. So a workgroup of
-// beam_chunk_kernel reads 8192 logits of a row once, into registers, and leaves their maximum, their sum of exp and the
-// `keep` best; beam_merge_kernel joins what a request's workgroups left. Rows in more parts than a merge takes are joined
-// row by row between the two (beam_row_kernel).
+// beam_part_kernel reads a run of a row's logits once, 4096 at a time, and leaves their sum of exp and the `keep` best;
+// beam_merge_kernel joins what a request's workgroups left. Rows in more parts than a merge takes are joined row by row
+// between the two (beam_row_kernel).
 //
 // Sums and v are in 64 bits: two candidates of different beams may lie as close as the rounding of a 32-bit sum, and
-// which of them is chosen is a whole number. The vector units do 64-bit multiply-adds at half the rate of 32-bit ones, so
-// it costs little: 2^f on [-1/2, 1/2] is a polynomial of degree 8 (relative error 1.1e-12, interpolated at Chebyshev's
-// points), about 13 64-bit operations a logit.
+// which of them is chosen is a whole number. 2^f on [-1/2, 1/2] is a polynomial of degree 7 (relative error 5.5e-11,
+// interpolated at Chebyshev's points). A 64-bit multiply-add takes a SIMD no longer than a 32-bit one, 4 cycles for 64
+// lanes, and a logit some 15 such instructions.
 #include "mma_ops.h"
 
 namespace mma {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 
-constexpr uint32_t kThreads = 512;
-constexpr uint32_t kPer = kBeamChunk / kThreads;  // logits of a thread
-constexpr uint32_t kList = 1024;                  // candidates that a workgroup ranks
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kPer = kBeamChunk / kThreads;  // logits of a thread at a time
+constexpr uint32_t kList = 1024;                  // candidates of a part
 constexpr uint32_t kMerge = 1024;                 // threads of a merge
 constexpr uint32_t kMergePer = kBeamMerge / kMerge;
+constexpr uint32_t kMergeList = 2816;             // candidates of a merge
+constexpr float kLeast = -3.4028234664e38f;       // the least finite number
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
@@ -44,37 +47,89 @@ __device__ __forceinline__ double unordered(uint64_t b) {
 
 // A candidate of a row: its logit, then the lower token first. 0: none.
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) {
-  return static_cast<uint64_t>(ordered(x)) << 32 | (0xffffffffu - token);
+  return static_cast<uint64_t>(ordered(x + 0.0f)) << 32 | (0xffffffffu - token);  // -0 as 0
 }
 
-// e^d of -700 <= d <= 0.
-__device__ __forceinline__ double exp_of(double d) {
-  constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: added, it leaves the nearest whole number in the low bits
-  const double t = fma(d, 1.4426950408889634, kMagic);
-  const double f = fma(d, 1.4426950408889634, kMagic - t);
-  double p = 1.325497460306718e-06;
-  p = fma(p, f, 1.531007807039615e-05);
-  p = fma(p, f, 0.00015403457039410448);
-  p = fma(p, f, 0.0013333450573018062);
-  p = fma(p, f, 0.009618129157656703);
-  p = fma(p, f, 0.055504109412010456);
-  p = fma(p, f, 0.24022650695821055);
-  p = fma(p, f, 0.6931471805459343);
-  p = fma(p, f, 0.9999999999999997);
-  const uint64_t b = __builtin_bit_cast(uint64_t, p);  // times 2^n: into the exponent
-  const uint32_t high = static_cast<uint32_t>(b >> 32) + (static_cast<uint32_t>(__builtin_bit_cast(uint64_t, t)) << 20);
-  return __builtin_bit_cast(double, static_cast<uint64_t>(high) << 32 | static_cast<uint32_t>(b));
+constexpr double kE2 = 1.4426950408889634;     // log2(e)
+constexpr double kMagic = 6755399441055744.0;  // 1.5 2^52: added, it leaves the nearest whole number in the low bits
+
+// e^d 2^-R, where `magic` is kMagic - R, for a whole number R: d up to 2^49 in size, the result from 2^-1000 to 2^1000.
+__device__ __forceinline__ double exp_of(double d, double magic = kMagic) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const double t = fma(d, kE2, magic);
+  const double f = fma(d, kE2, magic - t);
+  double p = 1.5303699001378845e-05;
+  p = fma(p, f, 0.00015469729140704658);
+  p = fma(p, f, 0.0013333478480888061);
+  p = fma(p, f, 0.009618025613598036);
+  p = fma(p, f, 0.055504109063177154);
+  p = fma(p, f, 0.24022651213495422);
+  p = fma(p, f, 0.6931471805568341);
+  p = fma(p, f, 0.9999999999595622);
+  u32x2 b = __builtin_bit_cast(u32x2, p);  // times 2^n: into the exponent
+  b[1] += static_cast<uint32_t>(__builtin_bit_cast(uint64_t, t)) << 20;
+  return __builtin_bit_cast(double, b);
 }
 
-__device__ __forceinline__ float max_of_wave(float v) {
+// The same of four numbers, no less than `floor`, added to `sums`: side by side, so that a wave by itself keeps the unit busy.
+__device__ __forceinline__ void exp_of_4(const float* x, float floor, double magic, double (&sums)[4]) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  constexpr double kTerms[7] = {0.00015469729140704658, 0.0013333478480888061, 0.009618025613598036, 0.055504109063177154,
+                                0.24022651213495422, 0.6931471805568341, 0.9999999999595622};
+  double d[4], t[4], p[4];
 #pragma unroll
-  for (int x = 1; x < kOpsWave; x *= 2) v = fmaxf(v, __shfl_xor(v, x, kOpsWave));
-  return v;
+  for (int i = 0; i < 4; ++i) d[i] = __builtin_amdgcn_fmed3f(x[i], floor, INFINITY);  // the larger one, in one instruction
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = fma(d[i], kE2, magic);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d[i] = fma(d[i], kE2, magic - t[i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = 1.5303699001378845e-05;
+#pragma unroll
+  for (int j = 0; j < 7; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = fma(p[i], d[i], kTerms[j]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32x2 b = __builtin_bit_cast(u32x2, p[i]);
+    b[1] += static_cast<uint32_t>(__builtin_bit_cast(uint64_t, t[i])) << 20;
+    sums[i] += __builtin_bit_cast(double, b);
+  }
+}
+
+// A lane's value from another place of its row of 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true);
+}
+// Joined over the wave's lanes, without LDS: neighbours, pairs, halves of a row and rows mirrored, then rows exchanged.
+template <class F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, F join) {
+  x = join(x, moved<0xb1>(x));
+  x = join(x, moved<0x4e>(x));
+  x = join(x, moved<0x141>(x));
+  x = join(x, moved<0x140>(x));
+  auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = join(static_cast<uint32_t>(a[0]), static_cast<uint32_t>(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return join(static_cast<uint32_t>(a[0]), static_cast<uint32_t>(a[1]));
+}
+__device__ __forceinline__ uint32_t max_of_wave(uint32_t x) {
+  return over_wave(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int CTRL>
+__device__ __forceinline__ double plus_moved(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint64_t m = static_cast<uint64_t>(moved<CTRL>(static_cast<uint32_t>(b >> 32))) << 32 | moved<CTRL>(static_cast<uint32_t>(b));
+  return v + __builtin_bit_cast(double, m);
+}
+__device__ __forceinline__ double sum_of_row(double v) {  // over 16 lanes
+  return plus_moved<0x140>(plus_moved<0x141>(plus_moved<0x4e>(plus_moved<0xb1>(v))));
 }
 __device__ __forceinline__ double sum_of_wave(double v) {
-#pragma unroll
-  for (int x = 1; x < kOpsWave; x *= 2) v += __shfl_xor(v, x, kOpsWave);
-  return v;
+  v = sum_of_row(v);
+  v += __shfl_xor(v, 16, kOpsWave);
+  return v + __shfl_xor(v, 32, kOpsWave);
 }
 
 // How many threads of the workgroup, over their N values each, hold what `is` says; the same for every thread.
@@ -91,18 +146,38 @@ __device__ __forceinline__ uint32_t count_of(uint32_t* waves, F is) {
   return n;
 }
 
-// A number that at least `keep` of 256 in LDS reach, and a quarter more at most where they differ: by one wave, bit by bit
-// from the top. (Each of 256 threads ranking its own number against the others took 17 us, waiting on LDS.)
+// A number that at least `keep` of N in LDS reach, and a quarter more at most where they differ: by one wave, from the
+// largest with as few of its low bits gone as it takes, then bit by bit. (Each of 256 threads ranking its own number
+// against the others took 17 us, waiting on LDS; all 32 bits one by one 2.3 us.)
+template <int N>
 __device__ __forceinline__ uint32_t bound_of(const uint32_t* numbers, uint32_t keep) {
-  const u32x4 x = *reinterpret_cast<const u32x4*>(numbers + threadIdx.x % kOpsWave * 4);
-  const uint32_t enough = keep + keep / 4;
-  uint32_t bound = 0;
-  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
-    const uint32_t next = bound | bit;
-    const uint32_t n = __popcll(__ballot(x[0] >= next)) + __popcll(__ballot(x[1] >= next)) + __popcll(__ballot(x[2] >= next)) +
-                       __popcll(__ballot(x[3] >= next));
-    if (n >= keep) bound = next;
-    if (n >= keep && n <= enough) break;
+  u32x4 x[N / 256];
+#pragma unroll
+  for (int i = 0; i < N / 256; ++i) x[i] = *reinterpret_cast<const u32x4*>(numbers + (i * kOpsWave + threadIdx.x % kOpsWave) * 4);
+  const auto reach = [&](uint32_t v) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < N / 256; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) n += __popcll(__ballot(x[i][j] >= v));
+    return n;
+  };
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < N / 256; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = x[i][j] > top ? x[i][j] : top;
+  top = __builtin_amdgcn_readfirstlane(max_of_wave(top));
+  uint32_t gone = 0;
+#pragma unroll 1
+  for (uint32_t half = 16; half; half /= 2)
+    if (reach(top >> (gone + half - 1) << (gone + half - 1)) < keep) gone += half;
+  uint32_t bound = top >> gone << gone, n = reach(bound);
+  if (n < keep) bound = 0, gone = 32, n = N;
+#pragma unroll 1
+  for (uint32_t bit = gone > 1 ? 1u << (gone - 2) : 0; bit && n > keep + keep / 4; bit >>= 1) {
+    const uint32_t next = reach(bound | bit);
+    if (next >= keep) bound |= bit, n = next;
   }
   return bound;
 }
@@ -115,22 +190,38 @@ __device__ __forceinline__ uint32_t place_of(uint64_t is, uint32_t* at) {
 }
 
 // Candidates of a list in LDS: larger values first, equal ones by place (PLACES; else there are no equal ones).
+template <int N>
 struct List {
-  uint64_t value[kList + 8];
-  uint32_t rank[kList];
-  uint32_t n;
+  uint64_t value[N + 8];
+  uint32_t rank[N];
 };
 
-// Ranks of the list's n candidates, counted by all of THREADS threads: of few candidates several threads have one, each
-// against its share of the others. The list is filled up with zeros to a multiple of 8.
-template <int THREADS, bool PLACES>
-__device__ __forceinline__ void rank_list(List& l, const uint32_t* places, uint32_t n) {
+// Ranks of the list's n candidates. Up to 64 are one wave's; of more, all of THREADS threads count, several of them for one
+// candidate where there are few, each against its share of the others. The list is filled up with zeros to a multiple of 8.
+template <int THREADS, bool PLACES, int N>
+__device__ __forceinline__ void rank_list(List<N>& l, const uint32_t* places, uint32_t n) {
   const uint32_t t = threadIdx.x, filled = (n + 7) & ~7u;
+  if (n <= kOpsWave) {
+    if (t < n) {
+      const uint64_t mine = l.value[t];
+      const uint32_t low = static_cast<uint32_t>(mine), high = static_cast<uint32_t>(mine >> 32), place = PLACES ? places[t] : 0;
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < n; ++j) {
+        const uint64_t other = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(high, j))) << 32 |
+                               static_cast<uint32_t>(__builtin_amdgcn_readlane(low, j));
+        rank += other > mine ? 1 : 0;
+        if constexpr (PLACES) rank += static_cast<uint32_t>(other == mine) & static_cast<uint32_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(place, j)) < place);
+      }
+      l.rank[t] = rank;
+    }
+    __syncthreads();
+    return;
+  }
   if (t < 8 && n + t < filled) l.value[n + t] = 0;
   for (uint32_t i = t; i < n; i += THREADS) l.rank[i] = 0;
   __syncthreads();
   const uint32_t waves = (n + kOpsWave - 1) / kOpsWave;  // that the candidates fill
-  const uint32_t parts = waves ? (THREADS / kOpsWave + waves - 1) / waves : 0, len = parts ? ((filled / 8 + parts - 1) / parts) * 8 : 0;
+  const uint32_t parts = (THREADS / kOpsWave + waves - 1) / waves, len = ((filled / 8 + parts - 1) / parts) * 8;
   for (uint32_t w = t / kOpsWave; w < waves * parts; w += THREADS / kOpsWave) {
     const uint32_t i = w % waves * kOpsWave + t % kOpsWave, begin = w / waves * len;
     const uint32_t end = begin + len < filled ? begin + len : filled;
@@ -150,6 +241,39 @@ __device__ __forceinline__ void rank_list(List& l, const uint32_t* places, uint3
   __syncthreads();
 }
 
+// Leaves of a list of n (more than keep, at most N) those that reach a bound which hardly more than `keep` do, by the upper
+// halves of their values; the others' order does not matter. Returns how many.
+template <int THREADS, int N>
+__device__ __forceinline__ uint32_t thin(List<N>& l, uint32_t* places, uint32_t* numbers, uint32_t* waves, uint32_t n, uint32_t keep) {
+  const uint32_t t = threadIdx.x;
+  constexpr uint32_t kMine = (N + THREADS - 1) / THREADS;
+  static_assert(N % 256 == 0, "");
+  uint64_t v[kMine];
+  uint32_t place[kMine];
+  for (uint32_t i = t; i < N; i += THREADS) numbers[i] = i < n ? static_cast<uint32_t>(l.value[i] >> 32) : 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kMine; ++i) {
+    v[i] = i * THREADS + t < n ? l.value[i * THREADS + t] : 0;
+    place[i] = places && i * THREADS + t < n ? places[i * THREADS + t] : 0;
+  }
+  __syncthreads();
+  if (t < kOpsWave) {
+    const uint32_t b = bound_of<N>(numbers, keep);
+    if (!t) waves[0] = b, waves[1] = 0;
+  }
+  __syncthreads();
+  const uint32_t b = waves[0];
+#pragma unroll
+  for (uint32_t i = 0; i < kMine; ++i)
+    if (v[i] && v[i] >> 32 >= b) {
+      const uint32_t to = atomicAdd(&waves[1], 1u);
+      l.value[to] = v[i];
+      if (places) places[to] = place[i];
+    }
+  __syncthreads();
+  return waves[1];
+}
+
 // A beam whose candidates come from its logits.
 __device__ __forceinline__ bool grows(const BeamArgs& a, uint32_t row) {
   return finite(a.scores[row]) && !(a.done && a.done[row]);
@@ -162,126 +286,210 @@ __device__ __forceinline__ float to_float(const u32x4& w, uint32_t j) {
   else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(word >> (j % 2 * 16))));
 }
 
-// 8192 logits of a row. Rows start at any multiple of an element: reads go from the 16 bytes that the row's start lies in.
-// The `keep` best: as many of the threads' maxima reach a bound, so the keep-th best logit does. What reaches it (few
-// more than keep) goes to a list and is ranked there. Where more reach it than the list holds, as of many equal
-// logits, the bound is found bit by bit over all logits instead. One wave looks for the bound while the others form
-// their sums.
+// A run of a row's logits, 4096 at a time, the next ones on their way; a time takes its 256 threads' 16 bytes from places that
+// the run's times share evenly, so that the first one is like the others. Rows start at any multiple of an element,
+// and a thread's logits go by their tokens all the same, not by 16 aligned bytes: equal rows so have equal sums, to the
+// last bit, and beams that are alike tie.
+//
+// The sum of exp is a thread's own, from its largest logit of the first time, until the end. The `keep` best: as many
+// of the threads' maxima of the first time reach a bound, so the keep-th best logit does; what reaches it goes to a list, and
+// nobody waits for another wave until, some times later, and then ever later, the list is thinned and the bound raised by
+// it. A list that overflows, as of equal logits, is found anew with a wait at every time (careful).
+//
+// 192 rows of 128001 in 32 bits: ...
 template <class T>
-__global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
-  constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC;
-  __shared__ List l;
-  __shared__ __attribute__((aligned(16))) uint32_t maxima[kThreads / 2];
-  __shared__ float tops[kThreads / kOpsWave];
-  __shared__ double sums[kThreads / kOpsWave];
-  __shared__ uint32_t waves[kThreads / kOpsWave], bound;
-  const uint32_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, t = threadIdx.x;
-  const uint64_t start = reinterpret_cast<uint64_t>(a.logits) + row * a.row_bytes;
-  const uint32_t ahead = static_cast<uint32_t>(start % 16) / sizeof(T);  // elements between there and the row's start
-  const uint64_t first = static_cast<uint64_t>(split) * kBeamChunk, end = static_cast<uint64_t>(a.vocab) + ahead;
-  const T* const from = reinterpret_cast<const T*>(start & ~15ull) + first;
-  const uint32_t here = end <= first ? 0 : end - first < kBeamChunk ? static_cast<uint32_t>(end - first) : kBeamChunk;  // 0: a part
-  // that only rows with another start have
+__global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
+  constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC, kWaves = kThreads / kOpsWave, kSegment = kThreads * VEC;
+  __shared__ List<kList> l;
+  __shared__ __attribute__((aligned(16))) uint32_t numbers[kList];
+  __shared__ float tops[kWaves];
+  __shared__ double sums[kWaves];
+  __shared__ uint32_t waves[kWaves], bound, listed;
+  const uint32_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, t = threadIdx.x, lane = t % kOpsWave, wave = t / kOpsWave;
+  const uint32_t first = split * a.run * kBeamChunk, all = a.vocab - first;  // of the part's first logit; logits from there on
+  const uint32_t many = all < a.run * kBeamChunk ? all : a.run * kBeamChunk, times = (many + kBeamChunk - 1) / kBeamChunk;
+  const uint16_t* const from = reinterpret_cast<const uint16_t*>(a.logits + row * a.row_bytes) + first * static_cast<uint64_t>(sizeof(T) / 2);
   if (!grows(a, row)) return;  // the merge does not read its part
-  float x[kPer], top = -INFINITY;
-  bool bad = false;
-  if ((first || !ahead) && here == kBeamChunk) {
-    u32x4 w[NC];
-#pragma unroll
-    for (uint32_t i = 0; i < NC; ++i) w[i] = *reinterpret_cast<const u32x4*>(from + (i * kThreads + t) * VEC);
-#pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) x[i] = to_float<T>(w[i / VEC], i % VEC) + 0.0f;
-  } else {
-    const uint32_t low = first ? 0 : ahead;
-    u32x4 w[NC];
+  u32x4 w[NC];
+  float x[kPer];
+  const auto place_at = [&](uint32_t time, uint32_t i) { return (i / VEC * times + time) * kSegment + t * VEC + i % VEC; };
+  const auto load = [&](uint32_t time) {
 #pragma unroll
     for (uint32_t i = 0; i < NC; ++i) {
-      const uint32_t v = (i * kThreads + t) * VEC;
-      w[i] = v < here ? *reinterpret_cast<const u32x4*>(from + v) : u32x4{0, 0, 0, 0};
-    }
+      const uint32_t at = (i * times + time) * kSegment;
+      const uint16_t* const p = from + static_cast<uint64_t>(at) * (sizeof(T) / 2) + t * 8;
+      if (at + kSegment <= many) {
+        w[i] = *reinterpret_cast<const u32x4_anywhere*>(p);
+      } else {
+        const uint32_t n = at < many ? (many - at) * static_cast<uint32_t>(sizeof(T) / 2) : 0, h = t * 8;  // halves of words that there are
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) {
-      const uint32_t v = (i / VEC * kThreads + t) * VEC + i % VEC;
-      const float y = to_float<T>(w[i / VEC], i % VEC) + 0.0f;
-      x[i] = v >= low && v < here ? y : -INFINITY;
+        for (uint32_t j = 0; j < 4; ++j)
+          w[i][j] = (h + 2 * j < n ? p[2 * j] : 0u) | (h + 2 * j + 1 < n ? static_cast<uint32_t>(p[2 * j + 1]) << 16 : 0u);
+      }
     }
-  }
-#pragma unroll
-  for (uint32_t i = 0; i < kPer; ++i) {
-    bad = bad || !(x[i] < INFINITY);
-    top = fmaxf(top, x[i]);
-  }
-  const auto token_of = [&](uint32_t i) {
-    return static_cast<uint32_t>(first - ahead) + (i / VEC * kThreads + t) * VEC + i % VEC;
   };
-  float high = fmaxf(top, __shfl_xor(top, 1, kOpsWave));
-  if (t % 2 == 0) maxima[t / 2] = ordered(high);
-  high = max_of_wave(high);
-  if (t % kOpsWave == 0) tops[t / kOpsWave] = high;
-  if (!t) l.n = 0;
-  __syncthreads();
-  float all = tops[0];
+  const auto arrive = [&](uint32_t time) {  // and ask for the next ones
 #pragma unroll
-  for (uint32_t i = 1; i < kThreads / kOpsWave; ++i) all = fmaxf(all, tops[i]);
-  if (t / kOpsWave == split % (kThreads / kOpsWave)) {
-    const uint32_t b = bound_of(maxima, a.keep);
-    if (t % kOpsWave == 0) bound = b;
-  }
-
-  // The sum, from the chunk's maximum. Logits far below it count for e^-600, nothing.
-  double sum[2] = {0, 0};
-  if (all > -INFINITY) {
-    const float floor = all - 600.0f;
-    const double from_top = all;
+    for (uint32_t i = 0; i < kPer; ++i) x[i] = to_float<T>(w[i / VEC], i % VEC);
+    if (times * kBeamChunk != many) {
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) sum[i % 2] += exp_of(static_cast<double>(fmaxf(x[i], floor)) - from_top);
-  }
-  if (bad) sum[0] = NAN;
-  sum[0] = sum_of_wave(sum[0] + sum[1]);
-  if (t % kOpsWave == 0) sums[t / kOpsWave] = sum[0];
-  __syncthreads();
-
-  // The candidates: no -infinity among them.
-  const float least = bound > ordered(-3.4028234664e38f) ? unordered(bound) : -3.4028234664e38f;
-  if (__any(top >= least)) {
-    uint32_t mine = 0, at = 0;
+      for (uint32_t i = 0; i < kPer; ++i) x[i] = place_at(time, i) < many ? x[i] : -INFINITY;
+    }
+    if (time + 1 < times) load(time + 1);
+    float top = x[0];
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) mine += __popcll(__ballot(x[i] >= least));
-    if (t % kOpsWave == 0) at = atomicAdd(&l.n, mine);
-    at = __builtin_amdgcn_readfirstlane(at);
+    for (uint32_t i = 1; i < kPer; ++i) top = fmaxf(top, x[i]);
+    return top;
+  };
+  const auto key_at = [&](uint32_t time, uint32_t i) { return key_of(x[i], first + place_at(time, i)); };
+  float ref = -INFINITY, floor = 0, least = kLeast;
+  // The sum of e^x 2^-R, R the whole number next to log2 e^ref; or of e^(x - ref), where `ref` is so large that the product
+  // with log2 e would lose the difference.
+  double sum = 0, magic = kMagic;
+  const auto near = [&] { return fabsf(ref) < 0x1p20f; };
+  bool bad = false;
+  if (!t) listed = 0;
+  uint32_t pause = 1 + 320 / a.keep, step = pause;  // after how many times the list is thinned
+  load(0);
+  for (uint32_t time = 0; time < times; ++time) {
+    const float top = arrive(time);
+    if (!time) {
+      numbers[t] = ordered(top != top ? -INFINITY : top + 0.0f);
+      __syncthreads();
+      if (wave == split % kWaves) {
+        const uint32_t b = bound_of<256>(numbers, a.keep);
+        if (!lane) bound = b;
+      }
+    }
+    bad = bad || top == INFINITY;
+    // A new `ref` where none was or the old one is far below: no power passes 64 bits' range, and logits far below it count for
+    // e^-596, nothing.
+    if ((top > ref + 300.0f || ref == -INFINITY) && top > -INFINITY && top < INFINITY) {
+      if (near()) sum /= exp_of(ref, magic);
+      sum = ref > top - 600.0f ? sum * exp_of(static_cast<double>(ref) - top) : 0.0;
+      ref = top;
+      magic = kMagic - rint(ref * kE2);
+      floor = ref - 596.0f;
+      if (near()) sum *= exp_of(ref, magic);
+    }
+    if (near()) {
+      double more[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i) {
-      const uint64_t is = __ballot(x[i] >= least);
-      if (!is) continue;
-      const uint32_t to = place_of(is, &at);
-      if (x[i] >= least && to < kList) l.value[to] = key_of(x[i], token_of(i));
+      for (uint32_t i = 0; i < kPer; i += 4) exp_of_4(x + i, floor, magic, more);
+      sum += (more[0] + more[1]) + (more[2] + more[3]);
+    } else if (ref > -INFINITY) {
+#pragma unroll
+      for (uint32_t i = 0; i < kPer; ++i) sum += exp_of(fmax(static_cast<double>(x[i]) - ref, -600.0));
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kPer; i += 2) bad = bad || __builtin_isunordered(x[i], x[i + 1]);
+    if (!time) {
+      __syncthreads();
+      least = bound > ordered(kLeast) ? unordered(bound) : kLeast;
+    }
+    // The candidates: no -infinity among them.
+    if (__any(top >= least)) {
+#pragma unroll
+      for (uint32_t i = 0; i < kPer; ++i) {
+        const uint64_t is = __ballot(x[i] >= least);
+        if (!is) continue;
+        uint32_t to = 0;
+        if (!lane) to = atomicAdd(&listed, static_cast<uint32_t>(__popcll(is)));
+        to = __builtin_amdgcn_readfirstlane(to);
+        const uint32_t place = place_of(is, &to);
+        if (x[i] >= least && place < kList) l.value[place] = key_at(time, i);
+      }
+    }
+    if (time + 1 == pause && time + 1 < times) {
+      __syncthreads();
+      const uint32_t n = listed;
+      step *= 2;
+      pause += step;
+      if (n > a.keep && n <= kList) {  // else there is nothing to raise the bound by, or the list is lost
+        const uint32_t left = thin<kThreads>(l, nullptr, numbers, waves, n, a.keep);
+        const uint32_t b = waves[0];
+        if (b > ordered(least)) least = unordered(b);
+        __syncthreads();
+        if (!t) listed = left;
+      }
+      __syncthreads();
     }
   }
+  // The threads' sums, from the largest of what they are taken from.
+  float high = unordered(max_of_wave(ordered(ref)));
+  if (!lane) tops[wave] = high;
+  __syncthreads();
+  high = tops[0];
+#pragma unroll
+  for (uint32_t i = 1; i < kWaves; ++i) high = fmaxf(high, tops[i]);
+  if (near()) sum /= exp_of(ref, magic);
+  if (ref > -INFINITY) sum *= exp_of(static_cast<double>(fmaxf(ref, high - 600.0f)) - high);
+  if (bad) sum = NAN;
+  sum = sum_of_wave(sum);
+  if (!lane) sums[wave] = sum;
+  uint32_t n = listed;
   __syncthreads();
   const uint64_t part = static_cast<uint64_t>(row) * a.splits + split;
   if (!t) {
-    a.part_max[part] = all;
     double add = sums[0];
 #pragma unroll
-    for (uint32_t i = 1; i < kThreads / kOpsWave; ++i) add += sums[i];
+    for (uint32_t i = 1; i < kWaves; ++i) add += sums[i];
+    a.part_max[part] = high;
     a.part_sum[part] = add;
   }
-  uint32_t n = l.n;
-  if (n > kList) {  // the largest key that at least `keep` candidates reach, which are then exactly so many
-    uint64_t key = 0;
+  if (n > kList) {  // careful: each time the list of the best so far and what beats its last one
+    n = 0;
+    least = kLeast;
+    load(0);
 #pragma unroll 1
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t next = key | 1ull << bit;
-      if (count_of<kPer>(waves, [&](int i) { return x[i] > -INFINITY && key_of(x[i], token_of(i)) >= next; }) >= a.keep) key = next;
-    }
-    __syncthreads();
-    if (!t) l.n = 0;
-    __syncthreads();
+    for (uint32_t time = 0; time < times; ++time) {
+      arrive(time);
+      if (!t) listed = n;
+      __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < kPer; ++i)
-      if (x[i] > -INFINITY && key_of(x[i], token_of(i)) >= key) l.value[atomicAdd(&l.n, 1u)] = key_of(x[i], token_of(i));
-    __syncthreads();
-    n = l.n;
+      for (uint32_t i = 0; i < kPer; ++i)
+        if (x[i] >= least) {
+          const uint32_t to = atomicAdd(&listed, 1u);
+          if (to < kList) l.value[to] = key_at(time, i);
+        }
+      __syncthreads();
+      uint32_t have = listed;
+      __syncthreads();
+      if (have > kList) {  // of these logits the largest key that at least `keep` reach, which are then exactly so many
+        uint64_t key = 0;
+#pragma unroll 1
+        for (int bit = 63; bit >= 0; --bit) {
+          const uint64_t next = key | 1ull << bit;
+          if (count_of<kPer>(waves, [&](int i) { return x[i] >= kLeast && key_at(time, i) >= next; }) >= a.keep) key = next;
+        }
+        if (!t) listed = n;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < kPer; ++i)
+          if (x[i] >= kLeast && key_at(time, i) >= key) l.value[atomicAdd(&listed, 1u)] = key_at(time, i);
+        __syncthreads();
+        have = listed;
+      }
+      if (have <= n) continue;  // nothing new
+      rank_list<kThreads, false>(l, nullptr, have);
+      uint64_t mine[kList / kThreads];
+      uint32_t rank[kList / kThreads];
+#pragma unroll
+      for (uint32_t i = 0; i < kList / kThreads; ++i) {
+        rank[i] = kList;
+        if (i * kThreads + t < have) mine[i] = l.value[i * kThreads + t], rank[i] = l.rank[i * kThreads + t];
+      }
+      __syncthreads();
+#pragma unroll
+      for (uint32_t i = 0; i < kList / kThreads; ++i)
+        if (rank[i] < a.keep) l.value[rank[i]] = mine[i];
+      n = have < a.keep ? have : a.keep;
+      __syncthreads();
+      // Equal ones of lower tokens may follow: they beat the last one too.
+      if (n == a.keep) least = unordered(static_cast<uint32_t>(l.value[n - 1] >> 32));
+    }
+  } else if (n > kOpsWave && n > a.keep + a.keep / 2) {
+    n = thin<kThreads>(l, nullptr, numbers, waves, n, a.keep);
   }
   rank_list<kThreads, false>(l, nullptr, n);
   uint64_t* const out = a.lists + part * a.keep;
@@ -290,78 +498,110 @@ __global__ __launch_bounds__(kThreads, 4) void beam_chunk_kernel(BeamArgs a) {
   for (uint32_t i = n + t; i < a.keep; i += kThreads) out[i] = 0;
 }
 
-// The `keep` best of `total` values, `per` of each of 1024 threads side by side (0: none), ties to the lower place thread *
-// per + i. Found as in beam_chunk_kernel, with the maxima of four threads each: values come in descending lists, and
-// these are the lists' first ones. (With values 1024 apart a thread has one rank of many lists, the bound was so low that the
-// list overflowed: 32 beams of 8 parts of 64, 42 us.) give(rank, value, place); returns how many there are.
-template <class F>
-__device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint32_t total, uint32_t per, uint32_t keep, F give) {
-  __shared__ List l;
-  __shared__ __attribute__((aligned(16))) uint32_t maxima[256];
-  __shared__ uint32_t places[kList + 8], waves[kMerge / kOpsWave], bound;
-  const uint32_t t = threadIdx.x;
-  if (!t) l.n = 0;
-  if (total > 256) {  // else all go to the list
-    uint64_t top = 0;
+// A thread's share of n keys in descending lists of `keep`, side by side; `lists` of them are a beam's.
+struct Keys {
+  uint64_t v[kMergePer];
+  uint32_t at, has;  // the place of the first one, and how many
+  uint32_t starts;   // bit i: the i-th is the first of a list, or of the thread's
+  uint32_t beam, more;  // of the first one; bit i: the i-th is of the next
+  __device__ __forceinline__ Keys(const uint64_t* from, uint32_t n, uint32_t keep, uint32_t lists) {
+    const uint32_t per = (n + kMerge - 1) / kMerge;
+    at = threadIdx.x * per;
+    has = at >= n ? 0 : n - at < per ? n - at : per;
 #pragma unroll
-    for (uint32_t i = 0; i < kMergePer; ++i) top = v[i] > top ? v[i] : top;
-    uint32_t high = static_cast<uint32_t>(top >> 32);
-#pragma unroll
-    for (int x = 1; x < 4; x *= 2) {
-      const uint32_t y = __shfl_xor(high, x, kOpsWave);
-      high = y > high ? y : high;
+    for (uint32_t i = 0; i < kMergePer; ++i) {
+      v[i] = 0;
+      if (i < has) v[i] = from[at + i];
     }
-    if (t % 4 == 0) maxima[t / 4] = high;
-    __syncthreads();
-    if (t < kOpsWave) {
-      const uint32_t b = bound_of(maxima, keep);
-      if (!t) bound = b;
+    uint32_t list = at / keep, in = at - list * keep;
+    beam = list / lists;
+    list -= beam * lists;
+    starts = 1;
+    more = 0;
+    for (uint32_t i = 1; i < per; ++i) {
+      if (++in < keep) continue;
+      in = 0;
+      starts |= 1u << i;
+      if (++list < lists) continue;
+      list = 0;
+      more |= 1u << i;
     }
   }
-  __syncthreads();
-  uint64_t least = total > 256 ? static_cast<uint64_t>(bound) << 32 : 1;
-  if (!least) least = 1;
-  uint32_t mine = 0, at = 0;
+  __device__ __forceinline__ uint32_t beam_of(uint32_t i) const { return beam + __popc(more & ((2u << i) - 1)); }
+};
+
+// The `keep` best of the threads' keys; value(i) is what counts of a thread's i-th (0: none), descending within a list. Ties go
+// to the lower place. Found as in beam_part_kernel: as many of the threads' largest, which are their lists' first ones, reach
+// a bound; of a list only what comes before the first value below it is looked at; and where a few lists hold most of the
+// best, so that much more does reach it, what was found is thinned once more before it is ranked (32 beams of 4 parts of
+// 64, scores apart by 6: 78 us without). give(rank, value, place); returns how many there are.
+template <class V, class F>
+__device__ __forceinline__ uint32_t best_of(const Keys& k, uint32_t keep, V value, F give) {
+  __shared__ List<kMergeList> l;
+  __shared__ __attribute__((aligned(16))) uint32_t numbers[kMergeList];
+  __shared__ uint32_t places[kMergeList + 8], waves[kMerge / kOpsWave], bound, listed;
+  const uint32_t t = threadIdx.x;
+  if (!t) listed = 0;
+  uint64_t top = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) mine += __popcll(__ballot(v[i] >= least));
-  if (mine && t % kOpsWave == 0) at = atomicAdd(&l.n, mine);
-  at = __builtin_amdgcn_readfirstlane(at);
+  for (uint32_t i = 0; i < kMergePer; ++i)
+    if (i < k.has && k.starts >> i & 1) {
+      const uint64_t v = value(i);
+      top = v > top ? v : top;
+    }
+  numbers[t] = static_cast<uint32_t>(top >> 32);
+  __syncthreads();
+  if (t < kOpsWave) {
+    const uint32_t b = bound_of<kMerge>(numbers, keep);
+    if (!t) bound = b;
+  }
+  __syncthreads();
+  const uint64_t least = bound ? static_cast<uint64_t>(bound) << 32 : 1;
+  bool before = true;  // whether the value before in the list reached the bound
 #pragma unroll
   for (uint32_t i = 0; i < kMergePer; ++i) {
-    const uint64_t is = __ballot(v[i] >= least);
-    if (!is) continue;
-    const uint32_t to = place_of(is, &at);
-    if (v[i] >= least && to < kList) l.value[to] = v[i], places[to] = t * per + i;
+    const bool look = i < k.has && (before || (k.starts >> i & 1));
+    if (!__any(look)) continue;
+    const uint64_t v = look ? value(i) : 0;
+    before = v >= least;
+    if (before) {
+      const uint32_t to = atomicAdd(&listed, 1u);
+      if (to < kMergeList) l.value[to] = v, places[to] = k.at + i;
+    }
   }
   __syncthreads();
-  uint32_t n = l.n;
-  if (n > kList) {
+  uint32_t n = listed;
+  if (n > kMergeList) {  // of many equal ones: the bound bit by bit over all
+    const auto is = [&](uint32_t i) { return i < k.has ? value(i) : 0; };
     uint64_t key = 0;
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t next = key | 1ull << bit;
-      if (count_of<kMergePer>(waves, [&](int i) { return v[i] >= next; }) >= keep) key = next;
+      if (count_of<kMergePer>(waves, [&](int i) { return is(i) >= next; }) >= keep) key = next;
     }
     // All above it, and of those that equal it the lowest places, up to `until`.
-    const uint32_t more = keep - count_of<kMergePer>(waves, [&](int i) { return v[i] > key; });
+    const uint32_t more = keep - count_of<kMergePer>(waves, [&](int i) { return is(i) > key; });
     uint32_t until = 0;
 #pragma unroll 1
     for (uint32_t bit = kBeamMerge; bit; bit /= 2) {
       const uint32_t next = until + bit;
-      if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return v[i] == key && t * per + i < next; }) < more) until = next;
+      if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return is(i) == key && k.at + i < next; }) < more) until = next;
     }
     __syncthreads();
-    if (!t) l.n = 0;
+    if (!t) listed = 0;
     __syncthreads();
 #pragma unroll
-    for (uint32_t i = 0; i < kMergePer; ++i)
-      if (v[i] > key || (v[i] == key && t * per + i <= until)) {
-        const uint32_t at = atomicAdd(&l.n, 1u);
-        if (at < kList) l.value[at] = v[i], places[at] = t * per + i;
+    for (uint32_t i = 0; i < kMergePer; ++i) {
+      const uint64_t v = is(i);
+      if (v && (v > key || (v == key && k.at + i <= until))) {
+        const uint32_t to = atomicAdd(&listed, 1u);
+        if (to < kMergeList) l.value[to] = v, places[to] = k.at + i;
       }
+    }
     __syncthreads();
-    n = l.n;
+    n = listed;
   }
+  if (n > 2 * keep + 64) n = thin<kMerge>(l, places, numbers, waves, n, keep);
   rank_list<kMerge, true>(l, places, n);
   for (uint32_t i = t; i < n; i += kMerge)
     if (l.rank[i] < keep) give(l.rank[i], l.value[i], places[i]);
@@ -372,16 +612,10 @@ __device__ __forceinline__ uint32_t best_of(const uint64_t (&v)[kMergePer], uint
 __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
   const uint32_t row = blockIdx.x, n = a.splits * a.keep, t = threadIdx.x;
   if (!grows(a, row)) return;
-  const uint64_t* from = a.lists + static_cast<uint64_t>(row) * n;
-  uint64_t v[kMergePer];
-  const uint32_t each = (n + kMerge - 1) / kMerge;
-#pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) {
-    v[i] = 0;
-    if (i < each && t * each + i < n) v[i] = from[t * each + i];
-  }
+  const Keys k(a.lists + static_cast<uint64_t>(row) * n, n, a.keep, a.splits);
   uint64_t* const out = a.rows + static_cast<uint64_t>(row) * a.keep;
-  const uint32_t found = best_of(v, n, each, a.keep, [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
+  const uint32_t found = best_of(k, a.keep, [&](uint32_t i) { return k.v[i]; },
+                                 [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) out[i] = 0;
 }
 
@@ -391,16 +625,9 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
   __shared__ uint8_t state[kBeamMost];  // 0: no candidates, 1: from its logits, 2: done
   const uint32_t item = blockIdx.x, t = threadIdx.x;
   constexpr uint32_t kLanes = kMerge / kBeamMost;  // of a beam
-  const uint64_t* const lists = a.rows ? a.rows : a.lists;
   const uint32_t per = a.rows ? a.keep : a.splits * a.keep, n = a.beams * per;  // candidates of a beam, of all
-  const uint64_t* const from = lists + static_cast<uint64_t>(item) * n;
-  uint64_t v[kMergePer];
-  const uint32_t each = (n + kMerge - 1) / kMerge;
-#pragma unroll
-  for (uint32_t i = 0; i < kMergePer; ++i) {  // the keys first; lists of beams that have none hold anything
-    v[i] = 0;
-    if (i < each && t * each + i < n) v[i] = from[t * each + i];
-  }
+  const uint64_t* const from = (a.rows ? a.rows : a.lists) + static_cast<uint64_t>(item) * n;
+  const Keys k(from, n, a.keep, a.rows ? 1 : a.splits);  // lists of beams that have none hold anything
   if (t / kLanes < a.beams) {
     const uint32_t beam = t / kLanes, lane = t % kLanes, row = item * a.beams + beam;
     const float* m = a.part_max + static_cast<uint64_t>(row) * a.splits;
@@ -418,12 +645,12 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
 #pragma unroll
       for (uint32_t x = 1; x < kLanes; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kLanes));
       const auto part = [&](float max, double sum) {
-        return sum * (max > -INFINITY ? exp_of(static_cast<double>(fmaxf(max, top - 600.0f)) - top) : 0.0);
+        return sum * (max > -INFINITY ? exp_of(static_cast<double>(fmaxf(max, top - 600.0f)) - top) : 1.0);
       };
       double sum = part(m0, s0);
       for (uint32_t i = lane + kLanes; i < a.splits; i += kLanes) sum += part(m[i], s[i]);
-#pragma unroll
-      for (uint32_t x = 1; x < kLanes; x *= 2) sum += __shfl_xor(sum, x, kLanes);
+      static_assert(kLanes == 16, "");
+      sum = sum_of_row(sum);
       if (!(sum > 0)) is = 0;  // no logit above -infinity, or one that is no number or +infinity
       lse = top + log(sum);
     }
@@ -434,28 +661,17 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
     }
   }
   __syncthreads();
-  {
-    uint32_t beam = t * each / per, in = t * each - beam * per, is = 0;  // of the thread's first value, then of the next
-    double score = 0, lse = 0;
-    bool fresh = true;
-#pragma unroll
-    for (uint32_t i = 0; i < kMergePer; ++i) {
-      if (i >= each || t * each + i >= n) break;
-      if (fresh) is = state[beam], score = scores[beam], lse = lses[beam];
-      const uint64_t key = v[i];
-      v[i] = 0;
-      if (is == 1 && key) v[i] = ordered(score + (unordered(static_cast<uint32_t>(key >> 32)) - lse) + 0.0);
-      if (is == 2 && !in) v[i] = ordered(score + 0.0);
-      fresh = ++in == per;
-      if (fresh) in = 0, ++beam;
-    }
-  }
+  const auto value = [&](uint32_t i) -> uint64_t {
+    const uint32_t beam = k.beam_of(i), is = state[beam];
+    if (is == 1 && k.v[i]) return ordered(scores[beam] + (unordered(static_cast<uint32_t>(k.v[i] >> 32)) - lses[beam]) + 0.0);
+    return is == 2 && k.at + i == beam * per ? ordered(scores[beam] + 0.0) : 0;
+  };
   const uint64_t to = static_cast<uint64_t>(item) * a.keep;
-  const uint32_t found = best_of(v, n, each, a.keep, [&](uint32_t rank, uint64_t value, uint32_t at) {
+  const uint32_t found = best_of(k, a.keep, value, [&](uint32_t rank, uint64_t v, uint32_t at) {
     const uint32_t beam = at / per;
     a.tokens[to + rank] = state[beam] == 2 ? a.done_token : static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(from[at]));
     a.parents[to + rank] = static_cast<int32_t>(item * a.beams + beam);
-    a.scores_out[to + rank] = static_cast<float>(unordered(value));
+    a.scores_out[to + rank] = static_cast<float>(unordered(v));
   });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) {
     a.tokens[to + i] = a.parents[to + i] = -1;
@@ -467,9 +683,9 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
 
 hipError_t launch_beam(const BeamArgs& a, uint32_t type, hipStream_t stream) {
   const uint32_t rows = a.batch * a.beams, grid = rows * a.splits;
-  hipError_t e = type == MMA_TYPE_F32   ? launch(beam_chunk_kernel<float>, grid, kThreads, stream, a)
-                 : type == MMA_TYPE_F16 ? launch(beam_chunk_kernel<_Float16>, grid, kThreads, stream, a)
-                                        : launch(beam_chunk_kernel<__bf16>, grid, kThreads, stream, a);
+  hipError_t e = type == MMA_TYPE_F32   ? launch(beam_part_kernel<float>, grid, kThreads, stream, a)
+                 : type == MMA_TYPE_F16 ? launch(beam_part_kernel<_Float16>, grid, kThreads, stream, a)
+                                        : launch(beam_part_kernel<__bf16>, grid, kThreads, stream, a);
   if (e != hipSuccess) return e;
   if (a.rows && (e = launch(beam_row_kernel, rows, kMerge, stream, a)) != hipSuccess) return e;
   return launch(beam_merge_kernel, a.batch, kMerge, stream, a);

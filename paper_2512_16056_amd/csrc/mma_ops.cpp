@@ -465,7 +465,7 @@ mma_status_t workspace(Call* call, void* p, uint64_t bytes, uint64_t need, uintp
 }
 
 struct BeamPlan {
-  uint32_t splits;
+  uint32_t splits, run;
   bool joined;  // each row's parts before the request's
   uint64_t sum_bytes, list_bytes, row_bytes, max_bytes, bytes;
 };
@@ -477,14 +477,15 @@ mma_status_t check_beam_sizes(const mma_beam_select_t* a, BeamPlan* p) {
   if (!a->beams || a->beams > kBeamMost) return fail(MMA_ERR_INVALID_ARG, "%u beams: from 1 to %u", a->beams, kBeamMost);
   if (!a->keep || a->keep > kBeamKeep) return fail(MMA_ERR_INVALID_ARG, "keep %u: from 1 to %u", a->keep, kBeamKeep);
   if (!a->vocab || a->vocab > INT32_MAX) return fail(MMA_ERR_INVALID_ARG, "a vocabulary of %u: from 1 to 2^31 - 1", a->vocab);
-  // Rows start anywhere in 16 bytes: up to 7 elements more.
-  const uint64_t splits = up(static_cast<uint64_t>(a->vocab) + 7, kBeamChunk), rows = static_cast<uint64_t>(a->batch) * a->beams;
-  if (splits * a->keep > kBeamMerge)
-    return fail(MMA_ERR_INVALID_ARG, "the %u best of a vocabulary of %u: keep times its parts of %u may not pass %u", a->keep,
-                a->vocab, kBeamChunk, kBeamMerge);
+  // A part is as long as lets 1024 workgroups, four on a CU, run at once, or as lets a row's parts fit a merge: to find a
+  // part's best costs as much as to sum some thousand logits, and what is found is merged.
+  const uint64_t chunks = up(a->vocab, kBeamChunk), rows = static_cast<uint64_t>(a->batch) * a->beams;
+  const uint64_t run = std::max(up(chunks, static_cast<uint32_t>(std::max<uint64_t>(1, 1024 / std::max<uint64_t>(1, rows)))), up(chunks, kBeamMerge / a->keep));
+  const uint64_t splits = up(chunks, static_cast<uint32_t>(std::min(run, chunks)));
   if (rows * splits >= 1u << 22)
     return fail(MMA_ERR_INVALID_ARG, "%u requests of %u beams are more workgroups than a launch takes", a->batch, a->beams);
   p->splits = static_cast<uint32_t>(splits);
+  p->run = static_cast<uint32_t>(up(chunks, p->splits));
   p->joined = splits * a->keep * a->beams > kBeamMerge;
   p->sum_bytes = rows * splits * 8;
   p->list_bytes = rows * splits * a->keep * 8;
@@ -821,6 +822,7 @@ mma_status_t mma_beam_select(const mma_beam_select_t* a, void* stream) try {
   k.vocab = a->vocab;
   k.keep = a->keep;
   k.splits = p.splits;
+  k.run = p.run;
   k.done_token = a->done_token;
   return launched(launch_beam(k, a->type, static_cast<hipStream_t>(stream)), "beam selection");
 } catch (...) {

@@ -121,7 +121,7 @@ struct EvictArgs {
 };
 
 // Beam search's selection. Parts of rows: [row][split], lists of `keep` keys each (mma_beam.hip).
-constexpr uint32_t kBeamChunk = 8192;   // logits of a part
+constexpr uint32_t kBeamChunk = 4096;   // logits that a workgroup takes at once
 constexpr uint32_t kBeamMerge = 16384;  // keys that a merge takes
 constexpr uint32_t kBeamMost = 64;      // beams of a request
 constexpr uint32_t kBeamKeep = 128;
@@ -138,7 +138,8 @@ struct BeamArgs {
   uint64_t* lists;
   uint64_t* rows;  // each row's parts joined, or NULL where a request's parts are few enough
   float* part_max;
-  uint32_t batch, beams, vocab, keep, splits;
+  uint32_t batch, beams, vocab, keep;
+  uint32_t splits, run;  // parts of a row, and how many times kBeamChunk logits each is
   int32_t done_token;
 };
 

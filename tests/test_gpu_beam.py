@@ -79,6 +79,31 @@ def test_select_joins_rows_first(dtype):
     check_select(some_logits(g, 1, 64, 60000, dtype), -torch.rand(1, 64, generator=g), 128)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_parts_of_several_runs(dtype):
+    """Rows enough for the workgroups to take several times 8192 logits each: the best late, early, in between, and equal."""
+    g = gen(6)
+    x = some_logits(g, 8, 40, 50000, dtype)
+    x[0] = torch.linspace(-20, 20, 50000).to(dtype)        # ever better: every logit is among the best of its time
+    x[1] = torch.linspace(20, -20, 50000).to(dtype)
+    x[2] = 1.0
+    x[3, :, 49990:] = 30.0
+    x[4, :, :40000] = -math.inf
+    x[5, 1, 20000] = math.nan
+    x[6, :, 30000:] += 800.0                               # past the range of a power taken from the first ones
+    x[7] = torch.where(torch.arange(50000) < 20000, -800.0, 0.0).to(dtype) + x[7]
+    scores = -torch.rand(8, 40, generator=g)
+    for keep in (3, 80, 128):
+        check_select(x, scores, keep)
+
+
+def test_select_large_vocabularies():
+    """More parts than a merge takes of one row, were they not longer: 128 of 2 million, 100 of 1.4 million."""
+    g = gen(7)
+    for vocab, keep in ((2_000_001, 128), (1_400_000, 100)):
+        check_select(some_logits(g, 1, 2, vocab, F16), torch.zeros(1, 2), keep)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 def test_select_rows_anywhere(dtype):
     """Rows that start at any element of 16 bytes, apart from each other, and one row for all beams."""
@@ -167,7 +192,7 @@ def test_select_done_beams():
     check_select(x, scores, 12, done != 0, 0)
 
 
-@pytest.mark.parametrize("scale,shift", [(1e-30, 0.0), (300.0, 0.0), (1.0, 1e6), (1.0, -1e6), (3.0, 1e4)])
+@pytest.mark.parametrize("scale,shift", [(1e-30, 0.0), (300.0, 0.0), (1.0, 1e6), (1.0, -1e6), (3.0, 1e4), (1.0, 3e7), (1e20, 0.0), (1e34, 0.0)])
 def test_select_scales(scale, shift):
     g = gen(10)
     x = some_logits(g, 2, 2, 20000, F32)
