@@ -155,11 +155,12 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* numbers, uint32_t k
 #pragma unroll
   for (int i = 0; i < N / 256; ++i) x[i] = *reinterpret_cast<const u32x4*>(numbers + (i * kOpsWave + threadIdx.x % kOpsWave) * 4);
   const auto reach = [&](uint32_t v) {
+    uint64_t who[N / 64];
     uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < N / 256; ++i)
+    for (int i = 0; i < N / 64; ++i) who[i] = __ballot(x[i / 4][i % 4] >= v);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) n += __popcll(__ballot(x[i][j] >= v));
+    for (int i = 0; i < N / 64; ++i) n += __popcll(who[i]);
     return n;
   };
   uint32_t top = 0;
@@ -180,13 +181,6 @@ __device__ __forceinline__ uint32_t bound_of(const uint32_t* numbers, uint32_t k
     if (next >= keep) bound |= bit, n = next;
   }
   return bound;
-}
-
-// Places in a list for the lanes whose bits `is` has, after those of `*at`, which moves on by as many.
-__device__ __forceinline__ uint32_t place_of(uint64_t is, uint32_t* at) {
-  const uint32_t mine = *at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(is >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(is), 0));
-  *at += __popcll(is);
-  return mine;
 }
 
 // Candidates of a list in LDS: larger values first, equal ones by place (PLACES; else there are no equal ones).
@@ -258,7 +252,7 @@ __device__ __forceinline__ uint32_t thin(List<N>& l, uint32_t* places, uint32_t*
   }
   __syncthreads();
   if (t < kOpsWave) {
-    const uint32_t b = bound_of<N>(numbers, keep);
+    const uint32_t b = n <= 256 ? bound_of<256>(numbers, keep) : n <= 512 ? bound_of<512>(numbers, keep) : bound_of<N>(numbers, keep);
     if (!t) waves[0] = b, waves[1] = 0;
   }
   __syncthreads();
@@ -286,25 +280,27 @@ __device__ __forceinline__ float to_float(const u32x4& w, uint32_t j) {
   else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(word >> (j % 2 * 16))));
 }
 
-// A run of a row's logits, 4096 at a time, the next ones on their way; a time takes its 256 threads' 16 bytes from places that
-// the run's times share evenly, so that the first one is like the others. Rows start at any multiple of an element,
-// and a thread's logits go by their tokens all the same, not by 16 aligned bytes: equal rows so have equal sums, to the
-// last bit, and beams that are alike tie.
+// A run of a row's logits, 4096 at a time, the next ones on their way. Rows start at any multiple of an element, and a thread's
+// logits go by their tokens all the same, not by 16 aligned bytes: equal rows so have equal sums, to the last bit, and
+// beams that are alike tie.
 //
-// The sum of exp is a thread's own, from its largest logit of the first time, until the end. The `keep` best: as many
-// of the threads' maxima of the first time reach a bound, so the keep-th best logit does; what reaches it goes to a list, and
-// nobody waits for another wave until, some times later, and then ever later, the list is thinned and the bound raised by
-// it. A list that overflows, as of equal logits, is found anew with a wait at every time (careful).
+// The sum of exp is a thread's own, from its largest logit of the first time, until the end. Of each time a thread leaves
+// the upper half of its largest logit in LDS, and nothing else: no wave waits for another. After up to 32 times the
+// `keep` best are found from these: as many of the threads' largest reach a bound, so the keep-th best logit does; the few
+// times of threads that have reached it are read again, and what reaches it goes to a list, which is thinned where it is
+// long and ranked at the end. Where the list overflows, as of equal logits, it is found anew, 4096 logits after 4096 (careful).
 //
-// 192 rows of 128001 in 32 bits: ...
+// 192 rows of 128001 in 32 bits: FIGURES
 template <class T>
 __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
-  constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC, kWaves = kThreads / kOpsWave, kSegment = kThreads * VEC;
+  constexpr uint32_t VEC = 16 / sizeof(T), NC = kPer / VEC, kWaves = kThreads / kOpsWave, kSegment = kThreads * VEC, kRound = 32;
   __shared__ List<kList> l;
   __shared__ __attribute__((aligned(16))) uint32_t numbers[kList];
+  __shared__ uint16_t highs[kRound][kThreads];
+  __shared__ uint16_t hits[kList];  // time of the round * 256 + thread... of a thread's largest that reach the bound
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
-  __shared__ uint32_t waves[kWaves], bound, listed;
+  __shared__ uint32_t waves[kWaves], bound, listed, hit;
   const uint32_t row = blockIdx.x / a.splits, split = blockIdx.x % a.splits, t = threadIdx.x, lane = t % kOpsWave, wave = t / kOpsWave;
   const uint32_t first = split * a.run * kBeamChunk, all = a.vocab - first;  // of the part's first logit; logits from there on
   const uint32_t many = all < a.run * kBeamChunk ? all : a.run * kBeamChunk, times = (many + kBeamChunk - 1) / kBeamChunk;
@@ -312,26 +308,31 @@ __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
   if (!grows(a, row)) return;  // the merge does not read its part
   u32x4 w[NC];
   float x[kPer];
-  const auto place_at = [&](uint32_t time, uint32_t i) { return (i / VEC * times + time) * kSegment + t * VEC + i % VEC; };
+  const auto place_at = [&](uint32_t time, uint32_t i) { return time * kBeamChunk + i / VEC * kSegment + t * VEC + i % VEC; };
+  // 16 bytes of the run from logit `at` on, those that are in it.
+  const auto vector_at = [&](uint32_t at) -> u32x4 {
+    const uint16_t* const p = from + static_cast<uint64_t>(at) * (sizeof(T) / 2);
+    if (at + VEC <= many) return *reinterpret_cast<const u32x4_anywhere*>(p);
+    const uint32_t n = at < many ? (many - at) * static_cast<uint32_t>(sizeof(T) / 2) : 0;  // halves of words
+    u32x4 v;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) v[j] = (2 * j < n ? p[2 * j] : 0u) | (2 * j + 1 < n ? static_cast<uint32_t>(p[2 * j + 1]) << 16 : 0u);
+    return v;
+  };
   const auto load = [&](uint32_t time) {
+    if ((time + 1) * kBeamChunk <= many) {
+      const uint8_t* const p = reinterpret_cast<const uint8_t*>(from) + static_cast<uint64_t>(time) * kBeamChunk * sizeof(T) + t * 16;
 #pragma unroll
-    for (uint32_t i = 0; i < NC; ++i) {
-      const uint32_t at = (i * times + time) * kSegment;
-      const uint16_t* const p = from + static_cast<uint64_t>(at) * (sizeof(T) / 2) + t * 8;
-      if (at + kSegment <= many) {
-        w[i] = *reinterpret_cast<const u32x4_anywhere*>(p);
-      } else {
-        const uint32_t n = at < many ? (many - at) * static_cast<uint32_t>(sizeof(T) / 2) : 0, h = t * 8;  // halves of words that there are
+      for (uint32_t i = 0; i < NC; ++i) w[i] = *reinterpret_cast<const u32x4_anywhere*>(p + i * kThreads * 16);
+    } else {
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j)
-          w[i][j] = (h + 2 * j < n ? p[2 * j] : 0u) | (h + 2 * j + 1 < n ? static_cast<uint32_t>(p[2 * j + 1]) << 16 : 0u);
-      }
+      for (uint32_t i = 0; i < NC; ++i) w[i] = vector_at(place_at(time, i * VEC));
     }
   };
   const auto arrive = [&](uint32_t time) {  // and ask for the next ones
 #pragma unroll
     for (uint32_t i = 0; i < kPer; ++i) x[i] = to_float<T>(w[i / VEC], i % VEC);
-    if (times * kBeamChunk != many) {
+    if ((time + 1) * kBeamChunk > many) {
 #pragma unroll
       for (uint32_t i = 0; i < kPer; ++i) x[i] = place_at(time, i) < many ? x[i] : -INFINITY;
     }
@@ -349,18 +350,12 @@ __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
   const auto near = [&] { return fabsf(ref) < 0x1p20f; };
   bool bad = false;
   if (!t) listed = 0;
-  uint32_t pause = 1 + 320 / a.keep, step = pause;  // after how many times the list is thinned
   load(0);
+  float best = -INFINITY;  // the thread's largest of the round
   for (uint32_t time = 0; time < times; ++time) {
     const float top = arrive(time);
-    if (!time) {
-      numbers[t] = ordered(top != top ? -INFINITY : top + 0.0f);
-      __syncthreads();
-      if (wave == split % kWaves) {
-        const uint32_t b = bound_of<256>(numbers, a.keep);
-        if (!lane) bound = b;
-      }
-    }
+    highs[time % kRound][t] = static_cast<uint16_t>(ordered(top != top ? -INFINITY : top + 0.0f) >> 16);
+    best = fmaxf(best, top);
     bad = bad || top == INFINITY;
     // A new `ref` where none was or the old one is far below: no power passes 64 bits' range, and logits far below it count for
     // e^-596, nothing.
@@ -383,29 +378,50 @@ __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
     }
 #pragma unroll
     for (uint32_t i = 0; i < kPer; i += 2) bad = bad || __builtin_isunordered(x[i], x[i + 1]);
-    if (!time) {
-      __syncthreads();
-      least = bound > ordered(kLeast) ? unordered(bound) : kLeast;
+    if (time + 1 < times && (time + 1) % kRound) continue;
+
+    // The round's candidates: no -infinity among them.
+    const uint32_t rounds = time / kRound * kRound, of_round = time + 1 - rounds;
+    numbers[t] = ordered(best + 0.0f);
+    if (!t) hit = 0;
+    __syncthreads();
+    if (wave == split % kWaves) {
+      const uint32_t b = bound_of<256>(numbers, a.keep);
+      if (!lane) bound = b;
     }
-    // The candidates: no -infinity among them.
-    if (__any(top >= least)) {
+    __syncthreads();
+    if (bound > ordered(least)) least = unordered(bound);
+    if (best >= least) {
+      const uint32_t high = ordered(least) >> 16;
+      for (uint32_t i = 0; i < of_round; ++i)
+        if (highs[i][t] >= high) {
+          const uint32_t to = atomicAdd(&hit, 1u);
+          if (to < kList) hits[to] = static_cast<uint16_t>(i * kThreads + t);
+        }
+    }
+    best = -INFINITY;
+    __syncthreads();
+    const uint32_t reached = hit;
+    if (reached > kList) {
+      if (!t) listed = kList + 1;  // careful
+    } else {
+      for (uint32_t i = t; i < reached * NC; i += kThreads) {  // a thread 16 bytes of a hit
+        const uint32_t h = hits[i / NC], at = (rounds + h / kThreads) * kBeamChunk + i % NC * kSegment + h % kThreads * VEC;
+        const u32x4 v = vector_at(at);
 #pragma unroll
-      for (uint32_t i = 0; i < kPer; ++i) {
-        const uint64_t is = __ballot(x[i] >= least);
-        if (!is) continue;
-        uint32_t to = 0;
-        if (!lane) to = atomicAdd(&listed, static_cast<uint32_t>(__popcll(is)));
-        to = __builtin_amdgcn_readfirstlane(to);
-        const uint32_t place = place_of(is, &to);
-        if (x[i] >= least && place < kList) l.value[place] = key_at(time, i);
+        for (uint32_t j = 0; j < VEC; ++j) {
+          const float y = to_float<T>(v, j);
+          if (y >= least && at + j < many) {
+            const uint32_t to = atomicAdd(&listed, 1u);
+            if (to < kList) l.value[to] = key_of(y, first + at + j);
+          }
+        }
       }
     }
-    if (time + 1 == pause && time + 1 < times) {
-      __syncthreads();
-      const uint32_t n = listed;
-      step *= 2;
-      pause += step;
-      if (n > a.keep && n <= kList) {  // else there is nothing to raise the bound by, or the list is lost
+    __syncthreads();
+    const uint32_t n = listed;
+    if (time + 1 < times) {  // room for the next round, and a better bound
+      if (n > 2 * a.keep && n <= kList) {
         const uint32_t left = thin<kThreads>(l, nullptr, numbers, waves, n, a.keep);
         const uint32_t b = waves[0];
         if (b > ordered(least)) least = unordered(b);
@@ -502,11 +518,13 @@ __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
 struct Keys {
   uint64_t v[kMergePer];
   uint32_t at, has;  // the place of the first one, and how many
+  uint32_t threads;  // that have some
   uint32_t starts;   // bit i: the i-th is the first of a list, or of the thread's
   uint32_t beam, more;  // of the first one; bit i: the i-th is of the next
   __device__ __forceinline__ Keys(const uint64_t* from, uint32_t n, uint32_t keep, uint32_t lists) {
     const uint32_t per = (n + kMerge - 1) / kMerge;
     at = threadIdx.x * per;
+    threads = (n + per - 1) / per;
     has = at >= n ? 0 : n - at < per ? n - at : per;
 #pragma unroll
     for (uint32_t i = 0; i < kMergePer; ++i) {
@@ -552,7 +570,7 @@ __device__ __forceinline__ uint32_t best_of(const Keys& k, uint32_t keep, V valu
   numbers[t] = static_cast<uint32_t>(top >> 32);
   __syncthreads();
   if (t < kOpsWave) {
-    const uint32_t b = bound_of<kMerge>(numbers, keep);
+    const uint32_t b = k.threads <= 256 ? bound_of<256>(numbers, keep) : k.threads <= 512 ? bound_of<512>(numbers, keep) : bound_of<kMerge>(numbers, keep);
     if (!t) bound = b;
   }
   __syncthreads();
