@@ -495,14 +495,21 @@ mma_status_t check_beam_sizes(const mma_beam_select_t* a, BeamPlan* p) {
   return MMA_OK;
 }
 
-// Pages from[k] to to[k] of every layer.
+// Pages from[k] to to[k] of every layer; of a compaction the table too.
 mma_status_t move_pages(const Call& call, const mma_kv_layout_t* layout, void* const* layers, const int32_t* from, const int32_t* to,
-                        const uint32_t* moves, uint32_t most, hipStream_t stream) {
-  if (!most) return MMA_OK;
+                        const uint32_t* moves, uint32_t most, const mma_kv_compact_t* table, hipStream_t stream) {
   static thread_local MoveArgs k;
   k.from = from;
   k.to = to;
   k.moves = moves;
+  k.places = 0;
+  k.num_blocks = call.c.num_blocks;
+  if (table) {
+    k.table = table->block_table;
+    k.table_out = table->table_out;
+    k.moved = table->moved;
+    k.places = static_cast<uint64_t>(table->num_seqs) * table->table_stride;
+  }
   k.piece = call.piece;
   k.v_offset = call.piece * call.c.num_blocks;
   k.most = most;
@@ -510,6 +517,7 @@ mma_status_t move_pages(const Call& call, const mma_kv_layout_t* layout, void* c
     k.layers = std::min(layout->num_layers - first, MoveArgs::kMaxLayers);
     for (uint32_t l = 0; l < k.layers; ++l) k.layer[l] = reinterpret_cast<uint64_t>(layers[first + l]);
     if (mma_status_t s = launched(launch_moves(k, stream), "KV page move")) return s;
+    k.places = 0;
   }
   return MMA_OK;
 }
@@ -898,7 +906,7 @@ mma_status_t mma_kv_fork(const mma_kv_layout_t* layout, void* const* gpu_layers,
   k.max_len = seqs->max_len;
   const hipStream_t on = static_cast<hipStream_t>(stream);
   if ((s = launched(launch_fork(k, on), "KV fork"))) return s;
-  return move_pages(call, layout, gpu_layers, k.from, k.to, nullptr, a->num_children, on);
+  return move_pages(call, layout, gpu_layers, k.from, k.to, nullptr, a->num_children, nullptr, on);
 } catch (...) {
   return ops_boundary_error("mma_kv_fork");
 }
@@ -943,8 +951,6 @@ mma_status_t mma_kv_compact(const mma_kv_layout_t* layout, void* const* gpu_laye
   for (uint32_t l = 0; l < layout->num_layers; ++l)
     if ((s = array(&call, "a layer tensor", gpu_layers[l], call.layer_bytes, 16))) return s;
   CompactArgs k{};
-  k.table = a->block_table;
-  k.table_out = a->table_out;
   k.refs = a->refs;
   k.refs_out = a->refs_out;
   k.moved = a->moved;
@@ -952,11 +958,10 @@ mma_status_t mma_kv_compact(const mma_kv_layout_t* layout, void* const* gpu_laye
   k.moves = static_cast<uint32_t*>(a->workspace);
   k.from = reinterpret_cast<int32_t*>(k.moves + 2);
   k.to = k.from + layout->gpu_num_blocks;
-  k.places = places;
   k.num_blocks = layout->gpu_num_blocks;
   const hipStream_t on = static_cast<hipStream_t>(stream);
   if ((s = launched(launch_compact(k, on), "KV compaction"))) return s;
-  return move_pages(call, layout, gpu_layers, k.from, k.to, k.moves, layout->gpu_num_blocks / 2, on);
+  return move_pages(call, layout, gpu_layers, k.from, k.to, k.moves, layout->gpu_num_blocks / 2, a, on);
 } catch (...) {
   return ops_boundary_error("mma_kv_compact");
 }

@@ -160,8 +160,6 @@ struct ForkArgs {
 };
 
 struct CompactArgs {
-  const int32_t* table;
-  int32_t* table_out;
   const int32_t* refs;
   int32_t* refs_out;
   int32_t* moved;
@@ -169,7 +167,6 @@ struct CompactArgs {
   int32_t* from;  // the moves
   int32_t* to;
   uint32_t* moves;  // how many
-  uint64_t places;
   uint32_t num_blocks;
 };
 
@@ -179,6 +176,11 @@ struct MoveArgs {
   const uint32_t* moves;  // how many, or NULL: `most`
   uint64_t piece;         // bytes of a block's K or V
   uint64_t v_offset;      // of V of block 0 from the layer's start
+  const int32_t* table;   // of a compaction: its places, and where blocks have moved
+  int32_t* table_out;
+  const int32_t* moved;
+  uint64_t places;
+  uint32_t num_blocks;
   uint32_t most, layers;
   static constexpr uint32_t kMaxLayers = 192;
   uint64_t layer[kMaxLayers];
