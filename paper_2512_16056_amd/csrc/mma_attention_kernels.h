@@ -255,10 +255,11 @@ __device__ __forceinline__ void shape8(const ShapedArgs& a, float factor, float 
 
 // Bit j: token `token` sees entry key + j, by shape.
 __device__ __forceinline__ uint32_t keys_seen(const ShapedArgs& a, const SeqSpan& sp, const Walk& w, uint32_t token, uint32_t key) {
-  const auto first_bits = [](int64_t n) { return n >= 8 ? 0xffu : n <= 0 ? 0u : (1u << n) - 1; };
+  const auto first_bits = [](int32_t n) { return (1u << (n < 0 ? 0 : n > 8 ? 8 : n)) - 1; };
   if (a.tree) return keys_seen(static_cast<const AttnArgs&>(a), sp, token, key);
-  const int64_t at = static_cast<int64_t>(sp.before) + token - key;  // of the token, from the first key on
-  return first_bits(static_cast<int64_t>(w.prefix) - key) | (first_bits(at + 1) & ~first_bits(a.window ? at + 1 - a.window : 0));
+  const int32_t at = static_cast<int32_t>(sp.before + token - key);  // of the token, from the first key on
+  const int32_t out = a.window && at > 0 ? at + 1 - static_cast<int32_t>(a.window) : 0;  // keys before its window
+  return first_bits(static_cast<int32_t>(w.prefix - key)) | (first_bits(at < 8 ? at + 1 : 8) & ~first_bits(out));
 }
 
 // 16-bit halves of an operand whose keys' bits are set; the others 0.
@@ -1212,20 +1213,32 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     return true;
   };
   if constexpr (kShaped) {  // whole and masked tiles follow each other in any order
-    const auto turn = [&](auto b) {
-      if (base >= end) return false;
+    const auto go_on = [&](auto b) {
+      if (base + S::KT > end || !w.full(base, S::KT)) return false;
       arrive(b);
-      const uint32_t e = entry(base);
-      const bool mine = work && (e < w.prefix || (e < my_end && e + S::KT > my_low));
-      if (base + S::KT <= end && w.full(base, S::KT) && absent[number % 8] != number) {
-        if (work) tile(std::false_type(), b);
-      } else if (mine) {
-        tile(std::true_type(), b);
-      }
+      arrived = absent[number % 8] == number;
+      if (arrived) return false;
+      if (work) tile(std::false_type(), b);
       leave(b);
       return true;
     };
-    while (turn(std::false_type()) && turn(std::true_type())) {
+    int b = 0;
+    while (base < end) {
+      while (true) {
+        if (!b) {
+          if (!go_on(std::false_type())) break;
+          b = 1;
+        }
+        if (!go_on(std::true_type())) break;
+        b = 0;
+      }
+      if (base >= end) break;
+      if (!arrived) b ? arrive(std::true_type()) : arrive(std::false_type());
+      arrived = false;
+      const uint32_t e = entry(base);
+      if (work && (e < w.prefix || (e < my_end && e + S::KT > my_low))) tile(std::true_type(), b);
+      b ? leave(std::true_type()) : leave(std::false_type());
+      b ^= 1;
     }
   } else {
     int b = 0;
@@ -1483,6 +1496,14 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
         from[t] = draft[t] * a.group;
       }
       for (uint32_t r0 = 0; r0 < some; r0 += 16) {
+        bool mixed = kMode == 3;  // whether some of the rows do not see some of the keys
+        if constexpr (kShaped) if (kMode == 3) {
+          const uint32_t first = (row0 + r0) / a.group, last = (row0 + (some - r0 < 16 ? some : r0 + 16) - 1) / a.group;  // tokens
+          const uint32_t key = base + kTile - 1;
+          const int32_t ahead = static_cast<int32_t>(sp.before + first - key), behind = static_cast<int32_t>(sp.before + last - base);
+          if (base >= prefix && (behind < 0 || (a.window && ahead >= 0 && static_cast<uint32_t>(ahead) >= a.window))) continue;
+          mixed = key >= prefix && (ahead < 0 || (a.window && static_cast<uint32_t>(behind) >= a.window));
+        }
         f32x4 x[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
@@ -1510,7 +1531,7 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
               const int32_t away = static_cast<int32_t>(sp.before + tokens[i] - (base + t * 16 + m));
               if (a.cap2 != 0) y = capped(a, y);
               if (a.slopes) y = fmaf(-slopes[i], fabsf(static_cast<float>(away)), y);
-              if constexpr (kMode == 3)
+              if (mixed)
                 see = see && (base + t * 16 + m < prefix || (away >= 0 && (!a.window || static_cast<uint32_t>(away) < a.window)));
             }
             const float p = __builtin_amdgcn_exp2f(y - l2[i]);
@@ -1525,9 +1546,13 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
           }
       }
     };
-    if (kShaped && !a.tree)
-      run(std::integral_constant<int, 3>());
-    else if (base + kTile <= sp.before)
+    if constexpr (kShaped) {
+      if (!a.tree) {
+        run(std::integral_constant<int, 3>());
+        return;
+      }
+    }
+    if (base + kTile <= sp.before)
       run(std::integral_constant<int, 0>());
     else if (!a.tree)
       run(std::integral_constant<int, 1>());

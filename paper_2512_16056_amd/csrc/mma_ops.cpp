@@ -271,7 +271,7 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
     const uint64_t most = up_to(prefix, 64) + std::min<uint64_t>(tokens, wg_rows / group + 2) + shape->window + 64;
     return static_cast<uint32_t>(std::min<uint64_t>(most, q.max_len));
   };
-  if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out) p.stream = false;
+  if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out && !(shape && (shape->slopes || shape->softcap != 0))) p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.wg_rows = per_tile * p.tiles_per_wave;
