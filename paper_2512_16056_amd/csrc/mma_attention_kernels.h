@@ -1418,7 +1418,12 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
   const uint32_t wave = threadIdx.x / kOpsWave, lane = threadIdx.x % kOpsWave, g = lane / 16, m = lane % 16;
   const uint32_t head = blockIdx.y, seq = blockIdx.z;
   const SeqSpan sp = span_of(a.s, seq);
-  const uint32_t begin = blockIdx.x * a.score_len;
+  uint32_t part = 0, block = blockIdx.x;
+  if constexpr (kShaped && STAY) {
+    part = block % a.score_parts;
+    block /= a.score_parts;
+  }
+  const uint32_t begin = block * a.score_len;
   if (begin >= sp.total) return;
   const uint32_t end = begin + a.score_len < sp.total ? begin + a.score_len : sp.total;
   const int32_t* table = a.s.table + static_cast<uint64_t>(seq) * a.s.table_stride;
@@ -1572,6 +1577,11 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
       start = 0;
     else if (a.window)
       last = below((static_cast<int64_t>(end) - 1 + a.window - sp.before) * a.group, rows);
+    if (STAY && a.score_parts > 1 && start < last) {
+      const uint32_t each = ((last - start + a.score_parts - 1) / a.score_parts + kRows - 1) / kRows * kRows;
+      start += part * each;
+      last = start >= last || last - start < each ? last : start + each;
+    }
   }
   if constexpr (STAY) {
     const uint32_t base = begin + wave * kTile;
@@ -1648,11 +1658,31 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
     }
   }
   __syncthreads();
+  if constexpr (kShaped && STAY) {
+    if (a.score_parts > 1) {
+      float* to = a.score_part + ((static_cast<uint64_t>(part) * a.s.num_seqs + seq) * a.c.heads + head) * a.s.max_len;
+      for (uint32_t i = threadIdx.x; begin + i < end; i += 256) to[begin + i] = sums[i];
+      return;
+    }
+  }
   for (uint32_t i = threadIdx.x; begin + i < end; i += 256) {
     const uint32_t key = begin + i;
     const uint64_t to = (static_cast<uint64_t>(seq) * a.c.heads + head) * a.scores_stride + key;
     a.scores_out[to] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[to] : 0.0f) + sums[i];
   }
+}
+
+// The weights of the rows' parts, one after the other.
+__global__ __launch_bounds__(256) void attention_add_scores_kernel(ShapedArgs a) {
+  const uint32_t head = blockIdx.y, seq = blockIdx.z, key = blockIdx.x * 256 + threadIdx.x;
+  const SeqSpan sp = span_of(a.s, seq);
+  if (key >= sp.total) return;
+  const uint64_t row = static_cast<uint64_t>(seq) * a.c.heads + head;
+  float w = 0;
+  for (uint32_t p = 0; p < a.score_parts; ++p)
+    w += a.score_part[(static_cast<uint64_t>(p) * a.s.num_seqs * a.c.heads + row) * a.s.max_len + key];
+  const uint64_t to = row * a.scores_stride + key;
+  a.scores_out[to] = (a.scores_in && key < sp.before ? a.decay * a.scores_in[to] : 0.0f) + w;
 }
 
 template <class T, bool F8, int DP, bool VX, class A>
@@ -1688,9 +1718,14 @@ hipError_t launch_of(const A& a, const AttnPlan& p, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   if (a.lse2) {
-    const dim3 grid((a.s.max_len + a.score_len - 1) / a.score_len, a.c.heads, a.s.num_seqs);
+    uint32_t parts = 1;
+    if constexpr (A::kShaped) parts = a.score_parts;
+    const dim3 grid((a.s.max_len + a.score_len - 1) / a.score_len * parts, a.c.heads, a.s.num_seqs);
     e = p.keys_stay ? launch(attention_scores_kernel<A, T, F8, DP, true>, grid, 256, stream, a)
                     : launch(attention_scores_kernel<A, T, F8, DP, false>, grid, 256, stream, a);
+    if constexpr (A::kShaped)
+      if (e == hipSuccess && parts > 1)
+        e = launch(attention_add_scores_kernel, dim3((a.s.max_len + 255) / 256, a.c.heads, a.s.num_seqs), 256, stream, a);
   }
   return e;
 }

@@ -310,9 +310,18 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
       p.lse_bytes = up_to(units * 4, 256);
       p.q_bytes = up_to(units * c.dim * 2, 256);  // of queries that `out` replaces before the weights are formed
     }
+    // Shaped scores of many rows over few keys: the rows in parts, so that 1024 workgroups share them, of 256 rows at least
+    // (3 x 1021 tokens x 4 heads, 8 KV heads, 8-bit x-packed: FIGURES).
+    p.score_parts = 1;
+    if (shape && p.keys_stay && !p.logits) {
+      const uint64_t keys = static_cast<uint64_t>(up(q.max_len, 128)) * c.heads * q.num_seqs;
+      p.score_parts = static_cast<uint32_t>(std::clamp<uint64_t>(1024 / std::max<uint64_t>(keys, 1), 1, std::max(1u, p.rows / 256)));
+      if (p.score_parts > 1)
+        p.score_bytes = up_to(extent(static_cast<uint64_t>(p.score_parts) * q.num_seqs * c.heads, q.max_len, 4), 256);
+    }
   }
   if (p.splits > 1 || p.logits) p.ml_bytes = up_to(units * p.splits * 8, 256);
-  p.bytes = p.part_bytes + p.ml_bytes + p.lse_bytes + p.q_bytes + p.logit_bytes;
+  p.bytes = p.part_bytes + p.ml_bytes + p.lse_bytes + p.q_bytes + p.logit_bytes + p.score_bytes;
   return p;
 }
 
@@ -436,6 +445,8 @@ mma_status_t attention(const mma_kv_layout_t* layout, const void* layer, const m
   k.window = std::min<uint32_t>(shape->window, INT32_MAX);
   k.cap2 = shape->softcap * 1.44269504088896340736f;
   k.wg_rows = p.wg_rows;
+  k.score_parts = std::max(1u, p.score_parts);
+  k.score_part = take(p.score_bytes);
   return launched(launch_attention_shaped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
 }
 

@@ -92,6 +92,8 @@ struct ShapedArgs : AttnArgs {
   uint32_t window;        // entries up to a token's own, at most 2^31 - 1; 0: all
   float cap2;             // the cap, base 2; 0: none
   uint32_t wg_rows;       // rows of a workgroup
+  float* score_part;      // weights of parts of the rows, [score_parts][num_seqs][heads][max_len], where there are several
+  uint32_t score_parts;
   static constexpr bool kShaped = true;
 };
 
@@ -203,7 +205,8 @@ struct AttnPlan {
   bool logits;              // scores from logits that the main kernel keeps
   bool keys_stay;           // else: attention_scores_kernel keeps a wave's keys, or the rows
   uint32_t logit_stride;
-  uint64_t part_bytes, ml_bytes, lse_bytes, q_bytes, logit_bytes, bytes;
+  uint32_t score_parts;     // with a shape: parts of the rows whose weights are added up at the end
+  uint64_t part_bytes, ml_bytes, lse_bytes, q_bytes, logit_bytes, score_bytes, bytes;
 };
 
 // Whether attention_stream_kernel is there for two tiles of rows, with their keys and values in registers: not with heads

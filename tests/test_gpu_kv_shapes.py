@@ -148,6 +148,17 @@ def test_edges_of_window_and_prefix(cache):
             check(c, window=n - edge, prefix=[n + count - edge])
 
 
+@pytest.mark.parametrize("layout,cache,lens,counts", [("xpacked", F8, [50], [300]), ("hnd", BF16, [0, 700], [290, 130]),
+                                                      ("piece", F16, [5], [520])])
+def test_weights_of_rows_in_parts(layout, cache, lens, counts):
+    """Many rows over few keys: the rows' weights come in parts that are added up."""
+    c = Case(layout, cache, lens, counts, 64, 1, 4, 16, F16 if cache is F16 else BF16)
+    n = len(lens)
+    check(c, prefix=[200, 13][:n], window=100, scores=True)
+    check(c, cap=9.0, slopes=alibi(c.heads_q), scores=True)
+    check(c, cap=9.0, tree=tree_bits(c.counts, c.g), scores=True)
+
+
 def test_prefix_is_bounded_and_may_be_of_nothing():
     c = Case("piece", BF16, [100, 40], [30, 5], heads=1)
     check(c, prefix=[-3, 0], window=7)
