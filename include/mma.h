@@ -659,7 +659,7 @@ typedef struct mma_beam_select {
 
 /* v = score + (logit - lse), lse the log of the sum of exp of the beam's logits; of each request the `keep`
  * largest, in order, ties to the lower beam, then the lower token. lse and v are 64-bit (lse within
- * 2^-39), v rounded at the store. Within a beam candidates go by their logits. A beam that has ended has
+ * 2^-33), v rounded at the store; beams with the same logits and score tie. Within a beam candidates go by their logits. A beam that has ended has
  * one candidate: done_token, with its score as it is. Logits of -infinity are no candidates; a beam
  * whose score or lse is not finite (a logit that is NaN or +infinity) has none. Where there are fewer than
  * `keep`, the rest have token and parent -1 and a score of -infinity. */

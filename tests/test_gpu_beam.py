@@ -1,7 +1,9 @@
 """Beam search's selection, and forking and compacting the paged cache, against the reference (oracle.beam).
 
 Whole numbers and moved bytes are compared exactly; a value of a selection is a 64-bit one rounded to 32 bits: 2^-24 of itself,
-and 2^-38 for the sums (log-sum-exp within 2^-39, and the reference's own).
+and 2^-33 for the sums: each power is formed with a relative error of 5.5e-11 (below 2^-34) at most, so the log of their sum is
+off by as much, and its own roundings are of 64 bits. Two beams' candidates may so come closer by 1.1e-10: inputs that come
+closer than 2.5e-10 do not tell which is larger.
 """
 import math
 
@@ -48,13 +50,13 @@ def check_select(logits, scores, keep, done=None, done_token=0, view=None, **kw)
     torch.cuda.synchronize()
     t, p, v, gap = ob.select(logits.double().numpy(), scores.double().numpy(), keep, None if done is None else done.numpy(),
                              done_token)
-    assert gap > 1e-10, "the inputs do not tell which is larger"
+    assert gap > 2.5e-10, "the inputs do not tell which is larger"
     assert np.array_equal(parents.cpu().numpy(), p)
     assert np.array_equal(tokens.cpu().numpy(), t)
     got = best.cpu().double().numpy()
     none = t < 0
     assert (got[none] == -math.inf).all()
-    assert (np.abs(got[~none] - v[~none]) <= np.abs(v[~none]) * 2.0 ** -24 + 2.0 ** -38).all()
+    assert (np.abs(got[~none] - v[~none]) <= np.abs(v[~none]) * 2.0 ** -24 + 2.0 ** -33).all()
     return tokens, parents, best
 
 
@@ -589,7 +591,7 @@ def test_a_beam_search(layout, cache):
     for step in range(steps):
         want = ob.select(logits.cpu().double().numpy(), scores.cpu().double().numpy(), beams)
         toks, parents, scores = mma.mma_beam_select(logits, scores, beams)
-        assert want[3] > 1e-10 and np.array_equal(toks.cpu().numpy(), want[0]) and np.array_equal(parents.cpu().numpy(), want[1])
+        assert want[3] > 2.5e-10 and np.array_equal(toks.cpu().numpy(), want[0]) and np.array_equal(parents.cpu().numpy(), want[1])
         rows_of = parents.flatten() if step else torch.div(parents.flatten(), beams, rounding_mode="floor").int()
         seqs = mma.kv_seqs(table, lens, max_tokens=0, max_len=width * tokens)
         want = ob.fork(table.tolist(), lens.tolist(), refs.tolist(), rows_of.tolist(), [1] * rows, tokens, width * tokens, width)
@@ -620,3 +622,16 @@ def test_a_beam_search(layout, cache):
                         assert torch.equal(c.values(flat, c.index(which, *at, h)), want)
         logits = (out.float().view(rows, -1) @ unembed).to(BF16).view(batch, beams, vocab)
     assert refs.sum().item() == (table >= 0).sum().item()
+
+
+@pytest.mark.parametrize("layout,cache", [("hnd", "bf16"), ("xpacked", "f8")])
+def test_example(layout, cache):
+    """The example, in its own process (it initialises the library itself)."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "kv_beam.py"), "--layers", "2", "--prompt", "70", "--steps", "20",
+                        "--layout", layout, "--cache", cache], capture_output=True, text=True, timeout=110)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "2 prompts of 70 tokens, 20 steps of 4 beams" in r.stdout and "pages moved to the front" in r.stdout, r.stdout
