@@ -271,7 +271,10 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
     const uint64_t most = up_to(prefix, 64) + std::min<uint64_t>(tokens, wg_rows / group + 2) + shape->window + 64;
     return static_cast<uint32_t>(std::min<uint64_t>(most, q.max_len));
   };
-  if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out && !(shape && (shape->slopes || shape->softcap != 0))) p.stream = false;
+  // Slopes and caps are more work for each entry, which the waves of attention_stream_kernel share and one wave of the other
+  // has alone (4 rows, 32 of 1k to 8k, bf16, slopes: head-major 126 us against 150, in pieces 138 against 149).
+  const bool shapes = shape && (shape->slopes || shape->softcap != 0);
+  if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out && !shapes) p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
   p.tiles_per_wave = p.rows > per_tile ? 2 : 1;
   p.wg_rows = per_tile * p.tiles_per_wave;
@@ -311,7 +314,7 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
       p.q_bytes = up_to(units * c.dim * 2, 256);  // of queries that `out` replaces before the weights are formed
     }
     // Shaped scores of many rows over few keys: the rows in parts, so that 1024 workgroups share them, of 256 rows at least
-    // (3 x 1021 tokens x 4 heads, 8 KV heads, 8-bit x-packed: FIGURES).
+    // (3 x 1021 tokens x 4 heads, 8 KV heads, 8-bit x-packed: the weights 98 us, in one part 258).
     p.score_parts = 1;
     if (shape && p.keys_stay && !p.logits) {
       const uint64_t keys = static_cast<uint64_t>(up(q.max_len, 128)) * c.heads * q.num_seqs;
@@ -489,7 +492,8 @@ mma_status_t check_beam_sizes(const mma_beam_select_t* a, BeamPlan* p) {
   if (!a->keep || a->keep > kBeamKeep) return fail(MMA_ERR_INVALID_ARG, "keep %u: from 1 to %u", a->keep, kBeamKeep);
   if (!a->vocab || a->vocab > INT32_MAX) return fail(MMA_ERR_INVALID_ARG, "a vocabulary of %u: from 1 to 2^31 - 1", a->vocab);
   // A part is as long as lets 1024 workgroups, four on a CU, run at once, or as lets a row's parts fit a merge: to find a
-  // part's best costs as much as to sum some thousand logits, and what is found is merged.
+  // part's best costs as much as to sum some thousand logits, and what is found is merged (192 rows of 128001 in 1152
+  // workgroups, of which the last 128 run alone: 46.5 us, in 960 40.9, both before the present kernel).
   const uint64_t chunks = up(a->vocab, kBeamChunk), rows = static_cast<uint64_t>(a->batch) * a->beams;
   const uint64_t run = std::max(up(chunks, static_cast<uint32_t>(std::max<uint64_t>(1, 1024 / std::max<uint64_t>(1, rows)))), up(chunks, kBeamMerge / a->keep));
   const uint64_t splits = up(chunks, static_cast<uint32_t>(std::min(run, chunks)));

@@ -15,7 +15,8 @@ constexpr uint32_t kWide = 1024;                 // threads of a workgroup that 
 constexpr uint32_t kWaves = kWide / kOpsWave;
 constexpr uint32_t kCopy = 16384;                // bytes that a workgroup copies at once
 constexpr uint32_t kForkBlocks = 32768;          // of a pool whose counts are in LDS
-constexpr uint64_t kForkPlaces = 16384;          // of tables that one workgroup goes through
+constexpr uint64_t kForkPlaces = 16384;          // of tables that one workgroup goes through (500 places: 5.6 us, in three
+                                                 // launches 19; 36000: 27 and 18.5)
 constexpr uint32_t kMasks = 2048;                // groups of 64 blocks whose bits are in LDS
 constexpr uint32_t kMoves = 4096;                // moves of a compaction that are
 
@@ -473,7 +474,8 @@ __global__ __launch_bounds__(kWide) void compact_list_kernel(CompactArgs a) {
 }
 
 // ---------------------------------------------------------------- copies
-// Pages from[k] to to[k] (where both are there) in every layer, K and V: 16 KiB at a time. Nothing is read that another
+// Pages from[k] to to[k] (where both are there) in every layer, K and V: 16 KiB at a time, past the caches (983 pages of 64 KiB
+// in 4 layers, 515 MB read and written: 99 us, 5.2 TB/s). Nothing is read that another
 // copy of the call writes. Of a compaction also the table's places.
 __global__ __launch_bounds__(256) void move_pages_kernel(MoveArgs a) {
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; i < a.places; i += gridDim.x * 256ull) {
