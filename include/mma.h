@@ -581,11 +581,12 @@ typedef struct mma_kv_shape {
   uint32_t max_prefix;      /* no sequence has a longer prefix (further entries are left out of it); with a window the
                                work is cut by it, as by max_len */
   uint32_t window;          /* 0: none */
-  float softcap;            /* 0: none; else from 1e-6 to 1e6 */
+  float softcap;            /* 0: none; else from 1e-6 to 1024 */
 } mma_kv_shape_t;
 
 /* mma_kv_attention with such scores; lse and the weights of the entries are of the shaped ones. NULL, or a
- * shape of nothing: mma_kv_attention. The cap's tanh is within 2^-22 of the cap. */
+ * shape of nothing: mma_kv_attention. The capped score is within 2^-22 of the cap: with the
+ * largest one 2^-12, an eighth of what the weights' rounding to bf16 makes. */
 mma_status_t mma_kv_attention_shaped(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
                                      const mma_kv_attention_t* args, const mma_kv_shape_t* shape, void* stream);
 

@@ -338,8 +338,8 @@ mma_status_t check_attention_sizes(const mma_kv_layout_t* layout, const mma_kv_s
   mma_status_t s;
   if (!a) return fail(MMA_ERR_INVALID_ARG, "NULL arguments");
   if (const mma_kv_shape_t* x = *shape) {
-    if (x->softcap != 0 && !(x->softcap >= 1e-6f && x->softcap <= 1e6f))
-      return fail(MMA_ERR_INVALID_ARG, "softcap has to be 0, or from 1e-6 to 1e6");
+    if (x->softcap != 0 && !(x->softcap >= 1e-6f && x->softcap <= 1024.0f))
+      return fail(MMA_ERR_INVALID_ARG, "softcap has to be 0, or from 1e-6 to 1024");
     if (a->tree && (x->slopes || x->prefix || x->window))
       return fail(MMA_ERR_INVALID_ARG, "a drafted token's distance is not told by its tree: no slopes, prefix or window with one");
     if (x->softcap == 0 && !x->slopes && !x->prefix && !x->window) *shape = nullptr;

@@ -248,7 +248,9 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   x.type = q.kind;
   x.cache_type = q.cache;
   mma_kv_shape_t shape{};
-  shape.softcap = static_cast<float>(real(a[15]));
+  const double cap = real(a[15]);
+  shape.softcap = static_cast<float>(cap);
+  if (cap != 0 && shape.softcap == 0) shape.softcap = -1.0f;  // too small a number is refused, not taken for none
   shape.window = count(a[16], "window");
   shape.slopes = flat_ptr<float>(a[17], "slopes", at::kFloat, {q.heads});
   shape.prefix = flat_ptr<int32_t>(a[18], "prefix", at::kInt, {c.seqs->num_seqs});
@@ -409,7 +411,7 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     b.done = static_cast<const uint8_t*>(flat(a[3], "done", d.scalar_type() == at::kBool ? at::kBool : at::kByte, {batch, beams}).data_ptr());
   }
   const double token = real(a[4]);
-  if (!(token >= -2147483648.0 && token <= 2147483647.0)) REFUSE("done_token: a token is wanted");
+  if (!(token >= -2147483648.0 && token <= 2147483647.0 && token == std::floor(token))) REFUSE("done_token: a token is wanted");
   b.done_token = static_cast<int32_t>(token);
   b.logits = x.data_ptr();
   b.scores = static_cast<const float*>(scores.data_ptr());

@@ -257,7 +257,8 @@ def test_select_refusals_and_nothing_to_do():
     refused(lambda: sel(keep=3, out=(t, t.clone(), s)))                               # and with an input
     for bad in (lambda: sel(keep=0), lambda: sel(x=x.double()), lambda: sel(x=x.cpu()), lambda: sel(s=s.double()),
                 lambda: sel(x=x[:, :2]), lambda: sel(x=x[..., ::2]), lambda: sel(done=done[:1]), lambda: sel(keep=-1),
-                lambda: sel(x=torch.zeros(2, 6, 50, device="cuda")[:, :3]), lambda: sel(done=done, done_token=2 ** 40)):
+                lambda: sel(x=torch.zeros(2, 6, 50, device="cuda")[:, :3]), lambda: sel(done=done, done_token=2 ** 40),
+                lambda: sel(done=done, done_token=2.5)):
         with pytest.raises(ValueError):
             bad()
     got = sel(x=torch.zeros(0, 50, device="cuda"), s=torch.zeros(0, 3, device="cuda"))
