@@ -314,7 +314,7 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
       p.q_bytes = up_to(units * c.dim * 2, 256);  // of queries that `out` replaces before the weights are formed
     }
     // Shaped scores of many rows over few keys: the rows in parts, so that 1024 workgroups share them, of 256 rows at least
-    // (3 x 1021 tokens x 4 heads, 8 KV heads, 8-bit x-packed: the weights 98 us, in one part 258).
+    // (3 x 1021 tokens x 4 heads, 8 KV heads, 8-bit x-packed: the weights 93 us, in one part 258; 61 with the present kernel).
     p.score_parts = 1;
     if (shape && p.keys_stay && !p.logits) {
       const uint64_t keys = static_cast<uint64_t>(up(q.max_len, 128)) * c.heads * q.num_seqs;
