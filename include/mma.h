@@ -418,11 +418,13 @@ mma_status_t mma_digest_u32(const void* dev_ptr, uint64_t bytes, uint64_t* dev_o
 /* What a decode step does with the paged KV cache that the calls above move: new
  * tokens written into it (append), attention over it (attention), a verified draft
  * moved together (commit), and the entries that little attention went to dropped
- * before the rest is offloaded (evict). All four work on the GPU layer tensors of
+ * before the rest is offloaded (evict); and for beam search the best continuations
+ * (beam_select), sequences that go on from others (fork), and held blocks moved together
+ * (compact). They work on the GPU layer tensors of
  * mma_kv_layout_t, in each of its block layouts, and are ordered on `stream` like a
  * kernel launch: they allocate nothing, wait for nothing and may be captured.
  *
- * `layout` is the one of the transfers; of it num_layers (commit only),
+ * `layout` is the one of the transfers; of it num_layers (commit, fork and compact only),
  * block_tokens, kv_heads, head_dim, elem_bytes, gpu_num_blocks and gpu_layout are
  * used. head_dim * elem_bytes has to be a multiple of 16, head_dim a multiple of 8
  * and at most 256, layer tensors 16-byte aligned, in every layout.
@@ -660,8 +662,9 @@ typedef struct mma_beam_select {
 
 /* v = score + (logit - lse), lse the log of the sum of exp of the beam's logits; of each request the `keep`
  * largest, in order, ties to the lower beam, then the lower token. lse and v are 64-bit (lse within
- * 2^-33), v rounded at the store; beams with the same logits and score tie. Within a beam candidates go by their logits. A beam that has ended has
- * one candidate: done_token, with its score as it is. Logits of -infinity are no candidates; a beam
+ * 2^-33), v rounded at the store; beams with the same logits and score tie. Within a beam candidates
+ * go by their logits. A beam that has ended has one candidate: done_token, with its score as it is.
+ * Logits of -infinity are no candidates; a beam
  * whose score or lse is not finite (a logit that is NaN or +infinity) has none. Where there are fewer than
  * `keep`, the rest have token and parent -1 and a score of -infinity. */
 mma_status_t mma_beam_select(const mma_beam_select_t* args, void* stream);

@@ -23,7 +23,9 @@
 //
 // Every kernel is compiled for AttnArgs (mma_attention.hip) and for ShapedArgs (mma_attention_shaped.hip): scores capped
 // by a tanh or biased by distance, entries out of a window passed over, a prefix seen by every token. What shapes cost
-// is paid by the second alone.
+// is paid by the second alone. One token of 8 sequences of 32k entries, f16, a window of 4096 and a prefix of 4: 29 us, 4.0 TB/s of what
+// is seen, and 4.6 to join; 32 sequences of 1k to 8k with slopes 133 us, 4.4 TB/s; 2048 tokens behind 6144 entries, capped, a window of
+// 4096: 208 us, 0.66 PFLOP/s, 171 without the cap: vector instructions, 14 a score instead of 8.
 #ifndef MMA_ATTENTION_KERNELS_H_
 #define MMA_ATTENTION_KERNELS_H_
 #include "mma_ops.h"

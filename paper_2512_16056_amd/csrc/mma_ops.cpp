@@ -1,6 +1,6 @@
 // Host side of the operators on the paged KV cache: argument checks, the split of an
-// attention call, and the rotary table. The kernels are in mma_attention.hip and
-// mma_kv_ops.hip; nothing here allocates or waits.
+// attention call and of a beam selection, and the rotary table. The kernels are in mma_attention_kernels.h,
+// mma_kv_ops.hip, mma_beam.hip and mma_pages.hip; nothing here allocates or waits.
 #include "mma_ops.h"
 
 #include <algorithm>
