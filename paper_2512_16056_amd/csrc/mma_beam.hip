@@ -252,7 +252,10 @@ __device__ __forceinline__ uint32_t thin(List<N>& l, uint32_t* places, uint32_t*
   }
   __syncthreads();
   if (t < kOpsWave) {
-    const uint32_t b = n <= 256 ? bound_of<256>(numbers, keep) : n <= 512 ? bound_of<512>(numbers, keep) : bound_of<N>(numbers, keep);
+    const uint32_t b = n <= 256    ? bound_of<256>(numbers, keep)
+                       : n <= 512  ? bound_of<512>(numbers, keep)
+                       : n <= 1024 ? bound_of<1024>(numbers, keep)
+                                   : bound_of<N>(numbers, keep);
     if (!t) waves[0] = b, waves[1] = 0;
   }
   __syncthreads();
