@@ -241,6 +241,46 @@ def test_select_other_stream_and_captured():
         assert all(same_bits(a, b) for a, b in zip(out, want))
 
 
+def test_select_many_requests():
+    """More requests than workgroups run at once, of few beams and few logits, odd rows; fewer candidates than are kept."""
+    g = gen(21)
+    for batch, beams, vocab, keep in ((3001, 2, 37, 3), (700, 1, 1, 2)):
+        logits = some_logits(g, batch, beams, vocab, F32)
+        check_select(logits, -torch.rand(batch, beams, generator=g), keep)
+
+
+def test_calls_at_once_on_two_streams():
+    """Selections, forks and compactions on two streams side by side, each with its own outputs and workspace."""
+    g = gen(22)
+    x = [some_logits(g, 3, 5, 20001, F32).cuda() for _ in range(2)]
+    scores = -torch.rand(3, 5, generator=g).cuda()
+    p = Pool([40, 90, 17, 64, 3], share=0.9, spare=60)
+    seqs = mma.kv_seqs(i32(p.table.tolist()).cuda(), i32(p.lens).cuda(), max_tokens=0, max_len=p.max_len)
+    counts, grow = i32(p.refs.tolist()).cuda(), i32([2] * 5).cuda()
+    parents = [i32([0, 0, 1, 3, 3]).cuda(), i32([4, 2, 2, 1, -1]).cuda()]
+    lay = p.layout()
+
+    def calls(i, layers, stream):
+        best = mma.mma_beam_select(x[i], scores, 7, stream=stream)
+        child = mma.mma_kv_fork(lay, layers, seqs, parents[i], counts, grow=grow, stream=stream)
+        return best + child + mma.mma_kv_compact(lay, layers, child[0], child[2], stream=stream)
+
+    want = []
+    for i in range(2):
+        layers = list(p.flat.cuda())
+        want.append((calls(i, layers, None), layers))
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    layers = [list(p.flat.cuda()) for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [calls(i, layers[i], streams[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(same_bits(a, b) for a, b in zip(got[i], want[i][0]))
+        assert all(torch.equal(a, b) for a, b in zip(layers[i], want[i][1]))
+
+
 def test_select_refusals_and_nothing_to_do():
     x, s = torch.zeros(2, 3, 50, device="cuda"), torch.zeros(2, 3, device="cuda")
     sel = lambda x=x, s=s, keep=4, **kw: mma.mma_beam_select(x, s, keep, **kw)  # noqa: E731
