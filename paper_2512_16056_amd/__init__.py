@@ -560,7 +560,7 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
                      stream=None) -> torch.Tensor:
     """Attention of the call's tokens over their sequences' entries; returns `out` (or a new tensor). `tree`: int64
     [tokens][words] bits. `scale`: 1 / sqrt(head_dim) unless given. `workspace`: a uint8 tensor of
-    kv_attention_workspace() bytes or more; a new one of the stream's unless given.
+    kv_attention_workspace() bytes of the call's shape or more; a new one of the stream's unless given.
 
     Scores have the shape of ``mma_kv_shape_t``: capped (`softcap`), less `slopes` (float32 [heads]) times the distance, seen
     within `window` entries up to the token's own, and in both directions within `prefix` (int32 [sequences]) entries, of
@@ -570,7 +570,8 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
             out = _empty_on(stream, q.shape, q.dtype, q.device)
         if workspace is None:
             need = kv_attention_workspace(layout, seqs, q.shape[0], q.shape[1], q.dtype, scores_out is not None, window=window,
-                                          prefix=prefix is not None, max_prefix=max_prefix)
+                                          prefix=prefix is not None, max_prefix=max_prefix, softcap=softcap,
+                                          slopes=slopes is not None)
             workspace = _empty_on(stream, (need,), torch.uint8, q.device)
     return _kv_ops.attention(layout, layer, seqs.address, q, out, scale, tree, lse, scores_in, scores_out, decay, k_scale,
                              v_scale, workspace, _stream(stream), softcap, window, slopes, prefix, max_prefix)
@@ -578,16 +579,17 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
 
 def kv_attention_workspace(layout: mma_kv_layout_t, seqs: KVSeqs, num_tokens: int, q_heads: int, dtype: torch.dtype,
                            scores: bool = False, *, window: int = 0, prefix: bool = False,
-                           max_prefix: Optional[int] = None) -> int:
-    """Bytes of workspace of an attention call of these sizes; with a window a call needs fewer."""
+                           max_prefix: Optional[int] = None, softcap: float = 0.0, slopes: bool = False) -> int:
+    """Bytes of workspace of an attention call of these sizes and this shape (of `prefix` and `slopes`, whether the call has
+    them): with a window a call needs fewer, with slopes or a cap it may need more."""
     kind = _TYPES.get(dtype)
     if kind is None:
         raise ValueError(f"queries of {dtype}: bfloat16 or float16 is wanted")
     a = mma_kv_attention_t(num_tokens=num_tokens, q_heads=q_heads, type=kind, scores_out=1 if scores else None,
                            cache_type=MMA_TYPE_F8 if layout.elem_bytes == 1 else kind)
     need = _U64()
-    shape = mma_kv_shape_t(prefix=1 if prefix else None, max_prefix=seqs.max_len if max_prefix is None else max_prefix,
-                           window=window)
+    shape = mma_kv_shape_t(slopes=1 if slopes else None, prefix=1 if prefix else None,
+                           max_prefix=seqs.max_len if max_prefix is None else max_prefix, window=window, softcap=softcap)
     _check(lib.mma_kv_attention_shaped_workspace(layout, seqs.c, a, shape, need), "mma_kv_attention_shaped_workspace")
     return need.value
 

@@ -129,3 +129,46 @@ def test_reference_shapes_by_hand():
     flat[c.index(0, 0, 0, 0)[0]] = 1.0
     q[0, 0, 0] = 1e4
     assert math.isclose(see(cap=math.log(3.0)), (3 * 1 + 2 + 4) / 5, rel_tol=1e-9)
+
+
+# ------------------------------------------------------------------ workspaces of shaped attention
+class Seqs:
+    """Bounds of a call's sequences, as the query takes them."""
+
+    def __init__(self, num_seqs, max_tokens, max_len, tokens=16):
+        self.max_len = max_len
+        self.c = mma.mma_kv_seqs_t(0, 0, 0, num_seqs, -(-max_len // tokens), max_tokens, max_len)
+
+
+SIZES = [  # layout, bytes of an element, heads, dim, sequences, tokens of each, entries: one token of many, rows in parts, a chunk
+    (0, 2, 8, 128, 32, 1, 8192), (2, 2, 8, 128, 8, 1, 32768), (1, 1, 8, 128, 3, 1021, 1071), (2, 2, 1, 64, 1, 300, 350),
+    (0, 2, 8, 128, 4, 9, 5000), (2, 2, 8, 128, 1, 2048, 8192), (1, 2, 2, 256, 64, 1, 9000), (0, 1, 8, 64, 2, 1, 100)]
+
+
+@pytest.mark.parametrize("scores", [False, True])
+@pytest.mark.parametrize("layout,elem,heads,dim,num,each,length", SIZES)
+def test_the_query_knows_every_part_of_a_shape(layout, elem, heads, dim, num, each, length, scores):
+    """What kv_attention_workspace says is what the call of that shape asks for, whatever the shape is made of."""
+    lay = mma.kv_layout(1, 16, heads, dim, elem, 70000, 1, layout)
+    seqs = Seqs(num, each, length)
+    a = mma.mma_kv_attention_t(num_tokens=num * each, q_heads=4 * heads, scores_out=1 if scores else None,
+                               cache_type=mma.MMA_TYPE_F8 if elem == 1 else mma.MMA_TYPE_BF16)
+    for cap in (0.0, 30.0):
+        for slopes in (False, True):
+            for window in (0, 700):
+                for prefix, most in ((False, None), (True, 40), (True, None)):
+                    shape = mma.mma_kv_shape_t(slopes=1 if slopes else None, prefix=1 if prefix else None,
+                                               max_prefix=length if most is None else most, window=window, softcap=cap)
+                    need = ctypes.c_uint64()
+                    assert mma.lib.mma_kv_attention_shaped_workspace(lay, seqs.c, a, shape, need) == mma.MMA_OK
+                    got = mma.kv_attention_workspace(lay, seqs, num * each, 4 * heads, torch.bfloat16, scores, window=window,
+                                                     prefix=prefix, max_prefix=most, softcap=cap, slopes=slopes)
+                    assert got == need.value
+
+
+def test_slopes_and_caps_need_their_own_workspace():
+    lay = mma.kv_layout(1, 16, 8, 128, 2, 70000, 1, 0)
+    need = lambda **kw: mma.kv_attention_workspace(lay, Seqs(32, 1, 8192), 32, 32, torch.bfloat16, **kw)  # noqa: E731
+    assert need(slopes=True) == need(softcap=30.0) == need(slopes=True, softcap=30.0) > need()
+    with pytest.raises(mma.MMAError):
+        need(softcap=-1.0)

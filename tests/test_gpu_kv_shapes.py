@@ -320,3 +320,42 @@ def test_refusals():
     need = mma.kv_attention_workspace(c.layout(), c.seqs(), 3, 8, BF16, True, window=5)
     ws = torch.empty(max(need - 1, 1), dtype=torch.uint8, device="cuda")
     refused(lambda: att(window=5, scores_out=torch.zeros(1, 2, 64, device="cuda"), workspace=ws), "MMA_ERR_BUFFER_TOO_SMALL")
+
+
+@pytest.mark.parametrize("layout,cache,lens,counts,scores,shape", [
+    ("piece", BF16, [4200] + [30] * 31, [1] * 32, False, dict(slopes=True)),    # one token each of many, with more splits than plain
+    ("hnd", F16, [4200] + [30] * 31, [1] * 32, False, dict(softcap=20.0)),
+    ("xpacked", F8, [50], [300], True, dict(softcap=9.0)),                      # weights of rows in parts
+    ("hnd", BF16, [0, 700], [290, 130], True, dict(slopes=True, softcap=9.0)),
+])
+def test_slopes_and_caps_on_a_stream_and_captured(layout, cache, lens, counts, scores, shape):
+    """The workspace is the shape's own, where a plain call's would be too small: the stream's, and one from the query."""
+    c = Case(layout, cache, lens, counts, 128 if len(lens) > 2 else 64, 2 if len(lens) > 2 else 1, 4, 16, F16 if cache is F16 else BF16)
+    q = normal(c.g, c.total, c.heads_q, c.c.dim, std=2.0).to(c.dtype).cuda()
+    layer, seqs, lay = c.flat[0].cuda(), c.seqs(), c.layout()
+    size = dict(softcap=shape.get("softcap", 0.0), slopes="slopes" in shape)
+    need = mma.kv_attention_workspace(lay, seqs, c.total, c.heads_q, c.dtype, scores, **size)
+    assert need > mma.kv_attention_workspace(lay, seqs, c.total, c.heads_q, c.dtype, scores)
+    kw = dict(c.scales(), **shape)
+    if "slopes" in kw:
+        kw["slopes"] = alibi(c.heads_q).cuda()
+    weights = lambda: torch.zeros(len(lens), c.c.heads, c.max_len, device="cuda") if scores else None  # noqa: E731
+    w = weights()
+    want = mma.mma_kv_attention(lay, layer, seqs, q, scores_out=w, **kw)
+    side, w2 = torch.cuda.Stream(), weights()
+    side.wait_stream(torch.cuda.current_stream())
+    got = mma.mma_kv_attention(lay, layer, seqs, q, stream=side, scores_out=w2, **kw)
+    side.synchronize()
+    assert same_bits(got, want) and (not scores or same_bits(w, w2))
+    out, ws = torch.empty_like(q), torch.empty(need, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mma.mma_kv_attention(lay, layer, seqs, q, out=out, workspace=ws, scores_out=w2, **kw)
+    for _ in range(3):
+        out.zero_()
+        ws.random_()
+        if scores:
+            w2.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same_bits(out, want) and (not scores or same_bits(w, w2))
