@@ -1588,13 +1588,14 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
     w += across(w, 16);
     return w + across(w, 32);
   };
-  // Rows of tokens before the first key's do not see these keys, nor, with a window, rows of tokens far behind them.
+  // Rows of tokens before the first key's do not see these keys, nor, with a window, rows of tokens far behind them. Both to
+  // whole 16 rows: a product adds up all of its 16, and whether some of them do not see a key is asked of those before `last`.
   uint32_t start = !a.tree && begin > sp.before ? (begin - sp.before) * a.group / 16 * 16 : 0, last = rows;
   if constexpr (kShaped) {
     if (begin < prefix)
       start = 0;
     else if (a.window)
-      last = below((static_cast<int64_t>(end) - 1 + a.window - sp.before) * a.group, rows);
+      last = below(((static_cast<int64_t>(end) - 1 + a.window - sp.before) * a.group + 15) & ~15ll, rows);
     if (STAY && a.score_parts > 1 && start < last) {
       const uint32_t each = ((last - start + a.score_parts - 1) / a.score_parts + kRows - 1) / kRows * kRows;
       start += part * each;

@@ -359,3 +359,16 @@ def test_slopes_and_caps_on_a_stream_and_captured(layout, cache, lens, counts, s
         graph.replay()
         torch.cuda.synchronize()
         assert same_bits(out, want) and (not scores or same_bits(w, w2))
+
+
+@pytest.mark.parametrize("max_len", [97, 128, 129, 130, 161])
+@pytest.mark.parametrize("group", [1, 3])
+def test_weights_of_a_last_key_that_few_rows_see(group, max_len):
+    """Tokens past max_len whose window ends before the last entry but which the prefix keeps alive, in the same 16 rows as
+    tokens that see it: one sequence (keys pass by), several and many rows (keys stay), rows in parts."""
+    for lens, counts in (([0], [200]), ([3, 0], [150, 200]), ([0], [400]), ([5, 70], [600, 1])):
+        c = Case("hnd", BF16, lens, counts, heads=1, group=group, dim=64)
+        c.max_len = max_len
+        n = len(lens)
+        check(c, window=60, prefix=[5] * n, scores=True)
+        check(c, window=41, prefix=[5] * n, cap=9.0, slopes=alibi(c.heads_q), scores=True)
