@@ -661,9 +661,10 @@ typedef struct mma_beam_select {
 } mma_beam_select_t;
 
 /* v = score + (logit - lse), lse the log of the sum of exp of the beam's logits; of each request the `keep`
- * largest, in order, ties to the lower beam, then the lower token. lse and v are 64-bit (lse within
- * 2^-33), v rounded at the store; beams with the same logits and score tie. Within a beam candidates
- * go by their logits. A beam that has ended has one candidate: done_token, with its score as it is.
+ * largest, in order, ties to the lower beam, within a beam to the larger logit (a score far below or tiny logits make
+ * equal values of logits that are not), then to the lower token. lse and v are 64-bit (lse within
+ * 2^-33), v rounded at the store; beams with the same logits and score tie.
+ * A beam that has ended has one candidate: done_token, with its score as it is.
  * Logits of -infinity are no candidates; a beam
  * whose score or lse is not finite (a logit that is NaN or +infinity) has none. Where there are fewer than
  * `keep`, the rest have token and parent -1 and a score of -infinity. */

@@ -9,7 +9,8 @@ import numpy as np
 
 def select(logits, scores, keep, done=None, done_token=0):
     """logits float64 [batch][beams][vocab], scores float64 [batch][beams]: (tokens, parents, values), lists of `keep` of each
-    request, and the least distance between the value of a chosen candidate and another's that does not equal it."""
+    request, and the least distance between the value of a chosen candidate and another's that does not equal it. Equal values:
+    the lower row first, then the larger logit, then the lower token."""
     res, gap = [], math.inf
     for b in range(logits.shape[0]):
         found = []
@@ -19,21 +20,21 @@ def select(logits, scores, keep, done=None, done_token=0):
             if not math.isfinite(s):
                 continue
             if done is not None and done[b, y]:
-                found.append((-s, row, done_token))
+                found.append((-s, row, 0.0, done_token))
                 continue
             if np.isnan(x).any() or not math.isfinite(x.max()):
                 continue
             z = x - x.max()
             lse = x.max() + math.log(math.fsum(np.exp(z)))
             order = np.lexsort((np.arange(len(x)), -x))[: keep + 1]
-            found += [(-(s + (float(x[t]) - lse)), row, int(t)) for t in order if x[t] > -math.inf]
+            found += [(-(s + (float(x[t]) - lse)), row, -float(x[t]), int(t)) for t in order if x[t] > -math.inf]
         found.sort()
-        values = [-v for v, _, _ in found]
+        values = [-f[0] for f in found]
         for i in range(min(keep, len(values) - 1)):
             if values[i] != values[i + 1]:
                 gap = min(gap, values[i] - values[i + 1])
-        found = found[:keep] + [(math.inf, -1, -1)] * (keep - len(found))
-        res.append(([t for _, _, t in found], [r for _, r, _ in found], [-v for v, _, _ in found]))
+        found = found[:keep] + [(math.inf, -1, 0.0, -1)] * (keep - len(found))
+        res.append(([t for _, _, _, t in found], [r for _, r, _, _ in found], [-v for v, _, _, _ in found]))
     return tuple(np.array([r[i] for r in res]) for i in range(3)) + (gap,)
 
 

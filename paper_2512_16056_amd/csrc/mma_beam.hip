@@ -25,6 +25,7 @@ constexpr uint32_t kList = 1024;                  // candidates of a part
 constexpr uint32_t kMerge = 1024;                 // threads of a merge
 constexpr uint32_t kMergePer = kBeamMerge / kMerge;
 constexpr uint32_t kMergeList = 2816;             // candidates of a merge
+constexpr int kOrderBits = 52;                    // of what equal values of a merge go by
 constexpr float kLeast = -3.4028234664e38f;       // the least finite number
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
@@ -132,18 +133,23 @@ __device__ __forceinline__ double sum_of_wave(double v) {
   return v + __shfl_xor(v, 32, kOpsWave);
 }
 
-// How many threads of the workgroup, over their N values each, hold what `is` says; the same for every thread.
-template <int N, class F>
-__device__ __forceinline__ uint32_t count_of(uint32_t* waves, F is) {
-  uint32_t n = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) n += __popcll(__ballot(is(i)));
+// The sum of what each wave has, for every thread.
+__device__ __forceinline__ uint32_t sum_of_waves(uint32_t* waves, uint32_t n) {
   __syncthreads();
   if (threadIdx.x % kOpsWave == 0) waves[threadIdx.x / kOpsWave] = n;
   __syncthreads();
   n = 0;
   for (uint32_t w = 0; w < blockDim.x / kOpsWave; ++w) n += waves[w];
   return n;
+}
+
+// How many threads of the workgroup, over their N values each, hold what `is` says; the same for every thread.
+template <int N, class F>
+__device__ __forceinline__ uint32_t count_of(uint32_t* waves, F is) {
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) n += __popcll(__ballot(is(i)));
+  return sum_of_waves(waves, n);
 }
 
 // A number that at least `keep` of N in LDS reach, and a quarter more at most where they differ: by one wave, from the
@@ -555,17 +561,19 @@ struct Keys {
 };
 
 // The `keep` best of the threads' keys; value(i) is what counts of a thread's i-th (0: none), descending within a list. Ties go
-// to the lower place. Found as in beam_part_kernel: as many of the threads' largest, which are their lists' first ones, reach
-// a bound; of a list only what comes before the first value below it is looked at; and where a few lists hold most of the
-// best, so that much more does reach it, what was found is thinned once more before it is ranked (32 beams of 4 parts of
-// 64, scores apart by 6: 78 us without). give(rank, value, place); returns how many there are.
-template <class V, class F>
-__device__ __forceinline__ uint32_t best_of(const Keys& k, uint32_t keep, V value, F give) {
+// to the lower place, which is the lower beam, the larger logit and the lower token, as long as equal values of a beam have equal
+// logits. Where rounding may have made other logits' values equal (TIES; near_zero(i), and give says so of what it is given), they
+// go by order(place), lower ones first, and are given once more. Found as in beam_part_kernel: as many of the threads' largest,
+// which are their lists' first ones, reach a bound; of a list only what comes before the first value below it is looked at; and
+// where a few lists hold most of the best, so that much more does reach it, what was found is thinned once more before it is
+// ranked (32 beams of 4 parts of 64, scores apart by 6: 78 us without). give(rank, value, place); returns how many there are.
+template <bool TIES, class V, class Z, class O, class F>
+__device__ __forceinline__ uint32_t best_of(const Keys& k, uint32_t keep, V value, Z near_zero, O order, F give) {
   __shared__ List<kMergeList> l;
   __shared__ __attribute__((aligned(16))) uint32_t numbers[kMergeList];
-  __shared__ uint32_t places[kMergeList + 8], waves[kMerge / kOpsWave], bound, listed;
+  __shared__ uint32_t places[kMergeList + 8], waves[kMerge / kOpsWave], bound, listed, merged;
   const uint32_t t = threadIdx.x;
-  if (!t) listed = 0;
+  if (!t) listed = merged = 0;
   uint64_t top = 0;
 #pragma unroll
   for (uint32_t i = 0; i < kMergePer; ++i)
@@ -596,39 +604,87 @@ __device__ __forceinline__ uint32_t best_of(const Keys& k, uint32_t keep, V valu
   __syncthreads();
   uint32_t n = listed;
   if (n > kMergeList) {  // of many equal ones: the bound bit by bit over all
-    const auto is = [&](uint32_t i) { return i < k.has ? value(i) : 0; };
+    uint64_t is[kMergePer];
+#pragma unroll
+    for (uint32_t i = 0; i < kMergePer; ++i) is[i] = i < k.has ? value(i) : 0;
     uint64_t key = 0;
 #pragma unroll 1
     for (int bit = 63; bit >= 0; --bit) {
       const uint64_t next = key | 1ull << bit;
-      if (count_of<kMergePer>(waves, [&](int i) { return is(i) >= next; }) >= keep) key = next;
+      if (count_of<kMergePer>(waves, [&](int i) { return is[i] >= next; }) >= keep) key = next;
     }
-    // All above it, and of those that equal it the lowest places, up to `until`.
-    const uint32_t more = keep - count_of<kMergePer>(waves, [&](int i) { return is(i) > key; });
-    uint32_t until = 0;
+    // All above it, and of those that equal it the lowest places, or by order, up to `until`.
+    const uint32_t more = keep - count_of<kMergePer>(waves, [&](int i) { return is[i] > key; });
+    uint32_t equal = 0, close = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kMergePer; ++i) {
+      equal |= (is[i] == key ? 1u : 0u) << i;
+      if constexpr (TIES) close |= is[i] == key && near_zero(i) ? 1 : 0;
+    }
+    const bool by_order = TIES && sum_of_waves(waves, __any(close));
+    const auto place = [&](uint32_t i) -> uint64_t {
+      if constexpr (TIES)
+        if (by_order) return order(k.at + i);
+      return k.at + i;
+    };
+    uint64_t until = 0;
 #pragma unroll 1
-    for (uint32_t bit = kBeamMerge; bit; bit /= 2) {
-      const uint32_t next = until + bit;
-      if (next <= kBeamMerge && count_of<kMergePer>(waves, [&](int i) { return is(i) == key && k.at + i < next; }) < more) until = next;
+    for (uint64_t bit = by_order ? 1ull << (kOrderBits - 1) : kBeamMerge / 2; bit; bit /= 2) {
+      uint32_t lower = 0;
+#pragma unroll 1
+      for (uint32_t rest = equal; rest; rest &= rest - 1) lower += place(__builtin_ctz(rest)) < until + bit ? 1 : 0;
+      if (sum_of_waves(waves, over_wave(lower, [](uint32_t x, uint32_t y) { return x + y; })) < more) until += bit;
     }
     __syncthreads();
     if (!t) listed = 0;
     __syncthreads();
+    const auto add = [&](uint64_t v, uint32_t i) {
+      const uint32_t to = atomicAdd(&listed, 1u);
+      if (to < kMergeList) l.value[to] = v, places[to] = k.at + i;
+    };
 #pragma unroll
-    for (uint32_t i = 0; i < kMergePer; ++i) {
-      const uint64_t v = is(i);
-      if (v && (v > key || (v == key && k.at + i <= until))) {
-        const uint32_t to = atomicAdd(&listed, 1u);
-        if (to < kMergeList) l.value[to] = v, places[to] = k.at + i;
-      }
-    }
+    for (uint32_t i = 0; i < kMergePer; ++i)
+      if (is[i] > key) add(is[i], i);
+#pragma unroll 1
+    for (uint32_t rest = equal; rest; rest &= rest - 1)
+      if (place(__builtin_ctz(rest)) <= until) add(key, __builtin_ctz(rest));
     __syncthreads();
     n = listed;
   }
   if (n > 2 * keep + 64) n = thin<kMerge>(l, places, numbers, waves, n, keep);
-  rank_list<kMerge, true>(l, places, n);
-  for (uint32_t i = t; i < n; i += kMerge)
-    if (l.rank[i] < keep) give(l.rank[i], l.value[i], places[i]);
+  constexpr uint32_t kMine = (kMergeList + kMerge - 1) / kMerge;
+  uint32_t at[kMine];
+  uint64_t v[kMine];
+#pragma unroll 1
+  for (uint32_t pass = 0;; ++pass) {  // by place; where that may not do, by order, whose ranks then take the places' place
+    rank_list<kMerge, true>(l, places, n);
+    if (pass != 1) {
+      bool close = false;
+#pragma unroll
+      for (uint32_t i = 0; i < kMine; ++i) {
+        const uint32_t c = i * kMerge + t;
+        if (c < n && l.rank[c] < keep) close |= give(l.rank[c], l.value[c], pass ? at[i] : places[c]);
+      }
+      if (!TIES || pass) break;
+      if (close) merged = 1;
+      __syncthreads();
+      if (!merged) break;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kMine; ++i) {
+      const uint32_t c = i * kMerge + t;
+      if (c >= n) continue;
+      if (pass) {
+        l.value[c] = v[i];
+        places[c] = l.rank[c];
+      } else {
+        v[i] = l.value[c];
+        at[i] = places[c];
+        if constexpr (TIES) l.value[c] = ~order(at[i]);
+      }
+    }
+    __syncthreads();
+  }
   return n < keep ? n : keep;
 }
 
@@ -638,8 +694,11 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
   if (!grows(a, row)) return;
   const Keys k(a.lists + static_cast<uint64_t>(row) * n, n, a.keep, a.splits);
   uint64_t* const out = a.rows + static_cast<uint64_t>(row) * a.keep;
-  const uint32_t found = best_of(k, a.keep, [&](uint32_t i) { return k.v[i]; },
-                                 [&](uint32_t rank, uint64_t key, uint32_t) { out[rank] = key; });
+  const uint32_t found = best_of<false>(k, a.keep, [&](uint32_t i) { return k.v[i]; }, nullptr, nullptr,
+                                        [&](uint32_t rank, uint64_t key, uint32_t) {
+                                          out[rank] = key;
+                                          return false;
+                                        });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) out[i] = 0;
 }
 
@@ -647,6 +706,9 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
 // 24 requests of 640 keys 10 us, 8 of 8192 17.6: a chain of loads, the log, the bound, the list and the ranks, a barrier after each.
 __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
   __shared__ double scores[kBeamMost], lses[kBeamMost];
+  // Two logits x < y of a beam have one value only where 2^-24 |x|, the least that x and y are apart, is no more than v's two
+  // roundings, 2^-53 of |x - lse| and of |v| each, make of both: |x| and |y| then are below 2^-27 (|score| + |lse|). Twice that.
+  __shared__ float near[kBeamMost];
   __shared__ uint8_t state[kBeamMost];  // 0: no candidates, 1: from its logits, 2: done
   const uint32_t item = blockIdx.x, t = threadIdx.x;
   constexpr uint32_t kLanes = kMerge / kBeamMost;  // of a beam
@@ -683,6 +745,7 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
       scores[beam] = score;
       lses[beam] = lse;
       state[beam] = is;
+      near[beam] = is == 1 ? static_cast<float>(0x1p-26 * (fabs(score) + fabs(lse))) : -1.0f;
     }
   }
   __syncthreads();
@@ -691,12 +754,21 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
     if (is == 1 && k.v[i]) return ordered(scores[beam] + (unordered(static_cast<uint32_t>(k.v[i] >> 32)) - lses[beam]) + 0.0);
     return is == 2 && k.at + i == beam * per ? ordered(scores[beam] + 0.0) : 0;
   };
+  const auto close = [&](uint32_t beam, uint64_t key) { return fabsf(unordered(static_cast<uint32_t>(key >> 32))) <= near[beam]; };
+  const auto near_zero = [&](uint32_t i) { return close(k.beam_of(i), k.v[i]); };
+  const auto order = [&](uint32_t place) -> uint64_t {  // beam, the logit's complement, place
+    const uint32_t beam = place / per, logit = state[beam] == 1 ? static_cast<uint32_t>(from[place] >> 32) : 0;
+    return static_cast<uint64_t>(beam) << 46 | static_cast<uint64_t>(~logit) << 14 | place;
+  };
+  static_assert(kBeamMerge == 1u << 14 && kBeamMost <= 64 && kOrderBits == 52, "");
   const uint64_t to = static_cast<uint64_t>(item) * a.keep;
-  const uint32_t found = best_of(k, a.keep, value, [&](uint32_t rank, uint64_t v, uint32_t at) {
+  const uint32_t found = best_of<true>(k, a.keep, value, near_zero, order, [&](uint32_t rank, uint64_t v, uint32_t at) {
     const uint32_t beam = at / per;
-    a.tokens[to + rank] = state[beam] == 2 ? a.done_token : static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(from[at]));
+    const uint64_t key = from[at];
+    a.tokens[to + rank] = state[beam] == 2 ? a.done_token : static_cast<int32_t>(0xffffffffu - static_cast<uint32_t>(key));
     a.parents[to + rank] = static_cast<int32_t>(item * a.beams + beam);
     a.scores_out[to + rank] = static_cast<float>(unordered(v));
+    return close(beam, key);
   });
   for (uint32_t i = found + t; i < a.keep; i += kMerge) {
     a.tokens[to + i] = a.parents[to + i] = -1;

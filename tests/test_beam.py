@@ -105,6 +105,13 @@ def test_reference_selection_by_hand():
     assert t.tolist() == [[1, -1, -1]] and p.tolist() == [[1, -1, -1]] and v[0, 0] == -1.0
 
 
+def test_reference_selection_of_equal_values_goes_by_logit():
+    """1e-20 and 0 make the same value: the larger logit first, then the lower token; the lower beam before both."""
+    x = np.array([[[0.0, 1e-20, 1e-20], [3e-20, 0.0, 0.0]]])
+    t, p, v, _ = ob.select(x, np.full((1, 2), -1.0), 5)
+    assert t.tolist() == [[1, 2, 0, 0, 1]] and p.tolist() == [[0, 0, 0, 1, 1]] and len(set(v[0])) == 1
+
+
 def test_reference_fork_by_hand():
     # blocks of 4: sequence 0 has 6 entries in blocks 5 and 2, sequence 1 4 in block 0; 1 and 3 are free, 4 is held elsewhere
     got = ob.fork([[5, 2, -1], [0, -1, -1]], [6, 4], [1, 0, 1, 0, 1, 1], [0, 0], [1, 3], 4, 12, 3)

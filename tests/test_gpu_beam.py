@@ -161,6 +161,45 @@ def test_select_near_ties_are_told_apart():
         assert tokens.tolist() == [[7]] and parents.tolist() == [[at]]
 
 
+def test_select_equal_values_of_a_beam_go_by_logit():
+    """Values that are equal though their logits are not, as a score far below or tiny logits make them: the larger logit first, then
+    the lower token, the same whether a row is in one part, in several, or has them joined first."""
+    g = gen(31)
+    vocab, keep = 70001, 100
+    for dtype, score in ((F32, -1e9), (F32, -1e30), (BF16, -1e30), (F16, -3e38)):
+        if score == -1e9:  # some 32 logits to a value: 2^-28 apart, values 2^-23
+            row = 2.0 ** -5 + torch.randperm(vocab, generator=g).double() * 2.0 ** -28
+        else:
+            row = normal(g, vocab)
+        row = row.to(dtype)[None, None]
+        s = torch.tensor([[score]])
+        tokens, _, best = check_select(row, s, keep)                              # 18 parts
+        many = mma.mma_beam_select(row.cuda().expand(1100, 1, vocab), s.cuda().expand(1100, 1).contiguous(), keep)  # one
+        assert torch.equal(many[0], tokens.expand(1100, keep)) and torch.equal(many[2], best.expand(1100, keep))
+        dead = torch.full((1, 64), -math.inf)
+        dead[0, 37] = score
+        joined = mma.mma_beam_select(row.cuda().expand(1, 64, vocab), dead.cuda(), keep)
+        assert torch.equal(joined[0], tokens) and (joined[1] == 37).all()
+
+
+@pytest.mark.parametrize("beams,vocab,keep", [(40, 12000, 100), (8, 12000, 20), (3, 9000, 7), (1, 40000, 128)])
+def test_select_equal_values_of_many_beams(beams, vocab, keep):
+    """Every value equal: the lowest beam's best, also where the list of a merge overflows or is thinned; with some of a later beam's
+    before them, and tiny logits, whose values are their beam's alone."""
+    g = gen(32)
+    for dtype in (F32, BF16):
+        x = some_logits(g, 2, beams, vocab, dtype)
+        scores = torch.full((2, beams), -1e30)
+        x[1, beams // 2, 5:] = -math.inf
+        scores[1, beams // 2] = 0.0
+        check_select(x, scores, keep)
+    tiny = normal(g, 1, beams, vocab) * 1e-30
+    check_select(tiny, -torch.rand(1, beams, generator=g), keep)
+    tiny[0, :, 3] = 0.0
+    tiny[0, :, 8000] = -0.0
+    check_select(tiny, torch.zeros(1, beams) if beams == 1 else -torch.rand(1, beams, generator=g), keep)
+
+
 def test_select_beams_without_candidates():
     g = gen(8)
     inf, nan = math.inf, math.nan
