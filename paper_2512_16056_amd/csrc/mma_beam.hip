@@ -72,7 +72,11 @@ __device__ __forceinline__ double exp_of(double d, double magic = kMagic) {
   return __builtin_bit_cast(double, b);
 }
 
-// The same of four numbers, no less than `floor`, added to `sums`: side by side, so that a wave by itself keeps the unit busy.
+// e^(x - top) for an x up to `top`, no less than e^-600. The difference is of 64 bits: from 2^33 on 32 bits round 600 less to 1024
+// less, or to `top` itself.
+__device__ __forceinline__ double power_below(float x, float top) { return exp_of(fmax(static_cast<double>(x) - top, -600.0)); }
+
+// Powers, as of exp_of, of four numbers, no less than `floor`, added to `sums`: side by side, so that a wave by itself keeps the unit busy.
 __device__ __forceinline__ void exp_of_4(const float* x, float floor, double magic, double (&sums)[4]) {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   constexpr double kTerms[7] = {0.00015469729140704658, 0.0013333478480888061, 0.009618025613598036, 0.055504109063177154,
@@ -451,7 +455,7 @@ __global__ __launch_bounds__(kThreads, 4) void beam_part_kernel(BeamArgs a) {
 #pragma unroll
   for (uint32_t i = 1; i < kWaves; ++i) high = fmaxf(high, tops[i]);
   if (near()) sum /= exp_of(ref, magic);
-  if (ref > -INFINITY) sum *= exp_of(static_cast<double>(fmaxf(ref, high - 600.0f)) - high);
+  if (ref > -INFINITY) sum *= power_below(ref, high);
   if (bad) sum = NAN;
   sum = sum_of_wave(sum);
   if (!lane) sums[wave] = sum;
@@ -732,7 +736,7 @@ __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
 #pragma unroll
       for (uint32_t x = 1; x < kLanes; x *= 2) top = fmaxf(top, __shfl_xor(top, x, kLanes));
       const auto part = [&](float max, double sum) {
-        return sum * (max > -INFINITY ? exp_of(static_cast<double>(fmaxf(max, top - 600.0f)) - top) : 1.0);
+        return sum * (max > -INFINITY ? power_below(max, top) : 1.0);
       };
       double sum = part(m0, s0);
       for (uint32_t i = lane + kLanes; i < a.splits; i += kLanes) sum += part(m[i], s[i]);

@@ -245,6 +245,21 @@ def test_select_scales(scale, shift):
     check_select(x * (1.0 if scale == 1e-30 else scale) + shift if scale != 1e-30 else x, -torch.rand(2, x.shape[1], generator=g), 4)
 
 
+@pytest.mark.parametrize("beams,vocab", [(2, 20000), (64, 3000), (1, 70000)])
+def test_select_logits_of_every_size(beams, vocab):
+    """A few logits far above the others, from 2^10 to 2^126, of both signs: what a part or a thread adds to the sum is nothing beside
+    a logit further than 600 above its own, wherever 32 bits do not tell 600 less from the logit itself, or round it to more."""
+    g = gen(33)
+    for e in list(range(10, 45)) + [60, 90, 126]:
+        x = normal(g, 2, beams, vocab)
+        x[1] -= 1.75 * 2.0 ** e
+        for b in range(beams):
+            at = torch.randperm(vocab, generator=g)[:4]
+            for sign, far in ((0, (1.5, 1.45, 1.25, 1.0)), (1, (-1.0, -1.25, -1.45, -1.5))):
+                x[sign, b, at] = torch.tensor(far) * 2.0 ** e
+        check_select(x, -torch.rand(2, beams, generator=g) * 6, 5)
+
+
 def test_select_peaked_rows():
     """A row whose mass is one logit, and masks of -1e9 and -1e4."""
     x = torch.full((1, 2, 30000), -1e9)
