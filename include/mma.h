@@ -587,8 +587,9 @@ typedef struct mma_kv_shape {
 } mma_kv_shape_t;
 
 /* mma_kv_attention with such scores; lse and the weights of the entries are of the shaped ones. NULL, or a
- * shape of nothing: mma_kv_attention. The capped score is within 2^-22 of the cap: with the
- * largest one 2^-12, an eighth of what the weights' rounding to bf16 makes. */
+ * shape of nothing: mma_kv_attention. Forming the capped score adds an error below 2^-21 of the cap to the score's own, also
+ * where the score is near 0: with the largest cap 2^-11, as much as a weight's rounding to f16 makes, an eighth of its
+ * rounding to bf16. */
 mma_status_t mma_kv_attention_shaped(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
                                      const mma_kv_attention_t* args, const mma_kv_shape_t* shape, void* stream);
 
@@ -663,7 +664,7 @@ typedef struct mma_beam_select {
 /* v = score + (logit - lse), lse the log of the sum of exp of the beam's logits; of each request the `keep`
  * largest, in order, ties to the lower beam, within a beam to the larger logit (a score far below or tiny logits make
  * equal values of logits that are not), then to the lower token. lse and v are 64-bit (lse within
- * 2^-33), v rounded at the store; beams with the same logits and score tie.
+ * 2^-33 and its own rounding to 64 bits), v rounded at the store; beams with the same logits and score tie.
  * A beam that has ended has one candidate: done_token, with its score as it is.
  * Logits of -infinity are no candidates; a beam
  * whose score or lse is not finite (a logit that is NaN or +infinity) has none. Where there are fewer than

@@ -372,3 +372,25 @@ def test_weights_of_a_last_key_that_few_rows_see(group, max_len):
         n = len(lens)
         check(c, window=60, prefix=[5] * n, scores=True)
         check(c, window=41, prefix=[5] * n, cap=9.0, slopes=alibi(c.heads_q), scores=True)
+
+
+@pytest.mark.parametrize("cap", [1.0, 30.0, 1024.0])
+@pytest.mark.parametrize("rows", [False, True])
+def test_a_capped_score_by_itself(rows, cap):
+    """Tokens that see one entry, whose lse so is the score. Products are exact (one value, times 1); the cap's arithmetic is
+    off by 3.5 * 2^-23 of it at most. The factor's seven roundings change the argument by 7 * 2^-24 of itself, what is capped by
+    0.448 of that (the maximum of u / cosh^2 u) of the cap. From top to lse there are four more, 2^-24 of it each."""
+    lens, counts = ([0], [512]) if rows else ([0] * 512, [1] * 512)
+    c = Case("hnd", BF16, lens, counts, heads=1, group=4, dim=8)
+    c.flat.zero_()
+    for s, (_, _, _, m) in enumerate(c.spans()):
+        for j in range(m):
+            c.flat[0][c.c.index(0, *c.c.entry(c.table[s], j), 0)[0]] = 1.0
+    x = torch.cat([sign * cap * 2.0 ** torch.linspace(-12, 3, 1024) for sign in (-1, 1)])[torch.randperm(2048, generator=c.g)]
+    q = torch.zeros(512, 4, 8, dtype=BF16)
+    q[:, :, 0] = x.view(512, 4).to(BF16)
+    lse = torch.empty(512, 4, device="cuda")
+    mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q.cuda(), scale=1.0, softcap=cap, window=1, lse=lse)
+    want = cap * torch.tanh(q[:, :, 0].double() / cap)
+    tol = cap * (3.5 * 2.0 ** -23 + 0.448 * 7 * 2.0 ** -24) + 4 * 2.0 ** -24 * want.abs()
+    assert ((lse.cpu().double() - want).abs() / tol).max().item() <= 1
