@@ -3,9 +3,10 @@
     python examples/kv_beam.py [--layers 4] [--requests 2] [--beams 4] [--prompt 300] [--steps 32] [--layout hnd] [--cache f8]
 
 An untrained model (random projections) whose scores are capped and whose tokens see the last 256 entries and the first
-four. Each request's prompt is written once and its beams fork from it: they share its pages, and every step a beam that
-goes on from another shares that one's pages and gets its own copy of the open one, on the GPU throughout. At the end
-the held pages are moved to the front of the pool and offloaded over all paths. Prints what each part did.
+four, those in both directions: a prompt's first three tokens see ahead up to the fourth. Each request's prompt is
+written once and its beams fork from it: they share its pages, and every step a beam that goes on from another shares
+that one's pages and gets its own copy of the open one, on the GPU throughout. At the end the held pages are moved to
+the front of the pool and offloaded over all paths. Prints what each part did.
 """
 import argparse
 import os
@@ -22,7 +23,7 @@ import paper_2512_16056_amd as mma  # noqa: E402
 
 LAYOUTS = {"piece": mma.MMA_KV_LAYOUT_PIECE, "xpacked": mma.MMA_KV_LAYOUT_XPACKED, "hnd": mma.MMA_KV_LAYOUT_HND}
 HEADS, GROUP, DIM, TOKENS, VOCAB = 4, 2, 64, 16, 5000
-CAP, WINDOW, FIRST = 30.0, 256, 4  # the model's scores: the cap, the window, the first entries that stay in sight
+CAP, WINDOW, FIRST = 30.0, 256, 4  # the model's scores: the cap, the window, the first entries, which every token sees
 END = VOCAB - 1  # a beam that takes this token has ended
 
 

@@ -573,9 +573,12 @@ mma_status_t mma_kv_attention_workspace(const mma_kv_layout_t* layout, const mma
 
 /* What a model makes of a score before the softmax, and which entries its tokens see. The token of entry
  * i and entry j (lens[s] + t is token t's entry): x = scale * q . K; with a cap c > 0, c tanh(x / c); then
- * less slopes[head] * |i - j|. It sees j < prefix[s] (in both directions: an image, a document read as
- * a whole, or with a window the first entries that stay in sight), and of the others those with j <= i
+ * less slopes[head] * |i - j|. It sees j < prefix[s], and of the others those with j <= i
  * and, with a window, i - j < window. Entries that a call's tokens do not see are not read.
+ * A prefix opens the sequence and is seen in both directions: an image, a document read as a whole. With a window it is
+ * also what stays in sight of later tokens. Where first entries are to stay in sight and yet see nothing ahead of them,
+ * the tokens before entry prefix - 1 go in a call without a prefix, the rest of the prompt in a second one with it: tokens
+ * from there on, and so all that are decoded, have none of it ahead.
  * The cap goes with a tree; the others do not, as a tree does not tell a drafted token's distance. */
 typedef struct mma_kv_shape {
   const float* slopes;      /* [q_heads] or NULL (0); -infinity, infinity and NaN make rows that are not numbers */

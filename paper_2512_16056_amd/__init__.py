@@ -564,7 +564,8 @@ def mma_kv_attention(layout: mma_kv_layout_t, layer, seqs: KVSeqs, q: torch.Tens
 
     Scores have the shape of ``mma_kv_shape_t``: capped (`softcap`), less `slopes` (float32 [heads]) times the distance, seen
     within `window` entries up to the token's own, and in both directions within `prefix` (int32 [sequences]) entries, of
-    which no sequence has more than `max_prefix` (max_len unless given)."""
+    which no sequence has more than `max_prefix` (max_len unless given). Tokens of the prefix see ahead in it: for first entries
+    that only stay in sight of a window, they go in a call without one."""
     if stream is not None:
         if out is None:
             out = _empty_on(stream, q.shape, q.dtype, q.device)

@@ -394,3 +394,31 @@ def test_a_capped_score_by_itself(rows, cap):
     want = cap * torch.tanh(q[:, :, 0].double() / cap)
     tol = cap * (3.5 * 2.0 ** -23 + 0.448 * 7 * 2.0 ** -24) + 4 * 2.0 ** -24 * want.abs()
     assert ((lse.cpu().double() - want).abs() / tol).max().item() <= 1
+
+
+@pytest.mark.parametrize("first", [1, 4, 23])
+def test_first_entries_that_stay_in_sight_and_see_nothing_ahead(first):
+    """A prompt in two calls, its tokens before entry `first` - 1 without a prefix: every token sees its window and the first
+    entries, and nothing behind itself. In one call tokens of the prefix see ahead, and are another's."""
+    c = Case("hnd", BF16, [0], [150], heads=1, group=2)
+    n, D, window, cut = 150, 128, 40, first - 1
+    q = normal(c.g, n, 2, D, std=2.0).to(BF16)
+    layer, table = c.flat[0].cuda(), c.table.cuda()
+
+    def part(a, b, **kw):
+        seqs = mma.kv_seqs(table, i32([a]).cuda(), max_tokens=b - a, max_len=b)
+        return mma.mma_kv_attention(c.layout(), layer, seqs, q[a:b].cuda(), window=window, **kw).cpu()
+    with_prefix = dict(prefix=i32([first]).cuda(), max_prefix=first)
+    out = torch.cat(([part(0, cut)] if cut else []) + [part(cut, n, **with_prefix)]).double()
+    k, v = (torch.stack([c.flat[0][c.c.index(w, *c.c.entry(c.table[0], j), 0)] for j in range(n)]).double() for w in (0, 1))
+    i, j = torch.arange(n)[:, None], torch.arange(n)[None]
+    sees = (j <= i) & ((i - j < window) | (j < first))
+    x = torch.einsum("ihd,jd->hij", q.double(), k) * D ** -0.5
+    p = torch.softmax(x.masked_fill(~sees, -math.inf), -1)
+    want, mag = (torch.einsum("hij,jd->ihd", p, y) for y in (v, v.abs()))
+    big = (torch.einsum("ihd,jd->hij", q.double().abs(), k.abs()) * D ** -0.5).amax(-1).T[..., None]
+    u = 2.0 ** -8
+    tol = u * want.abs() * (1 + 2 * u) + (u + 2 * D * EPS * big + 64 * EPS) * mag * (1 + 2 * u) + STEP[BF16]
+    assert ((out - want).abs() / tol).max().item() <= 1
+    ahead = ((part(0, n, **with_prefix).double() - want).abs() / tol).amax((1, 2))
+    assert (ahead[cut:] <= 1).all() and (ahead[:cut] > 1).all()
