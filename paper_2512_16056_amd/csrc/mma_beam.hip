@@ -73,8 +73,11 @@ __device__ __forceinline__ double exp_of(double d, double magic = kMagic) {
 }
 
 // e^(x - top) for an x up to `top`, no less than e^-600. The difference is of 64 bits: from 2^33 on 32 bits round 600 less to 1024
-// less, or to `top` itself.
-__device__ __forceinline__ double power_below(float x, float top) { return exp_of(fmax(static_cast<double>(x) - top, -600.0)); }
+// less, or to `top` itself. 1 of `top`, where the polynomial is 4e-11 less: a row's only candidate then has lse = its logit.
+__device__ __forceinline__ double power_below(float x, float top) {
+  const double p = exp_of(fmax(static_cast<double>(x) - top, -600.0));
+  return x == top ? 1.0 : p;
+}
 
 // Powers, as of exp_of, of four numbers, no less than `floor`, added to `sums`: side by side, so that a wave by itself keeps the unit busy.
 __device__ __forceinline__ void exp_of_4(const float* x, float floor, double magic, double (&sums)[4]) {

@@ -220,6 +220,21 @@ def test_select_beams_without_candidates():
     check_select(x, scores, 8)                         # -3.4e38 is -infinity there
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_select_beams_with_one_way_on(dtype):
+    """Rows of which a rule leaves one token: a value is the score itself, to the last bit, so that beams with the same score
+    tie whatever their logits are, in one part, several, or joined."""
+    g = gen(34)
+    for batch, beams, vocab in ((3, 8, 300), (1, 8, 60000), (1, 64, 60000)):
+        x = torch.full((batch, beams, vocab), -math.inf)
+        for b in range(batch):
+            for y in range(beams):
+                x[b, y, torch.randint(0, vocab, (1,), generator=g)] = float(normal(g, 1, std=30.0))
+        scores = -(torch.arange(beams) // 4 % 3).float().expand(batch, beams).contiguous()
+        _, _, best = check_select(x.to(dtype), scores, 128)
+        assert torch.equal(best.cpu()[:, :beams], scores.sort(-1, descending=True).values)
+
+
 def test_select_done_beams():
     g = gen(9)
     x = some_logits(g, 3, 6, 12345, BF16)
