@@ -710,7 +710,7 @@ __global__ __launch_bounds__(kMerge) void beam_row_kernel(BeamArgs a) {
 }
 
 // A request: of each beam log-sum-exp of its parts, then the best over all.
-// 24 requests of 640 keys 10 us, 8 of 8192 17.6: a chain of loads, the log, the bound, the list and the ranks, a barrier after each.
+// 24 requests of 640 keys 10.7 us, 8 of 8192 18.2: a chain of loads, the log, the bound, the list and the ranks, a barrier after each.
 __global__ __launch_bounds__(kMerge) void beam_merge_kernel(BeamArgs a) {
   __shared__ double scores[kBeamMost], lses[kBeamMost];
   // Two logits x < y of a beam have one value only where 2^-24 |x|, the least that x and y are apart, is no more than v's two

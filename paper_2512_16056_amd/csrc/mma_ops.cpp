@@ -272,7 +272,9 @@ AttnPlan attention_plan(const CacheArgs& c, const mma_kv_layout_t& layout, const
     return static_cast<uint32_t>(std::min<uint64_t>(most, q.max_len));
   };
   // Slopes and caps are more work for each entry, which the waves of attention_stream_kernel share and one wave of the other
-  // has alone (4 rows, 32 of 1k to 8k, bf16, slopes: head-major 126 us against 150, in pieces 138 against 149).
+  // has alone (4 rows, 32 of 1k to 8k, bf16, slopes: head-major 126 us against 150, in pieces 138 against 149). Windows go by
+  // the threshold of whole contexts, 4096, though the two do not cross there: with one of 4096 and the first 4, f16, head-major,
+  // 4 rows, keys in registers and in LDS take 12.8 and 19.7 us for one sequence, 30.9 and 33.4 for 8, 92.8 and 89.1 for 32.
   const bool shapes = shape && (shape->slopes || shape->softcap != 0);
   if (p.dim_pad == 128 && !two && walked(16) > 4096 && !a.scores_out && !shapes) p.stream = false;
   const uint32_t per_tile = p.stream ? 16 : 64;
