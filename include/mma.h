@@ -590,9 +590,8 @@ typedef struct mma_kv_shape {
 } mma_kv_shape_t;
 
 /* mma_kv_attention with such scores; lse and the weights of the entries are of the shaped ones. NULL, or a
- * shape of nothing: mma_kv_attention. Forming the capped score adds an error below 2^-21 of the cap to the score's own, also
- * where the score is near 0: with the largest cap 2^-11, as much as a weight's rounding to f16 makes, an eighth of its
- * rounding to bf16. */
+ * shape of nothing: mma_kv_attention. Forming the capped score adds an error below 2^-20 of itself to the product's own: with
+ * the largest cap at most 2^-10, a quarter of what a weight's rounding to bf16 makes. */
 mma_status_t mma_kv_attention_shaped(const mma_kv_layout_t* layout, const void* layer, const mma_kv_seqs_t* seqs,
                                      const mma_kv_attention_t* args, const mma_kv_shape_t* shape, void* stream);
 

@@ -34,6 +34,7 @@ SOURCES = {
     "mma_ops.cpp": ["-x", "c++", "-D__HIP_PLATFORM_AMD__", f"-I{os.path.join(ROCM, 'include')}"],
     "mma_attention.hip": DEVICE,
     "mma_attention_shaped.hip": DEVICE,
+    "mma_attention_capped.hip": DEVICE,
     "mma_kv_ops.hip": DEVICE,
     "mma_beam.hip": DEVICE,
     "mma_pages.hip": DEVICE,

@@ -21,11 +21,12 @@
 // LDS once for the workgroup's 64 or 128 rows; its waves split the rows. Which of them takes a
 // call, and in how many splits, is attention_plan's choice (mma_ops.cpp).
 //
-// Every kernel is compiled for AttnArgs (mma_attention.hip) and for ShapedArgs (mma_attention_shaped.hip): scores capped
-// by a tanh or biased by distance, entries out of a window passed over, a prefix seen by every token. What shapes cost
-// is paid by the second alone. One token of 8 sequences of 32k entries, f16, a window of 4096 and a prefix of 4: 29 us, 4.0 TB/s of what
-// is seen, and 4.6 to join; 32 sequences of 1k to 8k with slopes 133 us, 4.4 TB/s; 2048 tokens behind 6144 entries, capped, a window of
-// 4096: 208 us, 0.66 PFLOP/s, 171 without the cap: vector instructions, 14 a score instead of 8.
+// Every kernel is compiled for AttnArgs (mma_attention.hip), for ShapedArgs (mma_attention_shaped.hip): scores biased by
+// distance, entries out of a window passed over, a prefix seen by every token; and for CappedArgs (mma_attention_capped.hip): such
+// scores capped by a tanh too. What shapes cost is paid by the second and third alone, and a cap by the third, whose code for
+// two ranges of scores would cost short walks without one 4 %. One token of 8 sequences of 32k entries, f16, a window of 4096 and a prefix
+// of 4: 29 us, 4.0 TB/s of what is seen, and 4.6 to join; 32 sequences of 1k to 8k with slopes 133 us, 4.4 TB/s; 2048
+// tokens behind 6144 entries, capped, a window of 4096: 206 us, 0.67 PFLOP/s, 171 without the cap.
 #ifndef MMA_ATTENTION_KERNELS_H_
 #define MMA_ATTENTION_KERNELS_H_
 #include "mma_ops.h"
@@ -230,25 +231,52 @@ __device__ __forceinline__ Walk walk_of_row(const ShapedArgs& a, const SeqSpan& 
   return walk_of(a, sp, seq, first / a.group, (rows - first < a.wg_rows ? rows - 1 : first + a.wg_rows - 1) / a.group);
 }
 
-// Factor of a product q . k before `capped`: to base 2, or with a cap c to twice the tanh's argument, base 2.
-__device__ __forceinline__ float shaped_factor(const ShapedArgs& a, float scale) {
-  return a.cap2 != 0 ? scale * (2 * kLog2e * kLog2e) / a.cap2 : scale * kLog2e;
+// Factor of a product q . k: to base 2, or with a cap c to u = x / c.
+template <class A>
+__device__ __forceinline__ float shaped_factor(const A& a, float scale) {
+  if constexpr (A::kCapped) return scale * kLog2e / a.cap2;
+  else return scale * kLog2e;
 }
-// c tanh(x / c) in base 2 = cap2 (1 - 2 r), r = 1 / (1 + 2^y), y = 2 log2(e) x / c: exact at both ends (2^y infinite or 0). Between
-// them the power and the reciprocal are off by 2^-23 of themselves at most, the sum and the result by 2^-24: together
-// 2^-23 (2 r (1 - r) + 3 r + |1 - 2 r| / 2) of the cap, below 3.5 2^-23 < 2^-21.
-__device__ __forceinline__ float capped(const ShapedArgs& a, float y) {
-  return fmaf(-2 * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y)), a.cap2);
+
+// c tanh(u) in base 2. Up to kNear, u times a polynomial of u^2 (degree 4, the least relative error, 2^-24.9;
+// its coefficients come with the cap as their factor). Above, cap2 (1 - 2 r), r = 1 / (1 + 2^y), y = 2 log2(e) |u|: exact at the end (2^y
+// infinite); the power and the reciprocal are off by 2^-23 of themselves at most, the sum and the result by 2^-24: together
+// 2^-23 (2 r (1 - r) + 3 r + |1 - 2 r| / 2) of the cap, 2^-21.5 of the result where r is largest, 1/4. With the
+// roundings of u, seven of 2^-24 of which 0.8 count above, all of them below, either is within 2^-20 of itself.
+// A wave asks once for its scores of a tile whether one of them is above; scores beyond half of the cap are few. 2048 tokens behind
+// 6144 entries, a window of 4096, cap 20 to 50: 206 us; where most tiles have such scores (cap 10) 278. The upper formula alone, off by
+// 2^-21 of the cap also near 0, took 208; a polynomial of degree 6 up to the whole cap 219 and 287.
+constexpr float kNear = 0.55f;
+enum class Cap { kNone, kNear, kAll };  // of a wave's scores: not capped, all up to kNear, any
+
+template <Cap CAP, class A>
+__device__ __forceinline__ float capped(const A& a, float u) {
+  if constexpr (CAP == Cap::kNone) return u;
+  else {
+    const float z = u * u;
+    float near = a.cap_terms[4];
+#pragma unroll
+    for (int i = 3; i >= 0; --i) near = fmaf(near, z, a.cap_terms[i]);
+    near *= u;
+    if constexpr (CAP == Cap::kNear) return near;
+    const float far = fmaf(-2 * a.cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fabsf(u) * (2 * kLog2e))), a.cap2);
+    return fabsf(u) > kNear ? copysignf(far, u) : near;
+  }
+}
+
+// Calls f with the Cap of a wave, whose lanes' largest |u| is most(), as a constant.
+template <class A, class M, class F>
+__device__ __forceinline__ void with_cap(const A&, M most, F f) {
+  if constexpr (!A::kCapped) f(std::integral_constant<Cap, Cap::kNone>());
+  else if (!__any(most() > kNear)) f(std::integral_constant<Cap, Cap::kNear>());
+  else f(std::integral_constant<Cap, Cap::kAll>());
 }
 
 // 8 logits, base 2, of a row's products with entries `away` - 0 .. 7 before its own.
-__device__ __forceinline__ void shape8(const ShapedArgs& a, float factor, float slope2, int32_t away, float (&y)[8]) {
+template <Cap CAP, class A>
+__device__ __forceinline__ void shape8(const A& a, float factor, float slope2, int32_t away, float (&y)[8]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] *= factor;
-  if (a.cap2 != 0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = capped(a, y[j]);
-  }
+  for (int j = 0; j < 8; ++j) y[j] = capped<CAP>(a, y[j] * factor);
   if (a.slopes) {
     const float d = static_cast<float>(away);
 #pragma unroll
@@ -619,8 +647,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_stream_kerne
       float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = x[r][j / 4][j % 4] * (kShaped ? 1.0f : to_log2);
-      if constexpr (kShaped)
-        shape8(a, to_log2, slope2[r], static_cast<int32_t>(sp.before + token[r] - (entry(base) + g * 8)), y);
+      if constexpr (kShaped) {
+        const auto most = [&] {
+          float u = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) u = fmaxf(u, fabsf(y[j]));
+          return u * fabsf(to_log2);
+        };
+        with_cap(a, most, [&](auto cap) {
+          shape8<decltype(cap)::value>(a, to_log2, slope2[r], static_cast<int32_t>(sp.before + token[r] - (entry(base) + g * 8)), y);
+        });
+      }
       if constexpr (kMasked) {
         if constexpr (kShaped) seen[r] = okay & keys_seen(a, sp, w, token[r], entry(base) + g * 8);
         else seen[r] = okay & keys_seen(a, sp, token[r], base + g * 8);
@@ -1125,17 +1162,29 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void attention_rows_kernel(
     }
     const uint32_t at = entry(base);
     if constexpr (kShaped) {
+      const auto most = [&] {
+        float u = 0;
 #pragma unroll
-      for (int j = 0; j < S::SUB; ++j)
+        for (int j = 0; j < S::SUB; ++j)
 #pragma unroll
-        for (int r = 0; r < RW; ++r) {
-          float y[8];
+          for (int r = 0; r < RW; ++r)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = x[r][j][i / 4][i % 4];
-          shape8(a, to_log2, slope2[r], static_cast<int32_t>(sp.before + token[r] - (at + j * 32 + g * 8)), y);
+            for (int i = 0; i < 8; ++i) u = fmaxf(u, fabsf(x[r][j][i / 4][i % 4]));
+        return u * fabsf(to_log2);
+      };
+      with_cap(a, most, [&](auto cap) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[r][j][i / 4][i % 4] = y[i];
-        }
+        for (int j = 0; j < S::SUB; ++j)
+#pragma unroll
+          for (int r = 0; r < RW; ++r) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[r][j][i / 4][i % 4];
+            shape8<decltype(cap)::value>(a, to_log2, slope2[r], static_cast<int32_t>(sp.before + token[r] - (at + j * 32 + g * 8)), y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[r][j][i / 4][i % 4] = y[i];
+          }
+      });
     }
     uint32_t seen[S::SUB][RW];
     if constexpr (kMasked) {
@@ -1528,7 +1577,7 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
           const auto logit = [&](int t, int i) { return fmaf(x[t][i], to_log2, -l2[i]); };
           // Nothing to ask of any score, as of most: 3 x 1021 tokens x 4 heads behind 50 entries, 8 KV heads, 8-bit x-packed, 61 us; with
           // the questions asked and a division for each token 92. Rows that see nothing, and those past the last, have an lse of infinity.
-          if (!(mixed || a.cap2 != 0 || a.slopes || __any(fmaxf(fmaxf(l2[0], l2[1]), fmaxf(l2[2], l2[3])) == INFINITY))) {
+          if (!(mixed || A::kCapped || a.slopes || __any(fmaxf(fmaxf(l2[0], l2[1]), fmaxf(l2[2], l2[3])) == INFINITY))) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -1544,16 +1593,28 @@ __global__ __launch_bounds__(256) void attention_scores_kernel(A a) {
           tokens = *reinterpret_cast<const i32x4*>(token_of + n);
           slopes = *reinterpret_cast<const f32x4*>(slope_of + n);
         }
+        float logits[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) logits[i] = x[i / 4][i % 4] * to_log2;
+        const auto most = [&] {
+          float u = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u = fmaxf(u, fabsf(logits[i]));
+          return u;
+        };
+        with_cap(a, most, [&](auto cap) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) logits[i] = capped<decltype(cap)::value>(a, logits[i]);
+        });
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint32_t row = row0 + r0 + g * 4 + i;
             bool see = l2[i] != INFINITY;  // NaN does: its entries' weights are no numbers
-            float y = x[t][i] * to_log2;
+            float y = logits[t * 4 + i];
             if constexpr (kShaped) {
               const int32_t away = static_cast<int32_t>(sp.before + tokens[i] - (base + t * 16 + m));
-              if (a.cap2 != 0) y = capped(a, y);
               if (a.slopes) y = fmaf(-slopes[i], fabsf(static_cast<float>(away)), y);
               if (mixed)
                 see = see && (base + t * 16 + m < prefix || (away >= 0 && (!a.window || static_cast<uint32_t>(away) < a.window)));

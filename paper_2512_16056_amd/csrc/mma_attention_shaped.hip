@@ -1,5 +1,5 @@
-// Attention over the paged KV cache: the kernels for scores that are capped, biased by distance, kept to a window, or
-// seen both ways in a prefix. A file of its own, so that both sets are compiled side by side.
+// Attention over the paged KV cache: the kernels for scores that are biased by distance, kept to a window, or seen both ways in
+// a prefix. A file of its own, as the capped ones have, so that all sets are compiled side by side.
 #include "mma_attention_kernels.h"
 
 namespace mma {

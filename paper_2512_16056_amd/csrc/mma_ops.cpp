@@ -377,7 +377,7 @@ mma_status_t attention(const mma_kv_layout_t* layout, const void* layer, const m
   Device dev(call.device);
   if (rows_too && (s = check_layer(layer, &call))) return s;
   if ((s = check_seqs(seqs, layout->block_tokens, n, &call))) return s;
-  ShapedArgs k{};
+  CappedArgs k{};
   const uint64_t score_bytes = extent(static_cast<uint64_t>(seqs->num_seqs) * H, a->scores_stride, 4);
   if ((s = array(&call, "scores_in", a->scores_in, score_bytes, 4, true))) return s;
   if ((s = array(&call, "scores_out", a->scores_out, score_bytes, 4, true))) return s;
@@ -448,11 +448,15 @@ mma_status_t attention(const mma_kv_layout_t* layout, const void* layer, const m
   k.prefix = shape->prefix;
   k.max_prefix = shape->max_prefix;
   k.window = std::min<uint32_t>(shape->window, INT32_MAX);
-  k.cap2 = shape->softcap * 1.44269504088896340736f;
   k.wg_rows = p.wg_rows;
   k.score_parts = std::max(1u, p.score_parts);
   k.score_part = take(p.score_bytes);
-  return launched(launch_attention_shaped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
+  if (shape->softcap == 0) return launched(launch_attention_shaped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
+  const double cap2 = shape->softcap * 1.44269504088896340736;
+  k.cap2 = static_cast<float>(cap2);
+  constexpr double kTerms[5] = {0.9999999676372836, -0.3333279502358464, 0.1331887691419831, -0.052589319781746184, 0.01631544361405081};
+  for (int i = 0; i < 5; ++i) k.cap_terms[i] = static_cast<float>(cap2 * kTerms[i]);  // of tanh(u) / u in u^2, u up to 0.55
+  return launched(launch_attention_capped(k, p, kind, static_cast<hipStream_t>(stream)), "KV attention");
 }
 
 // Memory of a call that its kernels read or write.

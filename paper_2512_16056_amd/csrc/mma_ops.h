@@ -81,7 +81,7 @@ struct AttnArgs {
   uint32_t splits, split_len;  // entries of a split: a multiple of the tile
   uint32_t wide_q, wide_out, wide_score_q;  // rows start at 16 bytes
   float scale, decay;
-  static constexpr bool kShaped = false;
+  static constexpr bool kShaped = false, kCapped = false;
 };
 
 // Attention whose scores have a shape (mma_kv_shape_t).
@@ -90,11 +90,17 @@ struct ShapedArgs : AttnArgs {
   const int32_t* prefix;  // [num_seqs] or NULL
   uint32_t max_prefix;
   uint32_t window;        // entries up to a token's own, at most 2^31 - 1; 0: all
-  float cap2;             // the cap, base 2; 0: none
   uint32_t wg_rows;       // rows of a workgroup
   float* score_part;      // weights of parts of the rows, [score_parts][num_seqs][heads][max_len], where there are several
   uint32_t score_parts;
   static constexpr bool kShaped = true;
+};
+
+// And a cap.
+struct CappedArgs : ShapedArgs {
+  float cap2;          // base 2
+  float cap_terms[5];  // of small scores (capped)
+  static constexpr bool kCapped = true;
 };
 
 struct CommitArgs {
@@ -218,6 +224,7 @@ constexpr bool stream_two_tiles(uint32_t dim_pad, bool f8, bool xpacked) {
 hipError_t launch_append(const AppendArgs& a, const OpsKind& k, hipStream_t stream);
 hipError_t launch_attention(const AttnArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_attention_shaped(const ShapedArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
+hipError_t launch_attention_capped(const CappedArgs& a, const AttnPlan& p, const OpsKind& k, hipStream_t stream);
 hipError_t launch_commit(const CommitArgs& a, const OpsKind& k, hipStream_t stream);
 hipError_t launch_beam(const BeamArgs& a, uint32_t type, hipStream_t stream);
 hipError_t launch_fork(const ForkArgs& a, hipStream_t stream);

@@ -422,3 +422,28 @@ def test_first_entries_that_stay_in_sight_and_see_nothing_ahead(first):
     assert ((out - want).abs() / tol).max().item() <= 1
     ahead = ((part(0, n, **with_prefix).double() - want).abs() / tol).amax((1, 2))
     assert (ahead[cut:] <= 1).all() and (ahead[:cut] > 1).all()
+
+
+@pytest.mark.parametrize("cap", [1e-3, 1.0, 50.0, 1024.0])
+@pytest.mark.parametrize("rows", [False, True])
+def test_a_capped_score_near_zero_keeps_its_digits(rows, cap):
+    """As test_a_capped_score_by_itself, of scores down to 2^-12 of the cap: off by a part of the score, not of the cap. Its tanh is
+    within 2^-21.5 of itself (from 0.55 of the cap on; below 2^-22.5: five roundings of 2^-24, the last of them for what the
+    polynomial leaves), and the seven roundings of its factor come to 7 * 2^-24; from top to lse there are four more."""
+    lens, counts = ([0], [512]) if rows else ([0] * 512, [1] * 512)
+    c = Case("hnd", BF16, lens, counts, heads=1, group=4, dim=8)
+    c.flat.zero_()
+    for s, (_, _, _, m) in enumerate(c.spans()):
+        for j in range(m):
+            c.flat[0][c.c.index(0, *c.c.entry(c.table[s], j), 0)[0]] = 1.0
+    x = torch.cat([sign * cap * 2.0 ** torch.linspace(-12, 3, 1024) for sign in (-1, 1)])[torch.randperm(2048, generator=c.g)]
+    q = torch.zeros(512, 4, 8, dtype=BF16)
+    q[:, :, 0] = x.view(512, 4).to(BF16)
+    lse = torch.empty(512, 4, device="cuda")
+    weights = torch.zeros(len(lens), 1, c.max_len, device="cuda")
+    mma.mma_kv_attention(c.layout(), c.flat[0].cuda(), c.seqs(), q.cuda(), scale=1.0, softcap=cap, window=1, lse=lse, scores_out=weights)
+    want = cap * torch.tanh(q[:, :, 0].double() / cap)
+    tol = (2.0 ** -21.5 + (7 + 4) * 2.0 ** -24) * want.abs()
+    assert ((lse.cpu().double() - want).abs() / tol).max().item() <= 1
+    # an entry has its token's four rows, of weight 1 each: 2^(x - x), off by twice the error of a logit
+    assert (weights.cpu().double() - 4).abs().max().item() <= 4 * 2 * tol.max().item() + 8 * 2.0 ** -24
